@@ -451,6 +451,129 @@ tasp_status tasp_serve_turn(const tasp_router* router, const tasp_plan* task_pla
                             size_t workspace_bytes, int32_t* chosen, int32_t* reused,
                             void* stream);
 
+/* ---- sequences of their own lengths and trees of drafted tokens (paper, Sec. "Dependency-Closed
+ * Masks and Cache-Consistent Routing": the plan fixed for a turn runs every decode step; here several
+ * drafted tokens of a sequence, for instance from a sparser plan, are run and verified in one step).
+ *
+ * A typed cache holds, per layer, sequence and KV head, max_seq rows of head_dim values in BF16 or in 8
+ * bits (INT8 or E4M3) with one float32 scale per row: value = code * scale. len (device) is the
+ * number of rows each sequence holds: no call needs it on the host. Lengths outside 0..max_seq are not an
+ * error that a call can report: such a sequence is passed over (nothing written, zeros returned).
+ *
+ * The T nodes of a tree: parent (device int32 [batch][T]) is -1 for a root, an earlier node, or anything else
+ * for an absent node (shorter trees of a batch; nodes below an absent one, and nodes whose row would not fit
+ * max_seq, are absent too). NULL: a chain, parent[t] = t - 1. Node t of a sequence has cache row len + t
+ * and position len + its depth. T <= TASP_TREE_MAX with a tree. */
+#define TASP_TREE_MAX 64
+#define TASP_SEQ_MAX_BATCH 256
+enum { TASP_BF16 = 0, TASP_F32 = 1, TASP_INT8 = 2, TASP_E4M3 = 3 };
+
+typedef struct {
+  void* k;                /* (device) [n_layers][batch][n_kv_heads][max_seq][head_dim], 16-byte aligned */
+  void* v;
+  float* k_scale;         /* (device) [n_layers][batch][n_kv_heads][max_seq]; NULL for TASP_BF16 */
+  float* v_scale;
+  int32_t* len;           /* (device) [batch] */
+  int32_t type;           /* TASP_BF16, TASP_INT8 or TASP_E4M3 */
+  int32_t n_layers, batch, n_kv_heads, max_seq, head_dim;   /* batch 1..TASP_SEQ_MAX_BATCH, heads 1..64,
+                             head_dim 64 or 128, max_seq * head_dim < 2^30 */
+  uint64_t plan_sig;      /* the plan the rows belong to (tasp_tree_step), 0: none */
+} tasp_seq_cache;
+
+/* Rows of head vectors (device): element strides from one sequence, token and head to the next; the
+ * values of a head are contiguous. Address and strides keep every row 16-byte aligned. */
+typedef struct {
+  void* p;
+  int64_t seq, token, head;
+} tasp_rows;
+
+/* Rotary positions. layout: pairs (i, i + rot_dim / 2) or (2 i, 2 i + 1) of a head's first rot_dim values (a
+ * multiple of 16, up to head_dim; the others pass unchanged), turned by pos * f_i, f_i = theta^(-2 i / rot_dim),
+ * and multiplied by mscale. For contexts beyond orig_len positions the frequencies are scaled:
+ *   LINEAR      f / factor
+ *   WAVELENGTH  by the turns n = orig_len f / 2 pi: f for n >= high, f / factor for n <= low, between them
+ *               f (g + (1 - g) / factor), g = (n - low) / (high - low)
+ *   INDEX       by the pair's index: f ((1 - g) + g / factor), g = clamp((i - a) / (b - a)), a and b the indices
+ *               (rounded down and up, cut to 0..rot_dim - 1; b - a at least 0.001) of the pairs that make high
+ *               and low turns over orig_len */
+enum { TASP_ROPE_HALF = 0, TASP_ROPE_INTERLEAVED = 1 };
+enum { TASP_ROPE_NONE = 0, TASP_ROPE_LINEAR = 1, TASP_ROPE_WAVELENGTH = 2, TASP_ROPE_INDEX = 3 };
+typedef struct {
+  int32_t layout, rot_dim, scaling, orig_len;
+  double theta, factor, low, high, mscale;
+} tasp_rope;
+
+/* Write T tokens' k and v behind every sequence of layer `layer` (rows len..len + T - 1; len itself
+ * stays) and rotate q: q and k are turned by the nodes' positions (rope NULL: not at all), v is taken as it
+ * is, and rows of an 8-bit cache are quantised as they are written (scale = the row's largest magnitude
+ * / 127 or 448, codes rounded to nearest even; a row that holds an infinity or a NaN reads back as NaN). k, v: rows of
+ * n_kv_heads heads; q, q_out: n_q_heads (0: no queries, both NULL), neither q_out overlapping q, k or
+ * v; all of act_type TASP_BF16 or TASP_F32. Rows of absent nodes are not written, their q_out are zeros. Only
+ * k and v of a packed BF16 cache may be given this way too (rope NULL), to convert it. Arithmetic in float32, angles in
+ * float64. Stream-ordered, asynchronous, capturable, no workspace. Errors: TASP_ERR_INVALID_ARG (NULL, types,
+ * misaligned rows), TASP_ERR_SHAPE (cache fields, layer, T, head counts, rot_dim). */
+tasp_status tasp_seq_append(const tasp_seq_cache* cache, int32_t layer, const tasp_rope* rope,
+                            const int32_t* parent, int32_t T, int32_t act_type, const tasp_rows* q,
+                            const tasp_rows* k, const tasp_rows* v, int32_t n_q_heads,
+                            const tasp_rows* q_out, void* stream);
+
+/* Read rows first[b]..first[b] + n - 1 (device int32 [batch]; NULL: 0) of layer `layer` back as out_type
+ * TASP_BF16 or TASP_F32 values (token stride: from row to row); rows outside 0..max_seq - 1 read as zeros.
+ * Stream-ordered, capturable. Errors as tasp_seq_append. */
+tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int32_t* first,
+                          int32_t n, int32_t out_type, const tasp_rows* k_out,
+                          const tasp_rows* v_out, void* stream);
+
+/* Attention of T nodes (1..TASP_TREE_MAX; their rows already appended) of every sequence: node t sees rows
+ * 0..len - 1, its ancestors' rows and its own, with scores scale * q . k. q, out: n_q_heads heads (a multiple
+ * of n_kv_heads, at most 8 per KV head; query head h reads KV head h / (n_q_heads / n_kv_heads)) of act_type;
+ * out must not overlap q or the cache. Outputs of absent nodes are zeros, and what absent or unseen
+ * rows hold (NaN, infinities) reaches no output. TASP_BF16: q and V exact, probabilities in 16 bits, sums in
+ * float32; TASP_F32: everything to 24 bits. max_len: the largest length expected (0..max_seq): it sizes launches and
+ * workspace; longer sequences are served too. workspace: device, 256-byte aligned, at least
+ * tasp_tree_attention_workspace_bytes for the same cache shape, n_q_heads, T and max_len; its contents need
+ * no clearing; calls that overlap need one each. Stream-ordered, capturable (one or two kernels). Errors as
+ * tasp_seq_append, TASP_ERR_WORKSPACE. */
+tasp_status tasp_tree_attention_workspace_bytes(const tasp_seq_cache* cache, int32_t n_q_heads,
+                                                int32_t T, int32_t max_len, size_t* bytes);
+tasp_status tasp_tree_attention(const tasp_seq_cache* cache, int32_t layer, const int32_t* parent,
+                                int32_t T, int32_t act_type, const tasp_rows* q, int32_t n_q_heads,
+                                double scale, int32_t max_len, const tasp_rows* out,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Verify the drafted tokens of `batch` trees against the target's distributions and take one more token from
+ * given random numbers. logits (device float32 [batch][T][vocab]) are the target's behind each node, p_v =
+ * softmax(logits[v] / temperature); tokens (device int32 [batch][T]): node 0 is the last token of the text (a
+ * root), nodes t >= 1 are drafted; u (device float32 [batch][T], in [0, 1); NULL with temperature 0). From node
+ * 0 on, the current node v's children are tried in node order:
+ *   without draft_logits, child c is accepted when u[c] (1 - the share of the earlier children's distinct tokens
+ *   in p_v) < p_v(tokens[c]), a token tried before having no share;
+ *   with draft_logits (device float32 [batch][T - 1][vocab], behind nodes 0..T - 2; parent must be NULL) when
+ *   u[c] q_v(tokens[c]) < p_v(tokens[c]), q_v = softmax(draft_logits[v] / temperature).
+ * An accepted child becomes the current node. Where none is, the last token is the lowest one whose
+ * cumulative weight exceeds u[0] times the total, the weights being p_v without the children's tokens, or
+ * max(p_v - q_v, 0) at a refused child with draft_logits (p_v, should rounding leave no weight). Either way the emitted
+ * tokens are distributed as the target's own samples. temperature 0: p_v is the lowest index of the
+ * largest logit, draft_logits are not read. T = 1 samples one token from logits. NaN logits count as -inf;
+ * a row without a finite or +inf logit yields token -1; drafted tokens outside the vocabulary are never accepted.
+ *   n (device int32 [batch]): tokens emitted, the accepted ones and one more; ids (device int32 [batch][T]): those
+ *   tokens, then -1; path (device int32 [batch][T]): the nodes 0, ... of the accepted path (n entries), then -1.
+ * All sums in float64. workspace: device, 256-byte aligned, at least tasp_verify_workspace_bytes, needs no clearing;
+ * calls that overlap need one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, temperature
+ * negative or not finite, draft_logits with a tree), TASP_ERR_SHAPE (batch, T, vocab), TASP_ERR_WORKSPACE. */
+tasp_status tasp_verify_workspace_bytes(int32_t batch, int32_t T, int32_t vocab, size_t* bytes);
+tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float* u,
+                        const int32_t* parent, const float* draft_logits, int32_t batch, int32_t T,
+                        int32_t vocab, double temperature, int32_t* ids, int32_t* path, int32_t* n,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Keep an accepted path: in every layer, sequence and KV head, row len + path[b][i] moves to row len + i for
+ * i < n[b] (entries of path outside 0..T - 1 and rows past max_seq stay where they are), and len_out[b] = len[b] + n[b],
+ * cut to max_seq (device int32 [batch]; cache->len itself is allowed). path [batch][T] and n as tasp_verify
+ * returns them, T <= TASP_TREE_MAX. Stream-ordered, capturable. Errors as tasp_seq_append. */
+tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, const int32_t* n,
+                            int32_t T, int32_t* len_out, void* stream);
+
 /* Plain streaming copy of `bytes` (multiple of 16) from src to dst (device, not overlapping):
  * the reference kernel whose counter readings calibrate memory-traffic measurements (the byte
  * ledger of appendix "FLOP and storage validation" checked against hardware counters).

@@ -33,6 +33,8 @@ EXPORTS = ["tasp_plan_workspace_bytes", "tasp_compile_plan", "tasp_plan_counts",
            "tasp_decode_step_timed",
            "tasp_profile_stage", "tasp_mask_workspace_bytes", "tasp_build_mask",
            "tasp_router_workspace_bytes", "tasp_route", "tasp_route_noalloc", "tasp_serve_turn", "tasp_copy_probe",
+           "tasp_seq_append", "tasp_seq_read", "tasp_tree_attention_workspace_bytes", "tasp_tree_attention",
+           "tasp_verify_workspace_bytes", "tasp_verify", "tasp_seq_commit",
            "tasp_status_string", "tasp_last_error"]
 
 
@@ -95,7 +97,28 @@ class tasp_router(C.Structure):
                 ("w2", C.c_void_p), ("b2", C.c_void_p), ("w3", C.c_void_p), ("b3", C.c_void_p)]
 
 
+class tasp_seq_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("len", C.c_void_p), ("type", C.c_int32), ("n_layers", C.c_int32), ("batch", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("max_seq", C.c_int32), ("head_dim", C.c_int32),
+                ("plan_sig", C.c_uint64)]
+
+
+class tasp_rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("seq", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class tasp_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("scaling", C.c_int32),
+                ("orig_len", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("mscale", C.c_double)]
+
+
 ROUTER_SCALARS = 11
+BF16, F32, INT8, E4M3 = 0, 1, 2, 3
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "wavelength": 2, "index": 3}
+TREE_MAX, SEQ_MAX_BATCH = 64, 256
 
 _lib = None
 
@@ -144,6 +167,13 @@ def load(path: str = LIB_PATH):
                             I32, C.POINTER(tasp_kv_cache), P, P, P, P, SZ, C.POINTER(I32),
                             C.POINTER(I32), P],
         "tasp_copy_probe": [P, P, SZ, P],
+        "tasp_seq_append": [P, I32, P, P, I32, I32, P, P, P, I32, P, P],
+        "tasp_seq_read": [P, I32, P, I32, I32, P, P, P],
+        "tasp_tree_attention_workspace_bytes": [P, I32, I32, I32, C.POINTER(SZ)],
+        "tasp_tree_attention": [P, I32, P, I32, I32, P, I32, C.c_double, I32, P, P, SZ, P],
+        "tasp_verify_workspace_bytes": [I32, I32, I32, C.POINTER(SZ)],
+        "tasp_verify": [P, P, P, P, P, I32, I32, I32, C.c_double, P, P, P, P, SZ, P],
+        "tasp_seq_commit": [P, P, P, I32, P, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -325,3 +355,46 @@ def tasp_serve_turn(router, task_plans, dense_plan, text_ptr, n_text, logprob_pt
 
 def tasp_copy_probe(dst_ptr, src_ptr, nbytes, stream):
     _check(load().tasp_copy_probe(dst_ptr, src_ptr, nbytes, stream))
+
+
+def _ref(struct):
+    """The address of a struct, or None."""
+    return None if struct is None else C.addressof(struct)
+
+
+def tasp_seq_append(cache, layer, rope, parent_ptr, T, act_type, q, k, v, n_q_heads, q_out, stream):
+    """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs."""
+    _check(load().tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, _ref(q), _ref(k),
+                                  _ref(v), n_q_heads, _ref(q_out), stream))
+
+
+def tasp_seq_read(cache, layer, first_ptr, n, out_type, k_out, v_out, stream):
+    _check(load().tasp_seq_read(_ref(cache), layer, first_ptr, n, out_type, _ref(k_out), _ref(v_out), stream))
+
+
+def tasp_tree_attention_workspace_bytes(cache, n_q_heads, T, max_len):
+    n = C.c_size_t()
+    _check(load().tasp_tree_attention_workspace_bytes(_ref(cache), n_q_heads, T, max_len, C.byref(n)))
+    return n.value
+
+
+def tasp_tree_attention(cache, layer, parent_ptr, T, act_type, q, n_q_heads, scale, max_len, out, ws_ptr,
+                        ws_bytes, stream):
+    _check(load().tasp_tree_attention(_ref(cache), layer, parent_ptr, T, act_type, _ref(q), n_q_heads, scale,
+                                      max_len, _ref(out), ws_ptr, ws_bytes, stream))
+
+
+def tasp_verify_workspace_bytes(batch, T, vocab):
+    n = C.c_size_t()
+    _check(load().tasp_verify_workspace_bytes(batch, T, vocab, C.byref(n)))
+    return n.value
+
+
+def tasp_verify(logits_ptr, tokens_ptr, u_ptr, parent_ptr, draft_ptr, batch, T, vocab, temperature, ids_ptr,
+                path_ptr, n_ptr, ws_ptr, ws_bytes, stream):
+    _check(load().tasp_verify(logits_ptr, tokens_ptr, u_ptr, parent_ptr, draft_ptr, batch, T, vocab,
+                              temperature, ids_ptr, path_ptr, n_ptr, ws_ptr, ws_bytes, stream))
+
+
+def tasp_seq_commit(cache, path_ptr, n_ptr, T, len_out_ptr, stream):
+    _check(load().tasp_seq_commit(_ref(cache), path_ptr, n_ptr, T, len_out_ptr, stream))

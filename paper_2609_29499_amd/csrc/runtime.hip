@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "seq.hpp"
 #include "tasp.h"
 
 struct tasp_plan_s;
@@ -1988,6 +1989,260 @@ tasp_status tasp_build_mask(const tasp_model_desc* desc, const float* head_score
   HIP_TRY(hipStreamSynchronize(s));
   if (word[0] & 1u) return fail(TASP_ERR_INVALID_ARG, "non-finite score");
   if (flops_spent) *flops_spent = word[1];
+  return TASP_OK;
+}
+
+// ---- sequences of their own lengths, trees of drafted tokens
+
+namespace {
+
+constexpr int64_t kMaxGrid = (int64_t(1) << 24) - 1;   // workgroups of 256 in one dimension of a launch
+
+tasp_status check_seq_cache(const tasp_seq_cache* c, int32_t layer) {
+  if (!c) return fail(TASP_ERR_INVALID_ARG, "cache is NULL");
+  if (c->type != TASP_BF16 && c->type != TASP_INT8 && c->type != TASP_E4M3)
+    return fail(TASP_ERR_INVALID_ARG, "cache type %d", c->type);
+  if (c->n_layers < 1 || c->batch < 1 || c->batch > TASP_SEQ_MAX_BATCH || c->n_kv_heads < 1 ||
+      c->n_kv_heads > 64 || c->max_seq < 1 || (c->head_dim != 64 && c->head_dim != 128) ||
+      int64_t(c->max_seq) * c->head_dim >= (int64_t(1) << 30))
+    return fail(TASP_ERR_SHAPE, "cache of %d layers, batch %d, %d heads of %d, %d rows", c->n_layers, c->batch,
+                c->n_kv_heads, c->head_dim, c->max_seq);
+  if (layer < 0 || layer >= c->n_layers) return fail(TASP_ERR_SHAPE, "layer %d of %d", layer, c->n_layers);
+  return TASP_OK;
+}
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+tasp_status check_seq_buffers(const tasp_seq_cache* c) {
+  if (!c->k || !c->v || !c->len) return fail(TASP_ERR_INVALID_ARG, "cache k / v / len is NULL");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(TASP_ERR_INVALID_ARG, "cache k / v is not 16-byte aligned");
+  if (c->type != TASP_BF16 && (!c->k_scale || !c->v_scale))
+    return fail(TASP_ERR_INVALID_ARG, "an 8-bit cache needs k_scale and v_scale");
+  if (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4) || !aligned(c->len, 4))
+    return fail(TASP_ERR_INVALID_ARG, "scales / len are not 4-byte aligned");
+  return TASP_OK;
+}
+
+tasp_status check_rows(const tasp_rows* r, int act, const char* what, tasp::SeqRows* out) {
+  if (act != TASP_BF16 && act != TASP_F32) return fail(TASP_ERR_INVALID_ARG, "type %d of %s", act, what);
+  if (!r || !r->p) return fail(TASP_ERR_INVALID_ARG, "%s is NULL", what);
+  const int64_t e = act == TASP_BF16 ? 8 : 4;
+  if (!aligned(r->p, 16) || r->seq % e || r->token % e || r->head % e)
+    return fail(TASP_ERR_INVALID_ARG, "rows of %s are not 16-byte aligned", what);
+  *out = {r->p, long(r->seq), long(r->token), long(r->head)};
+  return TASP_OK;
+}
+
+tasp::SeqLayer seq_layer(const tasp_seq_cache* c, int layer) {
+  const size_t rows = size_t(layer) * c->batch * c->n_kv_heads * c->max_seq;
+  const size_t at = rows * c->head_dim * (c->type == TASP_BF16 ? 2 : 1);
+  tasp::SeqLayer y{};
+  y.k = static_cast<char*>(c->k) + at;
+  y.v = static_cast<char*>(c->v) + at;
+  if (c->type != TASP_BF16) {
+    y.ks = c->k_scale + rows;
+    y.vs = c->v_scale + rows;
+  }
+  y.len = c->len; y.type = c->type; y.batch = c->batch; y.n_kv = c->n_kv_heads; y.S = c->max_seq; y.dh = c->head_dim;
+  return y;
+}
+
+tasp_status check_tree(const int32_t* parent, int32_t T, bool chains) {
+  if (T < 1 || (T > TASP_TREE_MAX && (parent || !chains)))
+    return fail(TASP_ERR_SHAPE, "%d nodes (a tree has 1..%d)", T, TASP_TREE_MAX);
+  if (!aligned(parent, 4)) return fail(TASP_ERR_INVALID_ARG, "parent is not 4-byte aligned");
+  return TASP_OK;
+}
+
+// rotation of the append kernel from a tasp_rope (checked); NULL: none
+tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
+  if (!r) return TASP_OK;
+  if (r->layout != TASP_ROPE_HALF && r->layout != TASP_ROPE_INTERLEAVED)
+    return fail(TASP_ERR_INVALID_ARG, "rope layout %d", r->layout);
+  if (r->rot_dim < 0 || r->rot_dim > dh || r->rot_dim % 16)
+    return fail(TASP_ERR_SHAPE, "rot_dim %d (a multiple of 16 up to %d)", r->rot_dim, dh);
+  if (r->scaling < TASP_ROPE_NONE || r->scaling > TASP_ROPE_INDEX)
+    return fail(TASP_ERR_INVALID_ARG, "rope scaling %d", r->scaling);
+  if (!(r->theta > 1.0) || !std::isfinite(r->theta) || !std::isfinite(r->mscale))
+    return fail(TASP_ERR_INVALID_ARG, "rope theta must be above 1, mscale finite");
+  if (r->scaling != TASP_ROPE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
+    return fail(TASP_ERR_INVALID_ARG, "rope factor must be positive");
+  if (r->scaling >= TASP_ROPE_WAVELENGTH &&
+      (!(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high) || r->orig_len < 1))
+    return fail(TASP_ERR_INVALID_ARG, "rope scaling needs 0 < low < high and orig_len >= 1");
+  constexpr double kTurn = 6.28318530717958647693;
+  const int n = r->rot_dim;
+  a->rot = n;
+  a->interleaved = r->layout == TASP_ROPE_INTERLEAVED;
+  a->mscale = r->mscale;
+  double lo = 0.0, hi = 0.0;
+  if (r->scaling == TASP_ROPE_INDEX) {
+    auto index = [&](double turns) { return n * std::log(r->orig_len / (kTurn * turns)) / (2.0 * std::log(r->theta)); };
+    lo = std::max(std::floor(index(r->high)), 0.0);
+    hi = std::min(std::ceil(index(r->low)), double(n - 1));
+  }
+  // f_i by repeated multiplication: 64 roundings of 1e-16 at most, and no power function per call and pair
+  const double step = n ? std::exp(-2.0 * std::log(r->theta) / n) : 1.0;
+  double f = 1.0;
+  for (int i = 0; i < n / 2; ++i, f *= step) {
+    double g = 1.0;                    // share of the unscaled frequency
+    if (r->scaling == TASP_ROPE_LINEAR) g = 0.0;
+    if (r->scaling == TASP_ROPE_WAVELENGTH) g = (r->orig_len * f / kTurn - r->low) / (r->high - r->low);
+    if (r->scaling == TASP_ROPE_INDEX) g = 1.0 - (i - lo) / std::max(hi - lo, 0.001);
+    g = std::min(1.0, std::max(0.0, g));
+    a->inv_freq[i] = r->scaling == TASP_ROPE_NONE ? f : f * (g + (1.0 - g) / r->factor);
+  }
+  return TASP_OK;
+}
+
+tasp_status tree_attn_args(const tasp_seq_cache* c, int32_t n_q, int32_t T, int32_t max_len, tasp::TreeAttnArgs* a) {
+  tasp_status st = check_tree(nullptr, T, false);
+  if (st != TASP_OK) return st;
+  if (n_q < 1 || n_q % c->n_kv_heads || n_q / c->n_kv_heads > 8)
+    return fail(TASP_ERR_SHAPE, "%d query heads over %d KV heads (1..8 per KV head)", n_q, c->n_kv_heads);
+  if (max_len < 0 || max_len > c->max_seq) return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_seq);
+  a->T = T; a->n_q = n_q; a->group = n_q / c->n_kv_heads; a->max_len = max_len;
+  return TASP_OK;
+}
+
+tasp_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (!ws && need) return fail(TASP_ERR_INVALID_ARG, "workspace is NULL");
+  if (!aligned(ws, kAlign)) return fail(TASP_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  if (have < need) return fail(TASP_ERR_WORKSPACE, "workspace %zu < %zu bytes", have, need);
+  return TASP_OK;
+}
+
+}  // namespace
+
+tasp_status tasp_seq_append(const tasp_seq_cache* cache, int32_t layer, const tasp_rope* rope,
+                            const int32_t* parent, int32_t T, int32_t act_type, const tasp_rows* q,
+                            const tasp_rows* k, const tasp_rows* v, int32_t n_q_heads,
+                            const tasp_rows* q_out, void* stream) {
+  tasp_status st;
+  tasp::SeqAppendArgs a{};
+  if ((st = check_seq_cache(cache, layer)) || (st = check_seq_buffers(cache)) || (st = check_tree(parent, T, true)) ||
+      (st = check_rows(k, act_type, "k", &a.k)) || (st = check_rows(v, act_type, "v", &a.v)))
+    return st;
+  if (T > cache->max_seq) return fail(TASP_ERR_SHAPE, "%d tokens into %d rows", T, cache->max_seq);
+  if (int64_t(T) * cache->batch > kMaxGrid) return fail(TASP_ERR_SHAPE, "%d tokens of %d sequences", T, cache->batch);
+  if (n_q_heads < 0 || n_q_heads > 512) return fail(TASP_ERR_SHAPE, "%d query heads", n_q_heads);
+  if (n_q_heads > 0) {
+    if ((st = check_rows(q, act_type, "q", &a.q)) || (st = check_rows(q_out, act_type, "q_out", &a.q_out))) return st;
+  } else if ((q && q->p) || (q_out && q_out->p)) {
+    return fail(TASP_ERR_INVALID_ARG, "q given with 0 query heads");
+  }
+  if ((st = rope_args(rope, cache->head_dim, &a))) return st;
+  a.c = seq_layer(cache, layer);
+  a.parent = parent; a.T = T; a.act = act_type; a.n_q = n_q_heads; a.n_kv = cache->n_kv_heads;
+  HIP_TRY(tasp::launch_seq_append(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int32_t* first,
+                          int32_t n, int32_t out_type, const tasp_rows* k_out,
+                          const tasp_rows* v_out, void* stream) {
+  tasp_status st;
+  tasp::SeqReadArgs a{};
+  if ((st = check_seq_cache(cache, layer)) || (st = check_seq_buffers(cache)) ||
+      (st = check_rows(k_out, out_type, "k_out", &a.k)) || (st = check_rows(v_out, out_type, "v_out", &a.v)))
+    return st;
+  if (n < 1) return fail(TASP_ERR_SHAPE, "%d rows", n);
+  if (!aligned(first, 4)) return fail(TASP_ERR_INVALID_ARG, "first is not 4-byte aligned");
+  a.c = seq_layer(cache, layer);
+  a.first = first; a.n = n; a.out_type = out_type;
+  HIP_TRY(tasp::launch_seq_read(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+tasp_status tasp_tree_attention_workspace_bytes(const tasp_seq_cache* cache, int32_t n_q_heads,
+                                                int32_t T, int32_t max_len, size_t* bytes) {
+  tasp_status st = check_seq_cache(cache, 0);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  tasp::TreeAttnArgs a{};
+  if ((st = tree_attn_args(cache, n_q_heads, T, max_len, &a))) return st;
+  a.c = seq_layer(cache, 0);
+  *bytes = tasp::tree_attn_workspace_bytes(a);
+  return TASP_OK;
+}
+
+tasp_status tasp_tree_attention(const tasp_seq_cache* cache, int32_t layer, const int32_t* parent,
+                                int32_t T, int32_t act_type, const tasp_rows* q, int32_t n_q_heads,
+                                double scale, int32_t max_len, const tasp_rows* out,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  tasp_status st;
+  tasp::TreeAttnArgs a{};
+  if ((st = check_seq_cache(cache, layer)) || (st = check_seq_buffers(cache)) || (st = check_tree(parent, T, false)) ||
+      (st = check_rows(q, act_type, "q", &a.q)) || (st = check_rows(out, act_type, "out", &a.o)) ||
+      (st = tree_attn_args(cache, n_q_heads, T, max_len, &a)))
+    return st;
+  if (!(scale > 0.0) || !std::isfinite(scale)) return fail(TASP_ERR_INVALID_ARG, "scale must be positive");
+  a.c = seq_layer(cache, layer);
+  a.parent = parent; a.act = act_type;
+  a.scale2 = float(scale * 1.44269504088896340736);
+  if ((st = check_workspace(workspace, workspace_bytes, tasp::tree_attn_workspace_bytes(a)))) return st;
+  a.ws = static_cast<float*>(workspace);
+  HIP_TRY(tasp::launch_tree_attn(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+namespace {
+
+tasp_status check_verify_shape(int32_t batch, int32_t T, int32_t vocab) {
+  if (batch < 1 || batch > TASP_SEQ_MAX_BATCH || T < 1 || T > TASP_TREE_MAX || vocab < 1 || vocab > (1 << 24))
+    return fail(TASP_ERR_SHAPE, "batch %d (1..%d), %d nodes (1..%d), vocabulary %d (1..2^24)", batch,
+                TASP_SEQ_MAX_BATCH, T, TASP_TREE_MAX, vocab);
+  return TASP_OK;
+}
+
+}  // namespace
+
+tasp_status tasp_verify_workspace_bytes(int32_t batch, int32_t T, int32_t vocab, size_t* bytes) {
+  tasp_status st = check_verify_shape(batch, T, vocab);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = tasp::verify_workspace_bytes(batch, T, vocab);
+  return TASP_OK;
+}
+
+tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float* u,
+                        const int32_t* parent, const float* draft_logits, int32_t batch, int32_t T,
+                        int32_t vocab, double temperature, int32_t* ids, int32_t* path, int32_t* n,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  tasp_status st = check_verify_shape(batch, T, vocab);
+  if (st) return st;
+  if (!logits || !tokens || !ids || !path || !n)
+    return fail(TASP_ERR_INVALID_ARG, "logits / tokens / ids / path / n is NULL");
+  if (!(temperature >= 0.0) || !std::isfinite(temperature) || (temperature > 0.0 && !std::isfinite(1.0 / temperature)))
+    return fail(TASP_ERR_INVALID_ARG, "temperature must be 0 or positive");
+  if (temperature > 0.0 && !u) return fail(TASP_ERR_INVALID_ARG, "u is NULL");
+  if (draft_logits && parent) return fail(TASP_ERR_INVALID_ARG, "draft_logits go with chains (parent NULL)");
+  for (const void* p : {(const void*)logits, (const void*)tokens, (const void*)u, (const void*)parent,
+                        (const void*)draft_logits, (const void*)ids, (const void*)path, (const void*)n})
+    if (!aligned(p, 4)) return fail(TASP_ERR_INVALID_ARG, "an array is not 4-byte aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, tasp::verify_workspace_bytes(batch, T, vocab)))) return st;
+  tasp::VerifyArgs a{};
+  a.logits = logits; a.draft = draft_logits; a.tokens = tokens; a.u = u; a.parent = parent;
+  a.B = batch; a.T = T; a.V = vocab; a.inv_temp = temperature > 0.0 ? 1.0 / temperature : 0.0;
+  a.ids = ids; a.path = path; a.n = n; a.ws = workspace;
+  HIP_TRY(tasp::launch_verify(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, const int32_t* n,
+                            int32_t T, int32_t* len_out, void* stream) {
+  tasp_status st;
+  if ((st = check_seq_cache(cache, 0)) || (st = check_seq_buffers(cache)) || (st = check_tree(nullptr, T, false)))
+    return st;
+  if (!path || !n || !len_out) return fail(TASP_ERR_INVALID_ARG, "path / n / len_out is NULL");
+  if (!aligned(path, 4) || !aligned(n, 4) || !aligned(len_out, 4))
+    return fail(TASP_ERR_INVALID_ARG, "path / n / len_out is not 4-byte aligned");
+  if (int64_t(cache->n_layers) * cache->batch * cache->n_kv_heads > kMaxGrid)
+    return fail(TASP_ERR_SHAPE, "%d layers of %d sequences", cache->n_layers, cache->batch);
+  tasp::SeqCommitArgs a{};
+  a.c = seq_layer(cache, 0); a.n_layers = cache->n_layers;
+  a.path = path; a.ld = T; a.n = n; a.len_out = len_out;
+  HIP_TRY(tasp::launch_seq_commit(a, static_cast<hipStream_t>(stream)));
   return TASP_OK;
 }
 

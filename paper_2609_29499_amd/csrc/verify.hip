@@ -1,0 +1,471 @@
+// Verification of drafted tokens against the target's distributions at given random numbers.
+//
+// p = softmax(l / temperature) of each node's logits. From node 0 the children of the current node are
+// tried in node order: without draft logits child c with token x_c is accepted when
+// u_c (Z - sum of e(x) over the earlier children's distinct tokens) < e(x_c), e = exp((l - max) / temperature),
+// Z its sum, a token tried before counting 0 (the target's distribution without what was refused); with
+// draft logits (a chain) when u_c q(x_c) < p(x_c). Where nothing is accepted, the last token is the lowest
+// x whose cumulative weight exceeds u_0 times the total, of e without the children's tokens, or of
+// max(p - q, 0). Everything is held in 64 bits: a vocabulary has 10^5 borders between two tokens'
+// shares, and sums with an error of 10^-7 would move one of them across u_0 every few hundred calls.
+//
+// Launches: verify_stats_kernel (one chunk of 4096 logits per workgroup, held in registers: maximum,
+// its lowest index and sum of e) over all rows of the tree and the draft; then verify_walk_kernel,
+// which walks the tree and takes the last token. Without draft logits the chunks' weights follow
+// from the first launch, so one workgroup per sequence reads one chunk again; with them
+// each workgroup of a grid over the chunks walks the (short) chain for itself, sums its chunk of
+// max(p - q, 0), and the last to finish takes the token. Bound by the read of the logits.
+#include <algorithm>
+
+#include "device_common.hpp"
+#include "seq.hpp"
+
+namespace tasp {
+namespace {
+
+constexpr int kVChunk = 4096;          // logits per workgroup of the first launch
+constexpr int kVU = kVChunk / kBlock;  // logits per thread
+
+struct ChunkStat {
+  double z;                            // sum of exp((l - m) / temperature) over the chunk
+  float m;                             // its maximum
+  int at;                              // lowest index of it
+};
+
+// exp(z) for z <= 0: 2^n exp(r), |r| <= ln 2 / 2, by the Taylor polynomial of degree 11 (remainder below
+// 0.35^12 / 12! = 7e-15 of the result); z below -800 gives 0
+__device__ __forceinline__ double exp_neg(double z) {
+  z = fmax(z, -800.0);
+  const double n = rint(z * 1.44269504088896340736);
+  // ln 2 in two parts, the first with its last 21 bits clear: n times it is exact
+  double r = fma(-n, 6.93147180369123816490e-01, z);
+  r = fma(-n, 1.90821492927058770002e-10, r);
+  double p = 1.0 / 39916800.0;
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  return ldexp(p, int(n));
+}
+// exp((l - m) / temperature) of a logit whose row's maximum is m: NaN counts as -inf, a row without
+// anything above -inf has no weight, +inf shares it evenly
+__device__ __forceinline__ double weight(float l, float m, double inv_temp) {
+  if (!(l > -INFINITY)) return 0.0;
+  return l == m ? 1.0 : exp_neg((double(l) - double(m)) * inv_temp);
+}
+
+__device__ __forceinline__ double wave_sum_d(double v) {
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) v += __shfl_xor(v, k, kWave);
+  return v;
+}
+
+// Grid (chunks, rows). rows 0 .. n_target - 1 are the target's, the others the draft's. Also clears
+// the next launch's counters (cnt[B]).
+__global__ __launch_bounds__(kBlock) void verify_stats_kernel(VerifyArgs a, ChunkStat* stat, int* cnt) {
+  __shared__ float sm[4];
+  __shared__ int si[4];
+  __shared__ double sz[4];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int c = blockIdx.x, r = blockIdx.y, nt = a.B * a.T;
+  const float* row = r < nt ? a.logits + size_t(r) * a.V : a.draft + size_t(r - nt) * a.V;
+  if (c == 0 && r < a.B && tid == 0) cnt[r] = 0;
+  const int k0 = c * kVChunk + tid;
+  float x[kVU];
+#pragma unroll
+  for (int i = 0; i < kVU; ++i) {
+    const int k = k0 + i * kBlock;
+    x[i] = k < a.V ? row[k] : -INFINITY;
+  }
+  float m = -INFINITY;
+  int at = 0x7fffffff;
+#pragma unroll
+  for (int i = 0; i < kVU; ++i)
+    if (x[i] > m) {
+      m = x[i];
+      at = k0 + i * kBlock;
+    }
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) {
+    const float om = __shfl_xor(m, k, kWave);
+    const int oa = __shfl_xor(at, k, kWave);
+    if (om > m || (om == m && oa < at)) {
+      m = om;
+      at = oa;
+    }
+  }
+  if ((tid & 63) == 0) {
+    sm[wave] = m;
+    si[wave] = at;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (sm[w] > m || (sm[w] == m && si[w] < at)) {
+      m = sm[w];
+      at = si[w];
+    }
+  double z = 0.0;
+  if (a.inv_temp > 0.0) {
+#pragma unroll
+    for (int i = 0; i < kVU; ++i) z += weight(x[i], m, a.inv_temp);
+    z = wave_sum_d(z);
+    if ((tid & 63) == 0) sz[wave] = z;
+    __syncthreads();
+    z = (sz[0] + sz[1]) + (sz[2] + sz[3]);
+  }
+  if (tid == 0) stat[size_t(r) * gridDim.x + c] = {z, m, at};
+}
+
+struct RowStat {
+  double z;
+  float m;
+  int at;
+};
+
+struct WalkSmem {
+  RowStat row[2 * kTreeMax];           // the target's rows, then the draft's
+  double e[kTreeMax];                  // weight of a node's token at its parent
+  int token[kTreeMax];
+  unsigned long long children;         // of the last node
+  int last, n;
+  uint32_t gone[kVChunk / 32];         // tokens of a chunk that were refused
+  double part[kBlock / kWave + 1];
+  int cand[kBlock / kWave];
+  int found, is_last;
+  double base;
+};
+
+// Maxima and sums of rows `first` .. `first` + n - 1 from their chunks: four threads per row
+__device__ __forceinline__ void row_stats(const VerifyArgs& a, const ChunkStat* stat, size_t first, int n, int chunks, RowStat* out) {
+  const int t = threadIdx.x >> 2, q = threadIdx.x & 3;
+  if (t >= n) return;                  // (whole groups of four lanes)
+  const ChunkStat* s = stat + (first + t) * chunks;
+  float m = -INFINITY;
+  int at = 0x7fffffff;
+  for (int c = q; c < chunks; c += 4)
+    if (s[c].m > m) {
+      m = s[c].m;
+      at = s[c].at;
+    }
+#pragma unroll
+  for (int k = 1; k < 4; k <<= 1) {
+    const float om = __shfl_xor(m, k, kWave);
+    const int oa = __shfl_xor(at, k, kWave);
+    if (om > m || (om == m && oa < at)) {
+      m = om;
+      at = oa;
+    }
+  }
+  double z = 0.0;
+  if (a.inv_temp > 0.0)
+    for (int c = q; c < chunks; c += 4) z += s[c].z * weight(s[c].m, m, a.inv_temp);
+  z += __shfl_xor(z, 1, kWave);
+  z += __shfl_xor(z, 2, kWave);
+  if (q == 0) out[t] = {z, m, at};
+}
+
+// The tree's walk by the first wave, a node per lane; path and n are written when `out` is set.
+__device__ __forceinline__ void walk(const VerifyArgs& a, const ChunkStat* stat, int b, int chunks, WalkSmem& sm, bool out) {
+  const int tid = threadIdx.x, T = a.T;
+  const bool greedy = a.inv_temp == 0.0, draft = a.draft && !greedy;
+  row_stats(a, stat, size_t(b) * T, T, chunks, sm.row);
+  if (draft) row_stats(a, stat, size_t(a.B) * T + size_t(b) * (T - 1), T - 1, chunks, sm.row + kTreeMax);
+  __syncthreads();
+  if (tid < kWave) {
+    const int t = tid;
+    const TreeNode nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, T, t);
+    const bool node = nd.anc != 0 && nd.parent >= 0;
+    const int up = node ? nd.parent : -1;
+    const int x = t < T ? a.tokens[size_t(b) * T + t] : -1;
+    const bool word = node && x >= 0 && x < a.V;
+    const double u = t < T && !greedy ? double(a.u[size_t(b) * T + t]) : 0.0;
+    const RowStat rs = sm.row[max(up, 0)];
+    double e = 0.0, q = 0.0;
+    if (word && greedy) e = rs.at == x ? 1.0 : 0.0;
+    if (word && !greedy) e = weight(a.logits[(size_t(b) * T + up) * a.V + x], rs.m, a.inv_temp);
+    if (word && draft) {
+      const RowStat ds = sm.row[kTreeMax + up];
+      q = weight(a.draft[(size_t(b) * (T - 1) + up) * a.V + x], ds.m, a.inv_temp);
+      q = ds.z > 0.0 ? q / ds.z : 0.0;
+    }
+    bool good;
+    unsigned long long older = 0;      // earlier children of the same parent
+    if (draft) {
+      good = word && rs.z > 0.0 && u * q < e / rs.z;
+    } else {
+      bool again = false;              // the token was tried before
+      for (int j = 0; j < T; ++j) {
+        const int pj = __builtin_amdgcn_readlane(up, j), xj = __builtin_amdgcn_readlane(x, j);
+        if (node && j < t && pj == up) {
+          older |= 1ull << j;
+          again |= xj == x;
+        }
+      }
+      if (again) e = 0.0;
+      double before = 0.0;
+      for (int j = 0; j < T; ++j) {
+        const double ej = __shfl(e, j, kWave);
+        if ((older >> j) & 1) before += ej;
+      }
+      good = word && u * ((greedy ? 1.0 : rs.z) - before) < e;
+    }
+    sm.e[t] = e;
+    sm.token[t] = x;
+    const unsigned long long goods = __ballot(good);
+    const bool chosen = good && !(older & goods);
+    const unsigned long long taken = __ballot(chosen) | 1ull;
+    const bool on = nd.anc != 0 && (nd.anc & 1) && !(nd.anc & ~taken);
+    const unsigned long long path = __ballot(on);
+    // node 0 absent (its parent is not -1): nothing is on the path and the last node is 0
+    const int n = max(1, __popcll(path)), last = path ? 63 - __clzll(path) : 0;
+    const unsigned long long kids = __ballot(node && up == last);
+    if (t == 0) {
+      sm.n = n;
+      sm.last = last;
+      sm.children = kids;
+    }
+    if (out && t < T) {
+      const int before = __popcll(path & ((1ull << t) - 1));
+      int* po = a.path + size_t(b) * T;
+      int* io = a.ids + size_t(b) * T;
+      if (on || (t == 0 && !path)) po[before] = t;
+      if (on && t > 0) io[before - 1] = x;
+      if (t >= n) {
+        po[t] = -1;
+        io[t] = -1;
+      }
+      if (t == 0) a.n[b] = n;
+    }
+  }
+  __syncthreads();
+}
+
+// The token of a chunk whose cumulative weight first exceeds `target`, the weights before it being
+// `base`; also the chunk's last token with a weight. w(k): weight of token k. Thread t holds tokens
+// kVU t .. + kVU - 1 of the chunk, so sums run in token order. found: -1 none, else the token;
+// tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
+template <class W>
+__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem& sm, W&& w, int* found, int* tail) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int k0 = c * kVChunk + tid * kVU;
+  double v[kVU], sum = 0.0;
+  int end = -1;
+#pragma unroll
+  for (int i = 0; i < kVU; ++i) {
+    v[i] = k0 + i < a.V ? w(k0 + i) : 0.0;
+    sum += v[i];
+    if (v[i] > 0.0) end = k0 + i;
+  }
+  double inc = sum;
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) {
+    const double o = __shfl_up(inc, k, kWave);
+    if (lane >= k) inc += o;
+  }
+  __syncthreads();
+  if (lane == 63) sm.part[wave] = inc;
+  __syncthreads();
+  double cum = base + (inc - sum);
+  for (int j = 0; j < wave; ++j) cum += sm.part[j];
+  const double total = base + ((sm.part[0] + sm.part[1]) + (sm.part[2] + sm.part[3]));
+  int hit = 0x7fffffff;
+#pragma unroll
+  for (int i = 0; i < kVU; ++i) {
+    cum += v[i];
+    if (v[i] > 0.0 && cum > target && hit == 0x7fffffff) hit = k0 + i;
+  }
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) {
+    hit = min(hit, __shfl_xor(hit, k, kWave));
+    end = max(end, __shfl_xor(end, k, kWave));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    sm.cand[wave] = hit;
+    sm.gone[wave] = uint32_t(end);     // (the mask has been read)
+  }
+  __syncthreads();
+  hit = min(min(sm.cand[0], sm.cand[1]), min(sm.cand[2], sm.cand[3]));
+  end = max(max(int(sm.gone[0]), int(sm.gone[1])), max(int(sm.gone[2]), int(sm.gone[3])));
+  __syncthreads();
+  *found = hit == 0x7fffffff ? -1 : hit;
+  *tail = end;
+  return total;
+}
+
+// The chunk's refused tokens as a bit mask (none: empty)
+__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem& sm, bool any) {
+  for (int i = threadIdx.x; i < kVChunk / 32; i += kBlock) sm.gone[i] = 0;
+  __syncthreads();
+  const int t = threadIdx.x;
+  if (any && t < a.T && ((sm.children >> t) & 1)) {
+    const int k = sm.token[t] - c * kVChunk;
+    if (k >= 0 && k < kVChunk && sm.token[t] < a.V) atomicOr(&sm.gone[k >> 5], 1u << (k & 31));
+  }
+  __syncthreads();
+}
+
+// Takes the last token of sequence b by the whole workgroup: chunk_weight(c) is the weight of chunk c
+// (any thread may ask), w as for scan_chunk after mark_gone.
+template <class CW, class W>
+__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem& sm, bool remove, CW&& chunk_weight, W&& w) {
+  const int tid = threadIdx.x;
+  // the chunk in which the cumulative weight passes the target: by the first wave, chunk sums in order
+  if (tid < kWave) {
+    double total = 0.0;
+    for (int c0 = 0; c0 < chunks; c0 += kWave) total += wave_sum_d(c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0);
+    const double target = double(a.u[size_t(b) * a.T]) * total;
+    double base = 0.0;
+    int at = -1;
+    double before = 0.0;
+    for (int c0 = 0; c0 < chunks && at < 0; c0 += kWave) {
+      const double mine = c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0;
+      double inc = mine;
+#pragma unroll
+      for (int k = 1; k < kWave; k <<= 1) {
+        const double o = __shfl_up(inc, k, kWave);
+        if (tid >= k) inc += o;
+      }
+      const unsigned long long over = __ballot(base + inc > target && mine > 0.0);
+      if (over) {
+        const int l = __ffsll((long long)over) - 1;
+        at = c0 + l;
+        before = base + __shfl(inc - mine, l, kWave);
+      }
+      base += __shfl(inc, 63, kWave);
+    }
+    if (tid == 0) {
+      sm.found = total > 0.0 ? max(at, 0) : -1;
+      sm.base = before;
+      sm.part[kBlock / kWave] = target;
+    }
+  }
+  __syncthreads();
+  const int c_at = sm.found;
+  double base = sm.base;
+  const double target = sm.part[kBlock / kWave];
+  __syncthreads();
+  if (c_at < 0) return -1;             // nothing has a weight
+  int best = -1;                       // the last token with a weight, should rounding leave the target unreached
+  for (int c = c_at; c < chunks; ++c) {
+    int found, tail;
+    mark_gone(a, c, sm, remove);
+    base = scan_chunk(a, c, base, target, sm, w, &found, &tail);
+    if (found >= 0) return found;
+    if (tail >= 0) best = tail;
+  }
+  for (int c = c_at - 1; c >= 0 && best < 0; --c) {
+    int found, tail;
+    mark_gone(a, c, sm, remove);
+    scan_chunk(a, c, 0.0, INFINITY, sm, w, &found, &tail);
+    best = tail;
+  }
+  return best;
+}
+
+// Grid (1 or chunks, B): see the head of the file.
+__global__ __launch_bounds__(kBlock) void verify_walk_kernel(VerifyArgs a, const ChunkStat* stat, double* sums, int* cnt, int chunks) {
+  __shared__ WalkSmem sm;
+  const int tid = threadIdx.x, b = blockIdx.y, T = a.T;
+  const bool greedy = a.inv_temp == 0.0;
+  walk(a, stat, b, chunks, sm, blockIdx.x == 0);
+  const int last = sm.last, slot = sm.n - 1;
+  int* out = a.ids + size_t(b) * T + slot;
+  const RowStat rs = sm.row[last];
+  if (greedy) {
+    if (tid == 0) *out = rs.m > -INFINITY ? rs.at : -1;
+    return;
+  }
+  const size_t r = size_t(b) * T + last;
+  const float* row = a.logits + r * a.V;
+  const ChunkStat* st = stat + r * chunks;
+  const bool kids = sm.children != 0;
+  auto plain_sum = [&](int c) { return st[c].z * weight(st[c].m, rs.m, a.inv_temp); };
+  auto plain = [&](int k) { return weight(row[k], rs.m, a.inv_temp); };
+  if (!a.draft) {
+    // e without the children's tokens: what they weigh is taken off their chunks
+    auto left_sum = [&](int c) {
+      double z = plain_sum(c);
+      if (kids)
+        for (int t = 0; t < T; ++t)
+          if (((sm.children >> t) & 1) && sm.token[t] >= 0 && sm.token[t] / kVChunk == c) z -= sm.e[t];
+      return fmax(z, 0.0);
+    };
+    auto left = [&](int k) {
+      const int i = k % kVChunk;
+      return ((sm.gone[i >> 5] >> (i & 31)) & 1) ? 0.0 : plain(k);
+    };
+    int x = take(a, b, chunks, sm, kids, left_sum, left);
+    if (x < 0) x = take(a, b, chunks, sm, false, plain_sum, plain);
+    if (tid == 0) *out = x;
+    return;
+  }
+  // max(p - q, 0) at a chain's refused token, p behind its end
+  const RowStat ds = kids ? sm.row[kTreeMax + last] : RowStat{0.0, 0.0f, 0};
+  const float* drow = a.draft + (size_t(b) * (T - 1) + (kids ? last : 0)) * a.V;
+  const double pz = rs.z > 0.0 ? 1.0 / rs.z : 0.0, qz = ds.z > 0.0 ? 1.0 / ds.z : 0.0;
+  auto rest = [&](int k) {
+    const double p = weight(row[k], rs.m, a.inv_temp) * pz;
+    return kids ? fmax(p - weight(drow[k], ds.m, a.inv_temp) * qz, 0.0) : p;
+  };
+  const int c = blockIdx.x;
+  double z = 0.0;
+#pragma unroll
+  for (int i = 0; i < kVU; ++i) {
+    const int k = c * kVChunk + i * kBlock + tid;
+    if (k < a.V) z += rest(k);
+  }
+  z = wave_sum_d(z);
+  if ((tid & 63) == 0) sm.part[tid >> 6] = z;
+  __syncthreads();
+  const __amdgpu_buffer_rsrc_t rp = make_rsrc(sums + size_t(b) * chunks, uint32_t(chunks) * 8u);
+  if (tid == 0) {
+    z = (sm.part[0] + sm.part[1]) + (sm.part[2] + sm.part[3]);
+    buf_store8_device(__builtin_bit_cast(int2, z), rp, uint32_t(c) * 8u);
+    __builtin_amdgcn_s_waitcnt(0);                      // the sum is at the coherence point
+    sm.is_last = __hip_atomic_fetch_add(cnt + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
+  }
+  __syncthreads();
+  if (!sm.is_last) return;
+  auto rest_sum = [&](int j) { return __builtin_bit_cast(double, buf_load8_device(rp, uint32_t(j) * 8u)); };
+  int x = take(a, b, chunks, sm, false, rest_sum, rest);
+  if (x < 0) x = take(a, b, chunks, sm, false, plain_sum, plain);
+  if (tid == 0) *out = x;
+}
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t verify_workspace_bytes(int B, int T, int V) {
+  const size_t chunks = size_t(V + kVChunk - 1) / kVChunk;
+  return up256(size_t(B) * (2 * T - 1) * chunks * sizeof(ChunkStat)) + up256(size_t(B) * chunks * 8) + up256(size_t(B) * 4);
+}
+
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
+  const int chunks = (a.V + kVChunk - 1) / kVChunk;
+  const bool draft = a.draft && a.T > 1 && a.inv_temp > 0.0;
+  const int rows = a.B * a.T + (draft ? a.B * (a.T - 1) : 0);
+  char* ws = static_cast<char*>(a.ws);
+  ChunkStat* stat = reinterpret_cast<ChunkStat*>(ws);
+  ws += up256(size_t(a.B) * (2 * a.T - 1) * chunks * sizeof(ChunkStat));
+  double* sums = reinterpret_cast<double*>(ws);
+  ws += up256(size_t(a.B) * chunks * 8);
+  VerifyArgs v = a;
+  if (!draft) v.draft = nullptr;
+  hipLaunchKernelGGL(verify_stats_kernel, dim3(chunks, rows), dim3(kBlock), 0, s, v, stat, reinterpret_cast<int*>(ws));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(verify_walk_kernel, dim3(draft ? chunks : 1, a.B), dim3(kBlock), 0, s, v, stat, sums, reinterpret_cast<int*>(ws), chunks);
+  return hipGetLastError();
+}
+
+}  // namespace tasp

@@ -326,3 +326,195 @@ class Router:
             cache.struct, out.data_ptr(), scratch[0].data_ptr(), scratch[1].data_ptr(), base, nb,
             stream if stream is not None else current_stream())
         return c, reused, out
+
+
+# ------------------------------------------- sequences of their own lengths, drafted tokens
+
+_SEQ_TYPES = {torch.bfloat16: B.BF16, torch.float32: B.F32, torch.int8: B.INT8, torch.float8_e4m3fn: B.E4M3}
+
+
+class _On:
+    """The call's stream on the tensors' device: the current stream of that device unless one is given, and
+    that device current while the call launches."""
+
+    def __init__(self, t, stream):
+        self.dev = t.device.index
+        self.stream = stream if stream is not None else C.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+    def __enter__(self):
+        self.was = torch.cuda.current_device()
+        if self.was != self.dev:
+            torch.cuda.set_device(self.dev)
+        return self.stream
+
+    def __exit__(self, *_):
+        if self.was != self.dev:
+            torch.cuda.set_device(self.was)
+
+
+def _same_device(t, *others):
+    for o in others:
+        if o is not None and o.device != t.device:
+            raise ValueError(f"tensors on {t.device} and {o.device}")
+    if t.device.type != "cuda":
+        raise ValueError(f"tensors on {t.device}: a GPU is needed")
+
+
+def _ptr(t, shape, dtype, what):
+    """Address of a contiguous tensor of the given shape and type; None for None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(t, shape, dtype, what, order=(0, 1, 2)):
+    """tasp_rows of a tensor [.., .., .., head_dim]: `order` names its sequence, token and head axes."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.stride(3) != 1:
+        raise ValueError(f"{what} must be a {dtype} tensor of {tuple(shape)} with contiguous heads, not {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    # (the stride of an axis of one is never used, and may be anything)
+    st = [st[i] if t.shape[i] > 1 else 0 for i in order]
+    return B.tasp_rows(t.data_ptr(), *st)
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor of the call's stream: the current one of the device, or the raw stream given."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    raw = stream.value if isinstance(stream, C.c_void_p) else stream
+    with torch.cuda.stream(torch.cuda.ExternalStream(raw or 0, device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(nbytes, device, stream=None):
+    t = _empty(nbytes + 256, torch.uint8, device, stream)
+    return t, t.data_ptr() + (-t.data_ptr()) % 256, nbytes
+
+
+class SeqCache:
+    """A cache whose sequences have their own lengths: k, v ``[L][B][Hkv][S][dh]`` as bfloat16, int8 or
+    float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch."""
+
+    def __init__(self, k, v, length, k_scale=None, v_scale=None):
+        if k.dtype not in (torch.bfloat16, torch.int8, torch.float8_e4m3fn) or k.dim() != 5:
+            raise ValueError(f"k must be a bfloat16, int8 or float8_e4m3fn tensor [L][B][Hkv][S][dh], not {k.dtype} {tuple(k.shape)}")
+        _same_device(k, v, length, k_scale, v_scale)
+        self.k, self.v, self.len, self.k_scale, self.v_scale = k, v, length, k_scale, v_scale
+        wide = k.dtype == torch.bfloat16
+        if wide == (k_scale is not None) or wide == (v_scale is not None):
+            raise ValueError("scales go with caches in 8 bits, and only with them")
+        self.n_layers, self.batch, self.n_kv, self.max_seq, self.dh = k.shape
+        self.struct = B.tasp_seq_cache(
+            _ptr(k, k.shape, k.dtype, "k"), _ptr(v, k.shape, k.dtype, "v"),
+            _ptr(k_scale, k.shape[:4], torch.float32, "k_scale"), _ptr(v_scale, k.shape[:4], torch.float32, "v_scale"),
+            _ptr(length, (self.batch,), torch.int32, "len"), _SEQ_TYPES[k.dtype], *k.shape, 0)
+
+    @classmethod
+    def empty(cls, n_layers, batch, n_kv_heads, max_seq, head_dim, dtype=torch.int8, device="cuda"):
+        """A cache of empty sequences."""
+        shape = (n_layers, batch, n_kv_heads, max_seq, head_dim)
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        sc = [None, None] if dtype == torch.bfloat16 else [torch.zeros(shape[:4], device=device) for _ in range(2)]
+        return cls(k, v, torch.zeros(batch, dtype=torch.int32, device=device), *sc)
+
+    def _parent(self, parent, T):
+        return _ptr(parent, (self.batch, T), torch.int32, "parent")
+
+
+class Rope:
+    """Rotary positions (tasp_rope): layout "half" or "interleaved", scaling "none", "linear", "wavelength" or "index"."""
+
+    def __init__(self, layout="half", rot_dim=128, theta=500000.0, scaling="none", factor=1.0, low=1.0, high=4.0,
+                 orig_len=8192, mscale=1.0):
+        self.struct = B.tasp_rope(B.ROPE_LAYOUTS[layout], rot_dim, B.ROPE_SCALINGS[scaling], orig_len, theta, factor,
+                                  low, high, mscale)
+
+
+def seq_append(cache, layer, q, k, v, rope=None, parent=None, q_out=None, stream=None):
+    """Write k, v ``[B][T][Hkv][dh]`` behind the sequences (their lengths stay) and return q ``[B][T][Hq][dh]``
+    rotated (None without queries). Any strides whose rows are 16-byte aligned; bfloat16 or float32."""
+    _same_device(cache.k, q, k, v, parent, q_out)
+    T = k.shape[1]
+    kv = (cache.batch, T, cache.n_kv, cache.dh)
+    qs = os_ = None
+    n_q = 0
+    if q is not None:
+        n_q = q.shape[2]
+        if q_out is None:
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
+        qs = _rows(q, (cache.batch, T, n_q, cache.dh), k.dtype, "q")
+        os_ = _rows(q_out, q.shape, k.dtype, "q_out")
+    with _On(cache.k, stream) as s:
+        B.tasp_seq_append(cache.struct, layer, None if rope is None else rope.struct, cache._parent(parent, T), T,
+                          _SEQ_TYPES[k.dtype], qs, _rows(k, kv, k.dtype, "k"), _rows(v, kv, k.dtype, "v"), n_q, os_, s)
+    return q_out
+
+
+def seq_read(cache, layer, n, first=None, dtype=torch.bfloat16, out=None, stream=None):
+    """(k, v) ``[B][Hkv][n][dh]``: rows first .. first + n - 1 (device int32 [B]; None: 0) as values."""
+    shape = (cache.batch, cache.n_kv, n, cache.dh)
+    k, v = out if out is not None else (_empty(shape, dtype, cache.k.device, stream) for _ in range(2))
+    _same_device(cache.k, first, k, v)
+    with _On(cache.k, stream) as s:
+        B.tasp_seq_read(cache.struct, layer, _ptr(first, (cache.batch,), torch.int32, "first"), n, _SEQ_TYPES[k.dtype],
+                        _rows(k, shape, k.dtype, "k", (0, 2, 1)), _rows(v, shape, k.dtype, "v", (0, 2, 1)), s)
+    return k, v
+
+
+def tree_attention_workspace(cache, n_q_heads, T, max_len=None, stream=None):
+    """A workspace for tree_attention calls of this shape (any layer)."""
+    n = B.tasp_tree_attention_workspace_bytes(cache.struct, n_q_heads, T, cache.max_seq if max_len is None else max_len)
+    return _workspace(n, cache.k.device, stream)
+
+
+def tree_attention(cache, layer, q, parent=None, scale=None, max_len=None, out=None, workspace=None, stream=None):
+    """Attention of the appended nodes' queries ``[B][T][Hq][dh]`` over their sequences and ancestors. max_len: the
+    largest length expected; workspace: of tree_attention_workspace with the same arguments (else one of the call's own)."""
+    _same_device(cache.k, q, parent, out)
+    T, n_q = q.shape[1:3]
+    shape = (cache.batch, T, n_q, cache.dh)
+    if out is None:
+        out = _empty(shape, q.dtype, q.device, stream)
+    if max_len is None:
+        max_len = cache.max_seq
+    ws = workspace if workspace is not None else tree_attention_workspace(cache, n_q, T, max_len, stream)
+    with _On(cache.k, stream) as s:
+        B.tasp_tree_attention(cache.struct, layer, cache._parent(parent, T), T, _SEQ_TYPES[q.dtype],
+                              _rows(q, shape, q.dtype, "q"), n_q, cache.dh ** -0.5 if scale is None else scale, max_len,
+                              _rows(out, shape, q.dtype, "out"), ws[1], ws[2], s)
+    return out
+
+
+def verify_workspace(batch, T, vocab, device="cuda", stream=None):
+    """A workspace for verify calls of this shape."""
+    return _workspace(B.tasp_verify_workspace_bytes(batch, T, vocab), device, stream)
+
+
+def verify(logits, tokens, u, parent=None, draft_logits=None, temperature=1.0, workspace=None, stream=None):
+    """Verify drafted tokens int32 ``[B][T]`` (node 0: the text's last token) against float32 logits ``[B][T][V]``
+    with random numbers u ``[B][T]``. Returns (ids, path, n): the emitted tokens and the accepted nodes, -1 behind them."""
+    _same_device(logits, tokens, u, parent, draft_logits)
+    nb, T, V = logits.shape
+    ids, path = (_empty((nb, T), torch.int32, logits.device, stream) for _ in range(2))
+    n = _empty(nb, torch.int32, logits.device, stream)
+    ws = workspace if workspace is not None else verify_workspace(nb, T, V, logits.device, stream)
+    with _On(logits, stream) as s:
+        B.tasp_verify(_ptr(logits, (nb, T, V), torch.float32, "logits"), _ptr(tokens, (nb, T), torch.int32, "tokens"),
+                      _ptr(u, (nb, T), torch.float32, "u"), _ptr(parent, (nb, T), torch.int32, "parent"),
+                      _ptr(draft_logits, (nb, T - 1, V), torch.float32, "draft_logits"), nb, T, V, temperature,
+                      ids.data_ptr(), path.data_ptr(), n.data_ptr(), ws[1], ws[2], s)
+    return ids, path, n
+
+
+def seq_commit(cache, path, n, len_out=None, stream=None):
+    """Move the accepted paths' rows together in every layer and return the new lengths (len_out None: in cache.len)."""
+    _same_device(cache.k, path, n, len_out)
+    if len_out is None:
+        len_out = cache.len
+    with _On(cache.k, stream) as s:
+        B.tasp_seq_commit(cache.struct, _ptr(path, (cache.batch, path.shape[1]), torch.int32, "path"),
+                          _ptr(n, (cache.batch,), torch.int32, "n"), path.shape[1],
+                          _ptr(len_out, (cache.batch,), torch.int32, "len_out"), s)
+    return len_out

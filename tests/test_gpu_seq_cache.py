@@ -1,0 +1,218 @@
+"""Rows written behind sequences of their own lengths (rotary positions, 8 bits), read back and moved,
+against the float64 oracle.
+
+Tolerances. A rotated value a c - b s: sine and cosine within 4 units of 2^-24 (the angle itself is exact to
+2^-33 at these positions), and one rounding each for mscale, the products and the sum: 8 x 2^-24 (|a| + |b|)
+mscale. BF16 outputs add half a step, 2^-8 of the value. An 8-bit code is the nearest one to a value
+that far off: half a step more, scale / 2 in INT8, 2^-4 of the value (2^-10 scale at least) in E4M3; the scale's own
+rounding adds 2^-23 of the value."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree as O
+from paper_2609_29499_amd import binding as B
+from paper_2609_29499_amd import session as S
+from tests.seq_case import DTYPES, flush, gen, randn, random_parents, typed_cache
+
+pytestmark = pytest.mark.gpu
+F = 2.0 ** -24
+
+
+def expected(q, k, v, lens, parent, S_, layout, rot, freq, mscale):
+    """float64 q, rows {(b, t): (k [H][dh], v)}, and their rotation error bounds."""
+    Bn, T = k.shape[:2]
+    oq, eq = np.zeros(q.shape), np.zeros(q.shape)
+    rows = {}
+    for b in range(Bn):
+        ln = O.lines(None if parent is None else parent[b].tolist(), T, S_ - lens[b]) if 0 <= lens[b] <= S_ else [None] * T
+        for t in range(T):
+            if ln[t] is None:
+                continue
+            pos = lens[b] + len(ln[t]) - 1
+            turn = lambda x: np.stack([O.rotate(r, pos, layout, rot, freq, mscale) for r in x])  # noqa: E731
+
+            def bound(x):
+                m = np.zeros_like(x)
+                h = rot // 2
+                a, c = (slice(0, h), slice(h, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+                m[:, a] = m[:, c] = (np.abs(x[:, a]) + np.abs(x[:, c])) * mscale * 8 * F
+                return m
+
+            oq[b, t], eq[b, t] = turn(q[b, t]), bound(q[b, t])
+            rows[b, t] = (turn(k[b, t]), bound(k[b, t]), v[b, t])
+    return oq, eq, rows
+
+
+CASES = [
+    # lens, S, T, hq, hkv, dh, cache, act, tree, layout, rot, scaling
+    ([0], 8, 1, 8, 2, 64, "int8", "bf16", False, "half", 64, "none"),
+    ([37, 0, 100000, 9], 100010, 7, 6, 3, 64, "e4m3", "bf16", True, "interleaved", 48, "wavelength"),
+    ([5, 60, 33], 64, 9, 16, 4, 128, "bf16", "f32", True, "half", 112, "index"),      # two nodes do not fit
+    ([1000], 1300, 300, 4, 4, 128, "int8", "f32", False, "half", 128, "linear"),
+    ([3, 2], 140, 130, 9, 3, 64, "e4m3", "f32", False, "interleaved", 64, "none"),
+    ([64, 1, 17], 128, 64, 32, 8, 128, "int8", "bf16", True, "half", 0, "none"),
+    ([-1, 41, 3], 40, 3, 4, 2, 64, "int8", "bf16", False, "half", 32, "none"),        # lengths out of range
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_append_and_read(case):
+    lens, S_, T, hq, H, dh, kind, act, tree, layout, rot, scaling = CASES[case]
+    flush(f"case append {CASES[case]}")
+    Bn, dt = len(lens), DTYPES[act]
+    # strided inputs: slices of one fused buffer
+    qkv = randn((Bn, T, (hq + 2 * H) * dh), dt, case).cuda()
+    q = qkv[..., :hq * dh].unflatten(-1, (hq, dh))
+    k = qkv[..., hq * dh:(hq + H) * dh].unflatten(-1, (H, dh))
+    v = qkv[..., (hq + H) * dh:].unflatten(-1, (H, dh))
+    parent = random_parents(Bn, T, case) if tree else None
+    par = dict(factor=8.0, low=1.0, high=32.0 if scaling == "index" else 4.0, orig_len=8192)
+    mscale = 1.25 if scaling == "index" else 1.0
+    freq = O.frequencies(rot, 500000.0, scaling, **par) if rot else []
+    cache = S.SeqCache.empty(2, Bn, H, S_, dh, DTYPES[kind])
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8).fill_(0x55)
+    cache.len.copy_(torch.tensor(lens, dtype=torch.int32))
+    rope = S.Rope(layout, rot, scaling=scaling, mscale=mscale, **par) if rot else None
+    out = S.seq_append(cache, 1, q, k, v, rope, None if parent is None else parent.cuda())
+    got_k, got_v = S.seq_read(cache, 1, S_, dtype=torch.float32)
+    bf_k, _ = S.seq_read(cache, 1, S_)
+    torch.cuda.synchronize()
+    want, eq, rows = expected(*(x.double().cpu().numpy() for x in (q, k, v)), lens, parent, S_, layout, rot, freq, mscale)
+    g = out.double().cpu().numpy()
+    tol = eq + (np.abs(want) * 2.0 ** -8 if act == "bf16" else 0)
+    assert np.all(np.abs(g - want) <= tol), np.max(np.abs(g - want) - tol)
+    gk, gv = got_k.double().cpu().numpy(), got_v.double().cpu().numpy()
+    assert torch.equal(bf_k, got_k.to(torch.bfloat16))
+    for (b, t), (wk, ek, wv) in rows.items():
+        r = lens[b] + t
+        for g, w, e in ((gk[b, :, r], wk, ek), (gv[b, :, r], wv, 0 * wv)):
+            if kind == "bf16":
+                step = np.abs(w) * 2.0 ** -8
+            else:
+                scale = (np.abs(w).max(-1, keepdims=True) + np.max(e)) / O.QMAX[kind]
+                step = scale / 2 if kind == "int8" else np.maximum(np.abs(w) * 2.0 ** -4, scale * 2.0 ** -10)
+                step = step + np.abs(w) * 2.0 ** -23 + 127 * scale * F    # (the quotient's rounding)
+            assert np.all(np.abs(g - w) <= step * (1 + 2.0 ** -10) + e * (1 + 2.0 ** -4)), (b, t)
+    # every other row, and the other layer, as before
+    raw = cache.k.view(torch.uint8).cpu().numpy().reshape(2, Bn, H, S_, -1)
+    assert np.all(raw[0] == 0x55)
+    for b in range(Bn):
+        written = {lens[b] + t for (bb, t) in rows if bb == b}
+        rest = [r for r in range(S_) if r not in written]
+        assert np.all(raw[1][b][:, rest] == 0x55)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_append_special_rows(kind):
+    """Rows of zeros, of one value, far from 1, with infinities and NaN: each by itself."""
+    flush(f"case append special {kind}")
+    x = randn((1, 8, 1, 64), torch.float32, 5)
+    x[0, 0] = 0.0
+    x[0, 1] = -3.0
+    x[0, 2] *= 1e-42
+    x[0, 3] *= 1e-30
+    x[0, 4] *= 1e36
+    x[0, 5, 0, 7] = math.inf
+    x[0, 6, 0, 9] = math.nan
+    cache = S.SeqCache.empty(1, 1, 1, 8, 64, DTYPES[kind])
+    S.seq_append(cache, 0, None, x.cuda(), x.cuda())
+    got, gv = S.seq_read(cache, 0, 8, dtype=torch.float32)
+    torch.cuda.synchronize()
+    assert torch.equal(got.nan_to_num(7.0), gv.nan_to_num(7.0))
+    g, w = got[0, 0].cpu().double().numpy(), x[0, :, 0].double().numpy()
+    assert not g[0].any()
+    np.testing.assert_allclose(g[1], -3.0, rtol=2.0 ** -22)
+    assert np.isnan(g[5]).all() and np.isnan(g[6]).all()
+    for r in (3, 4, 7):
+        scale = np.abs(w[r]).max() / O.QMAX[kind]
+        step = scale / 2 if kind == "int8" else np.maximum(np.abs(w[r]) * 2.0 ** -4, scale * 2.0 ** -10)
+        assert np.all(np.abs(g[r] - w[r]) <= step * (1 + 2.0 ** -10))
+    # magnitudes below 2^-126: the scale itself is a multiple of 2^-149
+    assert np.all(np.isfinite(g[2])) and np.all(np.abs(g[2]) <= 2 * np.abs(w[2]).max() + O.QMAX[kind] * 2.0 ** -149)
+
+
+def test_bf16_values_on_code_borders():
+    """BF16 rows whose quotients x 127 / top are exactly halves: ties go to the even code, as in exact arithmetic."""
+    flush("case code borders")
+    x = torch.zeros((1, 1, 1, 64), dtype=torch.bfloat16)
+    x[0, 0, 0, :] = torch.arange(64) + 0.5
+    x[0, 0, 0, 63] = 127.0
+    cache = S.SeqCache.empty(1, 1, 1, 4, 64, torch.int8)
+    S.seq_append(cache, 0, None, x.cuda(), -x.cuda())
+    torch.cuda.synchronize()
+    want = np.round(x.double().numpy()[0, 0, 0])       # numpy rounds halves to even
+    np.testing.assert_array_equal(cache.k[0, 0, 0, 0].cpu().numpy(), want)
+    np.testing.assert_array_equal(cache.v[0, 0, 0, 0].cpu().numpy(), -want)
+
+
+def test_packing_a_plan_cache():
+    """Rows of a BF16 cache [B][H][S][dh] given as k and v: a chain from row 0 on, without rotation."""
+    flush("case pack")
+    src, kv, vv = typed_cache([0, 0], 3, 50, 128, "bf16", 3)
+    dst = S.SeqCache.empty(1, 2, 3, 64, 128, torch.bfloat16)
+    k, v = src.k[0].transpose(1, 2), src.v[0].transpose(1, 2)
+    assert S.seq_append(dst, 0, None, k, v) is None
+    torch.cuda.synchronize()
+    assert torch.equal(dst.k[0, :, :, :50], src.k[0]) and torch.equal(dst.v[0, :, :, :50], src.v[0])
+    assert not dst.k[0, :, :, 50:].any()
+
+
+@pytest.mark.parametrize("first", [[0, 3], [-2, 15], [2 ** 31 - 1, -2 ** 31]])
+def test_read_outside_the_cache_is_zeros(first):
+    flush(f"case read {first}")
+    c, kv, vv = typed_cache([0, 0], 2, 17, 64, "int8", 4)
+    k, v = S.seq_read(c, 0, 5, first=torch.tensor(first, dtype=torch.int32, device="cuda"), dtype=torch.float32)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for i in range(5):
+            r = first[b] + i
+            want = kv[0, b, :, r] if 0 <= r < 17 else np.zeros((2, 64))
+            np.testing.assert_allclose(k[b, :, i].cpu().numpy(), want, rtol=2.0 ** -23)
+
+
+def test_read_into_strided_rows():
+    flush("case read strided")
+    c, kv, vv = typed_cache([0, 0], 2, 17, 64, "e4m3", 5)
+    dst = S.KVCache(S.model_desc(1, 128, 2, 2, 64, 64), 2, 40)
+    dst.k.fill_(3.0)
+    S.seq_read(c, 0, 17, out=(dst.k[0, :, :, :17], dst.v[0, :, :, :17]))
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(dst.k[0, :, :, :17].double().cpu().numpy(),
+                                  torch.from_numpy(kv[0]).float().to(torch.bfloat16).double().numpy())
+    assert torch.all(dst.k[0, :, :, 17:] == 3.0)
+
+
+@pytest.mark.parametrize("kind,dh", [("bf16", 128), ("bf16", 64), ("int8", 128), ("e4m3", 64)])
+def test_commit(kind, dh):
+    flush(f"case commit {kind} {dh}")
+    lens = [0, 10, 70, 3, -4, 100]
+    c, kv, vv = typed_cache(lens, 3, 80, dh, kind, 6, layers=2)
+    T = 12
+    path = np.full((6, T), -1, np.int32)
+    path[0, :4] = [0, 1, 5, 11]
+    path[1, :12] = np.arange(12)                       # nothing moves
+    path[2, :5] = [0, 2, 3, 4, 11]                     # row 81 lies outside
+    path[3, :6] = [0, 3, 2, 99, -7, 1]                 # not ascending, and entries outside the tree
+    n = np.array([4, 12, 5, 6, 3, 2], np.int32)
+    before = {name: getattr(c, name).clone() for name in ("k", "v", "k_scale", "v_scale") if getattr(c, name) is not None}
+    out = torch.full((6,), -9, dtype=torch.int32, device="cuda")
+    S.seq_commit(c, torch.from_numpy(path).cuda(), torch.from_numpy(n).cuda(), len_out=out)
+    torch.cuda.synchronize()
+    assert out.tolist() == [4, 22, 75, 9, -4, 100] and c.len.tolist() == lens
+    for name, old in before.items():
+        want = old.clone()
+        for b in range(6):
+            if not 0 <= lens[b] <= 80:
+                continue
+            for i in range(n[b]):
+                if 0 <= path[b, i] < T and lens[b] + path[b, i] < 80 and lens[b] + i < 80:
+                    want[:, b, :, lens[b] + i] = old[:, b, :, lens[b] + path[b, i]]
+        assert torch.equal(getattr(c, name).view(torch.uint8), want.view(torch.uint8)), name
+    # in place: the lengths themselves
+    S.seq_commit(c, torch.from_numpy(path).cuda(), torch.from_numpy(n).cuda())
+    torch.cuda.synchronize()
+    assert c.len.tolist() == [4, 22, 75, 9, -4, 100]

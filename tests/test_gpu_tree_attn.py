@@ -1,0 +1,175 @@
+"""Attention of drafted nodes over cached rows and ancestors against the float64 oracle.
+
+Tolerance of one output: with A = sum of p |v| over the rows seen, n their number,
+  scores: a float32 dot product of dh exact products, |error| <= (dh + 4) 2^-24 scale sum |q_i k_i| = d, which
+  moves p by a factor within exp(2 d);
+  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; float32 sums n 2^-24;
+  the output's rounding 2^-8 of the value in BF16, 2^-24 in float32.
+|error| <= A (2 d + 2^-21 + 2^-16 or 2^-24 + n 2^-24) + |o| 2^-8 or 2^-24."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree as O
+from paper_2609_29499_amd import session as S
+from tests.seq_case import DTYPES, flush, gen, randn, random_parents, typed_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def check(got, q, kv, vv, lens, parent, S_, act, scale, nodes=None):
+    """got [B][T][Hq][dh] against the oracle, every node or the given ones."""
+    Bn, T, hq, dh = q.shape
+    H = kv.shape[1]
+    worst = 0.0
+    for b in range(Bn):
+        ln = O.lines(None if parent is None else parent[b].tolist(), T, S_ - lens[b]) if 0 <= lens[b] <= S_ else [None] * T
+        for t in range(T) if nodes is None else nodes:
+            if ln[t] is None:
+                assert not got[b, t].any(), (b, t)
+                continue
+            seen = list(range(lens[b])) + [lens[b] + j for j in ln[t]]
+            for h in range(hq):
+                k, v = kv[b, h // (hq // H)], vv[b, h // (hq // H)]
+                o, A = O.attention(q[b, t, h], k, v, seen, scale)
+                d = (dh + 4) * 2.0 ** -24 * scale * np.max(np.abs(k[seen]) @ np.abs(q[b, t, h]))
+                tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -16 if act == "bf16" else 2.0 ** -24) + len(seen) * 2.0 ** -24)
+                tol = tol + np.abs(o) * (2.0 ** -8 if act == "bf16" else 2.0 ** -24)
+                err = np.abs(got[b, t, h] - o)
+                worst = max(worst, float(np.max(err / tol)))
+                assert np.all(err <= tol), (b, t, h, float(np.max(err / tol)))
+    flush(f"   worst share of the tolerance {worst:.3f}")
+
+
+CASES = [
+    # lens, room behind, T, hq, hkv, dh, cache, act, tree
+    ([0], 0, 1, 4, 4, 64, "bf16", "bf16", False),
+    ([1], 3, 1, 8, 1, 128, "int8", "bf16", False),
+    ([0, 5, 31], 0, 3, 6, 3, 64, "int8", "bf16", True),
+    ([32, 31, 33, 0], 2, 5, 8, 2, 128, "e4m3", "bf16", True),
+    ([127, 128, 129], 0, 16, 4, 1, 128, "bf16", "bf16", True),
+    ([300, 0, 17], 5, 64, 8, 1, 128, "int8", "bf16", True),
+    ([77, 500], 0, 33, 9, 3, 64, "bf16", "f32", True),
+    ([600], 0, 7, 28, 4, 128, "e4m3", "f32", False),
+    ([2000, 3, 900, 0, 1500], 1, 2, 16, 2, 64, "e4m3", "bf16", True),
+    ([4100], 0, 1, 4, 1, 64, "int8", "f32", False),
+    ([-3, 50, 64], 0, 4, 4, 2, 64, "int8", "bf16", False),          # a length out of range
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_tree_attention(case):
+    lens, room, T, hq, H, dh, kind, act, tree = CASES[case]
+    flush(f"case attention {CASES[case]}")
+    S_ = max(lens) + T + room if case != 10 else 66                 # (the last case: two nodes do not fit)
+    c, kv, vv = typed_cache(lens, H, S_, dh, kind, case)
+    parent = random_parents(len(lens), T, case) if tree else None
+    q = randn((len(lens), T, hq, dh), DTYPES[act], 100 + case)
+    got = S.tree_attention(c, 0, q.cuda(), None if parent is None else parent.cuda())
+    torch.cuda.synchronize()
+    check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+def test_long_contexts_in_many_chunks(kind):
+    """Ragged sequences over several chunks, a hint of the length that is too small, strided q and out."""
+    lens = [20000, 700, 0, 9001]
+    flush(f"case long {kind}")
+    T, hq, H, dh = 3, 4, 2, 128
+    c, kv, vv = typed_cache(lens, H, 20010, dh, kind, 7)
+    parent = torch.tensor([[-1, 0, 0]] * 4, dtype=torch.int32)
+    wide = torch.zeros((4, T, 3, hq, dh), dtype=torch.bfloat16, device="cuda")
+    q = randn((4, T, hq, dh), torch.bfloat16, 8)
+    wide[:, :, 1] = q.cuda()
+    out = torch.full((4, T, hq + 1, dh), 5.0, dtype=torch.bfloat16, device="cuda")
+    outs = []
+    for hint in (20000, 4000, 100):
+        S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint, out=out[:, :, :hq])
+        torch.cuda.synchronize()
+        check(out[:, :, :hq].double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 20010, "bf16", dh ** -0.5)
+        assert torch.all(out[:, :, hq] == 5.0)
+        again = S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint)
+        torch.cuda.synchronize()
+        assert torch.equal(again, out[:, :, :hq])                   # the same call gives the same bits
+        outs.append(again)
+
+
+def test_layers_behind_32_bit_offsets():
+    """The last layer of a cache of more than 2^32 bytes."""
+    flush("case far layer")
+    L, H, S_, dh = 5, 8, 1 << 20, 128
+    k = torch.zeros((L, 1, H, S_, dh), dtype=torch.int8, device="cuda")
+    assert k.numel() > 1 << 32
+    v, sc = torch.zeros_like(k), torch.full((L, 1, H, S_), 0.01, device="cuda")
+    lens = S_ - 2
+    c = S.SeqCache(k, v, torch.tensor([lens], dtype=torch.int32, device="cuda"), sc, sc)
+    x = randn((1, 2, H, dh), torch.bfloat16, 9).cuda()
+    S.seq_append(c, L - 1, None, x, x)
+    # node 1 scores its own row far above the zeros': its value comes out
+    q = x * 40.0
+    out = S.tree_attention(c, L - 1, q, torch.tensor([[-1, -1]], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    step = x.float().abs().amax(-1, keepdim=True) / 127
+    assert torch.all((out.float() - x.float()).abs() <= step * 0.51 + x.float().abs() * 2.0 ** -7)
+    assert not c.k[:L - 1].any() and not c.k[L - 1, 0, :, :lens].any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+def test_unseen_rows_reach_nothing(kind):
+    """Infinities and NaN in rows of other branches, of absent nodes and behind the nodes."""
+    flush(f"case unseen {kind}")
+    lens, T, dh = [40, 0], 6, 64
+    S_ = 60
+    c, kv, vv = typed_cache(lens, 2, S_, dh, kind, 10)
+    parent = torch.tensor([[-1, 0, 0, 1, 2, -2], [-1, 0, 0, 1, 2, -2]], dtype=torch.int32)
+    q = randn((2, T, 4, dh), torch.bfloat16, 11)
+    clean = S.tree_attention(c, 0, q.cuda(), parent.cuda())
+    for b in range(2):
+        for r, what in ((2, math.nan), (5, math.inf), (7, math.nan)):      # node 2, an absent node, behind the tree
+            if kind == "bf16":
+                c.k[0, b, :, lens[b] + r] = what
+                c.v[0, b, :, lens[b] + r, ::5] = what
+                c.v[0, b, :, lens[b] + r, 1::5] = -math.inf
+            else:
+                c.k_scale[0, b, :, lens[b] + r] = math.nan
+                c.v_scale[0, b, :, lens[b] + r] = math.nan
+            if kind == "e4m3":
+                c.v.view(torch.uint8)[0, b, :, lens[b] + r] = 0x7f         # NaN codes
+    got = S.tree_attention(c, 0, q.cuda(), parent.cuda())
+    torch.cuda.synchronize()
+    for t in (0, 1, 3, 5):                                                 # nodes that do not see node 2
+        assert torch.equal(got[:, t], clean[:, t]), t
+    assert torch.isnan(got[:, 2]).any(-1).all() and torch.isnan(got[:, 4]).any(-1).all()
+
+
+def test_visible_infinities_stay_in_their_dimensions():
+    flush("case visible infinities")
+    c, kv, vv = typed_cache([10], 1, 20, 64, "bf16", 12)
+    q = randn((1, 3, 2, 64), torch.bfloat16, 13).cuda()
+    parent = torch.tensor([[-1, 0, 0]], dtype=torch.int32, device="cuda")
+    clean = S.tree_attention(c, 0, q, parent)
+    c.v[0, 0, 0, 11, 3], c.v[0, 0, 0, 11, 4], c.v[0, 0, 0, 11, 5] = math.inf, -math.inf, math.nan
+    c.v[0, 0, 0, 10, 4] = math.inf
+    got = S.tree_attention(c, 0, q, parent).float()
+    torch.cuda.synchronize()
+    assert torch.all(got[0, 1, :, 3] == math.inf) and torch.isnan(got[0, 1, :, 4:6]).all()   # node 1: its own row and node 0's
+    assert torch.all(got[0, 0, :, 4] == math.inf) and torch.all(got[0, 2, :, 4] == math.inf)
+    rest = [d for d in range(64) if d not in (3, 4, 5)]
+    assert torch.equal(got[0][:, :, rest], clean.float()[0][:, :, rest])
+
+
+def test_large_scores_and_one_step_rises():
+    """Scores that grow along the cache by far more than one power of two per step, and a scale of its own."""
+    flush("case rising scores")
+    c, kv, vv = typed_cache([700], 1, 704, 64, "bf16", 14)
+    ramp = torch.linspace(0, 1, 704)[:, None] * torch.ones(64)
+    c.k[0, 0, 0] = ramp.to(torch.bfloat16).cuda()
+    q = torch.full((1, 2, 2, 64), 1.0, dtype=torch.bfloat16)
+    q[0, 1] = -1.0
+    got = S.tree_attention(c, 0, q.cuda(), scale=30.0)
+    torch.cuda.synchronize()
+    k64 = c.k.double().cpu().numpy()
+    g = got.double().cpu().numpy()
+    check(g, q.double().numpy(), k64[0], vv[0], [700], None, 704, "bf16", 30.0)
