@@ -24,6 +24,7 @@
 // step. Sequences of one chunk are written at once; the others leave (maximum, sum, unnormalised output)
 // per query row in the workspace, which a second launch joins in chunk order.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "seq.hpp"
@@ -35,13 +36,17 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 constexpr int kStep = 32;              // cache rows per step
-constexpr int kTarget = 512;           // workgroups aimed at: two per CU
 constexpr int kMinSteps = 4;           // steps of a chunk at least: one per wave
 constexpr float kSlack = 8.0f;         // powers of two a score may pass the running maximum by
 
 // ---- which rows a workgroup serves
 // Sequence b has steps(b) = ceil((L + T) / 32) steps and is cut in chunks of `chunk` steps. A wave holds four
 // sequences per lane.
+// How a call is launched: query rows in rb blocks of 16 mt, `target` workgroups aimed at, at most `most`
+// chunks per sequence (what the workspace has room for), grid workgroups.
+struct TreeShape {
+  int mt, rb, target, most, grid;
+};
 struct Deal {
   int chunk;                           // steps per chunk
   int total;                           // chunks of all sequences
@@ -52,8 +57,7 @@ __device__ __forceinline__ int steps_of(const TreeAttnArgs& a, int b) {
   if (L == -2) return 0;               // no such sequence
   return L < 0 ? 1 : (min(L + a.T, a.c.S) + kStep - 1) / kStep;
 }
-// most: chunks per sequence that the workspace has room for
-__device__ __forceinline__ Deal deal(const TreeAttnArgs& a, int units, int most, int lane) {
+__device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, int lane) {
   Deal d;
   int n[4], sum = 0;
 #pragma unroll
@@ -63,12 +67,12 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, int units, int most,
   }
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) sum += __shfl_xor(sum, k, kWave);
-  const int chunk = max(kMinSteps, int((long(sum) * units + kTarget - 1) / kTarget));
+  const int chunk = max(kMinSteps, int((long(sum) * a.c.n_kv * y.rb + y.target - 1) / y.target));
   d.chunk = (chunk + 3) / 4 * 4;
   int own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    d.mine[i] = min((n[i] + d.chunk - 1) / d.chunk, most);
+    d.mine[i] = min((n[i] + d.chunk - 1) / d.chunk, y.most);
     d.before[i] = own;
     own += d.mine[i];
   }
@@ -127,11 +131,6 @@ __device__ __forceinline__ void terms(float v0, float v1, uint32_t* o, int strid
   }
 }
 
-// classes of non-finite BF16 halves: 0 NaN, 1 +inf, 2 -inf
-__device__ __forceinline__ bool half_is(uint32_t h, int cls) {
-  return cls == 0 ? (h & 0x7fffu) > 0x7f80u : h == (cls == 1 ? 0x7f80u : 0xff80u);
-}
-
 template <int DH, int TYPE>
 struct Rows32 {                        // a step's K and V as loaded
   static constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
@@ -142,20 +141,26 @@ struct Rows32 {                        // a step's K and V as loaded
   float ks[8], vs[8];
 };
 
-template <int DH, int TYPE, int ACT>
-__global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int layout_rb, int most) {
+// Waves per SIMD that the registers of MT tiles leave room for
+template <int DH, int TYPE, int ACT, int MT>
+constexpr int kWavesPerSimd = MT == 4 || (MT == 2 && DH == 128 && (TYPE == SEQ_BF16 || ACT == SEQ_F32)) ? 1 : 2;
+
+// MT: tiles of 16 query rows per wave
+template <int DH, int TYPE, int ACT, int MT>
+__global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tree_attn_kernel(TreeAttnArgs a, TreeShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
   constexpr int NKC = DH / 32;         // score products per tile
   constexpr int NDT = DH / 16;         // dimensions per lane of V and O
   constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 2;
   using Rows = Rows32<DH, TYPE>;
   __shared__ float s_o[4][16][DH + 4];
-  __shared__ float s_m[4][16], s_l[4][16];
+  __shared__ float s_m[4][16 * MT], s_l[4][16 * MT];
+  __shared__ int s_odd;                // a tree's row holds something not finite
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = lane & 15, c = lane >> 4;
-  const int units = a.c.n_kv * layout_rb;
-  const Deal d = deal(a, units, most, lane);
+  const int units = a.c.n_kv * y.rb;
+  const Deal d = deal(a, y, lane);
   // workgroup -> row block (slowest), chunk of a sequence, cache head
   const int w = blockIdx.x;
   if (w >= d.total * units) return;
@@ -165,10 +170,10 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
   for (int i = 0; i < 4; ++i)
     if (ch_all >= d.before[i] && ch_all < d.before[i] + d.mine[i]) hit = i;
   const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
-  const int b = 4 * owner + __shfl(hit, owner, kWave);
-  const int sub = b & 3;
-  const int before = __shfl(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], owner, kWave);
-  const int n_ch = __shfl(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner, kWave);
+  const int sub = __builtin_amdgcn_readlane(hit, owner);
+  const int b = 4 * owner + sub;
+  const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], owner);
+  const int n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
   const int ch = ch_all - before;
 
   const int L = seq_len(a.c.len, b, a.c.S);
@@ -178,34 +183,8 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
   // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
   const int per = n_ch * d.chunk >= steps ? d.chunk : ((steps + n_ch - 1) / n_ch + 3) / 4 * 4;
   const int s0 = ch * per, s1 = ch == n_ch - 1 ? steps : min(steps, s0 + per);
-
-  // this lane's query row, as a row of Q (B operand): node t, head h
-  const int R = a.T * a.group, row = rb * 16 + r;
-  const TreeNode nd = tree_node(a.parent ? a.parent + size_t(b) * a.T : nullptr, a.T, L < 0 ? 0 : a.c.S - L, lane);
-  const int t = min(row, R - 1) / a.group, h = g * a.group + min(row, R - 1) % a.group;
-  const unsigned long long all = __shfl(nd.anc, t, kWave);
-  const unsigned long long anc = row < R ? all : 0ull;
-
-  uint32_t qf[QT][NKC][4];
-  {
-    const long at = b * a.q.seq + t * a.q.token + h * a.q.head;
-#pragma unroll
-    for (int kk = 0; kk < NKC; ++kk) {
-      const int dim = ES == 2 ? 32 * kk + 8 * c : 64 * (kk >> 1) + 16 * c + 8 * (kk & 1);
-      if constexpr (ACT == SEQ_BF16) {
-        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.p) + at + dim);
-        qf[0][kk][0] = x.x; qf[0][kk][1] = x.y; qf[0][kk][2] = x.z; qf[0][kk][3] = x.w;
-      } else {
-        const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q.p) + at + dim);
-        const float4 x = f[0], y = f[1];
-        uint32_t* o = &qf[0][kk][0];
-        terms<QT>(x.x, x.y, o, NKC * 4);
-        terms<QT>(x.z, x.w, o + 1, NKC * 4);
-        terms<QT>(y.x, y.y, o + 2, NKC * 4);
-        terms<QT>(y.z, y.w, o + 3, NKC * 4);
-      }
-    }
-  }
+  // steps from s_edge on hold rows of the tree: at most three, so a wave has one at most
+  const int s_edge = min(Lr / kStep, s1);
 
   const size_t unit = size_t(b) * a.c.n_kv + g;
   const uint32_t row_bytes = DH * ES;
@@ -214,18 +193,30 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
   const __amdgpu_buffer_rsrc_t rks = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.ks + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
   const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
 
-  auto load = [&](int s, Rows& x) {                    // rows past `end` read as zeros
+  // Steps are loaded one ahead. Rows past `end`, and steps past `stop`, read as zeros without touching memory.
+  auto load = [&](int s, int stop, Rows& x) {
     const uint32_t t0 = uint32_t(s) * kStep;
+    const bool in = s < stop;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int j = 0; j < Rows::KW; ++j) {
-        const int4 p = buf_load16_stream(rk, (t0 + 16 * tt + r) * row_bytes + 64u * j + 16u * c);
+        const int4 p = buf_load16_stream(rk, in ? (t0 + 16 * tt + r) * row_bytes + 64u * j + 16u * c : kOOB);
         x.k[tt][j][0] = p.x; x.k[tt][j][1] = p.y; x.k[tt][j][2] = p.z; x.k[tt][j][3] = p.w;
       }
+    if constexpr (TYPE != SEQ_BF16) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const uint32_t off = in ? (t0 + 16 * tt + 4 * c) * 4u : kOOB;
+        const float4 p = __builtin_bit_cast(float4, buf_load16(rks, off));
+        const float4 q = __builtin_bit_cast(float4, buf_load16(rvs, off));
+        x.ks[4 * tt] = p.x; x.ks[4 * tt + 1] = p.y; x.ks[4 * tt + 2] = p.z; x.ks[4 * tt + 3] = p.w;
+        x.vs[4 * tt] = q.x; x.vs[4 * tt + 1] = q.y; x.vs[4 * tt + 2] = q.z; x.vs[4 * tt + 3] = q.w;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t off = (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r;
+      const uint32_t off = in ? (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r : kOOB;
       if constexpr (Rows::VW == 4) {
         const int4 p = buf_load16_stream(rv, off);
         x.v[i][0] = p.x; x.v[i][1] = p.y; x.v[i][2] = p.z; x.v[i][3] = p.w;
@@ -236,30 +227,60 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
         x.v[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rv, int(off), 0, kCpolStream);
       }
     }
-    if constexpr (TYPE != SEQ_BF16) {
+  };
+  const int s_own = s0 + wave;                         // this wave's steps: s_own, s_own + 4, ..
+  const int s_late = s_own + max(0, (s_edge - s_own + 3) / 4) * 4;   // its first step at or behind s_edge
+  const bool has_edge = s_late < s1;
+  Rows xa, xb;
+  load(s_late, s1, xa);
+  load(s_own, s_edge, xb);
+
+  // this lane's query rows, as rows of Q (B operand): node t, head h
+  const int R = a.T * a.group;
+  const TreeNode nd = tree_node(a.parent ? a.parent + size_t(b) * a.T : nullptr, a.T, L < 0 ? 0 : a.c.S - L, lane);
+  unsigned long long anc[MT];
+  uint32_t qf[MT][QT][NKC][4];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const float4 p = __builtin_bit_cast(float4, buf_load16(rks, (t0 + 16 * tt + 4 * c) * 4u));
-        const float4 q = __builtin_bit_cast(float4, buf_load16(rvs, (t0 + 16 * tt + 4 * c) * 4u));
-        x.ks[4 * tt] = p.x; x.ks[4 * tt + 1] = p.y; x.ks[4 * tt + 2] = p.z; x.ks[4 * tt + 3] = p.w;
-        x.vs[4 * tt] = q.x; x.vs[4 * tt + 1] = q.y; x.vs[4 * tt + 2] = q.z; x.vs[4 * tt + 3] = q.w;
+  for (int mt = 0; mt < MT; ++mt) {
+    const int row = min((rb * MT + mt) * 16 + r, R - 1);   // (rows past the last one repeat it and are not stored)
+    const int t = row / a.group, h = g * a.group + row % a.group;
+    anc[mt] = __shfl(nd.anc, t, kWave);
+    const long at = b * a.q.seq + t * a.q.token + h * a.q.head;
+#pragma unroll
+    for (int kk = 0; kk < NKC; ++kk) {
+      const int dim = ES == 2 ? 32 * kk + 8 * c : 64 * (kk >> 1) + 16 * c + 8 * (kk & 1);
+      if constexpr (ACT == SEQ_BF16) {
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.p) + at + dim);
+        qf[mt][0][kk][0] = x.x; qf[mt][0][kk][1] = x.y; qf[mt][0][kk][2] = x.z; qf[mt][0][kk][3] = x.w;
+      } else {
+        const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q.p) + at + dim);
+        const float4 x = f[0], z = f[1];
+        uint32_t* o = &qf[mt][0][kk][0];
+        terms<QT>(x.x, x.y, o, NKC * 4);
+        terms<QT>(x.z, x.w, o + 1, NKC * 4);
+        terms<QT>(z.x, z.y, o + 2, NKC * 4);
+        terms<QT>(z.z, z.w, o + 3, NKC * 4);
       }
     }
-  };
+  }
 
-  float m_run = -INFINITY, l_run = 0.0f;               // of query row r; l of this lane's cache rows
-  f32x4 o[NDT];                                        // lane (r, c): query rows 4 c + i, dimension NDT r + d
+  float m_run[MT], l_run[MT];                          // of query row r; l of this lane's cache rows
+  f32x4 o[MT][NDT];                                    // lane (r, c): query rows 4 c + i, dimension NDT r + d
 #pragma unroll
-  for (int i = 0; i < NDT; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int mt = 0; mt < MT; ++mt) {
+    m_run[mt] = -INFINITY;
+    l_run[mt] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
 
-  for (int s = s0 + wave; s < s1; s += 4) {
-    Rows x;
-    load(s, x);
-    // scores
-    f32x4 sc[2];
+  auto process = [&](Rows& x, int s, auto edge_) {
+    constexpr bool EDGE = decltype(edge_)::value;
+    f32x4 sc[MT][2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      sc[tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int kk = 0; kk < NKC; ++kk) {
         uint32_t kf[4];
@@ -271,48 +292,54 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
           widen<TYPE>(x.k[tt][kk >> 1][2 * (kk & 1) + 1], kf + 2);
         }
 #pragma unroll
-        for (int q = 0; q < QT; ++q) sc[tt] = mfma(kf, qf[q][kk], sc[tt]);
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int q = 0; q < QT; ++q) sc[mt][tt] = mfma(kf, qf[mt][q][kk], sc[mt][tt]);
       }
     }
-    float p[8];
+    uint32_t pf[MT][PT][4];
+    float ks[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = sc[i >> 2][i & 3] * (TYPE == SEQ_BF16 ? a.scale2 : x.ks[i] * a.scale2);
-    const int t0 = s * kStep;
-    const bool edge = t0 + kStep > Lr;                 // rows of the tree, or past the end
-    if (edge) {
+    for (int i = 0; i < 8; ++i) ks[i] = TYPE == SEQ_BF16 ? a.scale2 : x.ks[i] * a.scale2;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = sc[mt][i >> 2][i & 3] * ks[i];
+      uint32_t seen = 0xffu;                           // of the lane's eight cache rows
+      if constexpr (EDGE) {
+        seen = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = s * kStep + 16 * (i >> 2) + 4 * c + (i & 3) - Lr;
+          const bool in = j < 0 || (j < kTreeMax && ((anc[mt] >> (j & 63)) & 1));
+          seen |= uint32_t(in) << i;
+          p[i] = in ? p[i] : -INFINITY;
+        }
+      }
+      float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+      if (__ballot(top > m_run[mt] + kSlack)) {        // (also the first rows: m_run is -inf)
+        const float mn = fmaxf(m_run[mt], quad_max(top));
+        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[mt] - mn);
+        m_run[mt] = mn;
+        l_run[mt] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = __shfl(alpha, 4 * c + i, kWave);
+#pragma unroll
+          for (int e = 0; e < NDT; ++e) o[mt][e][i] *= f;
+        }
+      }
+      const float base = m_run[mt] == -INFINITY ? 0.0f : m_run[mt];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int j = t0 + 16 * (i >> 2) + 4 * c + (i & 3) - Lr;
-        const bool seen = j < 0 || (j < kTreeMax && ((anc >> (j & 63)) & 1));
-        p[i] = seen ? p[i] : -INFINITY;
-        if constexpr (TYPE != SEQ_BF16) x.vs[i] = seen ? x.vs[i] : 0.0f;
+        p[i] = __builtin_amdgcn_exp2f(p[i] - base);
+        l_run[mt] += p[i];
+        if constexpr (TYPE != SEQ_BF16) p[i] *= EDGE && !((seen >> i) & 1) ? 0.0f : x.vs[i];
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[mt][0][e], 4);
     }
-    float top = p[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, p[i]);
-    if (__ballot(top > m_run + kSlack)) {              // (also the first rows: m_run is -inf)
-      const float mn = fmaxf(m_run, quad_max(top));
-      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
-      m_run = mn;
-      l_run *= alpha;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float f = __shfl(alpha, 4 * c + i, kWave);
-#pragma unroll
-        for (int e = 0; e < NDT; ++e) o[e][i] *= f;
-      }
-    }
-    const float base = m_run == -INFINITY ? 0.0f : m_run;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - base);
-      l_run += p[i];
-      if constexpr (TYPE != SEQ_BF16) p[i] *= x.vs[i];
-    }
-    uint32_t pf[PT][4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[0][e], 4);
     // V: eight rows of NDT dimensions as BF16 pairs
     uint32_t v[8][NDT / 2];
 #pragma unroll
@@ -325,48 +352,19 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
         for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(x.v[i][e], &v[i][2 * e]);
       }
     }
-    // A row of the tree that some nodes do not see must not reach them through 0 * inf: at the tree's rows
-    // non-finite values are taken out of the product, and marked in the rows that see them
-    bool odd = false;
-    if (TYPE != SEQ_INT8 && edge) {
+    // A row of the tree that some nodes do not see must not reach them through 0 * inf: non-finite values of
+    // the tree's rows are left out of the product, and added at the end to the outputs that see them
+    if constexpr (EDGE && TYPE != SEQ_INT8) {
       uint32_t bad = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < NDT / 2; ++e)
-          bad |= uint32_t((v[i][e] & 0x7f80u) == 0x7f80u) | uint32_t((v[i][e] & 0x7f800000u) == 0x7f800000u);
-      odd = __ballot(bad != 0) != 0;
-    }
-    if (odd) {
-      uint32_t see[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) see[e] = (p[2 * e] != 0.0f ? 0x3f80u : 0u) | (p[2 * e + 1] != 0.0f ? 0x3f800000u : 0u);
-#pragma unroll 1
-      for (int cls = 0; cls < 3; ++cls) {
-        const float mark = cls == 0 ? __builtin_nanf("") : cls == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-        for (int e = 0; e < NDT; ++e) {
-          uint32_t vb[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t x0 = (e & 1) ? v[2 * i][e / 2] >> 16 : v[2 * i][e / 2] & 0xffffu;
-            const uint32_t x1 = (e & 1) ? v[2 * i + 1][e / 2] >> 16 : v[2 * i + 1][e / 2] & 0xffffu;
-            vb[i] = (half_is(x0, cls) ? 0x3f80u : 0u) | (half_is(x1, cls) ? 0x3f800000u : 0u);
-          }
-          const f32x4 n = mfma(see, vb, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[e][i] += n[i] > 0.0f ? mark : 0.0f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
         for (int e = 0; e < NDT / 2; ++e) {
-          uint32_t x0 = v[i][e] & 0xffffu, x1 = v[i][e] & 0xffff0000u;
-          if ((x0 & 0x7f80u) == 0x7f80u) x0 = 0;
-          if ((x1 & 0x7f800000u) == 0x7f800000u) x1 = 0;
-          v[i][e] = x0 | x1;
+          const uint32_t top = ((v[i][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's exponent is full
+          bad |= top;
+          v[i][e] &= ~((top >> 15) * 0xffffu);
         }
+      if (bad) s_odd = 1;
     }
 #pragma unroll
     for (int e = 0; e < NDT; ++e) {
@@ -375,78 +373,114 @@ __global__ __launch_bounds__(kBlock) void tree_attn_kernel(TreeAttnArgs a, int l
 #pragma unroll
       for (int i = 0; i < 4; ++i) vb[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], sel);
 #pragma unroll
-      for (int k = 0; k < PT; ++k) o[e] = mfma(pf[k], vb, o[e]);
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int k = 0; k < PT; ++k) o[mt][e] = mfma(pf[mt][k], vb, o[mt][e]);
     }
+  };
+  if constexpr (TYPE != SEQ_INT8) {
+    if (tid == 0) s_odd = 0;
+    __syncthreads();
+  }
+  if (has_edge) process(xa, s_late, std::true_type{});
+  for (int s = s_own; s < s_edge; s += 8) {
+    load(s + 4, s_edge, xa);
+    process(xb, s, std::false_type{});
+    if (s + 4 >= s_edge) break;
+    load(s + 8, s_edge, xb);
+    process(xa, s + 4, std::false_type{});
   }
 
-  // the four waves' results
-  l_run = quad_sum(l_run);
-  if (c == 0) {
-    s_m[wave][r] = m_run;
-    s_l[wave][r] = l_run;
-  }
+  // the four waves' results, 16 query rows at a time
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int e = 0; e < NDT; e += 4)
-      *reinterpret_cast<float4*>(&s_o[wave][4 * c + i][NDT * r + e]) = make_float4(o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]);
-  __syncthreads();
-  // thread: query row tid / 16 of the block, dimensions NDT (tid % 16) ..
-  const int qr = tid >> 4, d0 = NDT * (tid & 15);
-  float m = -INFINITY, l = 0.0f, f[4], v[NDT];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) m = fmaxf(m, s_m[k][qr]);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    f[k] = s_m[k][qr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[k][qr] - m);
-    // (a wave that saw only rows scored -inf or none holds zeros; NaN stays)
-    l += s_m[k][qr] == -INFINITY ? s_l[k][qr] : s_l[k][qr] * f[k];
-  }
-#pragma unroll
-  for (int e = 0; e < NDT; ++e) {
-    v[e] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[e] += s_m[k][qr] == -INFINITY ? s_o[k][qr][d0 + e] : s_o[k][qr][d0 + e] * f[k];
-  }
-  const int row_o = rb * 16 + qr;
-  const int t_o = min(row_o, R - 1) / a.group;
-  const bool there = __shfl(nd.anc, t_o, kWave) != 0;  // (a row of an absent node is zeros)
-  if (row_o >= R) return;
-  if (n_ch == 1) {
-    const float inv = there && l != 0.0f ? 1.0f / l : 0.0f;
-    const long at = b * a.o.seq + t_o * a.o.token + (g * a.group + row_o % a.group) * a.o.head + d0;
-#pragma unroll
-    for (int e = 0; e < NDT; e += 4) {
-      float y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = there && l != 0.0f ? v[e + i] * inv : 0.0f;
-      if constexpr (ACT == SEQ_BF16)
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.p) + at + e) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-      else
-        *reinterpret_cast<float4*>(static_cast<float*>(a.o.p) + at + e) = make_float4(y[0], y[1], y[2], y[3]);
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l_all = quad_sum(l_run[mt]);
+    if (c == 0) {
+      s_m[wave][16 * mt + r] = m_run[mt];
+      s_l[wave][16 * mt + r] = l_all;
     }
-  } else {
-    const size_t rec = (size_t(ch_all) * a.c.n_kv + g) * layout_rb + rb;
-    float* po = a.ws + (rec * 16 + qr) * (DH + 4);
-    if (d0 == 0) {
-      po[DH] = m;
-      po[DH + 1] = there ? l : 0.0f;
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    if (mt > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < NDT; e += 4)
+        *reinterpret_cast<float4*>(&s_o[wave][4 * c + i][NDT * r + e]) = make_float4(o[mt][e][i], o[mt][e + 1][i], o[mt][e + 2][i], o[mt][e + 3][i]);
+    __syncthreads();
+    // thread: query row tid / 16 of the tile, dimensions NDT (tid % 16) ..
+    const int qr = tid >> 4, d0 = NDT * (tid & 15);
+    float m = -INFINITY, l = 0.0f, f[4], v[NDT];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = fmaxf(m, s_m[k][16 * mt + qr]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // (a wave that saw only rows scored -inf or none holds zeros; NaN stays)
+      f[k] = s_m[k][16 * mt + qr] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s_m[k][16 * mt + qr] - m);
+      l += s_l[k][16 * mt + qr] * f[k];
     }
 #pragma unroll
-    for (int e = 0; e < NDT; e += 4)
-      *reinterpret_cast<float4*>(po + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    for (int e = 0; e < NDT; ++e) {
+      v[e] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[e] += s_o[k][qr][d0 + e] * f[k];
+    }
+    const int row_o = (rb * MT + mt) * 16 + qr;
+    const int t_o = min(row_o, R - 1) / a.group;
+    const unsigned long long anc_o = __shfl(nd.anc, t_o, kWave);
+    const bool there = anc_o != 0;     // (a row of an absent node is zeros)
+    if (row_o >= R) continue;
+    if constexpr (TYPE != SEQ_INT8) {
+      if (s_odd) {
+        for (int j = max(0, max(s_edge, s0) * kStep - Lr); j < a.T && Lr + j < s1 * kStep; ++j) {
+          if (!((anc_o >> j) & 1)) continue;
+          const char* row = static_cast<const char*>(a.c.v) + (unit * a.c.S + Lr + j) * row_bytes + d0 * ES;
+#pragma unroll
+          for (int e = 0; e < NDT; ++e) {
+            const float x = TYPE == SEQ_BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[e])
+                                             : (row[e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+            if (!(fabsf(x) < INFINITY)) v[e] += x;
+          }
+        }
+      }
+    }
+    if (n_ch == 1) {
+      const float inv = there && l != 0.0f ? 1.0f / l : 0.0f;
+      const long at = b * a.o.seq + t_o * a.o.token + (g * a.group + row_o % a.group) * a.o.head + d0;
+#pragma unroll
+      for (int e = 0; e < NDT; e += 4) {
+        float z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = there && l != 0.0f ? v[e + i] * inv : 0.0f;
+        if constexpr (ACT == SEQ_BF16)
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.p) + at + e) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+        else
+          *reinterpret_cast<float4*>(static_cast<float*>(a.o.p) + at + e) = make_float4(z[0], z[1], z[2], z[3]);
+      }
+    } else {
+      const size_t rec = ((size_t(ch_all) * a.c.n_kv + g) * y.rb + rb) * MT + mt;
+      float* po = a.ws + (rec * 16 + qr) * (DH + 4);
+      if (d0 == 0) {
+        po[DH] = m;
+        po[DH + 1] = there ? l : 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < NDT; e += 4)
+        *reinterpret_cast<float4*>(po + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    }
   }
 }
 
 // Joins the chunks' records of one query row: 32 lanes over the dimensions, eight groups over the
 // chunks. Grid (query rows of a sequence, sequences).
 template <int DH, int ACT>
-__global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, int layout_rb, int most) {
+__global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeShape y) {
   constexpr int E = DH / 32;           // dimensions per lane
   __shared__ float s_m[8], s_l[8], s_o[8][DH];
   const int tid = threadIdx.x, lane = tid & 63;
   const int b = blockIdx.y;
-  const Deal d = deal(a, a.c.n_kv * layout_rb, most, lane);
+  const Deal d = deal(a, y, lane);
   const int sub = b & 3;
   const int n = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], b >> 2);
   const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], b >> 2);
@@ -456,7 +490,7 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, int l
   const int grp = tid >> 5, d0 = E * (tid & 31);
   float m = -INFINITY, l = 0.0f, v[E] = {};
   for (int k = grp; k < n; k += 8) {
-    const size_t rec = (size_t(before + k) * a.c.n_kv + g) * layout_rb + row / 16;
+    const size_t rec = (size_t(before + k) * a.c.n_kv + g) * y.rb * y.mt + row / 16;
     const float* po = a.ws + (rec * 16 + row % 16) * (DH + 4);
     const float mk = po[DH], lk = po[DH + 1];
     const float mn = fmaxf(m, mk);
@@ -495,37 +529,42 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, int l
     *reinterpret_cast<float2*>(static_cast<float*>(a.o.p) + at) = make_float2(y0, y1);
 }
 
-// How a call is launched: row blocks of 16 query rows, and chunks per sequence at most.
-struct Shape {
-  int rb, most, grid;
-};
-Shape shape(const TreeAttnArgs& a) {
-  Shape s;
-  s.rb = (a.T * a.group + 15) / 16;
-  const int units = a.c.n_kv * s.rb;
+TreeShape shape(const TreeAttnArgs& a) {
+  TreeShape y;
+  const int tiles = (a.T * a.group + 15) / 16;
+  y.mt = a.act == SEQ_F32 ? std::min(tiles, 2) : tiles > 2 ? 4 : tiles;
+  y.rb = (tiles + y.mt - 1) / y.mt;
+  y.target = y.mt == 4 ? 256 : 512;    // workgroups of four tiles fill a CU's registers alone
+  const int units = a.c.n_kv * y.rb;
   const long steps = (std::min<long>(std::max(a.max_len, 0) + long(a.T), a.c.S) + kStep - 1) / kStep;
-  s.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (kTarget + units - 1) / units)));
+  y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (y.target + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
-  const long chunks = std::min<long>(long(a.c.batch) * s.most, kTarget / units + 1 + a.c.batch);
-  s.grid = int(chunks * units);
-  return s;
+  const long chunks = std::min<long>(long(a.c.batch) * y.most, y.target / units + 1 + a.c.batch);
+  y.grid = int(chunks * units);
+  return y;
 }
 
 }  // namespace
 
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
-  const Shape s = shape(a);
-  return s.most == 1 ? 0 : size_t(s.grid) * 16 * (a.c.dh + 4) * 4;
+  const TreeShape y = shape(a);
+  return y.most == 1 ? 0 : size_t(y.grid) * y.mt * 16 * (a.c.dh + 4) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
-  const Shape y = shape(a);
-#define ATTN(DH, TYPE, ACT) hipLaunchKernelGGL((tree_attn_kernel<DH, TYPE, ACT>), dim3(y.grid), dim3(kBlock), 0, s, a, y.rb, y.most)
-#define ATTN_TYPE(DH, ACT)                                   \
-  do {                                                       \
-    if (a.c.type == SEQ_BF16) ATTN(DH, SEQ_BF16, ACT);       \
-    else if (a.c.type == SEQ_INT8) ATTN(DH, SEQ_INT8, ACT);  \
-    else ATTN(DH, SEQ_E4M3, ACT);                            \
+  const TreeShape y = shape(a);
+#define ATTN(DH, TYPE, ACT, MT) hipLaunchKernelGGL((tree_attn_kernel<DH, TYPE, ACT, MT>), dim3(y.grid), dim3(kBlock), 0, s, a, y)
+#define ATTN_MT(DH, TYPE, ACT)                                            \
+  do {                                                                    \
+    if (y.mt == 1) ATTN(DH, TYPE, ACT, 1);                                \
+    else if (y.mt == 2) ATTN(DH, TYPE, ACT, 2);                           \
+    else if constexpr (ACT == SEQ_BF16) ATTN(DH, TYPE, ACT, 4);           \
+  } while (0)
+#define ATTN_TYPE(DH, ACT)                                      \
+  do {                                                          \
+    if (a.c.type == SEQ_BF16) ATTN_MT(DH, SEQ_BF16, ACT);       \
+    else if (a.c.type == SEQ_INT8) ATTN_MT(DH, SEQ_INT8, ACT);  \
+    else ATTN_MT(DH, SEQ_E4M3, ACT);                            \
   } while (0)
   if (a.c.dh == 128) {
     if (a.act == SEQ_BF16) ATTN_TYPE(128, SEQ_BF16);
@@ -535,10 +574,11 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
     else ATTN_TYPE(64, SEQ_F32);
   }
 #undef ATTN_TYPE
+#undef ATTN_MT
 #undef ATTN
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || y.most == 1) return e;
-#define JOIN(DH, ACT) hipLaunchKernelGGL((tree_join_kernel<DH, ACT>), dim3(a.T * a.n_q, a.c.batch), dim3(kBlock), 0, s, a, y.rb, y.most)
+#define JOIN(DH, ACT) hipLaunchKernelGGL((tree_join_kernel<DH, ACT>), dim3(a.T * a.n_q, a.c.batch), dim3(kBlock), 0, s, a, y)
   if (a.c.dh == 128) {
     if (a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
     else JOIN(128, SEQ_F32);
