@@ -358,18 +358,22 @@ def tasp_copy_probe(dst_ptr, src_ptr, nbytes, stream):
 
 
 def _ref(struct):
-    """The address of a struct, or None."""
-    return None if struct is None else C.addressof(struct)
+    """The address of a struct; bytes that hold one, and None, as they are."""
+    return struct if struct is None or type(struct) is bytes else C.addressof(struct)
 
 
 def tasp_seq_append(cache, layer, rope, parent_ptr, T, act_type, q, k, v, n_q_heads, q_out, stream):
-    """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs."""
-    _check(load().tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, _ref(q), _ref(k),
-                                  _ref(v), n_q_heads, _ref(q_out), stream))
+    """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs, or their bytes."""
+    st = (_lib or load()).tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, _ref(q), _ref(k),
+                                          _ref(v), n_q_heads, _ref(q_out), stream)
+    if st:
+        _check(st)
 
 
 def tasp_seq_read(cache, layer, first_ptr, n, out_type, k_out, v_out, stream):
-    _check(load().tasp_seq_read(_ref(cache), layer, first_ptr, n, out_type, _ref(k_out), _ref(v_out), stream))
+    st = (_lib or load()).tasp_seq_read(_ref(cache), layer, first_ptr, n, out_type, _ref(k_out), _ref(v_out), stream)
+    if st:
+        _check(st)
 
 
 def tasp_tree_attention_workspace_bytes(cache, n_q_heads, T, max_len):
@@ -380,8 +384,10 @@ def tasp_tree_attention_workspace_bytes(cache, n_q_heads, T, max_len):
 
 def tasp_tree_attention(cache, layer, parent_ptr, T, act_type, q, n_q_heads, scale, max_len, out, ws_ptr,
                         ws_bytes, stream):
-    _check(load().tasp_tree_attention(_ref(cache), layer, parent_ptr, T, act_type, _ref(q), n_q_heads, scale,
-                                      max_len, _ref(out), ws_ptr, ws_bytes, stream))
+    st = (_lib or load()).tasp_tree_attention(_ref(cache), layer, parent_ptr, T, act_type, _ref(q), n_q_heads, scale,
+                                              max_len, _ref(out), ws_ptr, ws_bytes, stream)
+    if st:
+        _check(st)
 
 
 def tasp_verify_workspace_bytes(batch, T, vocab):
@@ -392,9 +398,13 @@ def tasp_verify_workspace_bytes(batch, T, vocab):
 
 def tasp_verify(logits_ptr, tokens_ptr, u_ptr, parent_ptr, draft_ptr, batch, T, vocab, temperature, ids_ptr,
                 path_ptr, n_ptr, ws_ptr, ws_bytes, stream):
-    _check(load().tasp_verify(logits_ptr, tokens_ptr, u_ptr, parent_ptr, draft_ptr, batch, T, vocab,
-                              temperature, ids_ptr, path_ptr, n_ptr, ws_ptr, ws_bytes, stream))
+    st = (_lib or load()).tasp_verify(logits_ptr, tokens_ptr, u_ptr, parent_ptr, draft_ptr, batch, T, vocab,
+                                      temperature, ids_ptr, path_ptr, n_ptr, ws_ptr, ws_bytes, stream)
+    if st:
+        _check(st)
 
 
 def tasp_seq_commit(cache, path_ptr, n_ptr, T, len_out_ptr, stream):
-    _check(load().tasp_seq_commit(_ref(cache), path_ptr, n_ptr, T, len_out_ptr, stream))
+    st = (_lib or load()).tasp_seq_commit(_ref(cache), path_ptr, n_ptr, T, len_out_ptr, stream)
+    if st:
+        _check(st)

@@ -5,6 +5,7 @@ forwards calls. No arithmetic of the decode path happens here.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import numpy as np
 import torch
@@ -333,50 +334,50 @@ class Router:
 _SEQ_TYPES = {torch.bfloat16: B.BF16, torch.float32: B.F32, torch.int8: B.INT8, torch.float8_e4m3fn: B.E4M3}
 
 
-class _On:
-    """The call's stream on the tensors' device: the current stream of that device unless one is given, and
-    that device current while the call launches."""
-
-    def __init__(self, t, stream):
-        self.dev = t.device.index
-        self.stream = stream if stream is not None else C.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
-
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.dev:
-            torch.cuda.set_device(self.dev)
-        return self.stream
-
-    def __exit__(self, *_):
-        if self.was != self.dev:
-            torch.cuda.set_device(self.was)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (absent in builds without a GPU)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_pack_rows = struct.Struct("Pqqq").pack                              # a tasp_rows
 
 
-def _same_device(t, *others):
+def _launch(f, dev, stream, *args):
+    """f(*args, stream) on device `dev`: on its current stream unless one is given."""
+    if stream is None:
+        stream = _raw_stream(dev)
+    if dev == _current_device():
+        f(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            f(*args, stream)
+
+
+def _device(t, *others):
+    """The index of the GPU that holds every tensor given."""
+    dev = t.get_device()
     for o in others:
-        if o is not None and o.device != t.device:
+        if o is not None and o.get_device() != dev:
             raise ValueError(f"tensors on {t.device} and {o.device}")
-    if t.device.type != "cuda":
+    if dev < 0:
         raise ValueError(f"tensors on {t.device}: a GPU is needed")
+    return dev
 
 
 def _ptr(t, shape, dtype, what):
     """Address of a contiguous tensor of the given shape and type; None for None."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor of {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _rows(t, shape, dtype, what, order=(0, 1, 2)):
-    """tasp_rows of a tensor [.., .., .., head_dim]: `order` names its sequence, token and head axes."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.stride(3) != 1:
-        raise ValueError(f"{what} must be a {dtype} tensor of {tuple(shape)} with contiguous heads, not {t.dtype} {tuple(t.shape)}")
+def _rows(t, shape, dtype, what, token=1, head=2):
+    """The tasp_rows (as bytes) of a tensor [B][..][..][dh]; token, head: the axes between."""
     st = t.stride()
+    if t.shape != shape or t.dtype != dtype or st[3] != 1:
+        raise ValueError(f"{what} must be a {dtype} tensor of {tuple(shape)} with contiguous heads, not {t.dtype} {tuple(t.shape)}")
     # (the stride of an axis of one is never used, and may be anything)
-    st = [st[i] if t.shape[i] > 1 else 0 for i in order]
-    return B.tasp_rows(t.data_ptr(), *st)
+    return _pack_rows(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[token] if shape[token] > 1 else 0,
+                      st[head] if shape[head] > 1 else 0)
 
 
 def _empty(shape, dtype, device, stream):
@@ -400,7 +401,7 @@ class SeqCache:
     def __init__(self, k, v, length, k_scale=None, v_scale=None):
         if k.dtype not in (torch.bfloat16, torch.int8, torch.float8_e4m3fn) or k.dim() != 5:
             raise ValueError(f"k must be a bfloat16, int8 or float8_e4m3fn tensor [L][B][Hkv][S][dh], not {k.dtype} {tuple(k.shape)}")
-        _same_device(k, v, length, k_scale, v_scale)
+        self.dev = _device(k, v, length, k_scale, v_scale)
         self.k, self.v, self.len, self.k_scale, self.v_scale = k, v, length, k_scale, v_scale
         wide = k.dtype == torch.bfloat16
         if wide == (k_scale is not None) or wide == (v_scale is not None):
@@ -420,7 +421,7 @@ class SeqCache:
         return cls(k, v, torch.zeros(batch, dtype=torch.int32, device=device), *sc)
 
     def _parent(self, parent, T):
-        return _ptr(parent, (self.batch, T), torch.int32, "parent")
+        return None if parent is None else _ptr(parent, (self.batch, T), torch.int32, "parent")
 
 
 class Rope:
@@ -435,31 +436,32 @@ class Rope:
 def seq_append(cache, layer, q, k, v, rope=None, parent=None, q_out=None, stream=None):
     """Write k, v ``[B][T][Hkv][dh]`` behind the sequences (their lengths stay) and return q ``[B][T][Hq][dh]``
     rotated (None without queries). Any strides whose rows are 16-byte aligned; bfloat16 or float32."""
-    _same_device(cache.k, q, k, v, parent, q_out)
-    T = k.shape[1]
+    dev = _device(cache.k, q, k, v, parent, q_out)
+    T, dt = k.shape[1], k.dtype
     kv = (cache.batch, T, cache.n_kv, cache.dh)
-    qs = os_ = None
+    rq = ro = None
     n_q = 0
     if q is not None:
         n_q = q.shape[2]
+        shape = (cache.batch, T, n_q, cache.dh)
         if q_out is None:
-            q_out = _empty(q.shape, q.dtype, q.device, stream)
-        qs = _rows(q, (cache.batch, T, n_q, cache.dh), k.dtype, "q")
-        os_ = _rows(q_out, q.shape, k.dtype, "q_out")
-    with _On(cache.k, stream) as s:
-        B.tasp_seq_append(cache.struct, layer, None if rope is None else rope.struct, cache._parent(parent, T), T,
-                          _SEQ_TYPES[k.dtype], qs, _rows(k, kv, k.dtype, "k"), _rows(v, kv, k.dtype, "v"), n_q, os_, s)
+            q_out = _empty(shape, dt, q.device, stream)
+        rq, ro = _rows(q, shape, dt, "q"), _rows(q_out, shape, dt, "q_out")
+    _launch(B.tasp_seq_append, dev, stream, cache.struct, layer, None if rope is None else rope.struct,
+            cache._parent(parent, T), T, _SEQ_TYPES[dt], rq, _rows(k, kv, dt, "k"), _rows(v, kv, dt, "v"), n_q, ro)
     return q_out
 
 
 def seq_read(cache, layer, n, first=None, dtype=torch.bfloat16, out=None, stream=None):
     """(k, v) ``[B][Hkv][n][dh]``: rows first .. first + n - 1 (device int32 [B]; None: 0) as values."""
     shape = (cache.batch, cache.n_kv, n, cache.dh)
-    k, v = out if out is not None else (_empty(shape, dtype, cache.k.device, stream) for _ in range(2))
-    _same_device(cache.k, first, k, v)
-    with _On(cache.k, stream) as s:
-        B.tasp_seq_read(cache.struct, layer, _ptr(first, (cache.batch,), torch.int32, "first"), n, _SEQ_TYPES[k.dtype],
-                        _rows(k, shape, k.dtype, "k", (0, 2, 1)), _rows(v, shape, k.dtype, "v", (0, 2, 1)), s)
+    if out is not None:
+        k, v = out
+    else:
+        k, v = _empty(shape, dtype, cache.k.device, stream), _empty(shape, dtype, cache.k.device, stream)
+    dev, dt = _device(cache.k, first, k, v), k.dtype
+    _launch(B.tasp_seq_read, dev, stream, cache.struct, layer, _ptr(first, (cache.batch,), torch.int32, "first"), n,
+            _SEQ_TYPES[dt], _rows(k, shape, dt, "k", 2, 1), _rows(v, shape, dt, "v", 2, 1))
     return k, v
 
 
@@ -472,18 +474,17 @@ def tree_attention_workspace(cache, n_q_heads, T, max_len=None, stream=None):
 def tree_attention(cache, layer, q, parent=None, scale=None, max_len=None, out=None, workspace=None, stream=None):
     """Attention of the appended nodes' queries ``[B][T][Hq][dh]`` over their sequences and ancestors. max_len: the
     largest length expected; workspace: of tree_attention_workspace with the same arguments (else one of the call's own)."""
-    _same_device(cache.k, q, parent, out)
-    T, n_q = q.shape[1:3]
+    dev, dt = _device(cache.k, q, parent, out), q.dtype
+    T, n_q = q.shape[1], q.shape[2]
     shape = (cache.batch, T, n_q, cache.dh)
     if out is None:
-        out = _empty(shape, q.dtype, q.device, stream)
+        out = _empty(shape, dt, q.device, stream)
     if max_len is None:
         max_len = cache.max_seq
     ws = workspace if workspace is not None else tree_attention_workspace(cache, n_q, T, max_len, stream)
-    with _On(cache.k, stream) as s:
-        B.tasp_tree_attention(cache.struct, layer, cache._parent(parent, T), T, _SEQ_TYPES[q.dtype],
-                              _rows(q, shape, q.dtype, "q"), n_q, cache.dh ** -0.5 if scale is None else scale, max_len,
-                              _rows(out, shape, q.dtype, "out"), ws[1], ws[2], s)
+    _launch(B.tasp_tree_attention, dev, stream, cache.struct, layer, cache._parent(parent, T), T, _SEQ_TYPES[dt],
+            _rows(q, shape, dt, "q"), n_q, cache.dh ** -0.5 if scale is None else scale, max_len,
+            _rows(out, shape, dt, "out"), ws[1], ws[2])
     return out
 
 
@@ -495,26 +496,23 @@ def verify_workspace(batch, T, vocab, device="cuda", stream=None):
 def verify(logits, tokens, u, parent=None, draft_logits=None, temperature=1.0, workspace=None, stream=None):
     """Verify drafted tokens int32 ``[B][T]`` (node 0: the text's last token) against float32 logits ``[B][T][V]``
     with random numbers u ``[B][T]``. Returns (ids, path, n): the emitted tokens and the accepted nodes, -1 behind them."""
-    _same_device(logits, tokens, u, parent, draft_logits)
+    dev = _device(logits, tokens, u, parent, draft_logits)
     nb, T, V = logits.shape
-    ids, path = (_empty((nb, T), torch.int32, logits.device, stream) for _ in range(2))
-    n = _empty(nb, torch.int32, logits.device, stream)
+    ids, path = _empty((2, nb, T), torch.int32, logits.device, stream)
+    n = _empty((nb,), torch.int32, logits.device, stream)
     ws = workspace if workspace is not None else verify_workspace(nb, T, V, logits.device, stream)
-    with _On(logits, stream) as s:
-        B.tasp_verify(_ptr(logits, (nb, T, V), torch.float32, "logits"), _ptr(tokens, (nb, T), torch.int32, "tokens"),
-                      _ptr(u, (nb, T), torch.float32, "u"), _ptr(parent, (nb, T), torch.int32, "parent"),
-                      _ptr(draft_logits, (nb, T - 1, V), torch.float32, "draft_logits"), nb, T, V, temperature,
-                      ids.data_ptr(), path.data_ptr(), n.data_ptr(), ws[1], ws[2], s)
+    _launch(B.tasp_verify, dev, stream, _ptr(logits, (nb, T, V), torch.float32, "logits"),
+            _ptr(tokens, (nb, T), torch.int32, "tokens"), _ptr(u, (nb, T), torch.float32, "u"),
+            _ptr(parent, (nb, T), torch.int32, "parent"), _ptr(draft_logits, (nb, T - 1, V), torch.float32, "draft_logits"),
+            nb, T, V, temperature, ids.data_ptr(), path.data_ptr(), n.data_ptr(), ws[1], ws[2])
     return ids, path, n
 
 
 def seq_commit(cache, path, n, len_out=None, stream=None):
     """Move the accepted paths' rows together in every layer and return the new lengths (len_out None: in cache.len)."""
-    _same_device(cache.k, path, n, len_out)
     if len_out is None:
         len_out = cache.len
-    with _On(cache.k, stream) as s:
-        B.tasp_seq_commit(cache.struct, _ptr(path, (cache.batch, path.shape[1]), torch.int32, "path"),
-                          _ptr(n, (cache.batch,), torch.int32, "n"), path.shape[1],
-                          _ptr(len_out, (cache.batch,), torch.int32, "len_out"), s)
+    dev, nb, T = _device(cache.k, path, n, len_out), cache.batch, path.shape[1]
+    _launch(B.tasp_seq_commit, dev, stream, cache.struct, _ptr(path, (nb, T), torch.int32, "path"),
+            _ptr(n, (nb,), torch.int32, "n"), T, _ptr(len_out, (nb,), torch.int32, "len_out"))
     return len_out

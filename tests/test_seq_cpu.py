@@ -163,6 +163,7 @@ def test_session_refuses_tensors_before_the_library():
         S._ptr(ln, (3,), torch.int32, "len")
     with pytest.raises(ValueError):
         S._rows(k[0].transpose(2, 3), (2, 2, 64, 8), torch.bfloat16, "q")
-    r = S._rows(k[0], (2, 2, 8, 64), torch.bfloat16, "k", (0, 2, 1))
-    assert (r.seq, r.token, r.head) == (1024, 64, 512)
+    r = B.tasp_rows.from_buffer_copy(S._rows(k[0], (2, 2, 8, 64), torch.bfloat16, "k", 2, 1))
+    assert (r.p, r.seq, r.token, r.head) == (k.data_ptr(), 1024, 64, 512)
+    assert B.tasp_rows.from_buffer_copy(S._rows(k[0, :, :1], (2, 1, 8, 64), torch.bfloat16, "k")).token == 0
     assert C.sizeof(B.tasp_rows) == 32 and C.sizeof(B.tasp_seq_cache) == 72 and C.sizeof(B.tasp_rope) == 56
