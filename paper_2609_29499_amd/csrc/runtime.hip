@@ -2162,7 +2162,11 @@ tasp_status tasp_tree_attention_workspace_bytes(const tasp_seq_cache* cache, int
   tasp::TreeAttnArgs a{};
   if ((st = tree_attn_args(cache, n_q_heads, T, max_len, &a))) return st;
   a.c = seq_layer(cache, 0);
-  *bytes = tasp::tree_attn_workspace_bytes(a);
+  *bytes = 0;
+  for (int act : {TASP_BF16, TASP_F32}) {              // launched in blocks of other sizes
+    a.act = act;
+    *bytes = std::max(*bytes, tasp::tree_attn_workspace_bytes(a));
+  }
   return TASP_OK;
 }
 

@@ -3,15 +3,13 @@
 //
 // o = softmax(scale q K^T) V per query head; a sequence's nodes and the query heads of one cache head
 // form the rows of one product, row = node * group + head, so each K and V row is read once for all
-// of them. A wave holds 16 of these rows and walks cache rows in steps of 32, straight from memory in the
-// matrix instructions' layout (v_mfma_f32_16x16x32_bf16):
-//   * S^T = K Q^T: lane (r, c) holds cache row r of a tile of 16 and, of its dimensions, the pieces that 16
-//     bytes at 16 c of each 64 give (any order serves that q shares); it gets the scores of query row r
-//     against cache rows 4 c .. 4 c + 3: P stays in registers, and is the A operand of
-//   * O += P V over the step's two tiles: lane (r, c) loads cache rows 4 c .. 4 c + 3 of both tiles, dh / 16
-//     dimensions from dh / 16 * r on, as whole coalesced rows, and turns them in registers (two rows' halves per
+// of them. Tiles of 16 query rows by 32 cache rows (a step) run on v_mfma_f32_16x16x32_bf16:
+//   * S^T = K Q^T: lane (r, c) gets the scores of query row r against cache rows 4 c .. 4 c + 3 of each tile of
+//     16: P stays in registers, and is the A operand of
+//   * O += P V over the step's two tiles: lane (r, c) holds cache rows 4 c .. 4 c + 3 of both tiles, dh / 16
+//     dimensions from dh / 16 * r on: whole coalesced rows, turned in registers (two rows' halves per
 //     v_perm) into the operand's columns of eight rows. The output's dimensions are then dh / 16 * r + i: again
-//     neighbours, so rows are stored whole. No LDS is used before the waves' results meet.
+//     neighbours, so rows are stored whole.
 // Rows in 8 bits become BF16 exactly; their scales multiply scores and probabilities in 32 bits. P is
 // carried as two BF16 terms (16 bits; one alone would double the error of a BF16 output), float32 q and P
 // as three (24 bits, as exact as the products' float32 sums).
@@ -19,10 +17,17 @@
 // Softmax with a running maximum per query row, raised only when a score passes it by 8 powers of two (sums
 // are float32, so the slack costs no accuracy): most steps exchange nothing between lanes.
 //
+// Two kernels. Up to 32 query rows (tree_attn_kernel) a wave keeps all of them and walks every fourth step
+// straight from memory in the operands' layout, the next step's loads in flight; no LDS is used before
+// the four waves' results meet. More rows (tree_attn_wide_kernel) are dealt to the four waves, which share
+// steps of 64 cache rows through LDS: two waves load, widen and lay out V, two K, for the next step while all
+// compute on the present one, so that widening and turning are done once per row and not per wave.
+//
 // The cache rows of all sequences are cut into chunks of equal length (from the lengths on the device: no
-// host knows them), a workgroup takes one chunk of one cache head, its four waves every fourth
-// step. Sequences of one chunk are written at once; the others leave (maximum, sum, unnormalised output)
-// per query row in the workspace, which a second launch joins in chunk order.
+// host knows them); a workgroup takes one chunk of one cache head. A sequence of one chunk is written at
+// once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which a
+// second launch joins in chunk order. (Joining by the last workgroup of a sequence to finish was slower: one
+// workgroup's latencies in a row, 8 us for 16 chunks of 16 query rows, 29 us for 64 of 32, against 4 and 7 us.)
 #include <algorithm>
 #include <type_traits>
 
@@ -42,10 +47,10 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 // ---- which rows a workgroup serves
 // Sequence b has steps(b) = ceil((L + T) / 32) steps and is cut in chunks of `chunk` steps. A wave holds four
 // sequences per lane.
-// How a call is launched: query rows in rb blocks of 16 mt, `target` workgroups aimed at, at most `most`
+// How a call is launched: query rows in rb blocks (of 16 mt rows, wide: 64 mt), `target` workgroups aimed at, at most `most`
 // chunks per sequence (what the workspace has room for), grid workgroups.
 struct TreeShape {
-  int mt, rb, target, most, grid;
+  int wide, mt, rb, target, most, grid;
 };
 struct Deal {
   int chunk;                           // steps per chunk
@@ -131,6 +136,164 @@ __device__ __forceinline__ void terms(float v0, float v1, uint32_t* o, int strid
   }
 }
 
+// One query row's scores of a step (lane (r, c): cache rows 4 c + i of both tiles) to the terms of P.
+// t0: the step's first row minus the cached rows, i.e. rows from 0 on are the tree's; edge: there are
+// such rows (or rows behind them), of which the row sees those in anc.
+template <int NDT, int PT, bool SCALED>
+__device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks)[8], const float (&vs)[8], float scale2, bool edge, int t0, int c,
+                                          unsigned long long anc, float& m_run, float& l_run, f32x4 (&o)[NDT], uint32_t (&pf)[PT][4]) {
+  float p[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i] = sc[i >> 2][i & 3] * (SCALED ? ks[i] : scale2);
+  uint32_t seen = 0xffu;
+  if (edge) {
+    seen = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = t0 + 16 * (i >> 2) + 4 * c + (i & 3);
+      const bool in = j < 0 || (j < kTreeMax && ((anc >> (j & 63)) & 1));
+      seen |= uint32_t(in) << i;
+      p[i] = in ? p[i] : -INFINITY;
+    }
+  }
+  const float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+  if (__ballot(top > m_run + kSlack)) {                // (also the first rows: m_run is -inf)
+    const float mn = fmaxf(m_run, quad_max(top));
+    const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
+    m_run = mn;
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = __shfl(alpha, 4 * c + i, kWave);
+#pragma unroll
+      for (int e = 0; e < NDT; ++e) o[e][i] *= f;
+    }
+  }
+  const float base = m_run == -INFINITY ? 0.0f : m_run;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    p[i] = __builtin_amdgcn_exp2f(p[i] - base);
+    l_run += p[i];
+    if constexpr (SCALED) p[i] *= (seen >> i) & 1 ? vs[i] : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[0][e], 4);
+}
+
+// Non-finite halves of V words become zeros; returns a non-zero word if there are any.
+__device__ __forceinline__ uint32_t drop_odd(uint32_t& v) {
+  const uint32_t top = ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u;      // a half's exponent is full
+  v &= ~((top >> 15) * 0xffffu);
+  return top;
+}
+// Adds the non-finite values that drop_odd left out to one query row's outputs: of the tree's rows
+// from .. to - 1 (cache rows) that the row sees.
+template <int DH, int TYPE, int N>
+__device__ __forceinline__ void add_odd(const TreeAttnArgs& a, size_t unit, int Lr, int from, int to, unsigned long long anc, int d0, float (&v)[N]) {
+  constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
+  for (int j = max(0, from - Lr); j < a.T && Lr + j < to; ++j) {
+    if (!((anc >> j) & 1)) continue;
+    const char* row = static_cast<const char*>(a.c.v) + ((unit * a.c.S + Lr + j) * DH + d0) * ES;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float x = TYPE == SEQ_BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[e])
+                                       : (row[e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+      if (!(fabsf(x) < INFINITY)) v[e] += x;
+    }
+  }
+}
+
+// The part of the work that a workgroup takes.
+struct Place {
+  int b, g, rb;                        // sequence, cache head, block of query rows
+  int n_ch, ch, rec;                   // chunks of the sequence, this one, and its record
+  int L, Lr, end;                      // length (-1: passed over), rows cached, rows that may be read
+  int s0, s1;                          // steps
+};
+__device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, Place& p) {
+  const Deal d = deal(a, y, lane);
+  // Row blocks of one chunk and head read the same rows: eight workgroups apart (one XCD, one L2) and next to
+  // each other in time. Item: chunk of a sequence x cache head.
+  const int w = blockIdx.x, j = w >> 3;
+  p.rb = j % y.rb;
+  const int item = (j / y.rb) * 8 + (w & 7);
+  if (item >= d.total * a.c.n_kv) return false;
+  p.g = item % a.c.n_kv;
+  const int all = item / a.c.n_kv;
+  int hit = -1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (all >= d.before[i] && all < d.before[i] + d.mine[i]) hit = i;
+  const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
+  const int sub = __builtin_amdgcn_readlane(hit, owner);
+  p.b = 4 * owner + sub;
+  const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], owner);
+  p.n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
+  p.ch = all - before;
+  p.rec = item * y.rb + p.rb;
+  p.L = seq_len(a.c.len, p.b, a.c.S);
+  p.Lr = max(p.L, 0);
+  p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
+  const int steps = (p.end + kStep - 1) / kStep;
+  // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
+  const int per = p.n_ch * d.chunk >= steps ? d.chunk : ((steps + p.n_ch - 1) / p.n_ch + 3) / 4 * 4;
+  p.s0 = p.ch * per;
+  p.s1 = p.ch == p.n_ch - 1 ? steps : min(steps, p.s0 + per);
+  return true;
+}
+
+// One query row's NDT output values (unnormalised) with their sum l and maximum m: to the output, or to
+// row `row` of the chunk's record of RB rows. there: the row is that of a node that is present.
+template <int DH, int ACT, int N>
+__device__ __forceinline__ void put_output(const TreeAttnArgs& a, int b, int g, int row, int d0, float l, bool there, const float (&v)[N]) {
+  const float inv = there && l != 0.0f ? 1.0f / l : 0.0f;
+  const long at = b * a.o.seq + (row / a.group) * a.o.token + (g * a.group + row % a.group) * a.o.head + d0;
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    float z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = there && l != 0.0f ? v[e + i] * inv : 0.0f;
+    if constexpr (ACT == SEQ_BF16)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.p) + at + e) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(a.o.p) + at + e) = make_float4(z[0], z[1], z[2], z[3]);
+  }
+}
+
+// A record: [RB][DH] outputs, then [RB] (maximum, sum).
+template <int DH, int RB>
+constexpr size_t kRecFloats = size_t(RB) * (DH + 2);
+template <int DH, int RB, int N>
+__device__ __forceinline__ void put_record(const TreeAttnArgs& a, int rec, int row, int d0, float m, float l, const float (&v)[N]) {
+  float* po = a.ws + size_t(rec) * kRecFloats<DH, RB>;
+#pragma unroll
+  for (int e = 0; e < N; e += 4)
+    *reinterpret_cast<float4*>(po + row * DH + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+  if (d0 == 0) *reinterpret_cast<float2*>(po + RB * DH + 2 * row) = make_float2(m, l);
+}
+
+// A query row's operand: from `at` on (elements from q.p) 8 values for each of dh / 32 products, those of product
+// kk 32 kk further on, or (PAIRED) 64 floor(kk / 2) + 8 (kk mod 2)
+template <int DH, int ACT, int QT, bool PAIRED>
+__device__ __forceinline__ void load_q(const TreeAttnArgs& a, long at0, uint32_t (&qf)[QT][DH / 32][4]) {
+#pragma unroll
+  for (int kk = 0; kk < DH / 32; ++kk) {
+    const long at = at0 + (PAIRED ? 64 * (kk >> 1) + 8 * (kk & 1) : 32 * kk);
+    if constexpr (ACT == SEQ_BF16) {
+      const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.p) + at);
+      qf[0][kk][0] = x.x; qf[0][kk][1] = x.y; qf[0][kk][2] = x.z; qf[0][kk][3] = x.w;
+    } else {
+      const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q.p) + at);
+      const float4 x = f[0], z = f[1];
+      uint32_t* o = &qf[0][kk][0];
+      terms<QT>(x.x, x.y, o, DH / 8);
+      terms<QT>(x.z, x.w, o + 1, DH / 8);
+      terms<QT>(z.x, z.y, o + 2, DH / 8);
+      terms<QT>(z.z, z.w, o + 3, DH / 8);
+    }
+  }
+}
+
 template <int DH, int TYPE>
 struct Rows32 {                        // a step's K and V as loaded
   static constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
@@ -153,36 +316,16 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   constexpr int NDT = DH / 16;         // dimensions per lane of V and O
   constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 2;
   using Rows = Rows32<DH, TYPE>;
+  constexpr int RB = 16 * MT;
   __shared__ float s_o[4][16][DH + 4];
-  __shared__ float s_m[4][16 * MT], s_l[4][16 * MT];
+  __shared__ float s_m[4][RB], s_l[4][RB];
   __shared__ int s_odd;                // a tree's row holds something not finite
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = lane & 15, c = lane >> 4;
-  const int units = a.c.n_kv * y.rb;
-  const Deal d = deal(a, y, lane);
-  // workgroup -> row block (slowest), chunk of a sequence, cache head
-  const int w = blockIdx.x;
-  if (w >= d.total * units) return;
-  const int g = w % a.c.n_kv, ch_all = (w / a.c.n_kv) % d.total, rb = w / (a.c.n_kv * d.total);
-  int hit = -1;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (ch_all >= d.before[i] && ch_all < d.before[i] + d.mine[i]) hit = i;
-  const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
-  const int sub = __builtin_amdgcn_readlane(hit, owner);
-  const int b = 4 * owner + sub;
-  const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], owner);
-  const int n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
-  const int ch = ch_all - before;
-
-  const int L = seq_len(a.c.len, b, a.c.S);
-  const int Lr = max(L, 0);                            // cached rows (none of a sequence passed over)
-  const int end = L < 0 ? 0 : min(L + a.T, a.c.S);     // rows that may be read
-  const int steps = (end + kStep - 1) / kStep;
-  // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
-  const int per = n_ch * d.chunk >= steps ? d.chunk : ((steps + n_ch - 1) / n_ch + 3) / 4 * 4;
-  const int s0 = ch * per, s1 = ch == n_ch - 1 ? steps : min(steps, s0 + per);
+  Place p;
+  if (!place(a, y, lane, p)) return;
+  const int b = p.b, g = p.g, rb = p.rb, L = p.L, Lr = p.Lr, end = p.end, s0 = p.s0, s1 = p.s1;
   // steps from s_edge on hold rows of the tree: at most three, so a wave has one at most
   const int s_edge = min(Lr / kStep, s1);
 
@@ -245,23 +388,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     const int row = min((rb * MT + mt) * 16 + r, R - 1);   // (rows past the last one repeat it and are not stored)
     const int t = row / a.group, h = g * a.group + row % a.group;
     anc[mt] = __shfl(nd.anc, t, kWave);
-    const long at = b * a.q.seq + t * a.q.token + h * a.q.head;
-#pragma unroll
-    for (int kk = 0; kk < NKC; ++kk) {
-      const int dim = ES == 2 ? 32 * kk + 8 * c : 64 * (kk >> 1) + 16 * c + 8 * (kk & 1);
-      if constexpr (ACT == SEQ_BF16) {
-        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q.p) + at + dim);
-        qf[mt][0][kk][0] = x.x; qf[mt][0][kk][1] = x.y; qf[mt][0][kk][2] = x.z; qf[mt][0][kk][3] = x.w;
-      } else {
-        const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.q.p) + at + dim);
-        const float4 x = f[0], z = f[1];
-        uint32_t* o = &qf[mt][0][kk][0];
-        terms<QT>(x.x, x.y, o, NKC * 4);
-        terms<QT>(x.z, x.w, o + 1, NKC * 4);
-        terms<QT>(z.x, z.y, o + 2, NKC * 4);
-        terms<QT>(z.z, z.w, o + 3, NKC * 4);
-      }
-    }
+    load_q<DH, ACT, QT, ES == 1>(a, b * a.q.seq + t * a.q.token + h * a.q.head + (ES == 2 ? 8 : 16) * c, qf[mt]);
   }
 
   float m_run[MT], l_run[MT];                          // of query row r; l of this lane's cache rows
@@ -300,46 +427,10 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     uint32_t pf[MT][PT][4];
     float ks[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ks[i] = TYPE == SEQ_BF16 ? a.scale2 : x.ks[i] * a.scale2;
+    for (int i = 0; i < 8; ++i) ks[i] = TYPE == SEQ_BF16 ? 0.0f : x.ks[i] * a.scale2;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = sc[mt][i >> 2][i & 3] * ks[i];
-      uint32_t seen = 0xffu;                           // of the lane's eight cache rows
-      if constexpr (EDGE) {
-        seen = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int j = s * kStep + 16 * (i >> 2) + 4 * c + (i & 3) - Lr;
-          const bool in = j < 0 || (j < kTreeMax && ((anc[mt] >> (j & 63)) & 1));
-          seen |= uint32_t(in) << i;
-          p[i] = in ? p[i] : -INFINITY;
-        }
-      }
-      float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-      if (__ballot(top > m_run[mt] + kSlack)) {        // (also the first rows: m_run is -inf)
-        const float mn = fmaxf(m_run[mt], quad_max(top));
-        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[mt] - mn);
-        m_run[mt] = mn;
-        l_run[mt] *= alpha;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = __shfl(alpha, 4 * c + i, kWave);
-#pragma unroll
-          for (int e = 0; e < NDT; ++e) o[mt][e][i] *= f;
-        }
-      }
-      const float base = m_run[mt] == -INFINITY ? 0.0f : m_run[mt];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(p[i] - base);
-        l_run[mt] += p[i];
-        if constexpr (TYPE != SEQ_BF16) p[i] *= EDGE && !((seen >> i) & 1) ? 0.0f : x.vs[i];
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[mt][0][e], 4);
-    }
+    for (int mt = 0; mt < MT; ++mt)
+      soft_step<NDT, PT, TYPE != SEQ_BF16>(sc[mt], ks, x.vs, a.scale2, EDGE, s * kStep - Lr, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
     // V: eight rows of NDT dimensions as BF16 pairs
     uint32_t v[8][NDT / 2];
 #pragma unroll
@@ -358,12 +449,9 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
       uint32_t bad = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
+        if (s * kStep + 16 * (i >> 2) + 4 * c + (i & 3) >= Lr)
 #pragma unroll
-        for (int e = 0; e < NDT / 2; ++e) {
-          const uint32_t top = ((v[i][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's exponent is full
-          bad |= top;
-          v[i][e] &= ~((top >> 15) * 0xffffu);
-        }
+          for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
       if (bad) s_odd = 1;
     }
 #pragma unroll
@@ -432,115 +520,296 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     const bool there = anc_o != 0;     // (a row of an absent node is zeros)
     if (row_o >= R) continue;
     if constexpr (TYPE != SEQ_INT8) {
-      if (s_odd) {
-        for (int j = max(0, max(s_edge, s0) * kStep - Lr); j < a.T && Lr + j < s1 * kStep; ++j) {
-          if (!((anc_o >> j) & 1)) continue;
-          const char* row = static_cast<const char*>(a.c.v) + (unit * a.c.S + Lr + j) * row_bytes + d0 * ES;
+      if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, max(s_edge, s0) * kStep, s1 * kStep, anc_o, d0, v);
+    }
+    if (p.n_ch == 1) put_output<DH, ACT>(a, b, g, row_o, d0, l, there, v);
+    else put_record<DH, RB>(a, p.rec, 16 * mt + qr, d0, m, there ? l : 0.0f, v);
+  }
+}
+
+// MT: tiles of 16 query rows per wave; a workgroup holds 64 MT rows.
+template <int DH, int TYPE, int ACT, int MT>
+__global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs a, TreeShape y) {
+  constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
+  constexpr int NKC = DH / 32, NDT = DH / 16, RB = 64 * MT;
+  constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 2;
+  constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a K row as loaded
+  constexpr int KL = 32 * PPR / kWave; // K loads per thread: 32 rows per wave
+  constexpr int VW = NDT * ES / 4;     // words of V per lane and row
+  // Operands of a step of 64 rows, each 16 bytes per lane: K [tile of 16 rows][32 dimensions], V [32 rows][dimension i]
+  struct Step {
+    uint4 k[4][NKC][kWave];
+    uint4 v[2][NDT][kWave];
+  };
+  __shared__ Step s_step[2];
+  __shared__ float s_scale[2][2][64];  // [step][K / V][row]
+  __shared__ int s_odd;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = lane & 15, c = lane >> 4;
+  Place p;
+  if (!place(a, y, lane, p)) return;
+  const int Lr = p.Lr, end = p.end;
+  const size_t unit = size_t(p.b) * a.c.n_kv + p.g;
+  const uint32_t row_bytes = DH * ES;
+  const bool for_v = wave < 2;         // this wave brings V (32 rows), or K
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(for_v ? a.c.v : a.c.k) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
+  const __amdgpu_buffer_rsrc_t rks = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.ks + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
+  const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
+  const int half = 32 * (wave & 1);    // its rows of the step
+
+  uint32_t st[8][4];                   // what is on its way
+  float st_scale = 0.0f;
+  auto load = [&](int s) {             // (steps past the last read as zeros)
+    const uint32_t t0 = uint32_t(s) * kStep + half;
+    const bool in = s < p.s1;
+    if constexpr (TYPE != SEQ_BF16)
+      st_scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(for_v ? rvs : rks, int(in && lane < 32 ? (t0 + lane) * 4u : kOOB), 0, 0));
+    if (for_v) {
 #pragma unroll
-          for (int e = 0; e < NDT; ++e) {
-            const float x = TYPE == SEQ_BF16 ? bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[e])
-                                             : (row[e] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
-            if (!(fabsf(x) < INFINITY)) v[e] += x;
-          }
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t off = in ? (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r : kOOB;
+        if constexpr (VW == 4) {
+          const int4 q = buf_load16_stream(rx, off);
+          st[i][0] = q.x; st[i][1] = q.y; st[i][2] = q.z; st[i][3] = q.w;
+        } else if constexpr (VW == 2) {
+          const auto q = __builtin_amdgcn_raw_buffer_load_b64(rx, int(off), 0, kCpolStream);
+          st[i][0] = q[0]; st[i][1] = q[1];
+        } else {
+          st[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rx, int(off), 0, kCpolStream);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        const uint32_t row = t0 + i * (kWave / PPR) + lane / PPR;
+        const int4 q = buf_load16_stream(rx, in ? row * row_bytes + 16u * (lane % PPR) : kOOB);
+        st[i][0] = q.x; st[i][1] = q.y; st[i][2] = q.z; st[i][3] = q.w;
+      }
+    }
+  };
+  auto commit = [&](int buf, int s) {
+    Step& z = s_step[buf];
+    if constexpr (TYPE != SEQ_BF16)
+      if (lane < 32) s_scale[buf][for_v][half + lane] = for_v ? st_scale : st_scale * a.scale2;
+    if (for_v) {
+      uint32_t v[8][NDT / 2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (TYPE == SEQ_BF16) {
+#pragma unroll
+          for (int e = 0; e < NDT / 2; ++e) v[i][e] = st[i][e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(st[i][e], &v[i][2 * e]);
+        }
+      }
+      const int new_row = Lr - s * kStep - half;       // the first of the wave's rows that is the tree's
+      if (TYPE != SEQ_INT8 && new_row < 32) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
+#pragma unroll
+            for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
+        if (bad) s_odd = 1;
+      }
+#pragma unroll
+      for (int e = 0; e < NDT; ++e) {
+        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+        z.v[wave][e][lane] = make_uint4(__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel), __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel),
+                                        __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
+      }
+    } else {
+      // lane (r', c') of operand kk reads slot 16 c' + (r' ^ (4 kk + c')): the pieces of one row, written
+      // together, go to different banks
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        const int row = half + i * (kWave / PPR) + lane / PPR, j = lane % PPR;
+        auto put = [&](int piece, uint4 q) {
+          const int kk = piece >> 2, cc = piece & 3;
+          z.k[row >> 4][kk][16 * cc + ((row & 15) ^ (4 * kk + cc))] = q;
+        };
+        if constexpr (TYPE == SEQ_BF16) {
+          put(j, make_uint4(st[i][0], st[i][1], st[i][2], st[i][3]));
+        } else {
+          uint32_t w[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) widen<TYPE>(st[i][e], &w[2 * e]);
+          put(2 * j, make_uint4(w[0], w[1], w[2], w[3]));
+          put(2 * j + 1, make_uint4(w[4], w[5], w[6], w[7]));
         }
       }
     }
-    if (n_ch == 1) {
-      const float inv = there && l != 0.0f ? 1.0f / l : 0.0f;
-      const long at = b * a.o.seq + t_o * a.o.token + (g * a.group + row_o % a.group) * a.o.head + d0;
+  };
+
+  load(p.s0);
+  if (tid == 0) s_odd = 0;
+  // this lane's query rows, as rows of Q (B operand): node t, head h
+  const int R = a.T * a.group;
+  const TreeNode nd = tree_node(a.parent ? a.parent + size_t(p.b) * a.T : nullptr, a.T, p.L < 0 ? 0 : a.c.S - p.L, lane);
+  unsigned long long anc[MT];
+  uint32_t qf[MT][QT][NKC][4];
 #pragma unroll
-      for (int e = 0; e < NDT; e += 4) {
-        float z[4];
+  for (int mt = 0; mt < MT; ++mt) {
+    const int row = min(p.rb * RB + (wave * MT + mt) * 16 + r, R - 1);     // (rows past the last one repeat it and are not stored)
+    const int t = row / a.group, h = p.g * a.group + row % a.group;
+    anc[mt] = __shfl(nd.anc, t, kWave);
+    load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
+  }
+  float m_run[MT], l_run[MT];          // of query row r; l of this lane's cache rows
+  f32x4 o[MT][NDT];                    // lane (r, c): query rows 4 c + i, dimension NDT r + d
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = there && l != 0.0f ? v[e + i] * inv : 0.0f;
-        if constexpr (ACT == SEQ_BF16)
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.p) + at + e) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-        else
-          *reinterpret_cast<float4*>(static_cast<float*>(a.o.p) + at + e) = make_float4(z[0], z[1], z[2], z[3]);
+  for (int mt = 0; mt < MT; ++mt) {
+    m_run[mt] = -INFINITY;
+    l_run[mt] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  __syncthreads();                     // s_odd
+
+  // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
+  int buf = 0;
+  for (int s = p.s0; s < p.s1; s += 2, buf ^= 1) {
+    commit(buf, s);
+    load(s + 2);
+    __syncthreads();
+    const Step& z = s_step[buf];
+    const int t0 = s * kStep - Lr;
+    const bool edge = t0 + 64 > 0;
+#pragma unroll
+    for (int half_ = 0; half_ < 2; ++half_) {
+      f32x4 sc[MT][2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kk = 0; kk < NKC; ++kk) {
+          const uint4 q = z.k[2 * half_ + tt][kk][16 * c + (r ^ (4 * kk + c))];
+          const uint32_t kf[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int k = 0; k < QT; ++k) sc[mt][tt] = mfma(kf, qf[mt][k][kk], sc[mt][tt]);
+        }
       }
-    } else {
-      const size_t rec = ((size_t(ch_all) * a.c.n_kv + g) * y.rb + rb) * MT + mt;
-      float* po = a.ws + (rec * 16 + qr) * (DH + 4);
-      if (d0 == 0) {
-        po[DH] = m;
-        po[DH + 1] = there ? l : 0.0f;
-      }
+      float ks[8] = {}, vs[8] = {};
+      if constexpr (TYPE != SEQ_BF16) {
 #pragma unroll
-      for (int e = 0; e < NDT; e += 4)
-        *reinterpret_cast<float4*>(po + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        for (int tt = 0; tt < 2; ++tt) {
+          const float4 x = *reinterpret_cast<const float4*>(&s_scale[buf][0][32 * half_ + 16 * tt + 4 * c]);
+          const float4 w = *reinterpret_cast<const float4*>(&s_scale[buf][1][32 * half_ + 16 * tt + 4 * c]);
+          ks[4 * tt] = x.x; ks[4 * tt + 1] = x.y; ks[4 * tt + 2] = x.z; ks[4 * tt + 3] = x.w;
+          vs[4 * tt] = w.x; vs[4 * tt + 1] = w.y; vs[4 * tt + 2] = w.z; vs[4 * tt + 3] = w.w;
+        }
+      }
+      uint32_t pf[MT][PT][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+        soft_step<NDT, PT, TYPE != SEQ_BF16>(sc[mt], ks, vs, a.scale2, edge, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
+#pragma unroll
+      for (int e = 0; e < NDT; ++e) {
+        const uint4 q = z.v[half_][e][lane];
+        const uint32_t vb[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int k = 0; k < PT; ++k) o[mt][e] = mfma(pf[mt][k], vb, o[mt][e]);
+      }
+    }
+  }
+
+  // every wave holds its rows' results: lane (r, c) rows 4 c + i of a tile, their maxima and sums in lanes 4 c + i
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l_all = quad_sum(l_run[mt]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
+      const float m = __shfl(m_run[mt], 4 * c + i, kWave), l = __shfl(l_all, 4 * c + i, kWave);
+      const unsigned long long anc_o = __shfl(nd.anc, min(row, R - 1) / a.group, kWave);
+      float v[NDT];
+#pragma unroll
+      for (int e = 0; e < NDT; ++e) v[e] = o[mt][e][i];
+      if constexpr (TYPE != SEQ_INT8)
+        if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, p.s0 * kStep, p.s1 * kStep, anc_o, NDT * r, v);
+      if (row < R) {
+        if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, p.g, row, NDT * r, l, anc_o != 0, v);
+        else put_record<DH, RB>(a, p.rec, in, NDT * r, m, anc_o != 0 ? l : 0.0f, v);
+      }
     }
   }
 }
 
-// Joins the chunks' records of one query row: 32 lanes over the dimensions, eight groups over the
-// chunks. Grid (query rows of a sequence, sequences).
+// Joins the chunks' records of one query row: dh / 4 lanes over the dimensions, the others over the chunks.
+// Grid (query rows of a sequence, sequences).
 template <int DH, int ACT>
 __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeShape y) {
-  constexpr int E = DH / 32;           // dimensions per lane
-  __shared__ float s_m[8], s_l[8], s_o[8][DH];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int b = blockIdx.y;
-  const Deal d = deal(a, y, lane);
+  constexpr int LPR = DH / 4, GR = kBlock / LPR;       // lanes per row, chunks at a time
+  __shared__ float s_m[GR], s_l[GR];
+  __shared__ float4 s_o[GR][LPR];
+  const int tid = threadIdx.x, b = blockIdx.y;
+  const Deal d = deal(a, y, tid & 63);
   const int sub = b & 3;
   const int n = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], b >> 2);
   const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], b >> 2);
   if (n <= 1) return;                  // written already
   const int t = blockIdx.x / a.n_q, h = blockIdx.x % a.n_q;
   const int g = h / a.group, row = t * a.group + h % a.group;
-  const int grp = tid >> 5, d0 = E * (tid & 31);
-  float m = -INFINITY, l = 0.0f, v[E] = {};
-  for (int k = grp; k < n; k += 8) {
-    const size_t rec = (size_t(before + k) * a.c.n_kv + g) * y.rb * y.mt + row / 16;
-    const float* po = a.ws + (rec * 16 + row % 16) * (DH + 4);
-    const float mk = po[DH], lk = po[DH + 1];
-    const float mn = fmaxf(m, mk);
+  const int rows = (y.wide ? 64 : 16) * y.mt, rb = row / rows, in = row % rows;
+  const float* first = a.ws + (size_t(before) * a.c.n_kv + g) * y.rb * rows * (DH + 2) + size_t(rb) * rows * (DH + 2);
+  const size_t stride = size_t(a.c.n_kv) * y.rb * rows * (DH + 2);
+  const int grp = tid / LPR, d0 = 4 * (tid % LPR);
+  float m = -INFINITY, l = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int k = grp; k < n; k += GR) {
+    const float* po = first + k * stride;
+    const float2 q = *reinterpret_cast<const float2*>(po + rows * DH + 2 * in);
+    const float4 x = *reinterpret_cast<const float4*>(po + in * DH + d0);
+    const float mn = fmaxf(m, q.x);
     const float fa = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-    const float fb = mk == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mk - mn);
+    const float fb = q.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(q.x - mn);
     m = mn;
-    l = l * fa + lk * fb;
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = v[e] * fa + po[d0 + e] * fb;
+    l = l * fa + q.y * fb;
+    v.x = v.x * fa + x.x * fb; v.y = v.y * fa + x.y * fb; v.z = v.z * fa + x.z * fb; v.w = v.w * fa + x.w * fb;
   }
-  if ((tid & 31) == 0) {
+  if (d0 == 0) {
     s_m[grp] = m;
     s_l[grp] = l;
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) s_o[grp][d0 + e] = v[e];
+  s_o[grp][tid % LPR] = v;
   __syncthreads();
-  if (tid >= DH / 2) return;
-  float mm = -INFINITY, ll = 0.0f, y0 = 0.0f, y1 = 0.0f;
+  if (tid >= LPR) return;
+  m = -INFINITY;
+  l = 0.0f;
+  float z[4] = {};
 #pragma unroll
-  for (int k = 0; k < 8; ++k) mm = fmaxf(mm, s_m[k]);
+  for (int k = 0; k < GR; ++k) m = fmaxf(m, s_m[k]);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float f = s_m[k] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s_m[k] - mm);
-    ll += s_l[k] * f;
-    y0 += s_o[k][2 * tid] * f;
-    y1 += s_o[k][2 * tid + 1] * f;
+  for (int k = 0; k < GR; ++k) {
+    const float f = s_m[k] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s_m[k] - m);
+    l += s_l[k] * f;
+    z[0] += s_o[k][tid].x * f; z[1] += s_o[k][tid].y * f; z[2] += s_o[k][tid].z * f; z[3] += s_o[k][tid].w * f;
   }
-  const bool any = ll != 0.0f;
-  y0 = any ? y0 / ll : 0.0f;
-  y1 = any ? y1 / ll : 0.0f;
-  const long at = b * a.o.seq + t * a.o.token + h * a.o.head + 2 * tid;
-  if constexpr (ACT == SEQ_BF16)
-    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.o.p) + at) = pack_bf16(y0, y1);
-  else
-    *reinterpret_cast<float2*>(static_cast<float*>(a.o.p) + at) = make_float2(y0, y1);
+  put_output<DH, ACT>(a, b, g, row, d0, l, true, z);
 }
 
 TreeShape shape(const TreeAttnArgs& a) {
   TreeShape y;
   const int tiles = (a.T * a.group + 15) / 16;
-  y.mt = a.act == SEQ_F32 ? std::min(tiles, 2) : tiles > 2 ? 4 : tiles;
-  y.rb = (tiles + y.mt - 1) / y.mt;
-  y.target = y.mt == 4 ? 256 : 512;    // workgroups of four tiles fill a CU's registers alone
+  y.wide = tiles > 2;
+  y.mt = y.wide ? (tiles > 4 && a.act == SEQ_BF16 ? 2 : 1) : tiles;
+  const int block = (y.wide ? 4 : 1) * y.mt;           // tiles of a workgroup
+  y.rb = (tiles + block - 1) / block;
+  y.target = 512;                      // two workgroups per CU
   const int units = a.c.n_kv * y.rb;
   const long steps = (std::min<long>(std::max(a.max_len, 0) + long(a.T), a.c.S) + kStep - 1) / kStep;
   y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (y.target + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
   const long chunks = std::min<long>(long(a.c.batch) * y.most, y.target / units + 1 + a.c.batch);
-  y.grid = int(chunks * units);
+  y.grid = int((chunks * a.c.n_kv + 7) / 8 * 8 * y.rb);
   return y;
 }
 
@@ -548,17 +817,19 @@ TreeShape shape(const TreeAttnArgs& a) {
 
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
   const TreeShape y = shape(a);
-  return y.most == 1 ? 0 : size_t(y.grid) * y.mt * 16 * (a.c.dh + 4) * 4;
+  const size_t rows = size_t(y.wide ? 64 : 16) * y.mt;
+  return y.most == 1 ? 0 : size_t(y.grid) * rows * (a.c.dh + 2) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
   const TreeShape y = shape(a);
-#define ATTN(DH, TYPE, ACT, MT) hipLaunchKernelGGL((tree_attn_kernel<DH, TYPE, ACT, MT>), dim3(y.grid), dim3(kBlock), 0, s, a, y)
-#define ATTN_MT(DH, TYPE, ACT)                                            \
-  do {                                                                    \
-    if (y.mt == 1) ATTN(DH, TYPE, ACT, 1);                                \
-    else if (y.mt == 2) ATTN(DH, TYPE, ACT, 2);                           \
-    else if constexpr (ACT == SEQ_BF16) ATTN(DH, TYPE, ACT, 4);           \
+#define ATTN(KERNEL, DH, TYPE, ACT, MT) hipLaunchKernelGGL((KERNEL<DH, TYPE, ACT, MT>), dim3(y.grid), dim3(kBlock), 0, s, a, y)
+#define ATTN_MT(DH, TYPE, ACT)                                                                   \
+  do {                                                                                           \
+    if (!y.wide && y.mt == 1) ATTN(tree_attn_kernel, DH, TYPE, ACT, 1);                          \
+    else if (!y.wide) ATTN(tree_attn_kernel, DH, TYPE, ACT, 2);                                  \
+    else if (y.mt == 1) ATTN(tree_attn_wide_kernel, DH, TYPE, ACT, 1);                           \
+    else if constexpr (ACT == SEQ_BF16) ATTN(tree_attn_wide_kernel, DH, TYPE, ACT, 2);           \
   } while (0)
 #define ATTN_TYPE(DH, ACT)                                      \
   do {                                                          \
@@ -578,15 +849,11 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
 #undef ATTN
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || y.most == 1) return e;
-#define JOIN(DH, ACT) hipLaunchKernelGGL((tree_join_kernel<DH, ACT>), dim3(a.T * a.n_q, a.c.batch), dim3(kBlock), 0, s, a, y)
-  if (a.c.dh == 128) {
-    if (a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
-    else JOIN(128, SEQ_F32);
-  } else {
-    if (a.act == SEQ_BF16) JOIN(64, SEQ_BF16);
-    else JOIN(64, SEQ_F32);
-  }
-#undef JOIN
+  const dim3 rows(a.T * a.n_q, a.c.batch);
+  if (a.c.dh == 128 && a.act == SEQ_BF16) hipLaunchKernelGGL((tree_join_kernel<128, SEQ_BF16>), rows, dim3(kBlock), 0, s, a, y);
+  else if (a.c.dh == 128) hipLaunchKernelGGL((tree_join_kernel<128, SEQ_F32>), rows, dim3(kBlock), 0, s, a, y);
+  else if (a.act == SEQ_BF16) hipLaunchKernelGGL((tree_join_kernel<64, SEQ_BF16>), rows, dim3(kBlock), 0, s, a, y);
+  else hipLaunchKernelGGL((tree_join_kernel<64, SEQ_F32>), rows, dim3(kBlock), 0, s, a, y);
   return hipGetLastError();
 }
 

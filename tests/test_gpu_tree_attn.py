@@ -72,14 +72,15 @@ def test_tree_attention(case):
     check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
 
 
-@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
-def test_long_contexts_in_many_chunks(kind):
+@pytest.mark.parametrize("kind,T,hq,dh", [("bf16", 3, 4, 128), ("int8", 3, 4, 128), ("e4m3", 9, 8, 64),
+                                          ("int8", 12, 8, 128), ("bf16", 20, 8, 64), ("e4m3", 33, 8, 128)])
+def test_long_contexts_in_many_chunks(kind, T, hq, dh):
     """Ragged sequences over several chunks, a hint of the length that is too small, strided q and out."""
     lens = [20000, 700, 0, 9001]
-    flush(f"case long {kind}")
-    T, hq, H, dh = 3, 4, 2, 128
-    c, kv, vv = typed_cache(lens, H, 20010, dh, kind, 7)
-    parent = torch.tensor([[-1, 0, 0]] * 4, dtype=torch.int32)
+    flush(f"case long {kind} {T} {hq} {dh}")
+    H = 2
+    c, kv, vv = typed_cache(lens, H, 20040, dh, kind, 7)
+    parent = random_parents(4, T, 7, absent=False)
     wide = torch.zeros((4, T, 3, hq, dh), dtype=torch.bfloat16, device="cuda")
     q = randn((4, T, hq, dh), torch.bfloat16, 8)
     wide[:, :, 1] = q.cuda()
@@ -88,7 +89,7 @@ def test_long_contexts_in_many_chunks(kind):
     for hint in (20000, 4000, 100):
         S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint, out=out[:, :, :hq])
         torch.cuda.synchronize()
-        check(out[:, :, :hq].double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 20010, "bf16", dh ** -0.5)
+        check(out[:, :, :hq].double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 20040, "bf16", dh ** -0.5, sorted({0, T // 2, T - 1}))
         assert torch.all(out[:, :, hq] == 5.0)
         again = S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint)
         torch.cuda.synchronize()
@@ -116,15 +117,16 @@ def test_layers_behind_32_bit_offsets():
     assert not c.k[:L - 1].any() and not c.k[L - 1, 0, :, :lens].any()
 
 
+@pytest.mark.parametrize("hq", [4, 16])
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
-def test_unseen_rows_reach_nothing(kind):
+def test_unseen_rows_reach_nothing(kind, hq):
     """Infinities and NaN in rows of other branches, of absent nodes and behind the nodes."""
-    flush(f"case unseen {kind}")
+    flush(f"case unseen {kind} {hq}")
     lens, T, dh = [40, 0], 6, 64
     S_ = 60
     c, kv, vv = typed_cache(lens, 2, S_, dh, kind, 10)
     parent = torch.tensor([[-1, 0, 0, 1, 2, -2], [-1, 0, 0, 1, 2, -2]], dtype=torch.int32)
-    q = randn((2, T, 4, dh), torch.bfloat16, 11)
+    q = randn((2, T, hq, dh), torch.bfloat16, 11)
     clean = S.tree_attention(c, 0, q.cuda(), parent.cuda())
     for b in range(2):
         for r, what in ((2, math.nan), (5, math.inf), (7, math.nan)):      # node 2, an absent node, behind the tree
@@ -144,19 +146,22 @@ def test_unseen_rows_reach_nothing(kind):
     assert torch.isnan(got[:, 2]).any(-1).all() and torch.isnan(got[:, 4]).any(-1).all()
 
 
-def test_visible_infinities_stay_in_their_dimensions():
-    flush("case visible infinities")
-    c, kv, vv = typed_cache([10], 1, 20, 64, "bf16", 12)
-    q = randn((1, 3, 2, 64), torch.bfloat16, 13).cuda()
-    parent = torch.tensor([[-1, 0, 0]], dtype=torch.int32, device="cuda")
+@pytest.mark.parametrize("T", [3, 17])
+def test_visible_infinities_stay_in_their_dimensions(T):
+    flush(f"case visible infinities {T}")
+    c, kv, vv = typed_cache([10], 1, 30, 64, "bf16", 12)
+    q = randn((1, T, 2, 64), torch.bfloat16, 13).cuda()
+    parent = torch.tensor([[-1] + [0] * (T - 1)], dtype=torch.int32, device="cuda")
     clean = S.tree_attention(c, 0, q, parent)
     c.v[0, 0, 0, 11, 3], c.v[0, 0, 0, 11, 4], c.v[0, 0, 0, 11, 5] = math.inf, -math.inf, math.nan
     c.v[0, 0, 0, 10, 4] = math.inf
+    c.v[0, 0, 0, 6, 8] = math.nan                                       # a cached row, next to the tree's
     got = S.tree_attention(c, 0, q, parent).float()
     torch.cuda.synchronize()
     assert torch.all(got[0, 1, :, 3] == math.inf) and torch.isnan(got[0, 1, :, 4:6]).all()   # node 1: its own row and node 0's
     assert torch.all(got[0, 0, :, 4] == math.inf) and torch.all(got[0, 2, :, 4] == math.inf)
-    rest = [d for d in range(64) if d not in (3, 4, 5)]
+    assert torch.isnan(got[0, :, :, 8]).all()
+    rest = [d for d in range(64) if d not in (3, 4, 5, 8)]
     assert torch.equal(got[0][:, :, rest], clean.float()[0][:, :, rest])
 
 
