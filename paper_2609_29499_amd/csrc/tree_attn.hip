@@ -72,8 +72,28 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, 
   }
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) sum += __shfl_xor(sum, k, kWave);
-  const int chunk = max(kMinSteps, int((long(sum) * a.c.n_kv * y.rb + y.target - 1) / y.target));
-  d.chunk = (chunk + 3) / 4 * 4;
+  // (said to be the same in all lanes wherever it is: a buffer descriptor or a branch that the compiler takes for
+  // divergent becomes a loop over lanes, around every load)
+  sum = __builtin_amdgcn_readfirstlane(sum);
+  const int units = a.c.n_kv * y.rb, chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
+  d.chunk = chunk;
+  const int quota = y.target / units;
+  if (a.c.batch > 1 && 2 * a.c.batch <= quota) {
+    // Sequences are rounded up to whole chunks: the shortest chunk that keeps all workgroups within the target is
+    // looked for, a candidate per lane (workgroups beyond it would make a second round: the 64-node case
+    // 298 us with 1.5 rounds)
+    const int mine = chunk + lane * max(4, chunk / 256 * 4);
+    const float inv = 1.0f / float(mine);
+    int count = 0;
+    for (int b = 0; b < a.c.batch; ++b) {
+      const int i = b & 3, nb = __builtin_amdgcn_readlane(i == 0 ? n[0] : i == 1 ? n[1] : i == 2 ? n[2] : n[3], b >> 2);
+      int q = int(float(nb) * inv);                    // within one of the quotient; rounded up below
+      q += q * mine < nb ? 1 : 0;
+      count += q;
+    }
+    const unsigned long long fits = __ballot(count <= quota);
+    d.chunk = __builtin_amdgcn_readlane(mine, fits ? __ffsll((long long)fits) - 1 : kWave - 1);
+  }
   int own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -137,17 +157,16 @@ __device__ __forceinline__ void terms(float v0, float v1, uint32_t* o, int strid
 }
 
 // One query row's scores of a step (lane (r, c): cache rows 4 c + i of both tiles) to the terms of P.
-// t0: the step's first row minus the cached rows, i.e. rows from 0 on are the tree's; edge: there are
+// t0: the step's first row minus the cached rows, i.e. rows from 0 on are the tree's; EDGE: there are
 // such rows (or rows behind them), of which the row sees those in anc.
-template <int NDT, int PT, bool SCALED>
-__device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks)[8], const float (&vs)[8], float scale2, bool edge, int t0, int c,
+template <int NDT, int PT, bool SCALED, bool EDGE>
+__device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks)[8], const float (&vs)[8], float scale2, int t0, int c,
                                           unsigned long long anc, float& m_run, float& l_run, f32x4 (&o)[NDT], uint32_t (&pf)[PT][4]) {
   float p[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) p[i] = sc[i >> 2][i & 3] * (SCALED ? ks[i] : scale2);
-  uint32_t seen = 0xffu;
-  if (edge) {
-    seen = 0;
+  uint32_t seen = 0;
+  if constexpr (EDGE) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int j = t0 + 16 * (i >> 2) + 4 * c + (i & 3);
@@ -174,7 +193,7 @@ __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks
   for (int i = 0; i < 8; ++i) {
     p[i] = __builtin_amdgcn_exp2f(p[i] - base);
     l_run += p[i];
-    if constexpr (SCALED) p[i] *= (seen >> i) & 1 ? vs[i] : 0.0f;
+    if constexpr (SCALED) p[i] *= !EDGE || ((seen >> i) & 1) ? vs[i] : 0.0f;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[0][e], 4);
@@ -231,7 +250,7 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   p.n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
   p.ch = all - before;
   p.rec = item * y.rb + p.rb;
-  p.L = seq_len(a.c.len, p.b, a.c.S);
+  p.L = __builtin_amdgcn_readfirstlane(seq_len(a.c.len, p.b, a.c.S));
   p.Lr = max(p.L, 0);
   p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
   const int steps = (p.end + kStep - 1) / kStep;
@@ -308,7 +327,8 @@ struct Rows32 {                        // a step's K and V as loaded
 template <int DH, int TYPE, int ACT, int MT>
 constexpr int kWavesPerSimd = MT == 4 || (MT == 2 && DH == 128 && (TYPE == SEQ_BF16 || ACT == SEQ_F32)) ? 1 : 2;
 
-// MT: tiles of 16 query rows per wave
+// MT: tiles of 16 query rows per wave. (Lambdas here are inlined by order: called, they would keep what they
+// capture in memory, descriptors among it.)
 template <int DH, int TYPE, int ACT, int MT>
 __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tree_attn_kernel(TreeAttnArgs a, TreeShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
@@ -321,7 +341,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   __shared__ float s_m[4][RB], s_l[4][RB];
   __shared__ int s_odd;                // a tree's row holds something not finite
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, c = lane >> 4;
   Place p;
   if (!place(a, y, lane, p)) return;
@@ -337,7 +357,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
 
   // Steps are loaded one ahead. Rows past `end`, and steps past `stop`, read as zeros without touching memory.
-  auto load = [&](int s, int stop, Rows& x) {
+  auto load = [&](int s, int stop, Rows& x) __attribute__((always_inline)) {
     const uint32_t t0 = uint32_t(s) * kStep;
     const bool in = s < stop;
 #pragma unroll
@@ -401,28 +421,33 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  auto process = [&](Rows& x, int s, auto edge_) {
+  auto process = [&](Rows& x, int s, auto edge_) __attribute__((always_inline)) {
     constexpr bool EDGE = decltype(edge_)::value;
+    // (accumulators take turns: a product waits for the one before it on the same accumulator)
     f32x4 sc[MT][2];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int kk = 0; kk < NKC; ++kk) {
-        uint32_t kf[4];
+    for (int kk = 0; kk < NKC; ++kk) {
+      uint32_t kf[2][4];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
         if constexpr (TYPE == SEQ_BF16) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) kf[e] = x.k[tt][kk][e];
+          for (int e = 0; e < 4; ++e) kf[tt][e] = x.k[tt][kk][e];
         } else {
-          widen<TYPE>(x.k[tt][kk >> 1][2 * (kk & 1)], kf);
-          widen<TYPE>(x.k[tt][kk >> 1][2 * (kk & 1) + 1], kf + 2);
+          widen<TYPE>(x.k[tt][kk >> 1][2 * (kk & 1)], kf[tt]);
+          widen<TYPE>(x.k[tt][kk >> 1][2 * (kk & 1) + 1], kf[tt] + 2);
         }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int q = 0; q < QT; ++q) sc[mt][tt] = mfma(kf, qf[mt][q][kk], sc[mt][tt]);
       }
+#pragma unroll
+      for (int q = 0; q < QT; ++q)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = mfma(kf[tt], qf[mt][q][kk], sc[mt][tt]);
     }
     uint32_t pf[MT][PT][4];
     float ks[8];
@@ -430,7 +455,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     for (int i = 0; i < 8; ++i) ks[i] = TYPE == SEQ_BF16 ? 0.0f : x.ks[i] * a.scale2;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
-      soft_step<NDT, PT, TYPE != SEQ_BF16>(sc[mt], ks, x.vs, a.scale2, EDGE, s * kStep - Lr, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
+      soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, x.vs, a.scale2, s * kStep - Lr, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
     // V: eight rows of NDT dimensions as BF16 pairs
     uint32_t v[8][NDT / 2];
 #pragma unroll
@@ -455,15 +480,19 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
       if (bad) s_odd = 1;
     }
 #pragma unroll
-    for (int e = 0; e < NDT; ++e) {
-      const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-      uint32_t vb[4];
+    for (int e = 0; e < NDT; e += 2) {
+      uint32_t vb[2][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vb[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], sel);
+      for (int i = 0; i < 4; ++i) {
+        vb[0][i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], 0x05040100u);
+        vb[1][i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], 0x07060302u);
+      }
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int k = 0; k < PT; ++k)
 #pragma unroll
-        for (int k = 0; k < PT; ++k) o[mt][e] = mfma(pf[mt][k], vb, o[mt][e]);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) o[mt][e + i] = mfma(pf[mt][k], vb[i], o[mt][e + i]);
     }
   };
   if constexpr (TYPE != SEQ_INT8) {
@@ -536,6 +565,8 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a K row as loaded
   constexpr int KL = 32 * PPR / kWave; // K loads per thread: 32 rows per wave
   constexpr int VW = NDT * ES / 4;     // words of V per lane and row
+  constexpr int NW = 8 * VW;           // words per lane of 32 rows, of either
+  static_assert(NW == 4 * KL, "K and V rows are equally wide");
   // Operands of a step of 64 rows, each 16 bytes per lane: K [tile of 16 rows][32 dimensions], V [32 rows][dimension i]
   struct Step {
     uint4 k[4][NKC][kWave];
@@ -545,7 +576,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   __shared__ float s_scale[2][2][64];  // [step][K / V][row]
   __shared__ int s_odd;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, c = lane >> 4;
   Place p;
   if (!place(a, y, lane, p)) return;
@@ -558,25 +589,28 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
   const int half = 32 * (wave & 1);    // its rows of the step
 
-  uint32_t st[8][4];                   // what is on its way
-  float st_scale = 0.0f;
-  auto load = [&](int s) {             // (steps past the last read as zeros)
+  // what a wave has on its way: 32 rows of K or of V of the next step
+  struct Raw {
+    uint32_t w[NW];
+    float scale;
+  };
+  auto load = [&](Raw& x, int s) __attribute__((always_inline)) {     // (steps past the last read as zeros)
     const uint32_t t0 = uint32_t(s) * kStep + half;
     const bool in = s < p.s1;
     if constexpr (TYPE != SEQ_BF16)
-      st_scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(for_v ? rvs : rks, int(in && lane < 32 ? (t0 + lane) * 4u : kOOB), 0, 0));
+      x.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(for_v ? rvs : rks, int(in && lane < 32 ? (t0 + lane) * 4u : kOOB), 0, 0));
     if (for_v) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t off = in ? (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r : kOOB;
         if constexpr (VW == 4) {
           const int4 q = buf_load16_stream(rx, off);
-          st[i][0] = q.x; st[i][1] = q.y; st[i][2] = q.z; st[i][3] = q.w;
+          x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
         } else if constexpr (VW == 2) {
           const auto q = __builtin_amdgcn_raw_buffer_load_b64(rx, int(off), 0, kCpolStream);
-          st[i][0] = q[0]; st[i][1] = q[1];
+          x.w[2 * i] = q[0]; x.w[2 * i + 1] = q[1];
         } else {
-          st[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rx, int(off), 0, kCpolStream);
+          x.w[i] = __builtin_amdgcn_raw_buffer_load_b32(rx, int(off), 0, kCpolStream);
         }
       }
     } else {
@@ -584,41 +618,55 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
       for (int i = 0; i < KL; ++i) {
         const uint32_t row = t0 + i * (kWave / PPR) + lane / PPR;
         const int4 q = buf_load16_stream(rx, in ? row * row_bytes + 16u * (lane % PPR) : kOOB);
-        st[i][0] = q.x; st[i][1] = q.y; st[i][2] = q.z; st[i][3] = q.w;
+        x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
       }
     }
   };
-  auto commit = [&](int buf, int s) {
+  auto commit = [&](const Raw& x, int buf, int s) __attribute__((always_inline)) {
     Step& z = s_step[buf];
     if constexpr (TYPE != SEQ_BF16)
-      if (lane < 32) s_scale[buf][for_v][half + lane] = for_v ? st_scale : st_scale * a.scale2;
+      if (lane < 32) s_scale[buf][for_v][half + lane] = for_v ? x.scale : x.scale * a.scale2;
     if (for_v) {
-      uint32_t v[8][NDT / 2];
+      if constexpr (TYPE == SEQ_INT8) {
+        // byte d of eight rows' words -> one operand: widened, and packed two rows at a time
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (TYPE == SEQ_BF16) {
+        for (int e = 0; e < NDT; ++e) {
+          uint32_t q[4];
 #pragma unroll
-          for (int e = 0; e < NDT / 2; ++e) v[i][e] = st[i][e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(st[i][e], &v[i][2 * e]);
+          for (int i = 0; i < 4; ++i) {
+            const float f0 = float(int8_t(x.w[2 * i * VW + e / 4] >> (8 * (e & 3)))), f1 = float(int8_t(x.w[(2 * i + 1) * VW + e / 4] >> (8 * (e & 3))));
+            q[i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+          }
+          z.v[wave][e][lane] = make_uint4(q[0], q[1], q[2], q[3]);
         }
-      }
-      const int new_row = Lr - s * kStep - half;       // the first of the wave's rows that is the tree's
-      if (TYPE != SEQ_INT8 && new_row < 32) {
-        uint32_t bad = 0;
+      } else {
+        uint32_t v[8][NDT / 2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (TYPE == SEQ_BF16) {
 #pragma unroll
-            for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
-        if (bad) s_odd = 1;
-      }
+            for (int e = 0; e < NDT / 2; ++e) v[i][e] = x.w[i * VW + e];
+          } else {
 #pragma unroll
-      for (int e = 0; e < NDT; ++e) {
-        const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-        z.v[wave][e][lane] = make_uint4(__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel), __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel),
-                                        __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
+            for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(x.w[i * VW + e], &v[i][2 * e]);
+          }
+        }
+        const int new_row = Lr - s * kStep - half;     // the first of the wave's rows that is the tree's
+        if (new_row < 32) {
+          uint32_t bad = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
+#pragma unroll
+              for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
+          if (bad) s_odd = 1;
+        }
+#pragma unroll
+        for (int e = 0; e < NDT; ++e) {
+          const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+          z.v[wave][e][lane] = make_uint4(__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel), __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel),
+                                          __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
+        }
       }
     } else {
       // lane (r', c') of operand kk reads slot 16 c' + (r' ^ (4 kk + c')): the pieces of one row, written
@@ -626,16 +674,16 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 #pragma unroll
       for (int i = 0; i < KL; ++i) {
         const int row = half + i * (kWave / PPR) + lane / PPR, j = lane % PPR;
-        auto put = [&](int piece, uint4 q) {
+        auto put = [&](int piece, uint4 q) __attribute__((always_inline)) {
           const int kk = piece >> 2, cc = piece & 3;
           z.k[row >> 4][kk][16 * cc + ((row & 15) ^ (4 * kk + cc))] = q;
         };
         if constexpr (TYPE == SEQ_BF16) {
-          put(j, make_uint4(st[i][0], st[i][1], st[i][2], st[i][3]));
+          put(j, make_uint4(x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]));
         } else {
           uint32_t w[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) widen<TYPE>(st[i][e], &w[2 * e]);
+          for (int e = 0; e < 4; ++e) widen<TYPE>(x.w[4 * i + e], &w[2 * e]);
           put(2 * j, make_uint4(w[0], w[1], w[2], w[3]));
           put(2 * j + 1, make_uint4(w[4], w[5], w[6], w[7]));
         }
@@ -643,7 +691,8 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
     }
   };
 
-  load(p.s0);
+  Raw x;
+  load(x, p.s0);
   if (tid == 0) s_odd = 0;
   // this lane's query rows, as rows of Q (B operand): node t, head h
   const int R = a.T * a.group;
@@ -669,30 +718,32 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   __syncthreads();                     // s_odd
 
   // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
-  int buf = 0;
-  for (int s = p.s0; s < p.s1; s += 2, buf ^= 1) {
-    commit(buf, s);
-    load(s + 2);
+  auto step = [&](int s, int buf, auto edge_) __attribute__((always_inline)) {
+    constexpr bool EDGE = decltype(edge_)::value;
+    commit(x, buf, s);
+    load(x, s + 2);
     __syncthreads();
     const Step& z = s_step[buf];
     const int t0 = s * kStep - Lr;
-    const bool edge = t0 + 64 > 0;
-#pragma unroll
-    for (int half_ = 0; half_ < 2; ++half_) {
+#pragma unroll 1
+    for (int half_ = 0; half_ < 2; ++half_) {          // (unrolled, it does not fit the registers)
+      // (accumulators take turns: a product waits for the one before it on the same accumulator)
       f32x4 sc[MT][2];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int kk = 0; kk < NKC; ++kk) {
-          const uint4 q = z.k[2 * half_ + tt][kk][16 * c + (r ^ (4 * kk + c))];
-          const uint32_t kf[4] = {q.x, q.y, q.z, q.w};
+      for (int kk = 0; kk < NKC; ++kk) {
+        uint4 kf[2];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+        for (int tt = 0; tt < 2; ++tt) kf[tt] = z.k[2 * half_ + tt][kk][16 * c + (r ^ (4 * kk + c))];
 #pragma unroll
-            for (int k = 0; k < QT; ++k) sc[mt][tt] = mfma(kf, qf[mt][k][kk], sc[mt][tt]);
-        }
+        for (int k = 0; k < QT; ++k)
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = mfma({kf[tt].x, kf[tt].y, kf[tt].z, kf[tt].w}, qf[mt][k][kk], sc[mt][tt]);
       }
       float ks[8] = {}, vs[8] = {};
       if constexpr (TYPE != SEQ_BF16) {
@@ -707,18 +758,24 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
       uint32_t pf[MT][PT][4];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-        soft_step<NDT, PT, TYPE != SEQ_BF16>(sc[mt], ks, vs, a.scale2, edge, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
+        soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, vs, a.scale2, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
 #pragma unroll
-      for (int e = 0; e < NDT; ++e) {
-        const uint4 q = z.v[half_][e][lane];
-        const uint32_t vb[4] = {q.x, q.y, q.z, q.w};
+      for (int e = 0; e < NDT; e += 2) {
+        uint4 vb[2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int i = 0; i < 2; ++i) vb[i] = z.v[half_][e + i][lane];
 #pragma unroll
-          for (int k = 0; k < PT; ++k) o[mt][e] = mfma(pf[mt][k], vb, o[mt][e]);
+        for (int k = 0; k < PT; ++k)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[mt][e + i] = mfma(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i]);
       }
     }
-  }
+  };
+  int s = p.s0, buf = 0;
+  for (; s < p.s1 && (s + 2) * kStep <= Lr; s += 2, buf ^= 1) step(s, buf, std::false_type{});
+  for (; s < p.s1; s += 2, buf ^= 1) step(s, buf, std::true_type{});
 
   // every wave holds its rows' results: lane (r, c) rows 4 c + i of a tile, their maxima and sums in lanes 4 c + i
 #pragma unroll
@@ -742,58 +799,65 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   }
 }
 
-// Joins the chunks' records of one query row: dh / 4 lanes over the dimensions, the others over the chunks.
-// Grid (query rows of a sequence, sequences).
-template <int DH, int ACT>
+// Joins the chunks' records: dh / 4 lanes over a query row's dimensions, PARTS such groups of lanes over its
+// chunks, the rest of the workgroup over rows. Grid (query rows of a sequence / rows, sequences).
+template <int DH, int ACT, int PARTS>
 __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeShape y) {
-  constexpr int LPR = DH / 4, GR = kBlock / LPR;       // lanes per row, chunks at a time
-  __shared__ float s_m[GR], s_l[GR];
-  __shared__ float4 s_o[GR][LPR];
+  constexpr int LPR = DH / 4, ROWS = kBlock / (LPR * PARTS);
+  __shared__ float s_m[PARTS], s_l[PARTS];
+  __shared__ float4 s_o[PARTS][LPR];
   const int tid = threadIdx.x, b = blockIdx.y;
   const Deal d = deal(a, y, tid & 63);
   const int sub = b & 3;
   const int n = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], b >> 2);
   const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], b >> 2);
   if (n <= 1) return;                  // written already
-  const int t = blockIdx.x / a.n_q, h = blockIdx.x % a.n_q;
+  const int q_row = blockIdx.x * ROWS + (PARTS > 1 ? 0 : tid / LPR);
+  if (q_row >= a.T * a.n_q) return;    // (PARTS > 1: every row has a workgroup)
+  const int t = q_row / a.n_q, h = q_row % a.n_q;
   const int g = h / a.group, row = t * a.group + h % a.group;
   const int rows = (y.wide ? 64 : 16) * y.mt, rb = row / rows, in = row % rows;
-  const float* first = a.ws + (size_t(before) * a.c.n_kv + g) * y.rb * rows * (DH + 2) + size_t(rb) * rows * (DH + 2);
-  const size_t stride = size_t(a.c.n_kv) * y.rb * rows * (DH + 2);
-  const int grp = tid / LPR, d0 = 4 * (tid % LPR);
+  const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.c.n_kv * y.rb;
+  const float* first = a.ws + before * stride + (size_t(g) * y.rb + rb) * rec;
+  const int part = PARTS > 1 ? tid / LPR : 0, d0 = 4 * (tid % LPR);
   float m = -INFINITY, l = 0.0f;
-  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int k = grp; k < n; k += GR) {
-    const float* po = first + k * stride;
-    const float2 q = *reinterpret_cast<const float2*>(po + rows * DH + 2 * in);
-    const float4 x = *reinterpret_cast<const float4*>(po + in * DH + d0);
-    const float mn = fmaxf(m, q.x);
+  float v[4] = {};
+  auto add = [&](float mk, float lk, const float4& x) {
+    const float mn = fmaxf(m, mk);
     const float fa = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-    const float fb = q.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(q.x - mn);
+    const float fb = mk == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mk - mn);
     m = mn;
-    l = l * fa + q.y * fb;
-    v.x = v.x * fa + x.x * fb; v.y = v.y * fa + x.y * fb; v.z = v.z * fa + x.z * fb; v.w = v.w * fa + x.w * fb;
-  }
-  if (d0 == 0) {
-    s_m[grp] = m;
-    s_l[grp] = l;
-  }
-  s_o[grp][tid % LPR] = v;
-  __syncthreads();
-  if (tid >= LPR) return;
-  m = -INFINITY;
-  l = 0.0f;
-  float z[4] = {};
+    l = l * fa + lk * fb;
+    v[0] = v[0] * fa + x.x * fb; v[1] = v[1] * fa + x.y * fb; v[2] = v[2] * fa + x.z * fb; v[3] = v[3] * fa + x.w * fb;
+  };
+  // four records in flight
+  for (int k0 = part; k0 < n; k0 += 4 * PARTS) {
+    float2 q[4];
+    float4 x[4];
 #pragma unroll
-  for (int k = 0; k < GR; ++k) m = fmaxf(m, s_m[k]);
+    for (int i = 0; i < 4; ++i) {
+      const float* po = first + min(k0 + i * PARTS, n - 1) * stride;
+      q[i] = *reinterpret_cast<const float2*>(po + rows * DH + 2 * in);
+      x[i] = *reinterpret_cast<const float4*>(po + in * DH + d0);
+    }
 #pragma unroll
-  for (int k = 0; k < GR; ++k) {
-    const float f = s_m[k] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s_m[k] - m);
-    l += s_l[k] * f;
-    z[0] += s_o[k][tid].x * f; z[1] += s_o[k][tid].y * f; z[2] += s_o[k][tid].z * f; z[3] += s_o[k][tid].w * f;
+    for (int i = 0; i < 4; ++i)
+      if (k0 + i * PARTS < n) add(q[i].x, q[i].y, x[i]);
   }
-  put_output<DH, ACT>(a, b, g, row, d0, l, true, z);
+  if constexpr (PARTS > 1) {
+    if (d0 == 0) {
+      s_m[part] = m;
+      s_l[part] = l;
+    }
+    s_o[part][tid % LPR] = make_float4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+    if (tid >= LPR) return;
+    m = -INFINITY;
+    l = v[0] = v[1] = v[2] = v[3] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) add(s_m[k], s_l[k], s_o[k][tid]);
+  }
+  put_output<DH, ACT>(a, b, g, row, d0, l, true, v);
 }
 
 TreeShape shape(const TreeAttnArgs& a) {
@@ -849,11 +913,19 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
 #undef ATTN
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || y.most == 1) return e;
-  const dim3 rows(a.T * a.n_q, a.c.batch);
-  if (a.c.dh == 128 && a.act == SEQ_BF16) hipLaunchKernelGGL((tree_join_kernel<128, SEQ_BF16>), rows, dim3(kBlock), 0, s, a, y);
-  else if (a.c.dh == 128) hipLaunchKernelGGL((tree_join_kernel<128, SEQ_F32>), rows, dim3(kBlock), 0, s, a, y);
-  else if (a.act == SEQ_BF16) hipLaunchKernelGGL((tree_join_kernel<64, SEQ_BF16>), rows, dim3(kBlock), 0, s, a, y);
-  else hipLaunchKernelGGL((tree_join_kernel<64, SEQ_F32>), rows, dim3(kBlock), 0, s, a, y);
+  // few rows: a workgroup for each (latency); many: a group of lanes walks all of a row's chunks (the 64-node
+  // case took 72 us with a workgroup per row)
+#define JOIN(DH, ACT)                                                                                              \
+  do {                                                                                                             \
+    constexpr int PARTS = 4 * kBlock / DH;                                                                         \
+    if (long(a.T) * a.n_q * a.c.batch < 2048) hipLaunchKernelGGL((tree_join_kernel<DH, ACT, PARTS>), dim3(a.T * a.n_q, a.c.batch), dim3(kBlock), 0, s, a, y); \
+    else hipLaunchKernelGGL((tree_join_kernel<DH, ACT, 1>), dim3((a.T * a.n_q + PARTS - 1) / PARTS, a.c.batch), dim3(kBlock), 0, s, a, y); \
+  } while (0)
+  if (a.c.dh == 128 && a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
+  else if (a.c.dh == 128) JOIN(128, SEQ_F32);
+  else if (a.act == SEQ_BF16) JOIN(64, SEQ_BF16);
+  else JOIN(64, SEQ_F32);
+#undef JOIN
   return hipGetLastError();
 }
 
