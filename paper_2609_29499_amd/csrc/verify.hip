@@ -32,33 +32,45 @@ struct ChunkStat {
   int at;                              // lowest index of it
 };
 
-// exp(z) for z <= 0: 2^n exp(r), |r| <= ln 2 / 2, by the Taylor polynomial of degree 11 (remainder below
-// 0.35^12 / 12! = 7e-15 of the result); z below -800 gives 0
-__device__ __forceinline__ double exp_neg(double z) {
-  z = fmax(z, -800.0);
-  const double n = rint(z * 1.44269504088896340736);
-  // ln 2 in two parts, the first with its last 21 bits clear: n times it is exact
-  double r = fma(-n, 6.93147180369123816490e-01, z);
-  r = fma(-n, 1.90821492927058770002e-10, r);
-  double p = 1.0 / 39916800.0;
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return ldexp(p, int(n));
+// exp((l - m) / temperature) = 2^(t / 32), t = (l - m) (32 log2(e) / temperature): t is cut at the nearest
+// integer n, 2^((n mod 32) / 32) comes from a table in LDS, 2^(f / 32), |f| <= 1/2, from the Taylor polynomial of
+// degree 5 (remainder (ln 2 / 64)^6 / 720 = 2e-15). 15 instructions in 64 bits (26 without the table: the 32-node
+// case 107 us).
+__constant__ double kPow32[32] = {
+    1, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
+    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
+    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
+    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
+    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
+    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.6457554781539649,
+    1.681792830507429, 1.7186192981224779, 1.7562521603732995, 1.7947090750031072,
+    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+};
+constexpr double kLn2_32 = 0.69314718055994530942 / 32.0;
+struct Exp {
+  const double* table;                 // kPow32 in LDS
+  double scale;                        // 32 log2(e) / temperature; 0: greedy, nothing is asked for
+};
+// Fills the table (by the first 32 threads; a barrier follows before its use)
+__device__ __forceinline__ Exp exp_table(double* lds, double inv_temp) {
+  if (threadIdx.x < 32) lds[threadIdx.x] = kPow32[threadIdx.x];
+  return {lds, inv_temp * 32.0 * 1.44269504088896340736};
 }
-// exp((l - m) / temperature) of a logit whose row's maximum is m: NaN counts as -inf, a row without
-// anything above -inf has no weight, +inf shares it evenly
-__device__ __forceinline__ double weight(float l, float m, double inv_temp) {
-  if (!(l > -INFINITY)) return 0.0;
-  return l == m ? 1.0 : exp_neg((double(l) - double(m)) * inv_temp);
+// The weight of a logit whose row's maximum is m: NaN counts as -inf, a row without anything above -inf has
+// no weight, +inf shares it evenly.
+__device__ __forceinline__ double weight(float l, float m, const Exp& e) {
+  if (m == INFINITY) return l == m ? 1.0 : 0.0;
+  const double t = fmax((double(l) - double(m)) * e.scale, -1e6);    // (NaN too; 2^-31250 is 0)
+  const double n = rint(t), f = t - n;
+  const int i = int(n);
+  constexpr double c = kLn2_32;
+  double p = c * c * c * c * c / 120.0;
+  p = fma(p, f, c * c * c * c / 24.0);
+  p = fma(p, f, c * c * c / 6.0);
+  p = fma(p, f, c * c / 2.0);
+  p = fma(p, f, c);
+  p = fma(p, f, 1.0);
+  return ldexp(p * e.table[i & 31], i >> 5);
 }
 
 __device__ __forceinline__ double wave_sum_d(double v) {
@@ -72,7 +84,8 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 __global__ __launch_bounds__(kBlock) void verify_stats_kernel(VerifyArgs a, ChunkStat* stat, int* cnt) {
   __shared__ float sm[4];
   __shared__ int si[4];
-  __shared__ double sz[4];
+  __shared__ double sz[4], table[32];
+  const Exp ex = exp_table(table, a.inv_temp);
   const int tid = threadIdx.x, wave = tid >> 6;
   const int c = blockIdx.x, r = blockIdx.y, nt = a.B * a.T;
   const float* row = r < nt ? a.logits + size_t(r) * a.V : a.draft + size_t(r - nt) * a.V;
@@ -115,7 +128,7 @@ __global__ __launch_bounds__(kBlock) void verify_stats_kernel(VerifyArgs a, Chun
   double z = 0.0;
   if (a.inv_temp > 0.0) {
 #pragma unroll
-    for (int i = 0; i < kVU; ++i) z += weight(x[i], m, a.inv_temp);
+    for (int i = 0; i < kVU; ++i) z += weight(x[i], m, ex);
     z = wave_sum_d(z);
     if ((tid & 63) == 0) sz[wave] = z;
     __syncthreads();
@@ -130,70 +143,98 @@ struct RowStat {
   int at;
 };
 
+template <int NT>
 struct WalkSmem {
+  double table[32];
   RowStat row[2 * kTreeMax];           // the target's rows, then the draft's
   double e[kTreeMax];                  // weight of a node's token at its parent
   int token[kTreeMax];
   unsigned long long children;         // of the last node
   int last, n;
   uint32_t gone[kVChunk / 32];         // tokens of a chunk that were refused
-  double part[kBlock / kWave + 1];
-  int cand[kBlock / kWave];
+  double part[NT / kWave + 1];
+  int cand[NT / kWave];
   int found, is_last;
   double base;
 };
 
-// Maxima and sums of rows `first` .. `first` + n - 1 from their chunks: four threads per row
-__device__ __forceinline__ void row_stats(const VerifyArgs& a, const ChunkStat* stat, size_t first, int n, int chunks, RowStat* out) {
+// Maxima and sums of rows `first` .. `first` + n - 1 from their chunks: four threads per row, eight chunks of each
+// in flight together (they come from other dies' caches: one by one, 32 chunks took 6 us).
+__device__ __forceinline__ void row_stats(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, size_t first, int n, int chunks, RowStat* out) {
   const int t = threadIdx.x >> 2, q = threadIdx.x & 3;
   if (t >= n) return;                  // (whole groups of four lanes)
   const ChunkStat* s = stat + (first + t) * chunks;
+  double z = 0.0;
   float m = -INFINITY;
   int at = 0x7fffffff;
-  for (int c = q; c < chunks; c += 4)
-    if (s[c].m > m) {
-      m = s[c].m;
-      at = s[c].at;
-    }
+  for (int c0 = 0; c0 < chunks; c0 += 32) {
+    ChunkStat x[8];
 #pragma unroll
-  for (int k = 1; k < 4; k <<= 1) {
-    const float om = __shfl_xor(m, k, kWave);
-    const int oa = __shfl_xor(at, k, kWave);
-    if (om > m || (om == m && oa < at)) {
-      m = om;
-      at = oa;
+    for (int i = 0; i < 8; ++i) x[i] = s[min(c0 + 4 * i + q, chunks - 1)];
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (x[i].m > top) {
+        top = x[i].m;
+        at = x[i].at;
+      }
+#pragma unroll
+    for (int k = 1; k < 4; k <<= 1) {
+      const float om = __shfl_xor(top, k, kWave);
+      const int oa = __shfl_xor(at, k, kWave);
+      if (om > top || (om == top && oa < at)) {
+        top = om;
+        at = oa;
+      }
     }
+    if (a.inv_temp > 0.0) {
+      if (c0 > 0) z *= weight(m, top, ex);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c0 + 4 * i + q < chunks) z += x[i].z * weight(x[i].m, top, ex);
+    }
+    m = top;
   }
-  double z = 0.0;
-  if (a.inv_temp > 0.0)
-    for (int c = q; c < chunks; c += 4) z += s[c].z * weight(s[c].m, m, a.inv_temp);
   z += __shfl_xor(z, 1, kWave);
   z += __shfl_xor(z, 2, kWave);
   if (q == 0) out[t] = {z, m, at};
 }
 
 // The tree's walk by the first wave, a node per lane; path and n are written when `out` is set.
-__device__ __forceinline__ void walk(const VerifyArgs& a, const ChunkStat* stat, int b, int chunks, WalkSmem& sm, bool out) {
-  const int tid = threadIdx.x, T = a.T;
+template <int NT>
+__device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, int b, int chunks, WalkSmem<NT>& sm, bool out) {
+  const int tid = threadIdx.x, T = a.T, t = tid;
   const bool greedy = a.inv_temp == 0.0, draft = a.draft && !greedy;
-  row_stats(a, stat, size_t(b) * T, T, chunks, sm.row);
-  if (draft) row_stats(a, stat, size_t(a.B) * T + size_t(b) * (T - 1), T - 1, chunks, sm.row + kTreeMax);
+  // the tree and its tokens' logits are asked for first, so that they come with the chunks' records
+  TreeNode nd{0, -2};
+  int up = -1, x = -1;
+  bool node = false, word = false;
+  double u = 0.0;
+  float lx = 0.0f, dx = 0.0f;
+  if (tid < kWave) {
+    nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, T, t);
+    node = nd.anc != 0 && nd.parent >= 0;
+    up = node ? nd.parent : -1;
+    x = t < T ? a.tokens[size_t(b) * T + t] : -1;
+    word = node && x >= 0 && x < a.V;
+    u = t < T && !greedy ? double(a.u[size_t(b) * T + t]) : 0.0;
+    if (word && !greedy) {
+      lx = a.logits[(size_t(b) * T + up) * a.V + x];
+      if (draft) dx = a.draft[(size_t(b) * (T - 1) + up) * a.V + x];
+    }
+  }
+  __syncthreads();                     // the table
+  row_stats(a, ex, stat, size_t(b) * T, T, chunks, sm.row);
+  if (draft) row_stats(a, ex, stat, size_t(a.B) * T + size_t(b) * (T - 1), T - 1, chunks, sm.row + kTreeMax);
   __syncthreads();
   if (tid < kWave) {
-    const int t = tid;
-    const TreeNode nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, T, t);
-    const bool node = nd.anc != 0 && nd.parent >= 0;
-    const int up = node ? nd.parent : -1;
-    const int x = t < T ? a.tokens[size_t(b) * T + t] : -1;
-    const bool word = node && x >= 0 && x < a.V;
-    const double u = t < T && !greedy ? double(a.u[size_t(b) * T + t]) : 0.0;
     const RowStat rs = sm.row[max(up, 0)];
     double e = 0.0, q = 0.0;
     if (word && greedy) e = rs.at == x ? 1.0 : 0.0;
-    if (word && !greedy) e = weight(a.logits[(size_t(b) * T + up) * a.V + x], rs.m, a.inv_temp);
+    if (word && !greedy) e = weight(lx, rs.m, ex);
     if (word && draft) {
       const RowStat ds = sm.row[kTreeMax + up];
-      q = weight(a.draft[(size_t(b) * (T - 1) + up) * a.V + x], ds.m, a.inv_temp);
+      q = weight(dx, ds.m, ex);
       q = ds.z > 0.0 ? q / ds.z : 0.0;
     }
     bool good;
@@ -252,14 +293,15 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const ChunkStat* stat,
 // `base`; also the chunk's last token with a weight. w(k): weight of token k. Thread t holds tokens
 // kVU t .. + kVU - 1 of the chunk, so sums run in token order. found: -1 none, else the token;
 // tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
-template <class W>
-__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem& sm, W&& w, int* found, int* tail) {
+template <int NT, class W>
+__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem<NT>& sm, W&& w, int* found, int* tail) {
+  constexpr int U = kVChunk / NT, NWV = NT / kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int k0 = c * kVChunk + tid * kVU;
-  double v[kVU], sum = 0.0;
+  const int k0 = c * kVChunk + tid * U;
+  double v[U], sum = 0.0;
   int end = -1;
 #pragma unroll
-  for (int i = 0; i < kVU; ++i) {
+  for (int i = 0; i < U; ++i) {
     v[i] = k0 + i < a.V ? w(k0 + i) : 0.0;
     sum += v[i];
     if (v[i] > 0.0) end = k0 + i;
@@ -273,12 +315,15 @@ __device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double 
   __syncthreads();
   if (lane == 63) sm.part[wave] = inc;
   __syncthreads();
-  double cum = base + (inc - sum);
-  for (int j = 0; j < wave; ++j) cum += sm.part[j];
-  const double total = base + ((sm.part[0] + sm.part[1]) + (sm.part[2] + sm.part[3]));
+  double cum = base + (inc - sum), total = base;
+#pragma unroll
+  for (int j = 0; j < NWV; ++j) {
+    if (j < wave) cum += sm.part[j];
+    total += sm.part[j];
+  }
   int hit = 0x7fffffff;
 #pragma unroll
-  for (int i = 0; i < kVU; ++i) {
+  for (int i = 0; i < U; ++i) {
     cum += v[i];
     if (v[i] > 0.0 && cum > target && hit == 0x7fffffff) hit = k0 + i;
   }
@@ -293,8 +338,11 @@ __device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double 
     sm.gone[wave] = uint32_t(end);     // (the mask has been read)
   }
   __syncthreads();
-  hit = min(min(sm.cand[0], sm.cand[1]), min(sm.cand[2], sm.cand[3]));
-  end = max(max(int(sm.gone[0]), int(sm.gone[1])), max(int(sm.gone[2]), int(sm.gone[3])));
+#pragma unroll
+  for (int j = 0; j < NWV; ++j) {
+    hit = min(hit, sm.cand[j]);
+    end = max(end, int(sm.gone[j]));
+  }
   __syncthreads();
   *found = hit == 0x7fffffff ? -1 : hit;
   *tail = end;
@@ -302,8 +350,9 @@ __device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double 
 }
 
 // The chunk's refused tokens as a bit mask (none: empty)
-__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem& sm, bool any) {
-  for (int i = threadIdx.x; i < kVChunk / 32; i += kBlock) sm.gone[i] = 0;
+template <int NT>
+__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<NT>& sm, bool any) {
+  for (int i = threadIdx.x; i < kVChunk / 32; i += NT) sm.gone[i] = 0;
   __syncthreads();
   const int t = threadIdx.x;
   if (any && t < a.T && ((sm.children >> t) & 1)) {
@@ -315,19 +364,20 @@ __device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem& 
 
 // Takes the last token of sequence b by the whole workgroup: chunk_weight(c) is the weight of chunk c
 // (any thread may ask), w as for scan_chunk after mark_gone.
-template <class CW, class W>
-__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem& sm, bool remove, CW&& chunk_weight, W&& w) {
+template <int NT, class CW, class W>
+__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem<NT>& sm, bool remove, CW&& chunk_weight, W&& w) {
   const int tid = threadIdx.x;
   // the chunk in which the cumulative weight passes the target: by the first wave, chunk sums in order
   if (tid < kWave) {
-    double total = 0.0;
-    for (int c0 = 0; c0 < chunks; c0 += kWave) total += wave_sum_d(c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0);
+    const double w0 = tid < chunks ? chunk_weight(tid) : 0.0;        // (asked for once where there are up to 64)
+    double total = wave_sum_d(w0);
+    for (int c0 = kWave; c0 < chunks; c0 += kWave) total += wave_sum_d(c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0);
     const double target = double(a.u[size_t(b) * a.T]) * total;
     double base = 0.0;
     int at = -1;
     double before = 0.0;
     for (int c0 = 0; c0 < chunks && at < 0; c0 += kWave) {
-      const double mine = c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0;
+      const double mine = c0 == 0 ? w0 : c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0;
       double inc = mine;
 #pragma unroll
       for (int k = 1; k < kWave; k <<= 1) {
@@ -345,13 +395,13 @@ __device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, Walk
     if (tid == 0) {
       sm.found = total > 0.0 ? max(at, 0) : -1;
       sm.base = before;
-      sm.part[kBlock / kWave] = target;
+      sm.part[NT / kWave] = target;
     }
   }
   __syncthreads();
   const int c_at = sm.found;
   double base = sm.base;
-  const double target = sm.part[kBlock / kWave];
+  const double target = sm.part[NT / kWave];
   __syncthreads();
   if (c_at < 0) return -1;             // nothing has a weight
   int best = -1;                       // the last token with a weight, should rounding leave the target unreached
@@ -371,12 +421,15 @@ __device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, Walk
   return best;
 }
 
-// Grid (1 or chunks, B): see the head of the file.
-__global__ __launch_bounds__(kBlock) void verify_walk_kernel(VerifyArgs a, const ChunkStat* stat, double* sums, int* cnt, int chunks) {
-  __shared__ WalkSmem sm;
+// Grid (1, or chunks with draft logits, B): see the head of the file. NT threads: 1024 where one workgroup serves a
+// sequence (four logits of the chunk per thread instead of 16 shorten it), 256 over the chunks.
+template <int NT>
+__global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const ChunkStat* stat, double* sums, int* cnt, int chunks) {
+  __shared__ WalkSmem<NT> sm;
   const int tid = threadIdx.x, b = blockIdx.y, T = a.T;
   const bool greedy = a.inv_temp == 0.0;
-  walk(a, stat, b, chunks, sm, blockIdx.x == 0);
+  const Exp ex = exp_table(sm.table, a.inv_temp);
+  walk(a, ex, stat, b, chunks, sm, blockIdx.x == 0);
   const int last = sm.last, slot = sm.n - 1;
   int* out = a.ids + size_t(b) * T + slot;
   const RowStat rs = sm.row[last];
@@ -388,15 +441,16 @@ __global__ __launch_bounds__(kBlock) void verify_walk_kernel(VerifyArgs a, const
   const float* row = a.logits + r * a.V;
   const ChunkStat* st = stat + r * chunks;
   const bool kids = sm.children != 0;
-  auto plain_sum = [&](int c) { return st[c].z * weight(st[c].m, rs.m, a.inv_temp); };
-  auto plain = [&](int k) { return weight(row[k], rs.m, a.inv_temp); };
+  auto plain_sum = [&](int c) { return st[c].z * weight(st[c].m, rs.m, ex); };
+  auto plain = [&](int k) { return weight(row[k], rs.m, ex); };
   if (!a.draft) {
     // e without the children's tokens: what they weigh is taken off their chunks
     auto left_sum = [&](int c) {
       double z = plain_sum(c);
-      if (kids)
-        for (int t = 0; t < T; ++t)
-          if (((sm.children >> t) & 1) && sm.token[t] >= 0 && sm.token[t] / kVChunk == c) z -= sm.e[t];
+      for (unsigned long long k = sm.children; k; k &= k - 1) {
+        const int t = __ffsll((long long)k) - 1;
+        if (sm.token[t] >= 0 && sm.token[t] / kVChunk == c) z -= sm.e[t];
+      }
       return fmax(z, 0.0);
     };
     auto left = [&](int k) {
@@ -413,14 +467,14 @@ __global__ __launch_bounds__(kBlock) void verify_walk_kernel(VerifyArgs a, const
   const float* drow = a.draft + (size_t(b) * (T - 1) + (kids ? last : 0)) * a.V;
   const double pz = rs.z > 0.0 ? 1.0 / rs.z : 0.0, qz = ds.z > 0.0 ? 1.0 / ds.z : 0.0;
   auto rest = [&](int k) {
-    const double p = weight(row[k], rs.m, a.inv_temp) * pz;
-    return kids ? fmax(p - weight(drow[k], ds.m, a.inv_temp) * qz, 0.0) : p;
+    const double p = weight(row[k], rs.m, ex) * pz;
+    return kids ? fmax(p - weight(drow[k], ds.m, ex) * qz, 0.0) : p;
   };
   const int c = blockIdx.x;
   double z = 0.0;
 #pragma unroll
-  for (int i = 0; i < kVU; ++i) {
-    const int k = c * kVChunk + i * kBlock + tid;
+  for (int i = 0; i < kVChunk / NT; ++i) {
+    const int k = c * kVChunk + i * NT + tid;
     if (k < a.V) z += rest(k);
   }
   z = wave_sum_d(z);
@@ -428,7 +482,8 @@ __global__ __launch_bounds__(kBlock) void verify_walk_kernel(VerifyArgs a, const
   __syncthreads();
   const __amdgpu_buffer_rsrc_t rp = make_rsrc(sums + size_t(b) * chunks, uint32_t(chunks) * 8u);
   if (tid == 0) {
-    z = (sm.part[0] + sm.part[1]) + (sm.part[2] + sm.part[3]);
+    z = 0.0;
+    for (int j = 0; j < NT / kWave; ++j) z += sm.part[j];
     buf_store8_device(__builtin_bit_cast(int2, z), rp, uint32_t(c) * 8u);
     __builtin_amdgcn_s_waitcnt(0);                      // the sum is at the coherence point
     sm.is_last = __hip_atomic_fetch_add(cnt + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
@@ -464,7 +519,9 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(verify_stats_kernel, dim3(chunks, rows), dim3(kBlock), 0, s, v, stat, reinterpret_cast<int*>(ws));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_walk_kernel, dim3(draft ? chunks : 1, a.B), dim3(kBlock), 0, s, v, stat, sums, reinterpret_cast<int*>(ws), chunks);
+  int* cnt = reinterpret_cast<int*>(ws);
+  if (draft) hipLaunchKernelGGL((verify_walk_kernel<256>), dim3(chunks, a.B), dim3(256), 0, s, v, stat, sums, cnt, chunks);
+  else hipLaunchKernelGGL((verify_walk_kernel<1024>), dim3(1, a.B), dim3(1024), 0, s, v, stat, sums, cnt, chunks);
   return hipGetLastError();
 }
 
