@@ -574,6 +574,42 @@ tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float*
 tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, const int32_t* n,
                             int32_t T, int32_t* len_out, void* stream);
 
+/* Adopt a typed cache's rows for a plan (as tasp_kv_bind does for a tasp_kv_cache): checks that it has the plan's
+ * layers, KV heads and head_dim (TASP_ERR_SHAPE) and sets cache->plan_sig. Rows may come from tasp_seq_append of
+ * a prefilled tasp_kv_cache of the same plan (rope NULL: its keys are rotated already). */
+tasp_status tasp_seq_bind(tasp_plan plan, tasp_seq_cache* cache);
+
+/* Workspace bytes of a plan's step over trees of T nodes: tasp_tree_step's, enough for tasp_tree_forward. The step
+ * runs in the plan's prefill scratch, so cache->batch * T <= max_prefill (TASP_ERR_SHAPE; TASP_ERR_UNSUPPORTED for
+ * max_prefill 0). max_len as for tasp_tree_attention. */
+tasp_status tasp_tree_step_workspace_bytes(tasp_plan plan, const tasp_seq_cache* cache, int32_t T,
+                                           int32_t max_len, size_t* bytes);
+
+/* The plan's layers over trees of T nodes of every sequence (any plan format; projections as tasp_prefill, attention
+ * as tasp_tree_attention with TASP_F32 over the retained groups): x (device) float32 [batch][T][d_model], out (device, not overlapping
+ * x) float32 [batch][T][vocab], or [batch][T][d_model] without an LM head. Appends the nodes' k and v to every
+ * layer (positions len + depth, rotate-half RoPE with the plan's base; only retained groups' rows are written);
+ * the lengths stay. Rows of out of absent nodes hold values of no meaning. The cache must be bound to the plan
+ * (else TASP_ERR_CACHE_PLAN_MISMATCH). Stream-ordered, capturable; calls on one plan must be ordered. */
+tasp_status tasp_tree_forward(tasp_plan plan, const float* x, const int32_t* parent, int32_t T,
+                              const tasp_seq_cache* cache, int32_t max_len, float* out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* One step of decoding with drafted tokens: embeds tokens (device int32 [batch][T]; node 0 the last token of the
+ * text, whose row is not in the cache yet), runs tasp_tree_forward, verifies the drafts (tasp_verify; arguments as
+ * there) and keeps the accepted path (tasp_seq_commit, cache->len grows by n). The next step's node 0 is
+ * ids[b][n[b] - 1]. Nothing waits for the host: lengths, tokens and acceptance stay on the device, and a step can be
+ * captured into a HIP graph and replayed with new tokens in the same arrays (max_len then is an upper bound for the
+ * replays). embed, embed_scale as tasp_generate; x_scratch float32 [batch][T][d_model]; logits float32
+ * [batch][T][vocab] receive the target's logits. T = 1 decodes one token of every sequence by sampling or
+ * greedily. Requires an LM head (else TASP_ERR_UNSUPPORTED). */
+tasp_status tasp_tree_step(tasp_plan plan, const int8_t* embed, const float* embed_scale,
+                           const int32_t* tokens, const int32_t* parent, const float* u,
+                           const float* draft_logits, double temperature, int32_t T, int32_t max_len,
+                           const tasp_seq_cache* cache, int32_t* ids, int32_t* path, int32_t* n,
+                           float* x_scratch, float* logits, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* Plain streaming copy of `bytes` (multiple of 16) from src to dst (device, not overlapping):
  * the reference kernel whose counter readings calibrate memory-traffic measurements (the byte
  * ledger of appendix "FLOP and storage validation" checked against hardware counters).

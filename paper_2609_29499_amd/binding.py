@@ -35,6 +35,7 @@ EXPORTS = ["tasp_plan_workspace_bytes", "tasp_compile_plan", "tasp_plan_counts",
            "tasp_router_workspace_bytes", "tasp_route", "tasp_route_noalloc", "tasp_serve_turn", "tasp_copy_probe",
            "tasp_seq_append", "tasp_seq_read", "tasp_tree_attention_workspace_bytes", "tasp_tree_attention",
            "tasp_verify_workspace_bytes", "tasp_verify", "tasp_seq_commit",
+           "tasp_seq_bind", "tasp_tree_step_workspace_bytes", "tasp_tree_forward", "tasp_tree_step",
            "tasp_status_string", "tasp_last_error"]
 
 
@@ -174,6 +175,10 @@ def load(path: str = LIB_PATH):
         "tasp_verify_workspace_bytes": [I32, I32, I32, C.POINTER(SZ)],
         "tasp_verify": [P, P, P, P, P, I32, I32, I32, C.c_double, P, P, P, P, SZ, P],
         "tasp_seq_commit": [P, P, P, I32, P, P],
+        "tasp_seq_bind": [P, P],
+        "tasp_tree_step_workspace_bytes": [P, P, I32, I32, C.POINTER(SZ)],
+        "tasp_tree_forward": [P, P, P, I32, P, I32, P, P, SZ, P],
+        "tasp_tree_step": [P, P, P, P, P, P, P, C.c_double, I32, I32, P, P, P, P, P, P, P, SZ, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -408,3 +413,24 @@ def tasp_seq_commit(cache, path_ptr, n_ptr, T, len_out_ptr, stream):
     st = (_lib or load()).tasp_seq_commit(_ref(cache), path_ptr, n_ptr, T, len_out_ptr, stream)
     if st:
         _check(st)
+
+
+def tasp_seq_bind(plan, cache):
+    _check(load().tasp_seq_bind(plan, _ref(cache)))
+
+
+def tasp_tree_step_workspace_bytes(plan, cache, T, max_len):
+    n = C.c_size_t()
+    _check(load().tasp_tree_step_workspace_bytes(plan, _ref(cache), T, max_len, C.byref(n)))
+    return n.value
+
+
+def tasp_tree_forward(plan, x_ptr, parent_ptr, T, cache, max_len, out_ptr, ws_ptr, ws_bytes, stream):
+    _check(load().tasp_tree_forward(plan, x_ptr, parent_ptr, T, _ref(cache), max_len, out_ptr, ws_ptr, ws_bytes, stream))
+
+
+def tasp_tree_step(plan, embed_ptr, scale_ptr, tokens_ptr, parent_ptr, u_ptr, draft_ptr, temperature, T, max_len,
+                   cache, ids_ptr, path_ptr, n_ptr, x_ptr, logits_ptr, ws_ptr, ws_bytes, stream):
+    _check(load().tasp_tree_step(plan, embed_ptr, scale_ptr, tokens_ptr, parent_ptr, u_ptr, draft_ptr, temperature, T,
+                                 max_len, _ref(cache), ids_ptr, path_ptr, n_ptr, x_ptr, logits_ptr, ws_ptr, ws_bytes,
+                                 stream))

@@ -719,12 +719,13 @@ tasp::MfmaMode pf_mode(int kind) {
 // The normed inputs (QKV, gate/up) have theirs in pxd; the O and down inputs are written to pxw in
 // float32 and turned into operand rows there. One operand is in use at a time, so all share ptok and
 // pchunks.
-tasp_status prefill_impl(tasp_plan p, const float* x, int T, tasp_kv_cache* cache, int pos0, float* out,
-                         hipStream_t s, Timer* tm, bool last_only) {
+// attend(l, qkv, ld, ks): rotary positions, cache rows and attention of layer l from its QKV product (rows of ld
+// floats, the sum of ks arrays T ld floats apart), the retained heads' outputs into rows of pxw.
+template <class Attend>
+tasp_status prefill_layers(tasp_plan p, const float* x, int T, float* out, hipStream_t s, Timer* tm, bool last_only,
+                           Attend&& attend) {
   const tasp_model_desc& d = p->desc;
-  const int D = d.d_model, dh = d.head_dim, L = d.n_layers, Pm = d.max_prefill;
-  const uint32_t plane_q = uint32_t(size_t(d.n_q_heads) * Pm * dh);
-  const size_t layer_cache = size_t(cache->batch) * d.n_kv_heads * cache->max_seq * dh;
+  const int D = d.d_model, dh = d.head_dim, L = d.n_layers;
   float* wide = reinterpret_cast<float*>(p->pxw);
   tasp_status st;
   auto gemm = [&](int kind, tasp::PfI8Args& a) {
@@ -753,30 +754,11 @@ tasp_status prefill_impl(tasp_plan p, const float* x, int T, tasp_kv_cache* cach
     const LayerPlan& P = p->layers[l];
     const float* in = (l == 0) ? x : p->pr_io[(l - 1) & 1];
     float* lo = (l == L - 1 && d.vocab == 0) ? out : p->pr_io[l & 1];
-    uint16_t* kc = static_cast<uint16_t*>(cache->k) + l * layer_cache;
-    uint16_t* vc = static_cast<uint16_t*>(cache->v) + l * layer_cache;
     if (P.n_qkv > 0) {
       tasp::PfI8Args a = pf_projection(p, l, 0, T);
       a.x = reinterpret_cast<uint8_t*>(p->pxd); a.ldx = p->ld_xd; a.y = p->pqkv; a.ldy = p->ld_qkv;
       if ((st = gemm(0, a))) return st;
-      tasp::PfRopeArgs r{};
-      r.qkv = p->pqkv; r.ld_qkv = p->ld_qkv; r.ks = a.ks;
-      if (a.ks > 1) {
-        r.qkv = p->ppart; r.ld_qkv = P.n_qkv; r.split_stride = size_t(T) * P.n_qkv;
-      }
-      r.m_q = P.m_q; r.m_kv = P.m_kv; r.dh = dh;
-      for (int q = 0; q < P.m_kv; ++q) r.kv_idx[q] = P.kv_idx[q];
-      r.kc = kc; r.vc = vc; r.S = cache->max_seq; r.rope_cos = p->rope_cos; r.rope_sin = p->rope_sin;
-      r.pos0 = pos0; r.T = T; r.q_out = p->pq; r.q_plane = plane_q; r.T_ld = Pm;
-      if ((st = run_kernel(tm, 7, s, [&] { return tasp::launch_pf_rope(r, s); }))) return st;
-      tasp::PfAttnArgs t{};
-      t.q = p->pq; t.q_plane = plane_q; t.T_ld = Pm; t.m_kv = P.m_kv; t.dh = dh;
-      for (int q = 0; q < P.m_kv; ++q) t.kv_idx[q] = P.kv_idx[q];
-      for (int q = 0; q <= P.m_kv; ++q) t.slot_start[q] = P.slot_start[q];
-      t.kc = kc; t.vc = vc; t.S = cache->max_seq; t.pos0 = pos0; t.T = T;
-      t.o = wide; t.ldo = p->ld_xw;
-      t.part = p->ppart; t.part_floats = p->ppart_floats; t.cnt = p->pacnt; t.cnt_len = p->pacnt_len;
-      if ((st = run_kernel(tm, 1, s, [&] { return tasp::launch_pf_attn(t, s); }))) return st;
+      if ((st = a.ks > 1 ? attend(l, p->ppart, P.n_qkv, a.ks) : attend(l, p->pqkv, p->ld_qkv, 1))) return st;
     }
     {
       tasp::PfI8Args a = pf_projection(p, l, 2, T);
@@ -806,6 +788,37 @@ tasp_status prefill_impl(tasp_plan p, const float* x, int T, tasp_kv_cache* cach
     }
   }
   return d.vocab ? prefill_head(p, p->pr_io[(L - 1) & 1], T, out, s, tm, last_only) : TASP_OK;
+}
+
+// of one sequence at positions pos0 ..: RoPE from the plan's table, BF16 rows, causal attention
+tasp_status prefill_impl(tasp_plan p, const float* x, int T, tasp_kv_cache* cache, int pos0, float* out,
+                         hipStream_t s, Timer* tm, bool last_only) {
+  const tasp_model_desc& d = p->desc;
+  const int dh = d.head_dim, Pm = d.max_prefill;
+  const uint32_t plane_q = uint32_t(size_t(d.n_q_heads) * Pm * dh);
+  const size_t layer_cache = size_t(cache->batch) * d.n_kv_heads * cache->max_seq * dh;
+  auto attend = [&](int l, const float* qkv, int ld, int ks) -> tasp_status {
+    const LayerPlan& P = p->layers[l];
+    uint16_t* kc = static_cast<uint16_t*>(cache->k) + l * layer_cache;
+    uint16_t* vc = static_cast<uint16_t*>(cache->v) + l * layer_cache;
+    tasp_status st;
+    tasp::PfRopeArgs r{};
+    r.qkv = qkv; r.ld_qkv = ld; r.ks = ks; r.split_stride = ks > 1 ? size_t(T) * ld : 0;
+    r.m_q = P.m_q; r.m_kv = P.m_kv; r.dh = dh;
+    for (int q = 0; q < P.m_kv; ++q) r.kv_idx[q] = P.kv_idx[q];
+    r.kc = kc; r.vc = vc; r.S = cache->max_seq; r.rope_cos = p->rope_cos; r.rope_sin = p->rope_sin;
+    r.pos0 = pos0; r.T = T; r.q_out = p->pq; r.q_plane = plane_q; r.T_ld = Pm;
+    if ((st = run_kernel(tm, 7, s, [&] { return tasp::launch_pf_rope(r, s); }))) return st;
+    tasp::PfAttnArgs t{};
+    t.q = p->pq; t.q_plane = plane_q; t.T_ld = Pm; t.m_kv = P.m_kv; t.dh = dh;
+    for (int q = 0; q < P.m_kv; ++q) t.kv_idx[q] = P.kv_idx[q];
+    for (int q = 0; q <= P.m_kv; ++q) t.slot_start[q] = P.slot_start[q];
+    t.kc = kc; t.vc = vc; t.S = cache->max_seq; t.pos0 = pos0; t.T = T;
+    t.o = reinterpret_cast<float*>(p->pxw); t.ldo = p->ld_xw;
+    t.part = p->ppart; t.part_floats = p->ppart_floats; t.cnt = p->pacnt; t.cnt_len = p->pacnt_len;
+    return run_kernel(tm, 1, s, [&] { return tasp::launch_pf_attn(t, s); });
+  };
+  return prefill_layers(p, x, T, out, s, tm, last_only, attend);
 }
 
 tasp_status prefill_checked(tasp_plan p, const float* x, int32_t T, tasp_kv_cache* cache,
@@ -2101,7 +2114,9 @@ tasp_status tree_attn_args(const tasp_seq_cache* c, int32_t n_q, int32_t T, int3
   if (n_q < 1 || n_q % c->n_kv_heads || n_q / c->n_kv_heads > 8)
     return fail(TASP_ERR_SHAPE, "%d query heads over %d KV heads (1..8 per KV head)", n_q, c->n_kv_heads);
   if (max_len < 0 || max_len > c->max_seq) return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_seq);
-  a->T = T; a->n_q = n_q; a->group = n_q / c->n_kv_heads; a->max_len = max_len;
+  a->T = T; a->max_len = max_len; a->slots = c->n_kv_heads; a->group = n_q / c->n_kv_heads;
+  for (int j = 0; j < a->slots; ++j) a->kv_map[j] = (unsigned char)j;
+  for (int j = 0; j <= a->slots; ++j) a->q_start[j] = (unsigned short)(j * a->group);
   return TASP_OK;
 }
 
@@ -2199,6 +2214,24 @@ tasp_status check_verify_shape(int32_t batch, int32_t T, int32_t vocab) {
   return TASP_OK;
 }
 
+tasp_status check_verify(const float* logits, const int32_t* tokens, const float* u, const int32_t* parent,
+                         const float* draft_logits, int32_t batch, int32_t T, int32_t vocab, double temperature,
+                         const int32_t* ids, const int32_t* path, const int32_t* n, const void* workspace,
+                         size_t workspace_bytes) {
+  tasp_status st = check_verify_shape(batch, T, vocab);
+  if (st) return st;
+  if (!logits || !tokens || !ids || !path || !n)
+    return fail(TASP_ERR_INVALID_ARG, "logits / tokens / ids / path / n is NULL");
+  if (!(temperature >= 0.0) || !std::isfinite(temperature) || (temperature > 0.0 && !std::isfinite(1.0 / temperature)))
+    return fail(TASP_ERR_INVALID_ARG, "temperature must be 0 or positive");
+  if (temperature > 0.0 && !u) return fail(TASP_ERR_INVALID_ARG, "u is NULL");
+  if (draft_logits && parent) return fail(TASP_ERR_INVALID_ARG, "draft_logits go with chains (parent NULL)");
+  for (const void* p : {(const void*)logits, (const void*)tokens, (const void*)u, (const void*)parent,
+                        (const void*)draft_logits, (const void*)ids, (const void*)path, (const void*)n})
+    if (!aligned(p, 4)) return fail(TASP_ERR_INVALID_ARG, "an array is not 4-byte aligned");
+  return check_workspace(workspace, workspace_bytes, tasp::verify_workspace_bytes(batch, T, vocab));
+}
+
 }  // namespace
 
 tasp_status tasp_verify_workspace_bytes(int32_t batch, int32_t T, int32_t vocab, size_t* bytes) {
@@ -2213,18 +2246,9 @@ tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float*
                         const int32_t* parent, const float* draft_logits, int32_t batch, int32_t T,
                         int32_t vocab, double temperature, int32_t* ids, int32_t* path, int32_t* n,
                         void* workspace, size_t workspace_bytes, void* stream) {
-  tasp_status st = check_verify_shape(batch, T, vocab);
+  tasp_status st = check_verify(logits, tokens, u, parent, draft_logits, batch, T, vocab, temperature, ids, path, n,
+                                workspace, workspace_bytes);
   if (st) return st;
-  if (!logits || !tokens || !ids || !path || !n)
-    return fail(TASP_ERR_INVALID_ARG, "logits / tokens / ids / path / n is NULL");
-  if (!(temperature >= 0.0) || !std::isfinite(temperature) || (temperature > 0.0 && !std::isfinite(1.0 / temperature)))
-    return fail(TASP_ERR_INVALID_ARG, "temperature must be 0 or positive");
-  if (temperature > 0.0 && !u) return fail(TASP_ERR_INVALID_ARG, "u is NULL");
-  if (draft_logits && parent) return fail(TASP_ERR_INVALID_ARG, "draft_logits go with chains (parent NULL)");
-  for (const void* p : {(const void*)logits, (const void*)tokens, (const void*)u, (const void*)parent,
-                        (const void*)draft_logits, (const void*)ids, (const void*)path, (const void*)n})
-    if (!aligned(p, 4)) return fail(TASP_ERR_INVALID_ARG, "an array is not 4-byte aligned");
-  if ((st = check_workspace(workspace, workspace_bytes, tasp::verify_workspace_bytes(batch, T, vocab)))) return st;
   tasp::VerifyArgs a{};
   a.logits = logits; a.draft = draft_logits; a.tokens = tokens; a.u = u; a.parent = parent;
   a.B = batch; a.T = T; a.V = vocab; a.inv_temp = temperature > 0.0 ? 1.0 / temperature : 0.0;
@@ -2248,6 +2272,155 @@ tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, co
   a.path = path; a.ld = T; a.n = n; a.len_out = len_out;
   HIP_TRY(tasp::launch_seq_commit(a, static_cast<hipStream_t>(stream)));
   return TASP_OK;
+}
+
+namespace {
+
+// The cache of a tree step: the plan's shape, and its rows the plan's.
+tasp_status check_step_cache(const tasp_plan_s* p, const tasp_seq_cache* c) {
+  tasp_status st;
+  if (!p) return fail(TASP_ERR_INVALID_ARG, "plan is NULL");
+  if ((st = check_seq_cache(c, 0)) || (st = check_seq_buffers(c))) return st;
+  const tasp_model_desc& d = p->desc;
+  if (c->n_layers != d.n_layers || c->n_kv_heads != d.n_kv_heads || c->head_dim != d.head_dim)
+    return fail(TASP_ERR_SHAPE, "cache of %d layers, %d heads of %d; the plan has %d, %d of %d", c->n_layers,
+                c->n_kv_heads, c->head_dim, d.n_layers, d.n_kv_heads, d.head_dim);
+  return TASP_OK;
+}
+
+// Arguments of a step over trees of T nodes: the attention's of the widest layer (most retained groups, largest
+// group) size the workspace, since every layer's records fit what that one needs or less of a smaller grid.
+tasp_status step_layout(const tasp_plan_s* p, const tasp_seq_cache* c, int32_t T, int32_t max_len, size_t* attn,
+                        size_t* total) {
+  tasp_status st = check_tree(nullptr, T, false);
+  if (st) return st;
+  const tasp_model_desc& d = p->desc;
+  if (d.max_prefill < 1) return fail(TASP_ERR_UNSUPPORTED, "plan compiled with max_prefill 0");
+  if (int64_t(T) * c->batch > d.max_prefill)
+    return fail(TASP_ERR_SHAPE, "%d nodes of %d sequences above max_prefill %d", T, c->batch, d.max_prefill);
+  if (max_len < 0 || max_len > c->max_seq) return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_seq);
+  *attn = 0;
+  for (const LayerPlan& P : p->layers) {
+    if (P.m_kv < 1) continue;
+    tasp::TreeAttnArgs a{};
+    a.c = seq_layer(c, 0);
+    a.T = T; a.act = TASP_F32; a.max_len = max_len; a.slots = P.m_kv;
+    for (int j = 0; j < P.m_kv; ++j) a.group = std::max(a.group, P.slot_start[j + 1] - P.slot_start[j]);
+    *attn = std::max(*attn, align_up(tasp::tree_attn_workspace_bytes(a), kAlign));
+  }
+  *total = *attn + (d.vocab ? tasp::verify_workspace_bytes(c->batch, T, d.vocab) : 0);
+  return TASP_OK;
+}
+
+tasp_status tree_forward(tasp_plan p, const float* x, const int32_t* parent, int32_t T, const tasp_seq_cache* c,
+                         int32_t max_len, float* out, float* ws, hipStream_t s) {
+  const tasp_model_desc& d = p->desc;
+  const int dh = d.head_dim, n = c->batch * T;
+  tasp_rope rope{TASP_ROPE_HALF, dh, TASP_ROPE_NONE, 0, d.rope_theta, 1.0, 1.0, 2.0, 1.0};
+  float* q = reinterpret_cast<float*>(p->pq);          // [batch][T][m_q][dh] (as wide as the prefill's two BF16 planes)
+  auto attend = [&](int l, const float* qkv, int ld, int ks) -> tasp_status {
+    const LayerPlan& P = p->layers[l];
+    const tasp::SeqLayer layer = seq_layer(c, l);
+    tasp::SeqAppendArgs a{};
+    tasp_status st = rope_args(&rope, dh, &a);
+    if (st) return st;
+    a.c = layer; a.parent = parent; a.T = T; a.act = TASP_F32; a.n_q = P.m_q; a.n_kv = P.m_kv; a.kv_map = P.kv_idx.data();
+    a.ks = ks; a.split = long(n) * ld;
+    float* base = const_cast<float*>(qkv);             // (read only)
+    auto rows = [&](int first) { return tasp::SeqRows{base + size_t(first) * dh, long(T) * ld, ld, dh}; };
+    a.q = rows(0); a.k = rows(P.m_q); a.v = rows(P.m_q + P.m_kv);
+    a.q_out = {q, long(T) * P.m_q * dh, long(P.m_q) * dh, dh};
+    HIP_TRY(tasp::launch_seq_append(a, s));
+    tasp::TreeAttnArgs t{};
+    t.c = layer; t.parent = parent; t.T = T; t.act = TASP_F32; t.max_len = max_len; t.slots = P.m_kv;
+    for (int j = 0; j < P.m_kv; ++j) {
+      t.kv_map[j] = (unsigned char)P.kv_idx[j];
+      t.q_start[j] = (unsigned short)P.slot_start[j];
+      t.group = std::max(t.group, P.slot_start[j + 1] - P.slot_start[j]);
+    }
+    t.q_start[P.m_kv] = (unsigned short)P.m_q;
+    t.q = a.q_out;
+    t.o = {p->pxw, long(T) * p->ld_xw, p->ld_xw, dh};
+    t.scale2 = float(1.44269504088896340736 / std::sqrt(double(dh)));
+    t.ws = ws;
+    HIP_TRY(tasp::launch_tree_attn(t, s));
+    return TASP_OK;
+  };
+  return prefill_layers(p, x, n, out, s, nullptr, false, attend);
+}
+
+}  // namespace
+
+tasp_status tasp_seq_bind(tasp_plan p, tasp_seq_cache* cache) {
+  tasp_status st = check_step_cache(p, cache);
+  if (st) return st;
+  cache->plan_sig = p->sig;
+  return TASP_OK;
+}
+
+tasp_status tasp_tree_step_workspace_bytes(tasp_plan p, const tasp_seq_cache* cache, int32_t T, int32_t max_len,
+                                           size_t* bytes) {
+  tasp_status st = check_step_cache(p, cache);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  size_t attn = 0;
+  return step_layout(p, cache, T, max_len, &attn, bytes);
+}
+
+tasp_status tasp_tree_forward(tasp_plan p, const float* x, const int32_t* parent, int32_t T,
+                              const tasp_seq_cache* cache, int32_t max_len, float* out, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  tasp_status st;
+  size_t attn = 0, total = 0;
+  if ((st = check_step_cache(p, cache)) || (st = check_tree(parent, T, false)) ||
+      (st = step_layout(p, cache, T, max_len, &attn, &total)))
+    return st;
+  if (!x || !out) return fail(TASP_ERR_INVALID_ARG, "x / out is NULL");
+  if (cache->plan_sig != p->sig)
+    return fail(TASP_ERR_CACHE_PLAN_MISMATCH, "cache belongs to plan %016llx, not %016llx",
+                (unsigned long long)cache->plan_sig, (unsigned long long)p->sig);
+  const size_t rows = size_t(T) * cache->batch, width = p->desc.vocab ? p->desc.vocab : p->desc.d_model;
+  const char *xb = reinterpret_cast<const char*>(x), *ob = reinterpret_cast<const char*>(out);
+  if (ob < xb + rows * p->desc.d_model * 4 && xb < ob + rows * width * 4)
+    return fail(TASP_ERR_INVALID_ARG, "x and out overlap");
+  if ((st = check_workspace(workspace, workspace_bytes, attn))) return st;
+  return tree_forward(p, x, parent, T, cache, max_len, out, static_cast<float*>(workspace),
+                      static_cast<hipStream_t>(stream));
+}
+
+tasp_status tasp_tree_step(tasp_plan p, const int8_t* embed, const float* embed_scale, const int32_t* tokens,
+                           const int32_t* parent, const float* u, const float* draft_logits, double temperature,
+                           int32_t T, int32_t max_len, const tasp_seq_cache* cache, int32_t* ids, int32_t* path,
+                           int32_t* n, float* x_scratch, float* logits, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  tasp_status st;
+  size_t attn = 0, total = 0;
+  if ((st = check_step_cache(p, cache)) || (st = step_layout(p, cache, T, max_len, &attn, &total))) return st;
+  const tasp_model_desc& d = p->desc;
+  if (d.vocab < 1) return fail(TASP_ERR_UNSUPPORTED, "plan has no LM head");
+  if (!embed || !embed_scale || !tokens) return fail(TASP_ERR_INVALID_ARG, "embedding / tokens is NULL");
+  if ((st = check_workspace(workspace, workspace_bytes, total))) return st;
+  char* ws = static_cast<char*>(workspace);
+  // everything that the later calls would refuse is refused here, before the first launch
+  if ((st = check_verify(logits, tokens, u, parent, draft_logits, cache->batch, T, d.vocab, temperature, ids, path, n,
+                         ws + attn, total - attn)) ||
+      (st = check_tree(parent, T, false)))
+    return st;
+  if (!x_scratch) return fail(TASP_ERR_INVALID_ARG, "x_scratch is NULL");
+  const size_t rows = size_t(T) * cache->batch;
+  const char *xb = reinterpret_cast<const char*>(x_scratch), *ob = reinterpret_cast<const char*>(logits);
+  if (ob < xb + rows * d.d_model * 4 && xb < ob + rows * d.vocab * 4)
+    return fail(TASP_ERR_INVALID_ARG, "x_scratch and logits overlap");
+  if (cache->plan_sig != p->sig)
+    return fail(TASP_ERR_CACHE_PLAN_MISMATCH, "cache belongs to plan %016llx, not %016llx",
+                (unsigned long long)cache->plan_sig, (unsigned long long)p->sig);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  HIP_TRY(tasp::launch_embed(embed, embed_scale, d.vocab, d.d_model, tokens, T * cache->batch, x_scratch, s));
+  if ((st = tasp_tree_forward(p, x_scratch, parent, T, cache, max_len, logits, workspace, workspace_bytes, stream)) ||
+      (st = tasp_verify(logits, tokens, u, parent, draft_logits, cache->batch, T, d.vocab, temperature, ids, path, n,
+                        ws + attn, total - attn, stream)))
+    return st;
+  return tasp_seq_commit(cache, path, n, T, cache->len, stream);
 }
 
 tasp_status tasp_copy_probe(void* dst, const void* src, size_t bytes, void* stream) {

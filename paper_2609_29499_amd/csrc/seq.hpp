@@ -29,6 +29,7 @@ struct SeqAppendArgs {
   const int* parent; int T;            // [batch][T] or null: a chain
   int act;                             // SEQ_BF16 or SEQ_F32: type of q, k, v and q_out
   SeqRows q, k, v, q_out;
+  int ks; long split;                  // ks > 1 (SEQ_F32): q, k, v are sums of ks arrays `split` floats apart
   int n_q, n_kv;                       // head rows of q; of k and v
   const int* kv_map;                   // host: cache head of k / v head j (null: j), used by the launch
   int rot, interleaved;                // rotated dimensions of a head; pair layout
@@ -58,7 +59,11 @@ struct TreeAttnArgs {
   const int* parent; int T;
   int act;
   SeqRows q, o;
-  int n_q, group;                      // query heads, and per cache head
+  // slots: cache heads that are read; slot j reads head kv_map[j] for query heads q_start[j] .. q_start[j + 1] - 1,
+  // 1 .. group of them
+  int slots, group;
+  unsigned char kv_map[64];
+  unsigned short q_start[65];
   float scale2;                        // scale * log2(e)
   int max_len;                         // largest length expected (sizes the grid; any length is served)
   float* ws;                           // records, tree_attn_workspace_bytes

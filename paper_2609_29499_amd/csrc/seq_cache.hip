@@ -42,6 +42,19 @@ __device__ __forceinline__ Vec8 load8(const void* p, long at) {
   return x;
 }
 
+// the same of a sum of arrays (a projection's splits), in their order
+template <int ACT>
+__device__ __forceinline__ Vec8 load8(const void* p, long at, const SeqAppendArgs& a) {
+  Vec8 x = load8<ACT>(p, at);
+  if constexpr (ACT == SEQ_F32)
+    for (int z = 1; z < a.ks; ++z) {
+      const Vec8 y = load8<ACT>(p, at + z * a.split);
+#pragma unroll
+      for (int i = 0; i < kE; ++i) x.v[i] += y.v[i];
+    }
+  return x;
+}
+
 template <int ACT>
 __device__ __forceinline__ void store8(void* p, long at, const Vec8& x) {
   if constexpr (ACT == SEQ_BF16) {
@@ -108,7 +121,7 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
     Vec8 x{};
     if (in && there) {
       const long row = b * src.seq + t * src.token + h * src.head;
-      x = load8<ACT>(src.p, row + e0);
+      x = load8<ACT>(src.p, row + e0, a);
       if (kind < 2 && e0 < a.rot) {
         if (a.interleaved) {           // pairs (2 i, 2 i + 1)
 #pragma unroll
@@ -121,7 +134,7 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
         } else {                       // pairs (i, i + rot / 2): the partner's eight elements
           const int half = a.rot / 2;
           const bool first = e0 < half;
-          const Vec8 y = load8<ACT>(src.p, row + (first ? e0 + half : e0 - half));
+          const Vec8 y = load8<ACT>(src.p, row + (first ? e0 + half : e0 - half), a);
 #pragma unroll
           for (int i = 0; i < kE; ++i) {
             const float2 w = cs[(first ? e0 : e0 - half) + i];

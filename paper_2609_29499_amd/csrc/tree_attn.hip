@@ -47,10 +47,10 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 // ---- which rows a workgroup serves
 // Sequence b has steps(b) = ceil((L + T) / 32) steps and is cut in chunks of `chunk` steps. A wave holds four
 // sequences per lane.
-// How a call is launched: query rows in rb blocks (of 16 mt rows, wide: 64 mt), `target` workgroups aimed at, at most `most`
+// How a call is launched: query rows in rb blocks of `rows` (16 mt, wide: 64 mt), `target` workgroups aimed at, at most `most`
 // chunks per sequence (what the workspace has room for), grid workgroups.
 struct TreeShape {
-  int wide, mt, rb, target, most, grid;
+  int wide, mt, rows, rb, target, most, grid;
 };
 struct Deal {
   int chunk;                           // steps per chunk
@@ -75,7 +75,7 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, 
   // (said to be the same in all lanes wherever it is: a buffer descriptor or a branch that the compiler takes for
   // divergent becomes a loop over lanes, around every load)
   sum = __builtin_amdgcn_readfirstlane(sum);
-  const int units = a.c.n_kv * y.rb, chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
+  const int units = a.slots * y.rb, chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
   d.chunk = chunk;
   const int quota = y.target / units;
   if (a.c.batch > 1 && 2 * a.c.batch <= quota) {
@@ -224,7 +224,9 @@ __device__ __forceinline__ void add_odd(const TreeAttnArgs& a, size_t unit, int 
 
 // The part of the work that a workgroup takes.
 struct Place {
-  int b, g, rb;                        // sequence, cache head, block of query rows
+  int b, g, rb;                        // sequence, slot, block of query rows
+  int h0, group, R;                    // the slot's first query head, its heads, its query rows
+  size_t unit;                         // its cache head among those of all sequences
   int n_ch, ch, rec;                   // chunks of the sequence, this one, and its record
   int L, Lr, end;                      // length (-1: passed over), rows cached, rows that may be read
   int s0, s1;                          // steps
@@ -232,13 +234,13 @@ struct Place {
 __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, Place& p) {
   const Deal d = deal(a, y, lane);
   // Row blocks of one chunk and head read the same rows: eight workgroups apart (one XCD, one L2) and next to
-  // each other in time. Item: chunk of a sequence x cache head.
+  // each other in time. Item: chunk of a sequence x slot.
   const int w = blockIdx.x, j = w >> 3;
   p.rb = j % y.rb;
   const int item = (j / y.rb) * 8 + (w & 7);
-  if (item >= d.total * a.c.n_kv) return false;
-  p.g = item % a.c.n_kv;
-  const int all = item / a.c.n_kv;
+  if (item >= d.total * a.slots) return false;
+  p.g = item % a.slots;
+  const int all = item / a.slots;
   int hit = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -250,6 +252,11 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   p.n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
   p.ch = all - before;
   p.rec = item * y.rb + p.rb;
+  p.h0 = a.q_start[p.g];
+  p.group = a.q_start[p.g + 1] - p.h0;
+  p.R = a.T * p.group;
+  if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
+  p.unit = size_t(p.b) * a.c.n_kv + a.kv_map[p.g];
   p.L = __builtin_amdgcn_readfirstlane(seq_len(a.c.len, p.b, a.c.S));
   p.Lr = max(p.L, 0);
   p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
@@ -261,12 +268,12 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   return true;
 }
 
-// One query row's NDT output values (unnormalised) with their sum l and maximum m: to the output, or to
-// row `row` of the chunk's record of RB rows. there: the row is that of a node that is present.
+// One query row's output values (unnormalised) with their sum l: node t, head h from dimension d0 on. there: the
+// node is present. put_record: the same with the maximum m to row `row` of the chunk's record of RB rows.
 template <int DH, int ACT, int N>
-__device__ __forceinline__ void put_output(const TreeAttnArgs& a, int b, int g, int row, int d0, float l, bool there, const float (&v)[N]) {
+__device__ __forceinline__ void put_output(const TreeAttnArgs& a, int b, int t, int h, int d0, float l, bool there, const float (&v)[N]) {
   const float inv = there && l != 0.0f ? 1.0f / l : 0.0f;
-  const long at = b * a.o.seq + (row / a.group) * a.o.token + (g * a.group + row % a.group) * a.o.head + d0;
+  const long at = b * a.o.seq + t * a.o.token + h * a.o.head + d0;
 #pragma unroll
   for (int e = 0; e < N; e += 4) {
     float z[4];
@@ -345,11 +352,11 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   const int r = lane & 15, c = lane >> 4;
   Place p;
   if (!place(a, y, lane, p)) return;
-  const int b = p.b, g = p.g, rb = p.rb, L = p.L, Lr = p.Lr, end = p.end, s0 = p.s0, s1 = p.s1;
+  const int b = p.b, rb = p.rb, L = p.L, Lr = p.Lr, end = p.end, s0 = p.s0, s1 = p.s1;
   // steps from s_edge on hold rows of the tree: at most three, so a wave has one at most
   const int s_edge = min(Lr / kStep, s1);
 
-  const size_t unit = size_t(b) * a.c.n_kv + g;
+  const size_t unit = p.unit;
   const uint32_t row_bytes = DH * ES;
   const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char*>(a.c.k) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
   const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const char*>(a.c.v) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
@@ -399,14 +406,14 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   load(s_own, s_edge, xb);
 
   // this lane's query rows, as rows of Q (B operand): node t, head h
-  const int R = a.T * a.group;
+  const int R = p.R;
   const TreeNode nd = tree_node(a.parent ? a.parent + size_t(b) * a.T : nullptr, a.T, L < 0 ? 0 : a.c.S - L, lane);
   unsigned long long anc[MT];
   uint32_t qf[MT][QT][NKC][4];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = min((rb * MT + mt) * 16 + r, R - 1);   // (rows past the last one repeat it and are not stored)
-    const int t = row / a.group, h = g * a.group + row % a.group;
+    const int t = row / p.group, h = p.h0 + row % p.group;
     anc[mt] = __shfl(nd.anc, t, kWave);
     load_q<DH, ACT, QT, ES == 1>(a, b * a.q.seq + t * a.q.token + h * a.q.head + (ES == 2 ? 8 : 16) * c, qf[mt]);
   }
@@ -544,14 +551,14 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
       for (int k = 0; k < 4; ++k) v[e] += s_o[k][qr][d0 + e] * f[k];
     }
     const int row_o = (rb * MT + mt) * 16 + qr;
-    const int t_o = min(row_o, R - 1) / a.group;
+    const int t_o = min(row_o, R - 1) / p.group;
     const unsigned long long anc_o = __shfl(nd.anc, t_o, kWave);
     const bool there = anc_o != 0;     // (a row of an absent node is zeros)
     if (row_o >= R) continue;
     if constexpr (TYPE != SEQ_INT8) {
       if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, max(s_edge, s0) * kStep, s1 * kStep, anc_o, d0, v);
     }
-    if (p.n_ch == 1) put_output<DH, ACT>(a, b, g, row_o, d0, l, there, v);
+    if (p.n_ch == 1) put_output<DH, ACT>(a, b, t_o, p.h0 + row_o % p.group, d0, l, there, v);
     else put_record<DH, RB>(a, p.rec, 16 * mt + qr, d0, m, there ? l : 0.0f, v);
   }
 }
@@ -581,7 +588,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   Place p;
   if (!place(a, y, lane, p)) return;
   const int Lr = p.Lr, end = p.end;
-  const size_t unit = size_t(p.b) * a.c.n_kv + p.g;
+  const size_t unit = p.unit;
   const uint32_t row_bytes = DH * ES;
   const bool for_v = wave < 2;         // this wave brings V (32 rows), or K
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(for_v ? a.c.v : a.c.k) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
@@ -668,6 +675,9 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
                                           __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
         }
       }
+      // The two branches' last stores are kept apart by order: merged into one store behind both (three of its four
+      // words, for BF16 rows and float32 q at dh 64), the compiler took one of V's words from the wrong register.
+      asm volatile("; V is stored" ::: "memory");
     } else {
       // lane (r', c') of operand kk reads slot 16 c' + (r' ^ (4 kk + c')): the pieces of one row, written
       // together, go to different banks
@@ -688,6 +698,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
           put(2 * j + 1, make_uint4(w[4], w[5], w[6], w[7]));
         }
       }
+      asm volatile("; K is stored" ::: "memory");
     }
   };
 
@@ -695,14 +706,14 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   load(x, p.s0);
   if (tid == 0) s_odd = 0;
   // this lane's query rows, as rows of Q (B operand): node t, head h
-  const int R = a.T * a.group;
+  const int R = p.R;
   const TreeNode nd = tree_node(a.parent ? a.parent + size_t(p.b) * a.T : nullptr, a.T, p.L < 0 ? 0 : a.c.S - p.L, lane);
   unsigned long long anc[MT];
   uint32_t qf[MT][QT][NKC][4];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = min(p.rb * RB + (wave * MT + mt) * 16 + r, R - 1);     // (rows past the last one repeat it and are not stored)
-    const int t = row / a.group, h = p.g * a.group + row % a.group;
+    const int t = row / p.group, h = p.h0 + row % p.group;
     anc[mt] = __shfl(nd.anc, t, kWave);
     load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
   }
@@ -785,14 +796,15 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
     for (int i = 0; i < 4; ++i) {
       const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
       const float m = __shfl(m_run[mt], 4 * c + i, kWave), l = __shfl(l_all, 4 * c + i, kWave);
-      const unsigned long long anc_o = __shfl(nd.anc, min(row, R - 1) / a.group, kWave);
+      const int t = min(row, R - 1) / p.group;
+      const unsigned long long anc_o = __shfl(nd.anc, t, kWave);
       float v[NDT];
 #pragma unroll
       for (int e = 0; e < NDT; ++e) v[e] = o[mt][e][i];
       if constexpr (TYPE != SEQ_INT8)
         if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, p.s0 * kStep, p.s1 * kStep, anc_o, NDT * r, v);
       if (row < R) {
-        if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, p.g, row, NDT * r, l, anc_o != 0, v);
+        if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, t, p.h0 + row % p.group, NDT * r, l, anc_o != 0, v);
         else put_record<DH, RB>(a, p.rec, in, NDT * r, m, anc_o != 0 ? l : 0.0f, v);
       }
     }
@@ -813,11 +825,12 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], b >> 2);
   if (n <= 1) return;                  // written already
   const int q_row = blockIdx.x * ROWS + (PARTS > 1 ? 0 : tid / LPR);
-  if (q_row >= a.T * a.n_q) return;    // (PARTS > 1: every row has a workgroup)
-  const int t = q_row / a.n_q, h = q_row % a.n_q;
-  const int g = h / a.group, row = t * a.group + h % a.group;
-  const int rows = (y.wide ? 64 : 16) * y.mt, rb = row / rows, in = row % rows;
-  const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.c.n_kv * y.rb;
+  if (q_row >= a.T * a.slots * a.group) return;        // (PARTS > 1: every row has a workgroup)
+  const int t = q_row / (a.slots * a.group), g = q_row / a.group % a.slots, hh = q_row % a.group;
+  const int h0 = a.q_start[g], group = a.q_start[g + 1] - h0;
+  if (hh >= group) return;
+  const int row = t * group + hh, rows = y.rows, rb = row / rows, in = row % rows;
+  const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.slots * y.rb;
   const float* first = a.ws + before * stride + (size_t(g) * y.rb + rb) * rec;
   const int part = PARTS > 1 ? tid / LPR : 0, d0 = 4 * (tid % LPR);
   float m = -INFINITY, l = 0.0f;
@@ -857,7 +870,7 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) add(s_m[k], s_l[k], s_o[k][tid]);
   }
-  put_output<DH, ACT>(a, b, g, row, d0, l, true, v);
+  put_output<DH, ACT>(a, b, t, h0 + hh, d0, l, true, v);
 }
 
 TreeShape shape(const TreeAttnArgs& a) {
@@ -866,14 +879,15 @@ TreeShape shape(const TreeAttnArgs& a) {
   y.wide = tiles > 2;
   y.mt = y.wide ? (tiles > 4 && a.act == SEQ_BF16 ? 2 : 1) : tiles;
   const int block = (y.wide ? 4 : 1) * y.mt;           // tiles of a workgroup
+  y.rows = 16 * block;
   y.rb = (tiles + block - 1) / block;
   y.target = 512;                      // two workgroups per CU
-  const int units = a.c.n_kv * y.rb;
+  const int units = a.slots * y.rb;
   const long steps = (std::min<long>(std::max(a.max_len, 0) + long(a.T), a.c.S) + kStep - 1) / kStep;
   y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (y.target + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
   const long chunks = std::min<long>(long(a.c.batch) * y.most, y.target / units + 1 + a.c.batch);
-  y.grid = int((chunks * a.c.n_kv + 7) / 8 * 8 * y.rb);
+  y.grid = int((chunks * a.slots + 7) / 8 * 8 * y.rb);
   return y;
 }
 
@@ -881,8 +895,7 @@ TreeShape shape(const TreeAttnArgs& a) {
 
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
   const TreeShape y = shape(a);
-  const size_t rows = size_t(y.wide ? 64 : 16) * y.mt;
-  return y.most == 1 ? 0 : size_t(y.grid) * rows * (a.c.dh + 2) * 4;
+  return y.most == 1 ? 0 : size_t(y.grid) * y.rows * (a.c.dh + 2) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
@@ -913,13 +926,14 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
 #undef ATTN
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || y.most == 1) return e;
+  const int rows = a.T * a.slots * a.group;
   // few rows: a workgroup for each (latency); many: a group of lanes walks all of a row's chunks (the 64-node
   // case took 72 us with a workgroup per row)
 #define JOIN(DH, ACT)                                                                                              \
   do {                                                                                                             \
     constexpr int PARTS = 4 * kBlock / DH;                                                                         \
-    if (long(a.T) * a.n_q * a.c.batch < 2048) hipLaunchKernelGGL((tree_join_kernel<DH, ACT, PARTS>), dim3(a.T * a.n_q, a.c.batch), dim3(kBlock), 0, s, a, y); \
-    else hipLaunchKernelGGL((tree_join_kernel<DH, ACT, 1>), dim3((a.T * a.n_q + PARTS - 1) / PARTS, a.c.batch), dim3(kBlock), 0, s, a, y); \
+    if (rows * a.c.batch < 2048) hipLaunchKernelGGL((tree_join_kernel<DH, ACT, PARTS>), dim3(rows, a.c.batch), dim3(kBlock), 0, s, a, y); \
+    else hipLaunchKernelGGL((tree_join_kernel<DH, ACT, 1>), dim3((rows + PARTS - 1) / PARTS, a.c.batch), dim3(kBlock), 0, s, a, y); \
   } while (0)
   if (a.c.dh == 128 && a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
   else if (a.c.dh == 128) JOIN(128, SEQ_F32);

@@ -254,6 +254,54 @@ class Plan:
                                     stream if stream is not None else current_stream())
 
 
+    def seq_bind(self, cache):
+        B.tasp_seq_bind(self.handle, cache.struct)
+
+    def tree_workspace(self, cache, T, max_len=None, stream=None):
+        """A workspace for tree_forward and tree_step calls of this shape."""
+        n = B.tasp_tree_step_workspace_bytes(self.handle, cache.struct, T, cache.max_seq if max_len is None else max_len)
+        return _workspace(n, cache.k.device, stream)
+
+    def tree_forward(self, x, cache, parent=None, max_len=None, out=None, workspace=None, stream=None):
+        """The plan over trees of nodes: x float32 [B][T][d] -> logits [B][T][V] (or residuals [B][T][d])."""
+        dev = _device(cache.k, x, parent, out)
+        nb, T = x.shape[:2]
+        width = self.desc.vocab or self.desc.d_model
+        if out is None:
+            out = _empty((nb, T, width), torch.float32, x.device, stream)
+        ml = cache.max_seq if max_len is None else max_len
+        ws = workspace if workspace is not None else self.tree_workspace(cache, T, ml, stream)
+        _launch(B.tasp_tree_forward, dev, stream, self.handle, _ptr(x, (cache.batch, T, self.desc.d_model), torch.float32, "x"),
+                cache._parent(parent, T), T, cache.struct, ml, _ptr(out, (nb, T, width), torch.float32, "out"), ws[1], ws[2])
+        return out
+
+    def tree_step(self, embed, embed_scale, tokens, cache, u=None, parent=None, draft_logits=None, temperature=0.0,
+                  max_len=None, out=None, scratch=None, workspace=None, stream=None):
+        """One step over drafted tokens int32 [B][T] (node 0: the text's last token): returns (ids, path, n) as
+        ``verify`` does, and the cache has grown by the accepted rows. ``out``: those three; ``scratch``: (x [B][T][d],
+        logits [B][T][V])."""
+        dev = _device(cache.k, embed, embed_scale, tokens, u, parent, draft_logits)
+        nb, T = tokens.shape
+        D, V = self.desc.d_model, self.desc.vocab
+        if scratch is None:
+            scratch = (_empty((nb, T, D), torch.float32, tokens.device, stream),
+                       _empty((nb, T, max(V, 1)), torch.float32, tokens.device, stream))
+        if out is None:
+            ids, path = _empty((2, nb, T), torch.int32, tokens.device, stream)
+            out = ids, path, _empty((nb,), torch.int32, tokens.device, stream)
+        ml = cache.max_seq if max_len is None else max_len
+        ws = workspace if workspace is not None else self.tree_workspace(cache, T, ml, stream)
+        _device(cache.k, *out, *scratch)
+        _launch(B.tasp_tree_step, dev, stream, self.handle, _ptr(embed, (V, D), torch.int8, "embed"),
+                _ptr(embed_scale, (V,), torch.float32, "embed_scale"), _ptr(tokens, (cache.batch, T), torch.int32, "tokens"),
+                cache._parent(parent, T), _ptr(u, (nb, T), torch.float32, "u"),
+                _ptr(draft_logits, (nb, T - 1, V), torch.float32, "draft_logits"), temperature, T, ml, cache.struct,
+                _ptr(out[0], (nb, T), torch.int32, "ids"), _ptr(out[1], (nb, T), torch.int32, "path"),
+                _ptr(out[2], (nb,), torch.int32, "n"), _ptr(scratch[0], (nb, T, D), torch.float32, "x"),
+                _ptr(scratch[1], (nb, T, max(V, 1)), torch.float32, "logits"), ws[1], ws[2])
+        return out
+
+
 def build_mask(desc, head_scores, chan_scores, granule, target, stream=None):
     """Greedy dependency-closed mask from device float32 scores ([L][Hq], [L][d_ffn/granule]).
     Returns (q_keep, kv_keep, ffn_keep) as device uint8 tensors and the FLOPs spent."""

@@ -178,3 +178,19 @@ def test_large_scores_and_one_step_rises():
     k64 = c.k.double().cpu().numpy()
     g = got.double().cpu().numpy()
     check(g, q.double().numpy(), k64[0], vv[0], [700], None, 704, "bf16", 30.0)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_every_block_of_query_rows(dh, kind, act):
+    """1, 2, 3 .. 4, 5 .. 8 and more tiles of 16 query rows (every kernel), in one chunk and in several."""
+    flush(f"case blocks {dh} {kind} {act}")
+    for T, hq, lens in ((3, 4, [70, 1]), (5, 6, [33, 400]), (9, 6, [90, 700]), (13, 8, [5, 311]), (23, 8, [64, 190])):
+        S_ = max(lens) + T
+        c, kv, vv = typed_cache(lens, 1, S_, dh, kind, T)
+        parent = random_parents(2, T, T, absent=False)
+        q = randn((2, T, hq, dh), DTYPES[act], 50 + T)
+        got = S.tree_attention(c, 0, q.cuda(), parent.cuda())
+        torch.cuda.synchronize()
+        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
