@@ -2270,6 +2270,9 @@ tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, co
   tasp::SeqCommitArgs a{};
   a.c = seq_layer(cache, 0); a.n_layers = cache->n_layers;
   a.path = path; a.ld = T; a.n = n; a.len_out = len_out;
+  const size_t B = size_t(cache->batch);
+  auto apart = [&](const int32_t* q, size_t count) { return len_out + B <= q || q + count <= len_out; };
+  a.apart = apart(cache->len, B) && apart(n, B) && apart(path, B * size_t(T));
   HIP_TRY(tasp::launch_seq_commit(a, static_cast<hipStream_t>(stream)));
   return TASP_OK;
 }

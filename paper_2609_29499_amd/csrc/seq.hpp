@@ -51,6 +51,7 @@ struct SeqCommitArgs {
   const int* path; int ld;             // [batch][ld]
   const int* n;                        // [batch]
   int* len_out;                        // [batch]; may be c.len
+  bool apart;                          // len_out shares nothing with what the launch reads
 };
 hipError_t launch_seq_commit(const SeqCommitArgs& a, hipStream_t s);
 

@@ -232,6 +232,11 @@ __global__ __launch_bounds__(kBlock) void seq_read_kernel(SeqReadArgs a) {
   store8<OUT>(dst.p, b * dst.seq + i * dst.token + h * dst.head + e0, x);
 }
 
+__device__ __forceinline__ int next_len(const SeqCommitArgs& a, int b) {
+  const int L = a.c.len[b], n = max(0, min(min(a.n[b], a.ld), kTreeMax));
+  return L < 0 || L > a.c.S ? L : min(L + n, a.c.S);
+}
+
 // Rows len + path[i] -> len + i, i < n, of every layer, sequence and head: grid (heads of all layers
 // and sequences, k / v). The workgroup reads every row that moves before it writes the first (path may
 // name rows that earlier entries replace). Rows that stay are not touched.
@@ -241,6 +246,8 @@ __global__ __launch_bounds__(kBlock) void seq_commit_kernel(SeqCommitArgs a) {
   const int u = blockIdx.x, b = (u / a.c.n_kv) % a.c.batch;
   const int L = seq_len(a.c.len, b, a.c.S);
   const int n = min(min(a.n[b], a.ld), kTreeMax);
+  if (a.apart && u < a.c.batch * a.c.n_kv && u % a.c.n_kv == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+    a.len_out[b] = next_len(a, b);
   if (L < 0) return;
   char* base = static_cast<char*>(blockIdx.y ? a.c.v : a.c.k) + size_t(u) * a.c.S * RB;
   float* sc = a.c.ks ? (blockIdx.y ? a.c.vs : a.c.ks) + size_t(u) * a.c.S : nullptr;
@@ -274,8 +281,7 @@ __global__ __launch_bounds__(kBlock) void seq_commit_kernel(SeqCommitArgs a) {
 __global__ __launch_bounds__(kBlock) void seq_length_kernel(SeqCommitArgs a) {
   const int b = threadIdx.x;
   if (b >= a.c.batch) return;
-  const int L = a.c.len[b], n = max(0, min(min(a.n[b], a.ld), kTreeMax));
-  a.len_out[b] = L < 0 || L > a.c.S ? L : min(L + n, a.c.S);
+  a.len_out[b] = next_len(a, b);
 }
 
 }  // namespace
@@ -339,6 +345,7 @@ hipError_t launch_seq_commit(const SeqCommitArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((seq_commit_kernel<64>), grid, dim3(kBlock), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (a.apart) return hipSuccess;
   // a launch of its own: every workgroup above reads the lengths that this one replaces
   hipLaunchKernelGGL(seq_length_kernel, dim3(1), dim3(kBlock), 0, s, a);
   return hipGetLastError();

@@ -32,45 +32,61 @@ struct ChunkStat {
   int at;                              // lowest index of it
 };
 
-// exp((l - m) / temperature) = 2^(t / 32), t = (l - m) (32 log2(e) / temperature): t is cut at the nearest
-// integer n, 2^((n mod 32) / 32) comes from a table in LDS, 2^(f / 32), |f| <= 1/2, from the Taylor polynomial of
-// degree 5 (remainder (ln 2 / 64)^6 / 720 = 2e-15). 15 instructions in 64 bits (26 without the table: the 32-node
-// case 107 us).
-__constant__ double kPow32[32] = {
-    1, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237,
-    1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
-    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332,
-    1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
-    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228,
-    1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.6457554781539649,
-    1.681792830507429, 1.7186192981224779, 1.7562521603732995, 1.7947090750031072,
-    1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002,
+// exp((l - m) / temperature) = 2^(t / 64), t = (l - m) (64 log2(e) / temperature): t is cut at the nearest integer n by
+// adding 1.5 2^52, which leaves n in the sum's low word; 2^((n mod 64) / 64) comes from a table in LDS, 2^(f / 64),
+// |f| <= 1/2, from the Taylor polynomial of degree 4 (remainder (ln 2 / 128)^5 / 120 = 4e-14), and n / 64 is added to
+// the exponent. 17 instructions, three of them conversions or compares (with rint, a conversion and ldexp, in 64 bits
+// and at a quarter of the rate, the stats of the 32-node case took 80 us).
+__constant__ double kPow64[64] = {
+    1.0, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284,
+    1.0442737824274138, 1.0556451783605572, 1.0671404006768237, 1.0787607977571199,
+    1.0905077326652577, 1.102382583307841, 1.1143867425958924, 1.1265216186082418,
+    1.1387886347566916, 1.1511892299529827, 1.1637248587775775, 1.1763969916502812,
+    1.189207115002721, 1.202156731452703, 1.215247359980469, 1.22848053610687,
+    1.241857812073484, 1.255380757024691, 1.2690509571917332, 1.2828700160787783,
+    1.2968395546510096, 1.3109612115247644, 1.3252366431597413, 1.339667524053303,
+    1.3542555469368927, 1.3690024229745905, 1.383909881963832, 1.3989796725383112,
+    1.4142135623730951, 1.42961333839197, 1.4451808069770467, 1.460917794180647,
+    1.4768261459394993, 1.4929077282912648, 1.5091644275934228, 1.5255981507445384,
+    1.5422108254079407, 1.559004400237837, 1.5759808451078865, 1.593142151342267,
+    1.6104903319492543, 1.6280274218573478, 1.645755478153965, 1.6636765803267364,
+    1.681792830507429, 1.7001063537185235, 1.718619298122478, 1.7373338352737062,
+    1.7562521603732995, 1.7753764925265212, 1.7947090750031072, 1.8142521755003989,
+    1.8340080864093424, 1.8539791250833855, 1.8741676341103, 1.8945759815869656,
+    1.9152065613971474, 1.9360617934922943, 1.9571441241754002, 1.978456026387951,
 };
-constexpr double kLn2_32 = 0.69314718055994530942 / 32.0;
+constexpr double kLn2_64 = 0.69314718055994530942 / 64.0;
 struct Exp {
-  const double* table;                 // kPow32 in LDS
-  double scale;                        // 32 log2(e) / temperature; 0: greedy, nothing is asked for
+  const double* table;                 // kPow64 in LDS
+  double scale;                        // 64 log2(e) / temperature; greedy calls ask for no weight
+  double low;                          // l - m below which a weight is 0: 2^-1020, what 64 bits hold in full
 };
-// Fills the table (by the first 32 threads; a barrier follows before its use)
+// Fills the table (by the first 64 threads; a barrier follows before its use)
 __device__ __forceinline__ Exp exp_table(double* lds, double inv_temp) {
-  if (threadIdx.x < 32) lds[threadIdx.x] = kPow32[threadIdx.x];
-  return {lds, inv_temp * 32.0 * 1.44269504088896340736};
+  if (threadIdx.x < 64) lds[threadIdx.x] = kPow64[threadIdx.x];
+  const double scale = inv_temp * 64.0 * 1.44269504088896340736;
+  return {lds, scale, -64.0 * 1020.0 / scale};
+}
+// 2^(d scale / 64) for low <= d <= 0
+__device__ __forceinline__ double exp_of(double d, const Exp& e) {
+  constexpr double magic = 0x1.8p52;
+  const double s = fma(d, e.scale, magic), f = fma(d, e.scale, magic - s);
+  const int n = __double2loint(s);
+  constexpr double c = kLn2_64;
+  double p = c * c * c * c / 24.0;
+  p = fma(p, f, c * c * c / 6.0);
+  p = fma(p, f, c * c / 2.0);
+  p = fma(p, f, c);
+  const double t = e.table[n & 63], y = fma(t, p * f, t);
+  return __hiloint2double(__double2hiint(y) + int(uint32_t(n & ~63) << 14), __double2loint(y));
 }
 // The weight of a logit whose row's maximum is m: NaN counts as -inf, a row without anything above -inf has
 // no weight, +inf shares it evenly.
 __device__ __forceinline__ double weight(float l, float m, const Exp& e) {
   if (m == INFINITY) return l == m ? 1.0 : 0.0;
-  const double t = fmax((double(l) - double(m)) * e.scale, -1e6);    // (NaN too; 2^-31250 is 0)
-  const double n = rint(t), f = t - n;
-  const int i = int(n);
-  constexpr double c = kLn2_32;
-  double p = c * c * c * c * c / 120.0;
-  p = fma(p, f, c * c * c * c / 24.0);
-  p = fma(p, f, c * c * c / 6.0);
-  p = fma(p, f, c * c / 2.0);
-  p = fma(p, f, c);
-  p = fma(p, f, 1.0);
-  return ldexp(p * e.table[i & 31], i >> 5);
+  const double d = double(l) - double(m);
+  const double y = exp_of(fmax(d, e.low), e);
+  return d > e.low ? y : 0.0;
 }
 
 __device__ __forceinline__ double wave_sum_d(double v) {
@@ -84,7 +100,7 @@ __device__ __forceinline__ double wave_sum_d(double v) {
 __global__ __launch_bounds__(kBlock) void verify_stats_kernel(VerifyArgs a, ChunkStat* stat, int* cnt) {
   __shared__ float sm[4];
   __shared__ int si[4];
-  __shared__ double sz[4], table[32];
+  __shared__ double sz[4], table[64];
   const Exp ex = exp_table(table, a.inv_temp);
   const int tid = threadIdx.x, wave = tid >> 6;
   const int c = blockIdx.x, r = blockIdx.y, nt = a.B * a.T;
@@ -99,41 +115,56 @@ __global__ __launch_bounds__(kBlock) void verify_stats_kernel(VerifyArgs a, Chun
   }
   float m = -INFINITY;
   int at = 0x7fffffff;
+  if (a.inv_temp == 0.0) {             // greedy: the maximum and its place are all
 #pragma unroll
-  for (int i = 0; i < kVU; ++i)
-    if (x[i] > m) {
-      m = x[i];
-      at = k0 + i * kBlock;
+    for (int i = 0; i < kVU; ++i)
+      if (x[i] > m) {
+        m = x[i];
+        at = k0 + i * kBlock;
+      }
+#pragma unroll
+    for (int k = 1; k < kWave; k <<= 1) {
+      const float om = __shfl_xor(m, k, kWave);
+      const int oa = __shfl_xor(at, k, kWave);
+      if (om > m || (om == m && oa < at)) {
+        m = om;
+        at = oa;
+      }
     }
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) {
-    const float om = __shfl_xor(m, k, kWave);
-    const int oa = __shfl_xor(at, k, kWave);
-    if (om > m || (om == m && oa < at)) {
-      m = om;
-      at = oa;
+    if ((tid & 63) == 0) {
+      sm[wave] = m;
+      si[wave] = at;
     }
-  }
-  if ((tid & 63) == 0) {
-    sm[wave] = m;
-    si[wave] = at;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-    if (sm[w] > m || (sm[w] == m && si[w] < at)) {
-      m = sm[w];
-      at = si[w];
-    }
-  double z = 0.0;
-  if (a.inv_temp > 0.0) {
-#pragma unroll
-    for (int i = 0; i < kVU; ++i) z += weight(x[i], m, ex);
-    z = wave_sum_d(z);
-    if ((tid & 63) == 0) sz[wave] = z;
     __syncthreads();
-    z = (sz[0] + sz[1]) + (sz[2] + sz[3]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (sm[w] > m || (sm[w] == m && si[w] < at)) {
+        m = sm[w];
+        at = si[w];
+      }
+    if (tid == 0) stat[size_t(r) * gridDim.x + c] = {0.0, m, at};
+    return;
   }
+#pragma unroll
+  for (int i = 0; i < kVU; ++i) m = fmaxf(m, x[i]);
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) m = fmaxf(m, __shfl_xor(m, k, kWave));
+  if ((tid & 63) == 0) sm[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  double z = 0.0;
+  if (m == INFINITY) {                 // (uniform)
+#pragma unroll
+    for (int i = 0; i < kVU; ++i) z += x[i] == m ? 1.0 : 0.0;
+  } else if (m > -INFINITY) {
+    // what lies below the range adds 2^-1020 to a sum of 1 and more
+#pragma unroll
+    for (int i = 0; i < kVU; ++i) z += exp_of(fmax(double(x[i]) - double(m), ex.low), ex);
+  }
+  z = wave_sum_d(z);
+  if ((tid & 63) == 0) sz[wave] = z;
+  __syncthreads();
+  z = (sz[0] + sz[1]) + (sz[2] + sz[3]);
   if (tid == 0) stat[size_t(r) * gridDim.x + c] = {z, m, at};
 }
 
@@ -145,7 +176,7 @@ struct RowStat {
 
 template <int NT>
 struct WalkSmem {
-  double table[32];
+  double table[64];
   RowStat row[2 * kTreeMax];           // the target's rows, then the draft's
   double e[kTreeMax];                  // weight of a node's token at its parent
   int token[kTreeMax];
