@@ -102,6 +102,7 @@ __device__ __forceinline__ TreeNode tree_node(const int* parent, int T, int t_en
   int up = p, gone = p == -2;
 #pragma unroll
   for (int k = 0; k < 6; ++k) {
+    if (!__ballot(up >= 0)) break;     // (a tree of depth d takes the logarithm of d)
     const int at = up < 0 ? lane : up;
     const unsigned long long am = __shfl(m, at, kWave);
     const int ag = __shfl(gone, at, kWave), au = __shfl(up, at, kWave);

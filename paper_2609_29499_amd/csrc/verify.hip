@@ -83,17 +83,33 @@ __device__ __forceinline__ double exp_of(double d, const Exp& e) {
 // The weight of a logit whose row's maximum is m: NaN counts as -inf, a row without anything above -inf has
 // no weight, +inf shares it evenly.
 __device__ __forceinline__ double weight(float l, float m, const Exp& e) {
-  if (m == INFINITY) return l == m ? 1.0 : 0.0;
   const double d = double(l) - double(m);
   const double y = exp_of(fmax(d, e.low), e);
-  return d > e.low ? y : 0.0;
+  const double one = l == m ? 1.0 : 0.0;
+  return m == INFINITY ? one : d > e.low ? y : 0.0;
 }
 
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) v += __shfl_xor(v, k, kWave);
+// v of the lane that CTRL names, 0 where it names none, for the rows in ROWS; by DPP: through the lane crossbar
+// (ds_bpermute) a scan of 64 doubles took 0.4 us
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double dpp_d(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xF, false),
+                          __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ double lane_d(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+// Sums over lanes 0 .. own (row_shr:1, 2, 4, 8 within rows of 16, then row_bcast:15 and :31 between them)
+__device__ __forceinline__ double wave_scan(double v) {
+  v += dpp_d<0x111>(v);
+  v += dpp_d<0x112>(v);
+  v += dpp_d<0x114>(v);
+  v += dpp_d<0x118>(v);
+  v += dpp_d<0x142, 0xA>(v);
+  v += dpp_d<0x143, 0xC>(v);
   return v;
 }
+__device__ __forceinline__ double wave_sum_d(double v) { return lane_d(wave_scan(v), 63); }
 
 // Grid (chunks, rows). rows 0 .. n_target - 1 are the target's, the others the draft's. Also clears
 // the next launch's counters (cnt[B]).
@@ -184,51 +200,55 @@ struct WalkSmem {
   int last, n;
   uint32_t gone[kVChunk / 32];         // tokens of a chunk that were refused
   double part[NT / kWave + 1];
-  int cand[NT / kWave];
+  int cand[NT / kWave], tail[NT / kWave];
   int found, is_last;
   double base;
 };
 
-// Maxima and sums of rows `first` .. `first` + n - 1 from their chunks: four threads per row, eight chunks of each
-// in flight together (they come from other dies' caches: one by one, 32 chunks took 6 us).
-__device__ __forceinline__ void row_stats(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, size_t first, int n, int chunks, RowStat* out) {
-  const int t = threadIdx.x >> 2, q = threadIdx.x & 3;
-  if (t >= n) return;                  // (whole groups of four lanes)
-  const ChunkStat* s = stat + (first + t) * chunks;
-  double z = 0.0;
-  float m = -INFINITY;
-  int at = 0x7fffffff;
-  for (int c0 = 0; c0 < chunks; c0 += 32) {
-    ChunkStat x[8];
+// Maxima and sums from the chunks of rows `first` .. + n - 1 and, behind them, `first2` .. + n2 - 1: four threads per
+// row, eight chunks of each in flight together (they come from other dies' caches: one by one, 32 chunks took 6 us).
+template <int NT>
+__device__ __forceinline__ void row_stats(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, size_t first, int n, size_t first2,
+                                          int n2, int chunks, RowStat* out, RowStat* out2) {
+  const int q = threadIdx.x & 3;
+  for (int t = threadIdx.x >> 2; t < n + n2; t += NT / 4) {          // (whole groups of four lanes)
+    const ChunkStat* s = stat + (t < n ? first + t : first2 + (t - n)) * chunks;
+    double z = 0.0;
+    float m = -INFINITY;
+    int at = 0x7fffffff;
+    for (int c0 = 0; c0 < chunks; c0 += 32) {
+      ChunkStat x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[min(c0 + 4 * i + q, chunks - 1)];
-    float top = m;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (x[i].m > top) {
-        top = x[i].m;
-        at = x[i].at;
-      }
-#pragma unroll
-    for (int k = 1; k < 4; k <<= 1) {
-      const float om = __shfl_xor(top, k, kWave);
-      const int oa = __shfl_xor(at, k, kWave);
-      if (om > top || (om == top && oa < at)) {
-        top = om;
-        at = oa;
-      }
-    }
-    if (a.inv_temp > 0.0) {
-      if (c0 > 0) z *= weight(m, top, ex);
+      for (int i = 0; i < 8; ++i) x[i] = s[min(c0 + 4 * i + q, chunks - 1)];
+      float top = m;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (c0 + 4 * i + q < chunks) z += x[i].z * weight(x[i].m, top, ex);
+        if (x[i].m > top) {
+          top = x[i].m;
+          at = x[i].at;
+        }
+      auto other = [&](float om, int oa) {
+        if (om > top || (om == top && oa < at)) {
+          top = om;
+          at = oa;
+        }
+      };
+      other(dpp<kQuadXor1>(top), __builtin_amdgcn_mov_dpp(at, kQuadXor1, 0xF, 0xF, true));
+      other(dpp<kQuadXor2>(top), __builtin_amdgcn_mov_dpp(at, kQuadXor2, 0xF, 0xF, true));
+      if (a.inv_temp > 0.0) {
+        if (c0 > 0) z *= weight(m, top, ex);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const double w = x[i].z * weight(x[i].m, top, ex);
+          z += c0 + 4 * i + q < chunks ? w : 0.0;
+        }
+      }
+      m = top;
     }
-    m = top;
+    z += dpp_d<kQuadXor1>(z);
+    z += dpp_d<kQuadXor2>(z);
+    if (q == 0) (t < n ? out[t] : out2[t - n]) = {z, m, at};
   }
-  z += __shfl_xor(z, 1, kWave);
-  z += __shfl_xor(z, 2, kWave);
-  if (q == 0) out[t] = {z, m, at};
 }
 
 // The tree's walk by the first wave, a node per lane; path and n are written when `out` is set.
@@ -255,8 +275,8 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
     }
   }
   __syncthreads();                     // the table
-  row_stats(a, ex, stat, size_t(b) * T, T, chunks, sm.row);
-  if (draft) row_stats(a, ex, stat, size_t(a.B) * T + size_t(b) * (T - 1), T - 1, chunks, sm.row + kTreeMax);
+  row_stats<NT>(a, ex, stat, size_t(b) * T, T, size_t(a.B) * T + size_t(b) * (T - 1), draft ? T - 1 : 0, chunks, sm.row,
+                sm.row + kTreeMax);
   __syncthreads();
   if (tid < kWave) {
     const RowStat rs = sm.row[max(up, 0)];
@@ -283,10 +303,7 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
       }
       if (again) e = 0.0;
       double before = 0.0;
-      for (int j = 0; j < T; ++j) {
-        const double ej = __shfl(e, j, kWave);
-        if ((older >> j) & 1) before += ej;
-      }
+      for (int j = 0; j < T; ++j) before += (older >> j) & 1 ? lane_d(e, j) : 0.0;
       good = word && u * ((greedy ? 1.0 : rs.z) - before) < e;
     }
     sm.e[t] = e;
@@ -321,72 +338,70 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
 }
 
 // The token of a chunk whose cumulative weight first exceeds `target`, the weights before it being
-// `base`; also the chunk's last token with a weight. w(k): weight of token k. Thread t holds tokens
-// kVU t .. + kVU - 1 of the chunk, so sums run in token order. found: -1 none, else the token;
-// tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
-template <int NT, class W>
-__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem<NT>& sm, W&& w, int* found, int* tail) {
+// `base`; also the chunk's last token with a weight. w(k, read(k)): weight of token k; the reads of all of a thread's
+// tokens are in flight together. Thread t holds tokens kVU t .. + kVU - 1 of the chunk, so sums run in token
+// order. found: -1 none, else the token; tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
+template <int NT, class R, class W>
+__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem<NT>& sm, R&& read, W&& w,
+                                             int* found, int* tail) {
   constexpr int U = kVChunk / NT, NWV = NT / kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int k0 = c * kVChunk + tid * U;
+  decltype(read(0)) x[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) x[i] = read(min(k0 + i, a.V - 1));
   double v[U], sum = 0.0;
   int end = -1;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    v[i] = k0 + i < a.V ? w(k0 + i) : 0.0;
+    const double y = w(k0 + i, x[i]);
+    v[i] = k0 + i < a.V ? y : 0.0;
     sum += v[i];
     if (v[i] > 0.0) end = k0 + i;
   }
-  double inc = sum;
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) {
-    const double o = __shfl_up(inc, k, kWave);
-    if (lane >= k) inc += o;
-  }
-  __syncthreads();
+  const double inc = wave_scan(sum);
   if (lane == 63) sm.part[wave] = inc;
   __syncthreads();
   double cum = base + (inc - sum), total = base;
 #pragma unroll
   for (int j = 0; j < NWV; ++j) {
-    if (j < wave) cum += sm.part[j];
-    total += sm.part[j];
+    const double pj = sm.part[j];
+    cum += j < wave ? pj : 0.0;
+    total += pj;
   }
-  int hit = 0x7fffffff;
+  int hit = -1;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     cum += v[i];
-    if (v[i] > 0.0 && cum > target && hit == 0x7fffffff) hit = k0 + i;
+    if (v[i] > 0.0 && cum > target && hit < 0) hit = k0 + i;
   }
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) {
-    hit = min(hit, __shfl_xor(hit, k, kWave));
-    end = max(end, __shfl_xor(end, k, kWave));
-  }
-  __syncthreads();
+  // lanes run in token order: the first with a hit, the last with an end
+  const unsigned long long hits = __ballot(hit >= 0), ends = __ballot(end >= 0);
+  const int h = hits ? __builtin_amdgcn_readlane(hit, __ffsll((long long)hits) - 1) : -1;
+  const int l = ends ? __builtin_amdgcn_readlane(end, 63 - __clzll(ends)) : -1;
   if (lane == 0) {
-    sm.cand[wave] = hit;
-    sm.gone[wave] = uint32_t(end);     // (the mask has been read)
+    sm.cand[wave] = h;
+    sm.tail[wave] = l;
   }
   __syncthreads();
+  int f = -1, g = -1;
 #pragma unroll
   for (int j = 0; j < NWV; ++j) {
-    hit = min(hit, sm.cand[j]);
-    end = max(end, int(sm.gone[j]));
+    f = f < 0 ? sm.cand[j] : f;
+    g = max(g, sm.tail[j]);
   }
-  __syncthreads();
-  *found = hit == 0x7fffffff ? -1 : hit;
-  *tail = end;
+  *found = f;
+  *tail = g;
   return total;
 }
 
-// The chunk's refused tokens as a bit mask (none: empty)
+// The chunk's refused tokens as a bit mask
 template <int NT>
-__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<NT>& sm, bool any) {
+__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<NT>& sm) {
   for (int i = threadIdx.x; i < kVChunk / 32; i += NT) sm.gone[i] = 0;
   __syncthreads();
   const int t = threadIdx.x;
-  if (any && t < a.T && ((sm.children >> t) & 1)) {
+  if (t < a.T && ((sm.children >> t) & 1)) {
     const int k = sm.token[t] - c * kVChunk;
     if (k >= 0 && k < kVChunk && sm.token[t] < a.V) atomicOr(&sm.gone[k >> 5], 1u << (k & 31));
   }
@@ -394,34 +409,31 @@ __device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<N
 }
 
 // Takes the last token of sequence b by the whole workgroup: chunk_weight(c) is the weight of chunk c
-// (any thread may ask), w as for scan_chunk after mark_gone.
-template <int NT, class CW, class W>
-__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem<NT>& sm, bool remove, CW&& chunk_weight, W&& w) {
+// (any thread may ask), read and w as for scan_chunk after mark_gone (remove: w asks for its mask).
+template <int NT, class CW, class R, class W>
+__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem<NT>& sm, bool remove, CW&& chunk_weight, R&& read, W&& w) {
   const int tid = threadIdx.x;
   // the chunk in which the cumulative weight passes the target: by the first wave, chunk sums in order
   if (tid < kWave) {
+    const double u = double(a.u[size_t(b) * a.T]);
     const double w0 = tid < chunks ? chunk_weight(tid) : 0.0;        // (asked for once where there are up to 64)
-    double total = wave_sum_d(w0);
+    const double inc0 = wave_scan(w0);
+    double total = lane_d(inc0, 63);
     for (int c0 = kWave; c0 < chunks; c0 += kWave) total += wave_sum_d(c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0);
-    const double target = double(a.u[size_t(b) * a.T]) * total;
+    const double target = u * total;
     double base = 0.0;
     int at = -1;
     double before = 0.0;
     for (int c0 = 0; c0 < chunks && at < 0; c0 += kWave) {
       const double mine = c0 == 0 ? w0 : c0 + tid < chunks ? chunk_weight(c0 + tid) : 0.0;
-      double inc = mine;
-#pragma unroll
-      for (int k = 1; k < kWave; k <<= 1) {
-        const double o = __shfl_up(inc, k, kWave);
-        if (tid >= k) inc += o;
-      }
+      const double inc = c0 == 0 ? inc0 : wave_scan(mine);
       const unsigned long long over = __ballot(base + inc > target && mine > 0.0);
       if (over) {
         const int l = __ffsll((long long)over) - 1;
         at = c0 + l;
-        before = base + __shfl(inc - mine, l, kWave);
+        before = base + lane_d(inc - mine, l);
       }
-      base += __shfl(inc, 63, kWave);
+      base += lane_d(inc, 63);
     }
     if (tid == 0) {
       sm.found = total > 0.0 ? max(at, 0) : -1;
@@ -433,20 +445,19 @@ __device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, Walk
   const int c_at = sm.found;
   double base = sm.base;
   const double target = sm.part[NT / kWave];
-  __syncthreads();
   if (c_at < 0) return -1;             // nothing has a weight
   int best = -1;                       // the last token with a weight, should rounding leave the target unreached
   for (int c = c_at; c < chunks; ++c) {
     int found, tail;
-    mark_gone(a, c, sm, remove);
-    base = scan_chunk(a, c, base, target, sm, w, &found, &tail);
+    if (remove) mark_gone(a, c, sm);
+    base = scan_chunk(a, c, base, target, sm, read, w, &found, &tail);
     if (found >= 0) return found;
     if (tail >= 0) best = tail;
   }
   for (int c = c_at - 1; c >= 0 && best < 0; --c) {
     int found, tail;
-    mark_gone(a, c, sm, remove);
-    scan_chunk(a, c, 0.0, INFINITY, sm, w, &found, &tail);
+    if (remove) mark_gone(a, c, sm);
+    scan_chunk(a, c, 0.0, INFINITY, sm, read, w, &found, &tail);
     best = tail;
   }
   return best;
@@ -473,7 +484,8 @@ __global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const Chu
   const ChunkStat* st = stat + r * chunks;
   const bool kids = sm.children != 0;
   auto plain_sum = [&](int c) { return st[c].z * weight(st[c].m, rs.m, ex); };
-  auto plain = [&](int k) { return weight(row[k], rs.m, ex); };
+  auto read = [&](int k) { return row[k]; };
+  auto plain = [&](int, float l) { return weight(l, rs.m, ex); };
   if (!a.draft) {
     // e without the children's tokens: what they weigh is taken off their chunks
     auto left_sum = [&](int c) {
@@ -484,29 +496,41 @@ __global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const Chu
       }
       return fmax(z, 0.0);
     };
-    auto left = [&](int k) {
+    auto left = [&](int k, float l) {
       const int i = k % kVChunk;
-      return ((sm.gone[i >> 5] >> (i & 31)) & 1) ? 0.0 : plain(k);
+      const double y = plain(k, l);
+      return kids && ((sm.gone[i >> 5] >> (i & 31)) & 1) ? 0.0 : y;
     };
-    int x = take(a, b, chunks, sm, kids, left_sum, left);
-    if (x < 0) x = take(a, b, chunks, sm, false, plain_sum, plain);
+    int x = take(a, b, chunks, sm, kids, left_sum, read, left);
+    if (x < 0 && kids) {               // (uniform)
+      __syncthreads();
+      x = take(a, b, chunks, sm, false, plain_sum, read, plain);
+    }
     if (tid == 0) *out = x;
     return;
   }
   // max(p - q, 0) at a chain's refused token, p behind its end
   const RowStat ds = kids ? sm.row[kTreeMax + last] : RowStat{0.0, 0.0f, 0};
-  const float* drow = a.draft + (size_t(b) * (T - 1) + (kids ? last : 0)) * a.V;
+  const float* drow = kids ? a.draft + (size_t(b) * (T - 1) + last) * a.V : row;
   const double pz = rs.z > 0.0 ? 1.0 / rs.z : 0.0, qz = ds.z > 0.0 ? 1.0 / ds.z : 0.0;
-  auto rest = [&](int k) {
-    const double p = weight(row[k], rs.m, ex) * pz;
-    return kids ? fmax(p - weight(drow[k], ds.m, ex) * qz, 0.0) : p;
+  struct Two {
+    float l, d;
+  };
+  auto read2 = [&](int k) { return Two{row[k], drow[k]}; };
+  auto rest = [&](int, Two x) {
+    const double p = weight(x.l, rs.m, ex) * pz;
+    return kids ? fmax(p - weight(x.d, ds.m, ex) * qz, 0.0) : p;
   };
   const int c = blockIdx.x;
+  constexpr int U = kVChunk / NT;
+  Two in[U];                           // (all in flight together)
+#pragma unroll
+  for (int i = 0; i < U; ++i) in[i] = read2(min(c * kVChunk + i * NT + tid, a.V - 1));
   double z = 0.0;
 #pragma unroll
-  for (int i = 0; i < kVChunk / NT; ++i) {
-    const int k = c * kVChunk + i * NT + tid;
-    if (k < a.V) z += rest(k);
+  for (int i = 0; i < U; ++i) {
+    const double y = rest(0, in[i]);
+    z += c * kVChunk + i * NT + tid < a.V ? y : 0.0;
   }
   z = wave_sum_d(z);
   if ((tid & 63) == 0) sm.part[tid >> 6] = z;
@@ -522,8 +546,11 @@ __global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const Chu
   __syncthreads();
   if (!sm.is_last) return;
   auto rest_sum = [&](int j) { return __builtin_bit_cast(double, buf_load8_device(rp, uint32_t(j) * 8u)); };
-  int x = take(a, b, chunks, sm, false, rest_sum, rest);
-  if (x < 0) x = take(a, b, chunks, sm, false, plain_sum, plain);
+  int x = take(a, b, chunks, sm, false, rest_sum, read2, rest);
+  if (x < 0) {                         // (uniform)
+    __syncthreads();
+    x = take(a, b, chunks, sm, false, plain_sum, read, plain);
+  }
   if (tid == 0) *out = x;
 }
 
