@@ -56,25 +56,32 @@ struct Deal {
   int chunk;                           // steps per chunk
   int total;                           // chunks of all sequences
   int mine[4], before[4];              // of the lane's sequences: chunks, and chunks before them
+  int len[4];                          // and their lengths, -1: passed over
 };
-__device__ __forceinline__ int steps_of(const TreeAttnArgs& a, int b) {
-  const int L = b < a.c.batch ? seq_len(a.c.len, b, a.c.S) : -2;
-  if (L == -2) return 0;               // no such sequence
-  return L < 0 ? 1 : (min(L + a.T, a.c.S) + kStep - 1) / kStep;
+// Sums over lanes 0 .. own (row_shr:1, 2, 4, 8 within rows of 16, row_bcast:15 and :31 between them)
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
 }
 __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, int lane) {
   Deal d;
   int n[4], sum = 0;
 #pragma unroll
+  for (int i = 0; i < 4; ++i) d.len[i] = a.c.len[min(4 * lane + i, a.c.batch - 1)];    // (in flight together)
+#pragma unroll
   for (int i = 0; i < 4; ++i) {
-    n[i] = steps_of(a, 4 * lane + i);
+    const int L = d.len[i] = d.len[i] < 0 || d.len[i] > a.c.S ? -1 : d.len[i];
+    n[i] = 4 * lane + i >= a.c.batch ? 0 : L < 0 ? 1 : (min(L + a.T, a.c.S) + kStep - 1) / kStep;
     sum += n[i];
   }
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) sum += __shfl_xor(sum, k, kWave);
+  sum = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
   // (said to be the same in all lanes wherever it is: a buffer descriptor or a branch that the compiler takes for
   // divergent becomes a loop over lanes, around every load)
-  sum = __builtin_amdgcn_readfirstlane(sum);
   const int units = a.slots * y.rb, chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
   d.chunk = chunk;
   const int quota = y.target / units;
@@ -101,12 +108,7 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, 
     d.before[i] = own;
     own += d.mine[i];
   }
-  int inc = own;
-#pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) {
-    const int o = __shfl_up(inc, k, kWave);
-    if (lane >= k) inc += o;
-  }
+  const int inc = wave_scan(own);
 #pragma unroll
   for (int i = 0; i < 4; ++i) d.before[i] += inc - own;
   d.total = __builtin_amdgcn_readlane(inc, kWave - 1);
@@ -257,7 +259,7 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   p.R = a.T * p.group;
   if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
   p.unit = size_t(p.b) * a.c.n_kv + a.kv_map[p.g];
-  p.L = __builtin_amdgcn_readfirstlane(seq_len(a.c.len, p.b, a.c.S));
+  p.L = __builtin_amdgcn_readlane(sub == 0 ? d.len[0] : sub == 1 ? d.len[1] : sub == 2 ? d.len[2] : d.len[3], owner);
   p.Lr = max(p.L, 0);
   p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
   const int steps = (p.end + kStep - 1) / kStep;

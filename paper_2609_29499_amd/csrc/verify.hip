@@ -26,6 +26,10 @@ namespace {
 constexpr int kVChunk = 4096;          // logits per workgroup of the first launch
 constexpr int kVU = kVChunk / kBlock;  // logits per thread
 
+// threads of the second launch: with 256, chains of 9 x 8 take 17.1 us in it instead of 14.0 and 32 nodes x 16 14.8
+// instead of 12.0; with 1024 both as long as with 512
+constexpr int kWalk = 512;
+
 struct ChunkStat {
   double z;                            // sum of exp((l - m) / temperature) over the chunk
   float m;                             // its maximum
@@ -190,28 +194,27 @@ struct RowStat {
   int at;
 };
 
-template <int NT>
 struct WalkSmem {
   double table[64];
   RowStat row[2 * kTreeMax];           // the target's rows, then the draft's
   double e[kTreeMax];                  // weight of a node's token at its parent
   int token[kTreeMax];
+  unsigned long long kids[kTreeMax];   // a node's children
   unsigned long long children;         // of the last node
   int last, n;
   uint32_t gone[kVChunk / 32];         // tokens of a chunk that were refused
-  double part[NT / kWave + 1];
-  int cand[NT / kWave], tail[NT / kWave];
+  double part[kWalk / kWave + 1];
+  int cand[kWalk / kWave], tail[kWalk / kWave];
   int found, is_last;
   double base;
 };
 
 // Maxima and sums from the chunks of rows `first` .. + n - 1 and, behind them, `first2` .. + n2 - 1: four threads per
 // row, eight chunks of each in flight together (they come from other dies' caches: one by one, 32 chunks took 6 us).
-template <int NT>
 __device__ __forceinline__ void row_stats(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, size_t first, int n, size_t first2,
                                           int n2, int chunks, RowStat* out, RowStat* out2) {
   const int q = threadIdx.x & 3;
-  for (int t = threadIdx.x >> 2; t < n + n2; t += NT / 4) {          // (whole groups of four lanes)
+  for (int t = threadIdx.x >> 2; t < n + n2; t += kWalk / 4) {          // (whole groups of four lanes)
     const ChunkStat* s = stat + (t < n ? first + t : first2 + (t - n)) * chunks;
     double z = 0.0;
     float m = -INFINITY;
@@ -251,9 +254,11 @@ __device__ __forceinline__ void row_stats(const VerifyArgs& a, const Exp& ex, co
   }
 }
 
+// Nothing moves across: what a wave's lanes wrote to LDS before is there for its other lanes behind (LDS serves a wave in order)
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // The tree's walk by the first wave, a node per lane; path and n are written when `out` is set.
-template <int NT>
-__device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, int b, int chunks, WalkSmem<NT>& sm, bool out) {
+__device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const ChunkStat* stat, int b, int chunks, WalkSmem& sm, bool out) {
   const int tid = threadIdx.x, T = a.T, t = tid;
   const bool greedy = a.inv_temp == 0.0, draft = a.draft && !greedy;
   // the tree and its tokens' logits are asked for first, so that they come with the chunks' records
@@ -263,6 +268,7 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
   double u = 0.0;
   float lx = 0.0f, dx = 0.0f;
   if (tid < kWave) {
+    sm.kids[t] = 0;
     nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, T, t);
     node = nd.anc != 0 && nd.parent >= 0;
     up = node ? nd.parent : -1;
@@ -273,9 +279,12 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
       lx = a.logits[(size_t(b) * T + up) * a.V + x];
       if (draft) dx = a.draft[(size_t(b) * (T - 1) + up) * a.V + x];
     }
+    sm.token[t] = x;
+    wave_order();
+    if (node && !draft) atomicOr(&sm.kids[up], 1ull << t);
   }
   __syncthreads();                     // the table
-  row_stats<NT>(a, ex, stat, size_t(b) * T, T, size_t(a.B) * T + size_t(b) * (T - 1), draft ? T - 1 : 0, chunks, sm.row,
+  row_stats(a, ex, stat, size_t(b) * T, T, size_t(a.B) * T + size_t(b) * (T - 1), draft ? T - 1 : 0, chunks, sm.row,
                 sm.row + kTreeMax);
   __syncthreads();
   if (tid < kWave) {
@@ -293,21 +302,17 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
     if (draft) {
       good = word && rs.z > 0.0 && u * q < e / rs.z;
     } else {
+      // (lists of children in LDS: two loops over all nodes took 4 us for 32)
+      if (node) older = sm.kids[up] & ((1ull << t) - 1);
       bool again = false;              // the token was tried before
-      for (int j = 0; j < T; ++j) {
-        const int pj = __builtin_amdgcn_readlane(up, j), xj = __builtin_amdgcn_readlane(x, j);
-        if (node && j < t && pj == up) {
-          older |= 1ull << j;
-          again |= xj == x;
-        }
-      }
+      for (unsigned long long k = older; k; k &= k - 1) again |= sm.token[__ffsll((long long)k) - 1] == x;
       if (again) e = 0.0;
+      sm.e[t] = e;
+      wave_order();
       double before = 0.0;
-      for (int j = 0; j < T; ++j) before += (older >> j) & 1 ? lane_d(e, j) : 0.0;
+      for (unsigned long long k = older; k; k &= k - 1) before += sm.e[__ffsll((long long)k) - 1];
       good = word && u * ((greedy ? 1.0 : rs.z) - before) < e;
     }
-    sm.e[t] = e;
-    sm.token[t] = x;
     const unsigned long long goods = __ballot(good);
     const bool chosen = good && !(older & goods);
     const unsigned long long taken = __ballot(chosen) | 1ull;
@@ -315,7 +320,7 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
     const unsigned long long path = __ballot(on);
     // node 0 absent (its parent is not -1): nothing is on the path and the last node is 0
     const int n = max(1, __popcll(path)), last = path ? 63 - __clzll(path) : 0;
-    const unsigned long long kids = __ballot(node && up == last);
+    const unsigned long long kids = draft ? __ballot(node && up == last) : sm.kids[last];
     if (t == 0) {
       sm.n = n;
       sm.last = last;
@@ -339,49 +344,46 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
 
 // The token of a chunk whose cumulative weight first exceeds `target`, the weights before it being
 // `base`; also the chunk's last token with a weight. w(k, read(k)): weight of token k; the reads of all of a thread's
-// tokens are in flight together. Thread t holds tokens kVU t .. + kVU - 1 of the chunk, so sums run in token
-// order. found: -1 none, else the token; tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
-template <int NT, class R, class W>
-__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem<NT>& sm, R&& read, W&& w,
+// tokens are in flight together. A wave holds consecutive groups of 64 tokens (16 consecutive tokens per thread:
+// 15000 cycles for two rows of logits, for their strided loads), so sums run in token order. found: -1 none, else the token; tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
+template <class R, class W>
+__device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem& sm, R&& read, W&& w,
                                              int* found, int* tail) {
-  constexpr int U = kVChunk / NT, NWV = NT / kWave;
+  constexpr int U = kVChunk / kWalk, NWV = kWalk / kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int k0 = c * kVChunk + tid * U;
+  const int k0 = c * kVChunk + wave * (kWave * U) + lane;
   decltype(read(0)) x[U];
 #pragma unroll
-  for (int i = 0; i < U; ++i) x[i] = read(min(k0 + i, a.V - 1));
-  double v[U], sum = 0.0;
-  int end = -1;
+  for (int i = 0; i < U; ++i) x[i] = read(min(k0 + kWave * i, a.V - 1));
+  double v[U], inc[U], sum = 0.0;      // weights, their sums over the group up to the lane
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const double y = w(k0 + i, x[i]);
-    v[i] = k0 + i < a.V ? y : 0.0;
-    sum += v[i];
-    if (v[i] > 0.0) end = k0 + i;
+    const double y = w(k0 + kWave * i, x[i]);
+    v[i] = k0 + kWave * i < a.V ? y : 0.0;
+    inc[i] = wave_scan(v[i]);
+    sum += lane_d(inc[i], 63);
   }
-  const double inc = wave_scan(sum);
-  if (lane == 63) sm.part[wave] = inc;
+  if (lane == 0) sm.part[wave] = sum;
   __syncthreads();
-  double cum = base + (inc - sum), total = base;
+  double cum = base, total = base;
 #pragma unroll
   for (int j = 0; j < NWV; ++j) {
     const double pj = sm.part[j];
     cum += j < wave ? pj : 0.0;
     total += pj;
   }
-  int hit = -1;
+  int hit = -1, end = -1;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    cum += v[i];
-    if (v[i] > 0.0 && cum > target && hit < 0) hit = k0 + i;
+    const unsigned long long some = __ballot(v[i] > 0.0), over = __ballot(v[i] > 0.0 && cum + inc[i] > target);
+    const int g0 = c * kVChunk + wave * (kWave * U) + kWave * i;
+    if (over && hit < 0) hit = g0 + __ffsll((long long)over) - 1;
+    if (some) end = g0 + 63 - __clzll(some);
+    cum += lane_d(inc[i], 63);
   }
-  // lanes run in token order: the first with a hit, the last with an end
-  const unsigned long long hits = __ballot(hit >= 0), ends = __ballot(end >= 0);
-  const int h = hits ? __builtin_amdgcn_readlane(hit, __ffsll((long long)hits) - 1) : -1;
-  const int l = ends ? __builtin_amdgcn_readlane(end, 63 - __clzll(ends)) : -1;
   if (lane == 0) {
-    sm.cand[wave] = h;
-    sm.tail[wave] = l;
+    sm.cand[wave] = hit;
+    sm.tail[wave] = end;
   }
   __syncthreads();
   int f = -1, g = -1;
@@ -396,9 +398,8 @@ __device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double 
 }
 
 // The chunk's refused tokens as a bit mask
-template <int NT>
-__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<NT>& sm) {
-  for (int i = threadIdx.x; i < kVChunk / 32; i += NT) sm.gone[i] = 0;
+__device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem& sm) {
+  for (int i = threadIdx.x; i < kVChunk / 32; i += kWalk) sm.gone[i] = 0;
   __syncthreads();
   const int t = threadIdx.x;
   if (t < a.T && ((sm.children >> t) & 1)) {
@@ -410,8 +411,8 @@ __device__ __forceinline__ void mark_gone(const VerifyArgs& a, int c, WalkSmem<N
 
 // Takes the last token of sequence b by the whole workgroup: chunk_weight(c) is the weight of chunk c
 // (any thread may ask), read and w as for scan_chunk after mark_gone (remove: w asks for its mask).
-template <int NT, class CW, class R, class W>
-__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem<NT>& sm, bool remove, CW&& chunk_weight, R&& read, W&& w) {
+template <class CW, class R, class W>
+__device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, WalkSmem& sm, bool remove, CW&& chunk_weight, R&& read, W&& w) {
   const int tid = threadIdx.x;
   // the chunk in which the cumulative weight passes the target: by the first wave, chunk sums in order
   if (tid < kWave) {
@@ -438,13 +439,13 @@ __device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, Walk
     if (tid == 0) {
       sm.found = total > 0.0 ? max(at, 0) : -1;
       sm.base = before;
-      sm.part[NT / kWave] = target;
+      sm.part[kWalk / kWave] = target;
     }
   }
   __syncthreads();
   const int c_at = sm.found;
   double base = sm.base;
-  const double target = sm.part[NT / kWave];
+  const double target = sm.part[kWalk / kWave];
   if (c_at < 0) return -1;             // nothing has a weight
   int best = -1;                       // the last token with a weight, should rounding leave the target unreached
   for (int c = c_at; c < chunks; ++c) {
@@ -463,11 +464,9 @@ __device__ __forceinline__ int take(const VerifyArgs& a, int b, int chunks, Walk
   return best;
 }
 
-// Grid (1, or chunks with draft logits, B): see the head of the file. NT threads: 1024 where one workgroup serves a
-// sequence (four logits of the chunk per thread instead of 16 shorten it), 256 over the chunks.
-template <int NT>
-__global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const ChunkStat* stat, double* sums, int* cnt, int chunks) {
-  __shared__ WalkSmem<NT> sm;
+// Grid (1, or chunks with draft logits, B): see the head of the file.
+__global__ __launch_bounds__(kWalk) void verify_walk_kernel(VerifyArgs a, const ChunkStat* stat, double* sums, int* cnt, int chunks) {
+  __shared__ WalkSmem sm;
   const int tid = threadIdx.x, b = blockIdx.y, T = a.T;
   const bool greedy = a.inv_temp == 0.0;
   const Exp ex = exp_table(sm.table, a.inv_temp);
@@ -522,15 +521,15 @@ __global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const Chu
     return kids ? fmax(p - weight(x.d, ds.m, ex) * qz, 0.0) : p;
   };
   const int c = blockIdx.x;
-  constexpr int U = kVChunk / NT;
+  constexpr int U = kVChunk / kWalk;
   Two in[U];                           // (all in flight together)
 #pragma unroll
-  for (int i = 0; i < U; ++i) in[i] = read2(min(c * kVChunk + i * NT + tid, a.V - 1));
+  for (int i = 0; i < U; ++i) in[i] = read2(min(c * kVChunk + i * kWalk + tid, a.V - 1));
   double z = 0.0;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const double y = rest(0, in[i]);
-    z += c * kVChunk + i * NT + tid < a.V ? y : 0.0;
+    z += c * kVChunk + i * kWalk + tid < a.V ? y : 0.0;
   }
   z = wave_sum_d(z);
   if ((tid & 63) == 0) sm.part[tid >> 6] = z;
@@ -538,7 +537,7 @@ __global__ __launch_bounds__(NT) void verify_walk_kernel(VerifyArgs a, const Chu
   const __amdgpu_buffer_rsrc_t rp = make_rsrc(sums + size_t(b) * chunks, uint32_t(chunks) * 8u);
   if (tid == 0) {
     z = 0.0;
-    for (int j = 0; j < NT / kWave; ++j) z += sm.part[j];
+    for (int j = 0; j < kWalk / kWave; ++j) z += sm.part[j];
     buf_store8_device(__builtin_bit_cast(int2, z), rp, uint32_t(c) * 8u);
     __builtin_amdgcn_s_waitcnt(0);                      // the sum is at the coherence point
     sm.is_last = __hip_atomic_fetch_add(cnt + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == chunks - 1;
@@ -578,8 +577,7 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   int* cnt = reinterpret_cast<int*>(ws);
-  if (draft) hipLaunchKernelGGL((verify_walk_kernel<256>), dim3(chunks, a.B), dim3(256), 0, s, v, stat, sums, cnt, chunks);
-  else hipLaunchKernelGGL((verify_walk_kernel<1024>), dim3(1, a.B), dim3(1024), 0, s, v, stat, sums, cnt, chunks);
+  hipLaunchKernelGGL(verify_walk_kernel, dim3(draft ? chunks : 1, a.B), dim3(kWalk), 0, s, v, stat, sums, cnt, chunks);
   return hipGetLastError();
 }
 
