@@ -45,19 +45,32 @@ constexpr int kMinSteps = 4;           // steps of a chunk at least: one per wav
 constexpr float kSlack = 8.0f;         // powers of two a score may pass the running maximum by
 
 // ---- which rows a workgroup serves
-// Sequence b has steps(b) = ceil((L + T) / 32) steps and is cut in chunks of `chunk` steps. A wave holds four
-// sequences per lane.
+// Sequence b has steps(b) = ceil((L + T) / 32) steps. Two ways to deal them to workgroups, per cache head and block of
+// query rows:
+//   * span (few slots per sequence; the wide kernel): the sequences' steps in a row, each preceded by kSetup
+//     steps for what a piece costs before its first row, are cut into `quota` equal slots; a workgroup takes its slot's
+//     pieces one after the other. (In equal chunks of each sequence's own, eight sequences of 4608 .. 8192 rows in 16
+//     slots left the fullest workgroup with 132 steps where the mean was 101.)
+//   * otherwise each is cut in chunks of `chunk` steps, a workgroup for each.
+// A piece or chunk of a sequence that has several leaves a record. A wave holds four sequences per lane.
+//
 // How a call is launched: query rows in rb blocks of `rows` (16 mt, wide: 64 mt), `target` workgroups aimed at, at most `most`
-// chunks per sequence (what the workspace has room for), grid workgroups.
+// chunks per sequence (what the workspace has room for), quota: slots per unit, room: records (and workgroups of the second way)
+constexpr int kSetup = 4;
 struct TreeShape {
-  int wide, mt, rows, rb, target, most, grid;
+  int wide, mt, rows, rb, target, most, quota, span, room, grid;
 };
 struct Deal {
-  int chunk;                           // steps per chunk
-  int total;                           // chunks of all sequences
-  int mine[4], before[4];              // of the lane's sequences: chunks, and chunks before them
+  int chunk;                           // steps per chunk or slot
+  int total;                           // chunks of all sequences, or slots
+  int mine[4], before[4];              // of the lane's sequences: chunks or pieces, and those of the sequences before them
   int len[4];                          // and their lengths, -1: passed over
+  int at[4], steps[4];                 // span: place of the first step in the row; steps
 };
+// v[sub] of lane `owner`
+__device__ __forceinline__ int pick(const int (&v)[4], int owner, int sub) {
+  return __builtin_amdgcn_readlane(sub == 0 ? v[0] : sub == 1 ? v[1] : sub == 2 ? v[2] : v[3], owner);
+}
 // Sums over lanes 0 .. own (row_shr:1, 2, 4, 8 within rows of 16, row_bcast:15 and :31 between them)
 __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
@@ -68,53 +81,66 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
   return v;
 }
+template <bool SPAN>
 __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, int lane) {
   Deal d;
-  int n[4], sum = 0;
+  int n[4], cost[4], sum_own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) d.len[i] = a.c.len[min(4 * lane + i, a.c.batch - 1)];    // (in flight together)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int L = d.len[i] = d.len[i] < 0 || d.len[i] > a.c.S ? -1 : d.len[i];
     n[i] = 4 * lane + i >= a.c.batch ? 0 : L < 0 ? 1 : (min(L + a.T, a.c.S) + kStep - 1) / kStep;
-    sum += n[i];
+    cost[i] = SPAN && y.span && n[i] > 0 ? (n[i] + 3) / 4 * 4 + kSetup : n[i];
+    sum_own += cost[i];
   }
-  sum = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
+  const int inc = wave_scan(sum_own), sum = __builtin_amdgcn_readlane(inc, kWave - 1);
   // (said to be the same in all lanes wherever it is: a buffer descriptor or a branch that the compiler takes for
   // divergent becomes a loop over lanes, around every load)
-  const int units = a.slots * y.rb, chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
-  d.chunk = chunk;
-  const int quota = y.target / units;
-  if (a.c.batch > 1 && 2 * a.c.batch <= quota) {
-    // Sequences are rounded up to whole chunks: the shortest chunk that keeps all workgroups within the target is
-    // looked for, a candidate per lane (workgroups beyond it would make a second round: the 64-node case
-    // 298 us with 1.5 rounds)
-    const int mine = chunk + lane * max(4, chunk / 256 * 4);
-    const float inv = 1.0f / float(mine);
-    int count = 0;
-    for (int b = 0; b < a.c.batch; ++b) {
-      const int i = b & 3, nb = __builtin_amdgcn_readlane(i == 0 ? n[0] : i == 1 ? n[1] : i == 2 ? n[2] : n[3], b >> 2);
-      int q = int(float(nb) * inv);                    // within one of the quotient; rounded up below
-      q += q * mine < nb ? 1 : 0;
-      count += q;
+  d.total = y.quota;
+  if (SPAN && y.span) {
+    d.chunk = max(kMinSteps, ((sum + y.quota - 1) / y.quota + 3) / 4 * 4);
+    int at = inc - sum_own;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      d.at[i] = at + kSetup;
+      d.steps[i] = n[i];
+      d.mine[i] = cost[i] == 0 ? 0 : (at + cost[i] - 1) / d.chunk - d.at[i] / d.chunk + 1;
+      at += cost[i];
     }
-    const unsigned long long fits = __ballot(count <= quota);
-    d.chunk = __builtin_amdgcn_readlane(mine, fits ? __ffsll((long long)fits) - 1 : kWave - 1);
+  } else {
+    const int units = a.slots * y.rb;
+    d.chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
+    if (a.c.batch > 1 && 2 * a.c.batch <= y.quota) {
+      // Sequences are rounded up to whole chunks: the shortest chunk that keeps all workgroups within the target is
+      // looked for, a candidate per lane (workgroups beyond it would make a second round)
+      const int mine = d.chunk + lane * max(4, d.chunk / 256 * 4);
+      const float inv = 1.0f / float(mine);
+      int count = 0;
+      for (int b = 0; b < a.c.batch; ++b) {
+        const int nb = pick(n, b >> 2, b & 3);
+        int q = int(float(nb) * inv);                  // within one of the quotient; rounded up below
+        q += q * mine < nb ? 1 : 0;
+        count += q;
+      }
+      const unsigned long long fits = __ballot(count <= y.quota);
+      d.chunk = __builtin_amdgcn_readlane(mine, fits ? __ffsll((long long)fits) - 1 : kWave - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d.mine[i] = min((n[i] + d.chunk - 1) / d.chunk, y.most);
   }
   int own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    d.mine[i] = min((n[i] + d.chunk - 1) / d.chunk, y.most);
     d.before[i] = own;
     own += d.mine[i];
   }
-  const int inc = wave_scan(own);
+  const int all = wave_scan(own);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) d.before[i] += inc - own;
-  d.total = __builtin_amdgcn_readlane(inc, kWave - 1);
+  for (int i = 0; i < 4; ++i) d.before[i] += all - own;
+  if (!(SPAN && y.span)) d.total = __builtin_amdgcn_readlane(all, kWave - 1);
   return d;
 }
-
 __device__ __forceinline__ float quad_max(float v) {   // over lanes r, r + 16, r + 32, r + 48
   const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
@@ -229,12 +255,15 @@ struct Place {
   int b, g, rb;                        // sequence, slot, block of query rows
   int h0, group, R;                    // the slot's first query head, its heads, its query rows
   size_t unit;                         // its cache head among those of all sequences
-  int n_ch, ch, rec;                   // chunks of the sequence, this one, and its record
+  int n_ch, rec;                       // chunks or pieces of the sequence, and this one's record
   int L, Lr, end;                      // length (-1: passed over), rows cached, rows that may be read
   int s0, s1;                          // steps
+  bool more;                           // another piece follows
 };
-__device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, Place& p) {
-  const Deal d = deal(a, y, lane);
+// piece: 0, 1, .. of the workgroup's
+template <bool SPAN>
+__device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, int piece, Place& p) {
+  const Deal d = deal<SPAN>(a, y, lane);
   // Row blocks of one chunk and head read the same rows: eight workgroups apart (one XCD, one L2) and next to
   // each other in time. Item: chunk of a sequence x slot.
   const int w = blockIdx.x, j = w >> 3;
@@ -242,31 +271,51 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   const int item = (j / y.rb) * 8 + (w & 7);
   if (item >= d.total * a.slots) return false;
   p.g = item % a.slots;
-  const int all = item / a.slots;
-  int hit = -1;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (all >= d.before[i] && all < d.before[i] + d.mine[i]) hit = i;
-  const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
-  const int sub = __builtin_amdgcn_readlane(hit, owner);
-  p.b = 4 * owner + sub;
-  const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], owner);
-  p.n_ch = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], owner);
-  p.ch = all - before;
-  p.rec = item * y.rb + p.rb;
   p.h0 = a.q_start[p.g];
   p.group = a.q_start[p.g + 1] - p.h0;
   p.R = a.T * p.group;
   if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
+  const int all = item / a.slots;                      // chunk, or slot of the row
+  int ch;
+  p.more = false;
+  if (SPAN && y.span) {
+    // sequences that end before the slot come first; the slot's own follow one another
+    int ended = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      ended += __popcll(__ballot(d.mine[i] > 0 && d.at[i] + (d.steps[i] + 3) / 4 * 4 <= all * d.chunk));
+    p.b = ended + piece;
+    auto starts = [&](int b) { return b < a.c.batch && pick(d.at, b >> 2, b & 3) / d.chunk <= all; };
+    if (!starts(p.b)) return false;
+    p.more = starts(p.b + 1);
+    ch = all - pick(d.at, p.b >> 2, p.b & 3) / d.chunk;
+  } else {
+    int hit = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (all >= d.before[i] && all < d.before[i] + d.mine[i]) hit = i;
+    const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
+    p.b = 4 * owner + __builtin_amdgcn_readlane(hit, owner);
+    ch = all - pick(d.before, owner, p.b & 3);
+  }
+  const int owner = p.b >> 2, sub = p.b & 3;
+  p.n_ch = pick(d.mine, owner, sub);
+  p.rec = ((pick(d.before, owner, sub) + ch) * a.slots + p.g) * y.rb + p.rb;
   p.unit = size_t(p.b) * a.c.n_kv + a.kv_map[p.g];
-  p.L = __builtin_amdgcn_readlane(sub == 0 ? d.len[0] : sub == 1 ? d.len[1] : sub == 2 ? d.len[2] : d.len[3], owner);
+  p.L = pick(d.len, owner, sub);
   p.Lr = max(p.L, 0);
   p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
   const int steps = (p.end + kStep - 1) / kStep;
-  // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
-  const int per = p.n_ch * d.chunk >= steps ? d.chunk : ((steps + p.n_ch - 1) / p.n_ch + 3) / 4 * 4;
-  p.s0 = p.ch * per;
-  p.s1 = p.ch == p.n_ch - 1 ? steps : min(steps, p.s0 + per);
+  if (SPAN && y.span) {
+    const int at = all * d.chunk - pick(d.at, owner, sub);
+    p.s0 = max(at, 0);
+    p.s1 = min(at + d.chunk, steps);
+  } else {
+    // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
+    const int per = p.n_ch * d.chunk >= steps ? d.chunk : ((steps + p.n_ch - 1) / p.n_ch + 3) / 4 * 4;
+    p.s0 = ch * per;
+    p.s1 = ch == p.n_ch - 1 ? steps : min(steps, p.s0 + per);
+  }
   return true;
 }
 
@@ -353,7 +402,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, c = lane >> 4;
   Place p;
-  if (!place(a, y, lane, p)) return;
+  if (!place<false>(a, y, lane, 0, p)) return;
   const int b = p.b, rb = p.rb, L = p.L, Lr = p.Lr, end = p.end, s0 = p.s0, s1 = p.s1;
   // steps from s_edge on hold rows of the tree: at most three, so a wave has one at most
   const int s_edge = min(Lr / kStep, s1);
@@ -585,231 +634,237 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
   __shared__ float s_scale[2][2][64];  // [step][K / V][row]
   __shared__ int s_odd;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = lane & 15, c = lane >> 4;
-  Place p;
-  if (!place(a, y, lane, p)) return;
-  const int Lr = p.Lr, end = p.end;
-  const size_t unit = p.unit;
-  const uint32_t row_bytes = DH * ES;
-  const bool for_v = wave < 2;         // this wave brings V (32 rows), or K
-  const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(for_v ? a.c.v : a.c.k) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
-  const __amdgpu_buffer_rsrc_t rks = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.ks + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
-  const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
-  const int half = 32 * (wave & 1);    // its rows of the step
+  for (int piece = 0;; ++piece) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));      // (new to the compiler in each piece: kept over pieces, what follows from it spills)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, c = lane >> 4;
+    Place p;
+    if (!place<true>(a, y, lane, piece, p)) return;
+    if (piece > 0) __syncthreads();      // (LDS is read no more)
+    const int Lr = p.Lr, end = p.end;
+    const size_t unit = p.unit;
+    const uint32_t row_bytes = DH * ES;
+    const bool for_v = wave < 2;         // this wave brings V (32 rows), or K
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(for_v ? a.c.v : a.c.k) + unit * a.c.S * row_bytes, uint32_t(end) * row_bytes);
+    const __amdgpu_buffer_rsrc_t rks = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.ks + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
+    const __amdgpu_buffer_rsrc_t rvs = make_rsrc(TYPE == SEQ_BF16 ? nullptr : a.c.vs + unit * a.c.S, TYPE == SEQ_BF16 ? 0u : uint32_t(end) * 4u);
+    const int half = 32 * (wave & 1);    // its rows of the step
 
-  // what a wave has on its way: 32 rows of K or of V of the next step
-  struct Raw {
-    uint32_t w[NW];
-    float scale;
-  };
-  auto load = [&](Raw& x, int s) __attribute__((always_inline)) {     // (steps past the last read as zeros)
-    const uint32_t t0 = uint32_t(s) * kStep + half;
-    const bool in = s < p.s1;
-    if constexpr (TYPE != SEQ_BF16)
-      x.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(for_v ? rvs : rks, int(in && lane < 32 ? (t0 + lane) * 4u : kOOB), 0, 0));
-    if (for_v) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t off = in ? (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r : kOOB;
-        if constexpr (VW == 4) {
-          const int4 q = buf_load16_stream(rx, off);
-          x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
-        } else if constexpr (VW == 2) {
-          const auto q = __builtin_amdgcn_raw_buffer_load_b64(rx, int(off), 0, kCpolStream);
-          x.w[2 * i] = q[0]; x.w[2 * i + 1] = q[1];
-        } else {
-          x.w[i] = __builtin_amdgcn_raw_buffer_load_b32(rx, int(off), 0, kCpolStream);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        const uint32_t row = t0 + i * (kWave / PPR) + lane / PPR;
-        const int4 q = buf_load16_stream(rx, in ? row * row_bytes + 16u * (lane % PPR) : kOOB);
-        x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
-      }
-    }
-  };
-  auto commit = [&](const Raw& x, int buf, int s) __attribute__((always_inline)) {
-    Step& z = s_step[buf];
-    if constexpr (TYPE != SEQ_BF16)
-      if (lane < 32) s_scale[buf][for_v][half + lane] = for_v ? x.scale : x.scale * a.scale2;
-    if (for_v) {
-      if constexpr (TYPE == SEQ_INT8) {
-        // byte d of eight rows' words -> one operand: widened, and packed two rows at a time
-#pragma unroll
-        for (int e = 0; e < NDT; ++e) {
-          uint32_t q[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float f0 = float(int8_t(x.w[2 * i * VW + e / 4] >> (8 * (e & 3)))), f1 = float(int8_t(x.w[(2 * i + 1) * VW + e / 4] >> (8 * (e & 3))));
-            q[i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
-          }
-          z.v[wave][e][lane] = make_uint4(q[0], q[1], q[2], q[3]);
-        }
-      } else {
-        uint32_t v[8][NDT / 2];
+    // what a wave has on its way: 32 rows of K or of V of the next step
+    struct Raw {
+      uint32_t w[NW];
+      float scale;
+    };
+    auto load = [&](Raw& x, int s) __attribute__((always_inline)) {     // (steps past the last read as zeros)
+      const uint32_t t0 = uint32_t(s) * kStep + half;
+      const bool in = s < p.s1;
+      if constexpr (TYPE != SEQ_BF16)
+        x.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(for_v ? rvs : rks, int(in && lane < 32 ? (t0 + lane) * 4u : kOOB), 0, 0));
+      if (for_v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if constexpr (TYPE == SEQ_BF16) {
-#pragma unroll
-            for (int e = 0; e < NDT / 2; ++e) v[i][e] = x.w[i * VW + e];
+          const uint32_t off = in ? (t0 + 16 * (i >> 2) + 4 * c + (i & 3)) * row_bytes + uint32_t(NDT * ES) * r : kOOB;
+          if constexpr (VW == 4) {
+            const int4 q = buf_load16_stream(rx, off);
+            x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
+          } else if constexpr (VW == 2) {
+            const auto q = __builtin_amdgcn_raw_buffer_load_b64(rx, int(off), 0, kCpolStream);
+            x.w[2 * i] = q[0]; x.w[2 * i + 1] = q[1];
           } else {
-#pragma unroll
-            for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(x.w[i * VW + e], &v[i][2 * e]);
+            x.w[i] = __builtin_amdgcn_raw_buffer_load_b32(rx, int(off), 0, kCpolStream);
           }
         }
-        const int new_row = Lr - s * kStep - half;     // the first of the wave's rows that is the tree's
-        if (new_row < 32) {
-          uint32_t bad = 0;
+      } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
-#pragma unroll
-              for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
-          if (bad) s_odd = 1;
-        }
-#pragma unroll
-        for (int e = 0; e < NDT; ++e) {
-          const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-          z.v[wave][e][lane] = make_uint4(__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel), __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel),
-                                          __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
+        for (int i = 0; i < KL; ++i) {
+          const uint32_t row = t0 + i * (kWave / PPR) + lane / PPR;
+          const int4 q = buf_load16_stream(rx, in ? row * row_bytes + 16u * (lane % PPR) : kOOB);
+          x.w[4 * i] = q.x; x.w[4 * i + 1] = q.y; x.w[4 * i + 2] = q.z; x.w[4 * i + 3] = q.w;
         }
       }
-      // The two branches' last stores are kept apart by order: merged into one store behind both (three of its four
-      // words, for BF16 rows and float32 q at dh 64), the compiler took one of V's words from the wrong register.
-      asm volatile("; V is stored" ::: "memory");
-    } else {
-      // lane (r', c') of operand kk reads slot 16 c' + (r' ^ (4 kk + c')): the pieces of one row, written
-      // together, go to different banks
+    };
+    auto commit = [&](const Raw& x, int buf, int s) __attribute__((always_inline)) {
+      Step& z = s_step[buf];
+      if constexpr (TYPE != SEQ_BF16)
+        if (lane < 32) s_scale[buf][for_v][half + lane] = for_v ? x.scale : x.scale * a.scale2;
+      if (for_v) {
+        if constexpr (TYPE == SEQ_INT8) {
+          // byte d of eight rows' words -> one operand: widened, and packed two rows at a time
 #pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        const int row = half + i * (kWave / PPR) + lane / PPR, j = lane % PPR;
-        auto put = [&](int piece, uint4 q) __attribute__((always_inline)) {
-          const int kk = piece >> 2, cc = piece & 3;
-          z.k[row >> 4][kk][16 * cc + ((row & 15) ^ (4 * kk + cc))] = q;
-        };
-        if constexpr (TYPE == SEQ_BF16) {
-          put(j, make_uint4(x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]));
+          for (int e = 0; e < NDT; ++e) {
+            uint32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float f0 = float(int8_t(x.w[2 * i * VW + e / 4] >> (8 * (e & 3)))), f1 = float(int8_t(x.w[(2 * i + 1) * VW + e / 4] >> (8 * (e & 3))));
+              q[i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+            }
+            z.v[wave][e][lane] = make_uint4(q[0], q[1], q[2], q[3]);
+          }
         } else {
-          uint32_t w[8];
+          uint32_t v[8][NDT / 2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) widen<TYPE>(x.w[4 * i + e], &w[2 * e]);
-          put(2 * j, make_uint4(w[0], w[1], w[2], w[3]));
-          put(2 * j + 1, make_uint4(w[4], w[5], w[6], w[7]));
+          for (int i = 0; i < 8; ++i) {
+            if constexpr (TYPE == SEQ_BF16) {
+#pragma unroll
+              for (int e = 0; e < NDT / 2; ++e) v[i][e] = x.w[i * VW + e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(x.w[i * VW + e], &v[i][2 * e]);
+            }
+          }
+          const int new_row = Lr - s * kStep - half;     // the first of the wave's rows that is the tree's
+          if (new_row < 32) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
+#pragma unroll
+                for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
+            if (bad) s_odd = 1;
+          }
+#pragma unroll
+          for (int e = 0; e < NDT; ++e) {
+            const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+            z.v[wave][e][lane] = make_uint4(__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel), __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel),
+                                            __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel), __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel));
+          }
         }
+        // The two branches' last stores are kept apart by order: merged into one store behind both (three of its four
+        // words, for BF16 rows and float32 q at dh 64), the compiler took one of V's words from the wrong register.
+        asm volatile("; V is stored" ::: "memory");
+      } else {
+        // lane (r', c') of operand kk reads slot 16 c' + (r' ^ (4 kk + c')): the pieces of one row, written
+        // together, go to different banks
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          const int row = half + i * (kWave / PPR) + lane / PPR, j = lane % PPR;
+          auto put = [&](int piece, uint4 q) __attribute__((always_inline)) {
+            const int kk = piece >> 2, cc = piece & 3;
+            z.k[row >> 4][kk][16 * cc + ((row & 15) ^ (4 * kk + cc))] = q;
+          };
+          if constexpr (TYPE == SEQ_BF16) {
+            put(j, make_uint4(x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]));
+          } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) widen<TYPE>(x.w[4 * i + e], &w[2 * e]);
+            put(2 * j, make_uint4(w[0], w[1], w[2], w[3]));
+            put(2 * j + 1, make_uint4(w[4], w[5], w[6], w[7]));
+          }
+        }
+        asm volatile("; K is stored" ::: "memory");
       }
-      asm volatile("; K is stored" ::: "memory");
+    };
+
+    Raw x;
+    load(x, p.s0);
+    if (tid == 0) s_odd = 0;
+    // this lane's query rows, as rows of Q (B operand): node t, head h
+    const int R = p.R;
+    const TreeNode nd = tree_node(a.parent ? a.parent + size_t(p.b) * a.T : nullptr, a.T, p.L < 0 ? 0 : a.c.S - p.L, lane);
+    unsigned long long anc[MT];
+    uint32_t qf[MT][QT][NKC][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int row = min(p.rb * RB + (wave * MT + mt) * 16 + r, R - 1);     // (rows past the last one repeat it and are not stored)
+      const int t = row / p.group, h = p.h0 + row % p.group;
+      anc[mt] = __shfl(nd.anc, t, kWave);
+      load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
     }
-  };
+    float m_run[MT], l_run[MT];          // of query row r; l of this lane's cache rows
+    f32x4 o[MT][NDT];                    // lane (r, c): query rows 4 c + i, dimension NDT r + d
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      m_run[mt] = -INFINITY;
+      l_run[mt] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __syncthreads();                     // s_odd
 
-  Raw x;
-  load(x, p.s0);
-  if (tid == 0) s_odd = 0;
-  // this lane's query rows, as rows of Q (B operand): node t, head h
-  const int R = p.R;
-  const TreeNode nd = tree_node(a.parent ? a.parent + size_t(p.b) * a.T : nullptr, a.T, p.L < 0 ? 0 : a.c.S - p.L, lane);
-  unsigned long long anc[MT];
-  uint32_t qf[MT][QT][NKC][4];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int row = min(p.rb * RB + (wave * MT + mt) * 16 + r, R - 1);     // (rows past the last one repeat it and are not stored)
-    const int t = row / p.group, h = p.h0 + row % p.group;
-    anc[mt] = __shfl(nd.anc, t, kWave);
-    load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
-  }
-  float m_run[MT], l_run[MT];          // of query row r; l of this lane's cache rows
-  f32x4 o[MT][NDT];                    // lane (r, c): query rows 4 c + i, dimension NDT r + d
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    m_run[mt] = -INFINITY;
-    l_run[mt] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  __syncthreads();                     // s_odd
-
-  // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
-  auto step = [&](int s, int buf, auto edge_) __attribute__((always_inline)) {
-    constexpr bool EDGE = decltype(edge_)::value;
-    commit(x, buf, s);
-    load(x, s + 2);
-    __syncthreads();
-    const Step& z = s_step[buf];
-    const int t0 = s * kStep - Lr;
+    // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
+    auto step = [&](int s, int buf, auto edge_) __attribute__((always_inline)) {
+      constexpr bool EDGE = decltype(edge_)::value;
+      commit(x, buf, s);
+      load(x, s + 2);
+      __syncthreads();
+      const Step& z = s_step[buf];
+      const int t0 = s * kStep - Lr;
 #pragma unroll 1
-    for (int half_ = 0; half_ < 2; ++half_) {          // (unrolled, it does not fit the registers)
-      // (accumulators take turns: a product waits for the one before it on the same accumulator)
-      f32x4 sc[MT][2];
+      for (int half_ = 0; half_ < 2; ++half_) {          // (unrolled, it does not fit the registers)
+        // (accumulators take turns: a product waits for the one before it on the same accumulator)
+        f32x4 sc[MT][2];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int kk = 0; kk < NKC; ++kk) {
-        uint4 kf[2];
+        for (int kk = 0; kk < NKC; ++kk) {
+          uint4 kf[2];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) kf[tt] = z.k[2 * half_ + tt][kk][16 * c + (r ^ (4 * kk + c))];
+          for (int tt = 0; tt < 2; ++tt) kf[tt] = z.k[2 * half_ + tt][kk][16 * c + (r ^ (4 * kk + c))];
 #pragma unroll
-        for (int k = 0; k < QT; ++k)
+          for (int k = 0; k < QT; ++k)
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
+            for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = mfma({kf[tt].x, kf[tt].y, kf[tt].z, kf[tt].w}, qf[mt][k][kk], sc[mt][tt]);
-      }
-      float ks[8] = {}, vs[8] = {};
-      if constexpr (TYPE != SEQ_BF16) {
+              for (int mt = 0; mt < MT; ++mt) sc[mt][tt] = mfma({kf[tt].x, kf[tt].y, kf[tt].z, kf[tt].w}, qf[mt][k][kk], sc[mt][tt]);
+        }
+        float ks[8] = {}, vs[8] = {};
+        if constexpr (TYPE != SEQ_BF16) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          const float4 x = *reinterpret_cast<const float4*>(&s_scale[buf][0][32 * half_ + 16 * tt + 4 * c]);
-          const float4 w = *reinterpret_cast<const float4*>(&s_scale[buf][1][32 * half_ + 16 * tt + 4 * c]);
-          ks[4 * tt] = x.x; ks[4 * tt + 1] = x.y; ks[4 * tt + 2] = x.z; ks[4 * tt + 3] = x.w;
-          vs[4 * tt] = w.x; vs[4 * tt + 1] = w.y; vs[4 * tt + 2] = w.z; vs[4 * tt + 3] = w.w;
+          for (int tt = 0; tt < 2; ++tt) {
+            const float4 x = *reinterpret_cast<const float4*>(&s_scale[buf][0][32 * half_ + 16 * tt + 4 * c]);
+            const float4 w = *reinterpret_cast<const float4*>(&s_scale[buf][1][32 * half_ + 16 * tt + 4 * c]);
+            ks[4 * tt] = x.x; ks[4 * tt + 1] = x.y; ks[4 * tt + 2] = x.z; ks[4 * tt + 3] = x.w;
+            vs[4 * tt] = w.x; vs[4 * tt + 1] = w.y; vs[4 * tt + 2] = w.z; vs[4 * tt + 3] = w.w;
+          }
+        }
+        uint32_t pf[MT][PT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, vs, a.scale2, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
+#pragma unroll
+        for (int e = 0; e < NDT; e += 2) {
+          uint4 vb[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) vb[i] = z.v[half_][e + i][lane];
+#pragma unroll
+          for (int k = 0; k < PT; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) o[mt][e + i] = mfma(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i]);
         }
       }
-      uint32_t pf[MT][PT][4];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, vs, a.scale2, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
-#pragma unroll
-      for (int e = 0; e < NDT; e += 2) {
-        uint4 vb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) vb[i] = z.v[half_][e + i][lane];
-#pragma unroll
-        for (int k = 0; k < PT; ++k)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) o[mt][e + i] = mfma(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i]);
-      }
-    }
-  };
-  int s = p.s0, buf = 0;
-  for (; s < p.s1 && (s + 2) * kStep <= Lr; s += 2, buf ^= 1) step(s, buf, std::false_type{});
-  for (; s < p.s1; s += 2, buf ^= 1) step(s, buf, std::true_type{});
+    };
+    int s = p.s0, buf = 0;
+    for (; s < p.s1 && (s + 2) * kStep <= Lr; s += 2, buf ^= 1) step(s, buf, std::false_type{});
+    for (; s < p.s1; s += 2, buf ^= 1) step(s, buf, std::true_type{});
 
-  // every wave holds its rows' results: lane (r, c) rows 4 c + i of a tile, their maxima and sums in lanes 4 c + i
+    // every wave holds its rows' results: lane (r, c) rows 4 c + i of a tile, their maxima and sums in lanes 4 c + i
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const float l_all = quad_sum(l_run[mt]);
+    for (int mt = 0; mt < MT; ++mt) {
+      const float l_all = quad_sum(l_run[mt]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
-      const float m = __shfl(m_run[mt], 4 * c + i, kWave), l = __shfl(l_all, 4 * c + i, kWave);
-      const int t = min(row, R - 1) / p.group;
-      const unsigned long long anc_o = __shfl(nd.anc, t, kWave);
-      float v[NDT];
+      for (int i = 0; i < 4; ++i) {
+        const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
+        const float m = __shfl(m_run[mt], 4 * c + i, kWave), l = __shfl(l_all, 4 * c + i, kWave);
+        const int t = min(row, R - 1) / p.group;
+        const unsigned long long anc_o = __shfl(nd.anc, t, kWave);
+        float v[NDT];
 #pragma unroll
-      for (int e = 0; e < NDT; ++e) v[e] = o[mt][e][i];
-      if constexpr (TYPE != SEQ_INT8)
-        if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, p.s0 * kStep, p.s1 * kStep, anc_o, NDT * r, v);
-      if (row < R) {
-        if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, t, p.h0 + row % p.group, NDT * r, l, anc_o != 0, v);
-        else put_record<DH, RB>(a, p.rec, in, NDT * r, m, anc_o != 0 ? l : 0.0f, v);
+        for (int e = 0; e < NDT; ++e) v[e] = o[mt][e][i];
+        if constexpr (TYPE != SEQ_INT8)
+          if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, p.s0 * kStep, p.s1 * kStep, anc_o, NDT * r, v);
+        if (row < R) {
+          if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, t, p.h0 + row % p.group, NDT * r, l, anc_o != 0, v);
+          else put_record<DH, RB>(a, p.rec, in, NDT * r, m, anc_o != 0 ? l : 0.0f, v);
+        }
       }
     }
+    if (!p.more) return;
   }
 }
 
@@ -821,10 +876,8 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   __shared__ float s_m[PARTS], s_l[PARTS];
   __shared__ float4 s_o[PARTS][LPR];
   const int tid = threadIdx.x, b = blockIdx.y;
-  const Deal d = deal(a, y, tid & 63);
-  const int sub = b & 3;
-  const int n = __builtin_amdgcn_readlane(sub == 0 ? d.mine[0] : sub == 1 ? d.mine[1] : sub == 2 ? d.mine[2] : d.mine[3], b >> 2);
-  const int before = __builtin_amdgcn_readlane(sub == 0 ? d.before[0] : sub == 1 ? d.before[1] : sub == 2 ? d.before[2] : d.before[3], b >> 2);
+  const Deal d = deal<true>(a, y, tid & 63);
+  const int n = pick(d.mine, b >> 2, b & 3), before = pick(d.before, b >> 2, b & 3);
   if (n <= 1) return;                  // written already
   const int q_row = blockIdx.x * ROWS + (PARTS > 1 ? 0 : tid / LPR);
   if (q_row >= a.T * a.slots * a.group) return;        // (PARTS > 1: every row has a workgroup)
@@ -889,7 +942,12 @@ TreeShape shape(const TreeAttnArgs& a) {
   y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (y.target + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
   const long chunks = std::min<long>(long(a.c.batch) * y.most, y.target / units + 1 + a.c.batch);
-  y.grid = int((chunks * a.slots + 7) / 8 * 8 * y.rb);
+  y.room = int((chunks * a.slots + 7) / 8 * 8 * y.rb);
+  // Spanned: two to eight slots per sequence (with more, chunks differ little, and a tree of 16 at 4 x 4096 rows took
+  // 21.5 us instead of 19.7: two pieces in a row), and a record for every piece: a slot each and one more per further sequence
+  y.quota = y.target / units;
+  y.span = y.wide && 2 * a.c.batch <= y.quota && y.quota < 8 * a.c.batch && y.quota + a.c.batch - 1 <= chunks;
+  y.grid = y.span ? (y.quota * a.slots + 7) / 8 * 8 * y.rb : y.room;
   return y;
 }
 
@@ -897,7 +955,7 @@ TreeShape shape(const TreeAttnArgs& a) {
 
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
   const TreeShape y = shape(a);
-  return y.most == 1 ? 0 : size_t(y.grid) * y.rows * (a.c.dh + 2) * 4;
+  return y.most == 1 ? 0 : size_t(y.room) * y.rows * (a.c.dh + 2) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {

@@ -194,3 +194,19 @@ def test_every_block_of_query_rows(dh, kind, act):
         got = S.tree_attention(c, 0, q.cuda(), parent.cuda())
         torch.cuda.synchronize()
         check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
+
+
+@pytest.mark.parametrize("kind,act,dh", [("int8", "bf16", 128), ("bf16", "bf16", 64), ("e4m3", "f32", 64), ("bf16", "f32", 128)])
+def test_wide_trees_of_a_ragged_batch(kind, act, dh):
+    """Few workgroups per sequence: they take pieces of neighbouring sequences, of which some are empty, one row, out
+    of range or longer than expected."""
+    flush(f"case ragged {kind} {act} {dh}")
+    lens, T, H = [900, 0, 1, 610, -2, 33, 500, 64], 64, 8 if act == "bf16" else 4
+    hq = 8 * H
+    c, kv, vv = typed_cache(lens, H, 964, dh, kind, 11)
+    parent = random_parents(len(lens), T, 11)
+    q = randn((len(lens), T, hq, dh), DTYPES[act], 12)
+    for max_len in (900, 640):
+        got = S.tree_attention(c, 0, q.cuda(), parent.cuda(), max_len=max_len)
+        torch.cuda.synchronize()
+        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 964, act, dh ** -0.5, nodes=[0, 17, 63])
