@@ -54,22 +54,31 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 //   * otherwise each is cut in chunks of `chunk` steps, a workgroup for each.
 // A piece or chunk of a sequence that has several leaves a record. A wave holds four sequences per lane.
 //
-// How a call is launched: query rows in rb blocks of `rows` (16 mt, wide: 64 mt), `target` workgroups aimed at, at most `most`
-// chunks per sequence (what the workspace has room for), quota: slots per unit, room: records (and workgroups of the second way)
+// How a call is launched: query rows in rb blocks of `rows` = 2^rows_log (16 mt, wide: 64 mt), at most `most` chunks per
+// sequence (what the workspace has room for), quota: slots per unit, room: records, items: of the grid
 constexpr int kSetup = 4;
+constexpr int kTarget = 512;           // workgroups aimed at: two per CU
 struct TreeShape {
-  int wide, mt, rows, rb, target, most, quota, span, room, grid;
+  int wide, mt, rows, rows_log, rb, most, quota, span, room, items;
 };
 struct Deal {
   int chunk;                           // steps per chunk or slot
   int total;                           // chunks of all sequences, or slots
   int mine[4], before[4];              // of the lane's sequences: chunks or pieces, and those of the sequences before them
   int len[4];                          // and their lengths, -1: passed over
-  int at[4], steps[4];                 // span: place of the first step in the row; steps
+  int at[4], slot[4], steps[4];        // span: place of the first step in the row, and its slot; steps
 };
 // v[sub] of lane `owner`
 __device__ __forceinline__ int pick(const int (&v)[4], int owner, int sub) {
   return __builtin_amdgcn_readlane(sub == 0 ? v[0] : sub == 1 ? v[1] : sub == 2 ? v[2] : v[3], owner);
+}
+// a / d for rows and items (a < 2^21): a + 1/2 is 1 / (2 d) away from a multiple of d at least, the product off by a / d 2^-22.
+// (An integer division is 40 instructions one after the other: dealing took 2.9 us with a dozen of them.)
+__device__ __forceinline__ int quot(int a, int d) { return int((float(a) + 0.5f) * __builtin_amdgcn_rcpf(float(d))); }
+// a / d for steps, with a / d < 2^20: the product is off by less than one
+__device__ __forceinline__ int quot_steps(int a, int d, float inv) {
+  const int q = int(float(a) * inv), rest = a - q * d;
+  return rest < 0 ? q - 1 : rest >= d ? q + 1 : q;
 }
 // Sums over lanes 0 .. own (row_shr:1, 2, 4, 8 within rows of 16, row_bcast:15 and :31 between them)
 __device__ __forceinline__ int wave_scan(int v) {
@@ -99,35 +108,37 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, 
   // divergent becomes a loop over lanes, around every load)
   d.total = y.quota;
   if (SPAN && y.span) {
-    d.chunk = max(kMinSteps, ((sum + y.quota - 1) / y.quota + 3) / 4 * 4);
+    d.chunk = max(kMinSteps, (quot_steps(sum + y.quota - 1, y.quota, __builtin_amdgcn_rcpf(float(y.quota))) + 3) / 4 * 4);
+    const float inv = __builtin_amdgcn_rcpf(float(d.chunk));
     int at = inc - sum_own;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       d.at[i] = at + kSetup;
       d.steps[i] = n[i];
-      d.mine[i] = cost[i] == 0 ? 0 : (at + cost[i] - 1) / d.chunk - d.at[i] / d.chunk + 1;
+      d.slot[i] = quot_steps(d.at[i], d.chunk, inv);
+      d.mine[i] = cost[i] == 0 ? 0 : quot_steps(at + cost[i] - 1, d.chunk, inv) - d.slot[i] + 1;
       at += cost[i];
     }
   } else {
     const int units = a.slots * y.rb;
-    d.chunk = max(kMinSteps, (int((long(sum) * units + y.target - 1) / y.target) + 3) / 4 * 4);
+    d.chunk = max(kMinSteps, (int((long(sum) * units + kTarget - 1) / kTarget) + 3) / 4 * 4);
     if (a.c.batch > 1 && 2 * a.c.batch <= y.quota) {
       // Sequences are rounded up to whole chunks: the shortest chunk that keeps all workgroups within the target is
       // looked for, a candidate per lane (workgroups beyond it would make a second round)
       const int mine = d.chunk + lane * max(4, d.chunk / 256 * 4);
-      const float inv = 1.0f / float(mine);
+      const float inv = __builtin_amdgcn_rcpf(float(mine));
       int count = 0;
       for (int b = 0; b < a.c.batch; ++b) {
         const int nb = pick(n, b >> 2, b & 3);
-        int q = int(float(nb) * inv);                  // within one of the quotient; rounded up below
-        q += q * mine < nb ? 1 : 0;
-        count += q;
+        const int q = int(float(nb) * inv);            // within one of the quotient; rounded up
+        count += q + (q * mine < nb ? 1 : 0);
       }
       const unsigned long long fits = __ballot(count <= y.quota);
       d.chunk = __builtin_amdgcn_readlane(mine, fits ? __ffsll((long long)fits) - 1 : kWave - 1);
     }
+    const float inv = __builtin_amdgcn_rcpf(float(d.chunk));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) d.mine[i] = min((n[i] + d.chunk - 1) / d.chunk, y.most);
+    for (int i = 0; i < 4; ++i) d.mine[i] = min(quot_steps(n[i] + d.chunk - 1, d.chunk, inv), y.most);
   }
   int own = 0;
 #pragma unroll
@@ -264,18 +275,17 @@ struct Place {
 template <bool SPAN>
 __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, int piece, Place& p) {
   const Deal d = deal<SPAN>(a, y, lane);
-  // Row blocks of one chunk and head read the same rows: eight workgroups apart (one XCD, one L2) and next to
-  // each other in time. Item: chunk of a sequence x slot.
-  const int w = blockIdx.x, j = w >> 3;
-  p.rb = j % y.rb;
-  const int item = (j / y.rb) * 8 + (w & 7);
+  // Grid (8, row blocks, items / 8): row blocks of one chunk and head read the same rows, and are eight workgroups
+  // apart (one XCD, one L2) and next to each other in time. Item: chunk of a sequence x slot.
+  p.rb = blockIdx.y;
+  const int item = blockIdx.z * 8 + blockIdx.x;
   if (item >= d.total * a.slots) return false;
-  p.g = item % a.slots;
+  const int all = quot(item, a.slots);                 // chunk, or slot of the row
+  p.g = item - all * a.slots;
   p.h0 = a.q_start[p.g];
   p.group = a.q_start[p.g + 1] - p.h0;
   p.R = a.T * p.group;
   if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
-  const int all = item / a.slots;                      // chunk, or slot of the row
   int ch;
   p.more = false;
   if (SPAN && y.span) {
@@ -285,10 +295,10 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
     for (int i = 0; i < 4; ++i)
       ended += __popcll(__ballot(d.mine[i] > 0 && d.at[i] + (d.steps[i] + 3) / 4 * 4 <= all * d.chunk));
     p.b = ended + piece;
-    auto starts = [&](int b) { return b < a.c.batch && pick(d.at, b >> 2, b & 3) / d.chunk <= all; };
+    auto starts = [&](int b) { return b < a.c.batch && pick(d.slot, b >> 2, b & 3) <= all; };
     if (!starts(p.b)) return false;
     p.more = starts(p.b + 1);
-    ch = all - pick(d.at, p.b >> 2, p.b & 3) / d.chunk;
+    ch = all - pick(d.slot, p.b >> 2, p.b & 3);
   } else {
     int hit = -1;
 #pragma unroll
@@ -464,7 +474,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int row = min((rb * MT + mt) * 16 + r, R - 1);   // (rows past the last one repeat it and are not stored)
-    const int t = row / p.group, h = p.h0 + row % p.group;
+    const int t = quot(row, p.group), h = p.h0 + row - t * p.group;
     anc[mt] = __shfl(nd.anc, t, kWave);
     load_q<DH, ACT, QT, ES == 1>(a, b * a.q.seq + t * a.q.token + h * a.q.head + (ES == 2 ? 8 : 16) * c, qf[mt]);
   }
@@ -602,14 +612,14 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
       for (int k = 0; k < 4; ++k) v[e] += s_o[k][qr][d0 + e] * f[k];
     }
     const int row_o = (rb * MT + mt) * 16 + qr;
-    const int t_o = min(row_o, R - 1) / p.group;
+    const int t_o = quot(min(row_o, R - 1), p.group);
     const unsigned long long anc_o = __shfl(nd.anc, t_o, kWave);
     const bool there = anc_o != 0;     // (a row of an absent node is zeros)
     if (row_o >= R) continue;
     if constexpr (TYPE != SEQ_INT8) {
       if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, max(s_edge, s0) * kStep, s1 * kStep, anc_o, d0, v);
     }
-    if (p.n_ch == 1) put_output<DH, ACT>(a, b, t_o, p.h0 + row_o % p.group, d0, l, there, v);
+    if (p.n_ch == 1) put_output<DH, ACT>(a, b, t_o, p.h0 + row_o - t_o * p.group, d0, l, there, v);
     else put_record<DH, RB>(a, p.rec, 16 * mt + qr, d0, m, there ? l : 0.0f, v);
   }
 }
@@ -768,7 +778,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const int row = min(p.rb * RB + (wave * MT + mt) * 16 + r, R - 1);     // (rows past the last one repeat it and are not stored)
-      const int t = row / p.group, h = p.h0 + row % p.group;
+      const int t = quot(row, p.group), h = p.h0 + row - t * p.group;
       anc[mt] = __shfl(nd.anc, t, kWave);
       load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
     }
@@ -851,7 +861,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
       for (int i = 0; i < 4; ++i) {
         const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
         const float m = __shfl(m_run[mt], 4 * c + i, kWave), l = __shfl(l_all, 4 * c + i, kWave);
-        const int t = min(row, R - 1) / p.group;
+        const int t = quot(min(row, R - 1), p.group);
         const unsigned long long anc_o = __shfl(nd.anc, t, kWave);
         float v[NDT];
 #pragma unroll
@@ -859,7 +869,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
         if constexpr (TYPE != SEQ_INT8)
           if (s_odd) add_odd<DH, TYPE>(a, unit, Lr, p.s0 * kStep, p.s1 * kStep, anc_o, NDT * r, v);
         if (row < R) {
-          if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, t, p.h0 + row % p.group, NDT * r, l, anc_o != 0, v);
+          if (p.n_ch == 1) put_output<DH, ACT>(a, p.b, t, p.h0 + row - t * p.group, NDT * r, l, anc_o != 0, v);
           else put_record<DH, RB>(a, p.rec, in, NDT * r, m, anc_o != 0 ? l : 0.0f, v);
         }
       }
@@ -881,10 +891,10 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   if (n <= 1) return;                  // written already
   const int q_row = blockIdx.x * ROWS + (PARTS > 1 ? 0 : tid / LPR);
   if (q_row >= a.T * a.slots * a.group) return;        // (PARTS > 1: every row has a workgroup)
-  const int t = q_row / (a.slots * a.group), g = q_row / a.group % a.slots, hh = q_row % a.group;
+  const int th = quot(q_row, a.group), hh = q_row - th * a.group, t = quot(th, a.slots), g = th - t * a.slots;
   const int h0 = a.q_start[g], group = a.q_start[g + 1] - h0;
   if (hh >= group) return;
-  const int row = t * group + hh, rows = y.rows, rb = row / rows, in = row % rows;
+  const int row = t * group + hh, rows = y.rows, rb = row >> y.rows_log, in = row & (rows - 1);
   const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.slots * y.rb;
   const float* first = a.ws + before * stride + (size_t(g) * y.rb + rb) * rec;
   const int part = PARTS > 1 ? tid / LPR : 0, d0 = 4 * (tid % LPR);
@@ -935,19 +945,19 @@ TreeShape shape(const TreeAttnArgs& a) {
   y.mt = y.wide ? (tiles > 4 && a.act == SEQ_BF16 ? 2 : 1) : tiles;
   const int block = (y.wide ? 4 : 1) * y.mt;           // tiles of a workgroup
   y.rows = 16 * block;
+  y.rows_log = 31 - __builtin_clz(y.rows);
   y.rb = (tiles + block - 1) / block;
-  y.target = 512;                      // two workgroups per CU
   const int units = a.slots * y.rb;
   const long steps = (std::min<long>(std::max(a.max_len, 0) + long(a.T), a.c.S) + kStep - 1) / kStep;
-  y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (y.target + units - 1) / units)));
+  y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (kTarget + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
-  const long chunks = std::min<long>(long(a.c.batch) * y.most, y.target / units + 1 + a.c.batch);
-  y.room = int((chunks * a.slots + 7) / 8 * 8 * y.rb);
+  const long chunks = std::min<long>(long(a.c.batch) * y.most, kTarget / units + 1 + a.c.batch);
+  y.room = int(chunks) * a.slots * y.rb;
   // Spanned: two to eight slots per sequence (with more, chunks differ little, and a tree of 16 at 4 x 4096 rows took
   // 21.5 us instead of 19.7: two pieces in a row), and a record for every piece: a slot each and one more per further sequence
-  y.quota = y.target / units;
+  y.quota = kTarget / units;
   y.span = y.wide && 2 * a.c.batch <= y.quota && y.quota < 8 * a.c.batch && y.quota + a.c.batch - 1 <= chunks;
-  y.grid = y.span ? (y.quota * a.slots + 7) / 8 * 8 * y.rb : y.room;
+  y.items = ((y.span ? y.quota : int(chunks)) * a.slots + 7) / 8 * 8;
   return y;
 }
 
@@ -960,7 +970,7 @@ size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
   const TreeShape y = shape(a);
-#define ATTN(KERNEL, DH, TYPE, ACT, MT) hipLaunchKernelGGL((KERNEL<DH, TYPE, ACT, MT>), dim3(y.grid), dim3(kBlock), 0, s, a, y)
+#define ATTN(KERNEL, DH, TYPE, ACT, MT) hipLaunchKernelGGL((KERNEL<DH, TYPE, ACT, MT>), dim3(8, y.rb, y.items / 8), dim3(kBlock), 0, s, a, y)
 #define ATTN_MT(DH, TYPE, ACT)                                                                   \
   do {                                                                                           \
     if (!y.wide && y.mt == 1) ATTN(tree_attn_kernel, DH, TYPE, ACT, 1);                          \
