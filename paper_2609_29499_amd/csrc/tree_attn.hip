@@ -883,21 +883,21 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 template <int DH, int ACT, int PARTS>
 __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeShape y) {
   constexpr int LPR = DH / 4, ROWS = kBlock / (LPR * PARTS);
-  __shared__ float s_m[PARTS], s_l[PARTS];
-  __shared__ float4 s_o[PARTS][LPR];
+  __shared__ float s_m[ROWS][PARTS], s_l[ROWS][PARTS];
+  __shared__ float4 s_o[ROWS][PARTS][LPR];
   const int tid = threadIdx.x, b = blockIdx.y;
   const Deal d = deal<true>(a, y, tid & 63);
   const int n = pick(d.mine, b >> 2, b & 3), before = pick(d.before, b >> 2, b & 3);
   if (n <= 1) return;                  // written already
-  const int q_row = blockIdx.x * ROWS + (PARTS > 1 ? 0 : tid / LPR);
-  if (q_row >= a.T * a.slots * a.group) return;        // (PARTS > 1: every row has a workgroup)
-  const int th = quot(q_row, a.group), hh = q_row - th * a.group, t = quot(th, a.slots), g = th - t * a.slots;
+  const int mine = tid / (LPR * PARTS), q_row = blockIdx.x * ROWS + mine;
+  const int th = quot(min(q_row, a.T * a.slots * a.group - 1), a.group), t = quot(th, a.slots), g = th - t * a.slots;
   const int h0 = a.q_start[g], group = a.q_start[g + 1] - h0;
-  if (hh >= group) return;
+  const int own = q_row - th * a.group, hh = min(own, group - 1);
+  const bool there = own < group;      // (others repeat a row, and store nothing)
   const int row = t * group + hh, rows = y.rows, rb = row >> y.rows_log, in = row & (rows - 1);
   const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.slots * y.rb;
   const float* first = a.ws + before * stride + (size_t(g) * y.rb + rb) * rec;
-  const int part = PARTS > 1 ? tid / LPR : 0, d0 = 4 * (tid % LPR);
+  const int part = tid / LPR % PARTS, d0 = 4 * (tid % LPR);
   float m = -INFINITY, l = 0.0f;
   float v[4] = {};
   auto add = [&](float mk, float lk, const float4& x) {
@@ -924,18 +924,18 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   }
   if constexpr (PARTS > 1) {
     if (d0 == 0) {
-      s_m[part] = m;
-      s_l[part] = l;
+      s_m[mine][part] = m;
+      s_l[mine][part] = l;
     }
-    s_o[part][tid % LPR] = make_float4(v[0], v[1], v[2], v[3]);
+    s_o[mine][part][tid % LPR] = make_float4(v[0], v[1], v[2], v[3]);
     __syncthreads();
-    if (tid >= LPR) return;
+    if (part > 0) return;
     m = -INFINITY;
     l = v[0] = v[1] = v[2] = v[3] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) add(s_m[k], s_l[k], s_o[k][tid]);
+    for (int k = 0; k < PARTS; ++k) add(s_m[mine][k], s_l[mine][k], s_o[mine][k][tid % LPR]);
   }
-  put_output<DH, ACT>(a, b, t, h0 + hh, d0, l, true, v);
+  if (there) put_output<DH, ACT>(a, b, t, h0 + hh, d0, l, true, v);
 }
 
 TreeShape shape(const TreeAttnArgs& a) {
@@ -997,19 +997,24 @@ hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || y.most == 1) return e;
   const int rows = a.T * a.slots * a.group;
-  // few rows: a workgroup for each (latency); many: a group of lanes walks all of a row's chunks (the 64-node
-  // case took 72 us with a workgroup per row)
-#define JOIN(DH, ACT)                                                                                              \
-  do {                                                                                                             \
-    constexpr int PARTS = 4 * kBlock / DH;                                                                         \
-    if (rows * a.c.batch < 2048) hipLaunchKernelGGL((tree_join_kernel<DH, ACT, PARTS>), dim3(rows, a.c.batch), dim3(kBlock), 0, s, a, y); \
-    else hipLaunchKernelGGL((tree_join_kernel<DH, ACT, 1>), dim3((rows + PARTS - 1) / PARTS, a.c.batch), dim3(kBlock), 0, s, a, y); \
+  // Few rows: a workgroup for each (latency); many: a group of lanes walks all of a row's records, which are few then
+  // (the 64-node case took 72 us with a workgroup per row); between, four groups (a tree of 16 at 4 x 4096 rows, 16
+  // records: 7.5 us with one).
+#define JOIN_PARTS(DH, ACT, PARTS)                                                                                        \
+  hipLaunchKernelGGL((tree_join_kernel<DH, ACT, PARTS>), dim3((rows * PARTS + 4 * kBlock / DH - 1) / (4 * kBlock / DH), a.c.batch), \
+                     dim3(kBlock), 0, s, a, y)
+#define JOIN(DH, ACT)                                                            \
+  do {                                                                           \
+    if (rows * a.c.batch < 2048) JOIN_PARTS(DH, ACT, 4 * kBlock / DH);           \
+    else if (rows * a.c.batch < 8192) JOIN_PARTS(DH, ACT, 4);                    \
+    else JOIN_PARTS(DH, ACT, 1);                                                 \
   } while (0)
   if (a.c.dh == 128 && a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
   else if (a.c.dh == 128) JOIN(128, SEQ_F32);
   else if (a.act == SEQ_BF16) JOIN(64, SEQ_BF16);
   else JOIN(64, SEQ_F32);
 #undef JOIN
+#undef JOIN_PARTS
   return hipGetLastError();
 }
 
