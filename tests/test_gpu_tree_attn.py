@@ -3,9 +3,11 @@
 Tolerance of one output: with A = sum of p |v| over the rows seen, n their number,
   scores: a float32 dot product of dh exact products, |error| <= (dh + 4) 2^-24 scale sum |q_i k_i| = d, which
   moves p by a factor within exp(2 d);
-  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; float32 sums n 2^-24;
+  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; over rows in 8 bits with more
+  than 32 BF16 query rows P is one FP16 term: half a step 2^-11, and where P times the row's scale falls below 2^-18 of the largest scale M,
+  a subnormal's half step 2^-25 in units of 2^-4 M or less: n 2^-29 max |v| together; float32 sums n 2^-24;
   the output's rounding 2^-8 of the value in BF16, 2^-24 in float32.
-|error| <= A (2 d + 2^-21 + 2^-16 or 2^-24 + n 2^-24) + |o| 2^-8 or 2^-24."""
+|error| <= A (2 d + 2^-21 + 2^-11, 2^-16 or 2^-24 + n 2^-24) + (n 2^-29 max |v|) + |o| 2^-8 or 2^-24."""
 import math
 
 import numpy as np
@@ -19,10 +21,11 @@ from tests.seq_case import DTYPES, flush, gen, randn, random_parents, typed_cach
 pytestmark = pytest.mark.gpu
 
 
-def check(got, q, kv, vv, lens, parent, S_, act, scale, nodes=None):
+def check(got, q, kv, vv, lens, parent, S_, act, scale, nodes=None, kind="bf16"):
     """got [B][T][Hq][dh] against the oracle, every node or the given ones."""
     Bn, T, hq, dh = q.shape
     H = kv.shape[1]
+    half = kind != "bf16" and act == "bf16" and T * (hq // H) > 32
     worst = 0.0
     for b in range(Bn):
         ln = O.lines(None if parent is None else parent[b].tolist(), T, S_ - lens[b]) if 0 <= lens[b] <= S_ else [None] * T
@@ -35,7 +38,8 @@ def check(got, q, kv, vv, lens, parent, S_, act, scale, nodes=None):
                 k, v = kv[b, h // (hq // H)], vv[b, h // (hq // H)]
                 o, A = O.attention(q[b, t, h], k, v, seen, scale)
                 d = (dh + 4) * 2.0 ** -24 * scale * np.max(np.abs(k[seen]) @ np.abs(q[b, t, h]))
-                tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -16 if act == "bf16" else 2.0 ** -24) + len(seen) * 2.0 ** -24)
+                tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -11 if half else 2.0 ** -16 if act == "bf16" else 2.0 ** -24) + len(seen) * 2.0 ** -24)
+                tol = tol + half * len(seen) * 2.0 ** -29 * np.max(np.abs(v[seen]))
                 tol = tol + np.abs(o) * (2.0 ** -8 if act == "bf16" else 2.0 ** -24)
                 err = np.abs(got[b, t, h] - o)
                 worst = max(worst, float(np.max(err / tol)))
@@ -69,7 +73,7 @@ def test_tree_attention(case):
     q = randn((len(lens), T, hq, dh), DTYPES[act], 100 + case)
     got = S.tree_attention(c, 0, q.cuda(), None if parent is None else parent.cuda())
     torch.cuda.synchronize()
-    check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
+    check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5, kind=kind)
 
 
 @pytest.mark.parametrize("kind,T,hq,dh", [("bf16", 3, 4, 128), ("int8", 3, 4, 128), ("e4m3", 9, 8, 64),
@@ -89,7 +93,7 @@ def test_long_contexts_in_many_chunks(kind, T, hq, dh):
     for hint in (20000, 4000, 100):
         S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint, out=out[:, :, :hq])
         torch.cuda.synchronize()
-        check(out[:, :, :hq].double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 20040, "bf16", dh ** -0.5, sorted({0, T // 2, T - 1}))
+        check(out[:, :, :hq].double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 20040, "bf16", dh ** -0.5, sorted({0, T // 2, T - 1}), kind=kind)
         assert torch.all(out[:, :, hq] == 5.0)
         again = S.tree_attention(c, 0, wide[:, :, 1], parent.cuda(), max_len=hint)
         torch.cuda.synchronize()
@@ -193,7 +197,7 @@ def test_every_block_of_query_rows(dh, kind, act):
         q = randn((2, T, hq, dh), DTYPES[act], 50 + T)
         got = S.tree_attention(c, 0, q.cuda(), parent.cuda())
         torch.cuda.synchronize()
-        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5)
+        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, S_, act, dh ** -0.5, kind=kind)
 
 
 @pytest.mark.parametrize("kind,act,dh", [("int8", "bf16", 128), ("bf16", "bf16", 64), ("e4m3", "f32", 64), ("bf16", "f32", 128)])
@@ -209,4 +213,40 @@ def test_wide_trees_of_a_ragged_batch(kind, act, dh):
     for max_len in (900, 640):
         got = S.tree_attention(c, 0, q.cuda(), parent.cuda(), max_len=max_len)
         torch.cuda.synchronize()
-        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 964, act, dh ** -0.5, nodes=[0, 17, 63])
+        check(got.double().cpu().numpy(), q.double().numpy(), kv[0], vv[0], lens, parent, 964, act, dh ** -0.5, nodes=[0, 17, 63], kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("order", ["rising", "falling", "mixed", "zeros"])
+def test_scales_of_any_size(kind, order):
+    """Values that grow or shrink by 40 powers of two along the cache, or are nothing but zeros, under wide trees."""
+    flush(f"case scales {kind} {order}")
+    lens, T, hq, dh = [500, 130], 12, 8, 64
+    c, kv, vv = typed_cache(lens, 1, 520, dh, kind, 15)
+    x = torch.linspace(-20, 20, 520)
+    if order == "mixed":
+        x = x[torch.randperm(520, generator=gen(16))]
+    f = torch.zeros(520) if order == "zeros" else torch.exp2((x if order != "falling" else -x).round())
+    c.v_scale.mul_(f.cuda())
+    parent = random_parents(2, T, 15)
+    q = randn((2, T, hq, dh), torch.bfloat16, 17)
+    got = S.tree_attention(c, 0, q.cuda(), parent.cuda())
+    torch.cuda.synchronize()
+    values = np.asarray(vv[0]) * f.double().numpy()[:, None]
+    check(got.double().cpu().numpy(), q.double().numpy(), kv[0], values, lens, parent, 520, "bf16", dh ** -0.5, kind=kind)
+    if order == "zeros":
+        assert not got.any()
+
+
+def test_visible_scales_that_are_not_finite():
+    """A cached row whose scale is infinite or NaN: its nodes' outputs are not finite, and others' stay what they are."""
+    flush("case scales not finite")
+    T, dh = 12, 64
+    c, kv, vv = typed_cache([100, 100], 1, 120, dh, "int8", 18)
+    q = randn((2, T, 8, dh), torch.bfloat16, 19).cuda()
+    clean = S.tree_attention(c, 0, q)
+    for what in (math.inf, math.nan):
+        c.v_scale[0, 1, 0, 50] = what
+        got = S.tree_attention(c, 0, q)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], clean[0]) and not torch.isfinite(got[1]).any()
