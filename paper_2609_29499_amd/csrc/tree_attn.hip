@@ -253,7 +253,11 @@ __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks
     if constexpr (HALF) {
       wide = 0.0f;                     // (a scale that is not finite has no part in it)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) wide = fmaxf(wide, w[i] < INFINITY ? w[i] : 0.0f);
+      for (int i = 0; i < 8; ++i) {
+        float x = w[i];
+        asm volatile("" : "+v"(x));    // (or all of this is done ahead of the branch)
+        wide = fmaxf(wide, x < INFINITY ? x : 0.0f);
+      }
       wide = quad_max(wide);
       if (wide > lift.limit) {
         const float by = wide > 0.0f ? float(min(max(5 - __builtin_amdgcn_frexp_expf(wide), -123), 110)) : 0.0f;
@@ -408,6 +412,15 @@ __device__ __forceinline__ void put_record(const TreeAttnArgs& a, int rec, int r
   if (d0 == 0) *reinterpret_cast<float2*>(po + RB * DH + 2 * row) = make_float2(m, l);
 }
 
+// What load_q brought is here. Said in front of a loop over steps: a load that may still be on its way at its first
+// turn is waited for in every turn, and with it all of the next step's loads, which are younger.
+template <int QT, int NKC>
+__device__ __forceinline__ void arrived(uint32_t (&qf)[QT][NKC][4]) {
+#pragma unroll
+  for (int k = 0; k < QT; ++k)
+#pragma unroll
+    for (int j = 0; j < NKC; ++j) asm volatile("" : "+v"(qf[k][j][0]), "+v"(qf[k][j][1]), "+v"(qf[k][j][2]), "+v"(qf[k][j][3]));
+}
 // A query row's operand: from `at` on (elements from q.p) 8 values for each of dh / 32 products, those of product
 // kk 32 kk further on, or (PAIRED) 64 floor(kk / 2) + 8 (kk mod 2)
 template <int DH, int ACT, int QT, bool PAIRED>
@@ -617,6 +630,8 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     if (tid == 0) s_odd = 0;
     __syncthreads();
   }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) arrived(qf[mt]);
   if (has_edge) process(xa, s_late, std::true_type{});
   for (int s = s_own; s < s_edge; s += 8) {
     load(s + 4, s_edge, xa);
@@ -844,6 +859,8 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 #pragma unroll
       for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) arrived(qf[mt]);
     __syncthreads();                     // s_odd
 
     // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
