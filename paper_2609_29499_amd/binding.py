@@ -363,14 +363,16 @@ def tasp_copy_probe(dst_ptr, src_ptr, nbytes, stream):
 
 
 def _ref(struct):
-    """The address of a struct; bytes that hold one, and None, as they are."""
-    return struct if struct is None or type(struct) is bytes else C.addressof(struct)
+    """The address of a struct; bytes that hold one, its address and None as they are."""
+    return struct if struct is None or type(struct) is bytes or type(struct) is int else C.addressof(struct)
 
 
 def tasp_seq_append(cache, layer, rope, parent_ptr, T, act_type, q, k, v, n_q_heads, q_out, stream):
-    """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs, or their bytes."""
-    st = (_lib or load()).tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, _ref(q), _ref(k),
-                                          _ref(v), n_q_heads, _ref(q_out), stream)
+    """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs, their bytes or their addresses."""
+    if type(k) is not bytes:           # (bytes, as the tensor wrappers pass them, are told apart once: a call each costs 0.1 us)
+        q, k, v, q_out = _ref(q), _ref(k), _ref(v), _ref(q_out)
+    st = (_lib or load()).tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, q, k, v, n_q_heads,
+                                          q_out, stream)
     if st:
         _check(st)
 

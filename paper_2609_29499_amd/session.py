@@ -379,8 +379,12 @@ class Router:
 
 # ------------------------------------------- sequences of their own lengths, drafted tokens
 
-_SEQ_TYPES = {torch.bfloat16: B.BF16, torch.float32: B.F32, torch.int8: B.INT8, torch.float8_e4m3fn: B.E4M3}
+class _Types(dict):
+    def __missing__(self, dtype):
+        raise ValueError(f"{dtype} is none of {', '.join(map(str, self))}")
 
+
+_SEQ_TYPES = _Types({torch.bfloat16: B.BF16, torch.float32: B.F32, torch.int8: B.INT8, torch.float8_e4m3fn: B.E4M3})
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (absent in builds without a GPU)
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
@@ -426,6 +430,11 @@ def _rows(t, shape, dtype, what, token=1, head=2):
     # (the stride of an axis of one is never used, and may be anything)
     return _pack_rows(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[token] if shape[token] > 1 else 0,
                       st[head] if shape[head] > 1 else 0)
+
+
+def _dense(t, seq, token, head):
+    """The tasp_rows of a contiguous tensor made here, with its strides."""
+    return _pack_rows(t.data_ptr(), seq, token, head)
 
 
 def _empty(shape, dtype, device, stream):
@@ -499,9 +508,12 @@ def seq_append(cache, layer, q, k, v, rope=None, parent=None, q_out=None, stream
     if q is not None:
         n_q = q.shape[2]
         shape = (cache.batch, T, n_q, cache.dh)
+        rq = _rows(q, shape, dt, "q")
         if q_out is None:
             q_out = _like(q, stream)
-        rq, ro = _rows(q, shape, dt, "q"), _rows(q_out, shape, dt, "q_out")
+            ro = _dense(q_out, T * n_q * cache.dh, n_q * cache.dh, cache.dh)
+        else:
+            ro = _rows(q_out, shape, dt, "q_out")
     _launch(B.tasp_seq_append, dev, stream, cache.struct, layer, None if rope is None else rope.struct,
             cache._parent(parent, T), T, _SEQ_TYPES[dt], rq, _rows(k, kv, dt, "k"), _rows(v, kv, dt, "v"), n_q, ro)
     return q_out
@@ -512,12 +524,16 @@ def seq_read(cache, layer, n, first=None, dtype=torch.bfloat16, out=None, stream
     shape = (cache.batch, cache.n_kv, n, cache.dh)
     if out is not None:
         k, v = out
+        dev, dt = _device(cache.k, first, k, v), k.dtype
+        rk, rv = _rows(k, shape, dt, "k", 2, 1), _rows(v, shape, dt, "v", 2, 1)
     else:
-        k = _empty(shape, dtype, cache.k.device, stream)
+        dev, dt = _device(cache.k, first), dtype
+        k = _empty(shape, dt, cache.k.device, stream)
         v = _like(k, stream)
-    dev, dt = _device(cache.k, first, k, v), k.dtype
+        strides = cache.n_kv * n * cache.dh, cache.dh, n * cache.dh
+        rk, rv = _dense(k, *strides), _dense(v, *strides)
     _launch(B.tasp_seq_read, dev, stream, cache.struct, layer, _ptr(first, (cache.batch,), torch.int32, "first"), n,
-            _SEQ_TYPES[dt], _rows(k, shape, dt, "k", 2, 1), _rows(v, shape, dt, "v", 2, 1))
+            _SEQ_TYPES[dt], rk, rv)
     return k, v
 
 
@@ -533,14 +549,17 @@ def tree_attention(cache, layer, q, parent=None, scale=None, max_len=None, out=N
     dev, dt = _device(cache.k, q, parent, out), q.dtype
     T, n_q = q.shape[1], q.shape[2]
     shape = (cache.batch, T, n_q, cache.dh)
+    rq = _rows(q, shape, dt, "q")
     if out is None:
         out = _like(q, stream)
+        ro = _dense(out, T * n_q * cache.dh, n_q * cache.dh, cache.dh)
+    else:
+        ro = _rows(out, shape, dt, "out")
     if max_len is None:
         max_len = cache.max_seq
     ws = workspace if workspace is not None else tree_attention_workspace(cache, n_q, T, max_len, stream)
     _launch(B.tasp_tree_attention, dev, stream, cache.struct, layer, cache._parent(parent, T), T, _SEQ_TYPES[dt],
-            _rows(q, shape, dt, "q"), n_q, cache.dh ** -0.5 if scale is None else scale, max_len,
-            _rows(out, shape, dt, "out"), ws[1], ws[2])
+            rq, n_q, cache.dh ** -0.5 if scale is None else scale, max_len, ro, ws[1], ws[2])
     return out
 
 
