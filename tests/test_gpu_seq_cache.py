@@ -216,3 +216,26 @@ def test_commit(kind, dh):
     S.seq_commit(c, torch.from_numpy(path).cuda(), torch.from_numpy(n).cuda())
     torch.cuda.synchronize()
     assert c.len.tolist() == [4, 22, 75, 9, -4, 100]
+
+
+@pytest.mark.parametrize("kind,dh", [("bf16", 128), ("int8", 128), ("e4m3", 64)])
+def test_commit_of_many_heads(kind, dh):
+    """Several heads per workgroup, long paths that name rows which earlier entries replace."""
+    flush(f"case commit of many heads {kind} {dh}")
+    lens, T = [5, 0, 31, -1], 64
+    c, kv, vv = typed_cache(lens, 8, 96, dh, kind, 7, layers=64)
+    rng = np.random.default_rng(8)
+    path = np.stack([np.sort(rng.permutation(T)) if b == 0 else rng.integers(0, T, T) for b in range(4)]).astype(np.int32)
+    path[1, :40] = np.arange(40)[::-1]                 # rows swapped end for end
+    n = np.array([64, 40, 64, 7], np.int32)
+    before = {name: getattr(c, name).clone() for name in ("k", "v", "k_scale", "v_scale") if getattr(c, name) is not None}
+    out = S.seq_commit(c, torch.from_numpy(path).cuda(), torch.from_numpy(n).cuda(), len_out=torch.zeros(4, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert out.tolist() == [69, 40, 95, -1]
+    for name, old in before.items():
+        want = old.clone()
+        for b in range(3):
+            for i in range(n[b]):
+                if lens[b] + path[b, i] < 96 and lens[b] + i < 96:
+                    want[:, b, :, lens[b] + i] = old[:, b, :, lens[b] + path[b, i]]
+        assert torch.equal(getattr(c, name).view(torch.uint8), want.view(torch.uint8)), name
