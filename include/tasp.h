@@ -528,8 +528,9 @@ tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int3
  * 0..len - 1, its ancestors' rows and its own, with scores scale * q . k. q, out: n_q_heads heads (a multiple
  * of n_kv_heads, at most 8 per KV head; query head h reads KV head h / (n_q_heads / n_kv_heads)) of act_type;
  * out must not overlap q or the cache. Outputs of absent nodes are zeros, and what absent or unseen
- * rows hold (NaN, infinities) reaches no output. TASP_BF16: q and V exact, probabilities in 16 bits, sums in
- * float32; TASP_F32: everything to 24 bits. max_len: the largest length expected (0..max_seq): it sizes launches and
+ * rows hold (NaN, infinities) reaches no output. TASP_BF16: q and V exact, probabilities in 16 bits (with more than
+ * 32 query rows, T x heads per KV head, over an 8-bit cache: in 11 bits, and to 2^-29 of the largest value that the row
+ * sees), sums in float32; TASP_F32: everything to 24 bits. max_len: the largest length expected (0..max_seq): it sizes launches and
  * workspace; longer sequences are served too. workspace: device, 256-byte aligned, at least
  * tasp_tree_attention_workspace_bytes for the same cache shape, n_q_heads, T and max_len; its contents need
  * no clearing; calls that overlap need one each. Stream-ordered, capturable (one or two kernels). Errors as
@@ -559,8 +560,8 @@ tasp_status tasp_tree_attention(const tasp_seq_cache* cache, int32_t layer, cons
  *   n (device int32 [batch]): tokens emitted, the accepted ones and one more; ids (device int32 [batch][T]): those
  *   tokens, then -1; path (device int32 [batch][T]): the nodes 0, ... of the accepted path (n entries), then -1.
  * All sums in float64. workspace: device, 256-byte aligned, at least tasp_verify_workspace_bytes, needs no clearing;
- * calls that overlap need one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, temperature
- * negative or not finite, draft_logits with a tree), TASP_ERR_SHAPE (batch, T, vocab), TASP_ERR_WORKSPACE. */
+ * calls that overlap need one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, a temperature
+ * neither 0 nor in 1e-30..1e30, draft_logits with a tree), TASP_ERR_SHAPE (batch, T, vocab), TASP_ERR_WORKSPACE. */
 tasp_status tasp_verify_workspace_bytes(int32_t batch, int32_t T, int32_t vocab, size_t* bytes);
 tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float* u,
                         const int32_t* parent, const float* draft_logits, int32_t batch, int32_t T,
@@ -587,7 +588,7 @@ tasp_status tasp_tree_step_workspace_bytes(tasp_plan plan, const tasp_seq_cache*
 
 /* The plan's layers over trees of T nodes of every sequence (any plan format; projections as tasp_prefill, attention
  * as tasp_tree_attention with TASP_F32 over the retained groups): x (device) float32 [batch][T][d_model], out (device, not overlapping
- * x) float32 [batch][T][vocab], or [batch][T][d_model] without an LM head. Appends the nodes' k and v to every
+ * x; both 16-byte aligned) float32 [batch][T][vocab], or [batch][T][d_model] without an LM head. Appends the nodes' k and v to every
  * layer (positions len + depth, rotate-half RoPE with the plan's base; only retained groups' rows are written);
  * the lengths stay. Rows of out of absent nodes hold values of no meaning. The cache must be bound to the plan
  * (else TASP_ERR_CACHE_PLAN_MISMATCH). Stream-ordered, capturable; calls on one plan must be ordered. */
@@ -601,7 +602,8 @@ tasp_status tasp_tree_forward(tasp_plan plan, const float* x, const int32_t* par
  * ids[b][n[b] - 1]. Nothing waits for the host: lengths, tokens and acceptance stay on the device, and a step can be
  * captured into a HIP graph and replayed with new tokens in the same arrays (max_len then is an upper bound for the
  * replays). embed, embed_scale as tasp_generate; x_scratch float32 [batch][T][d_model]; logits float32
- * [batch][T][vocab] receive the target's logits. T = 1 decodes one token of every sequence by sampling or
+ * [batch][T][vocab] receive the target's logits (both 16-byte aligned). A drafted token outside the vocabulary is not
+ * accepted, and reaches its descendants alone. T = 1 decodes one token of every sequence by sampling or
  * greedily. Requires an LM head (else TASP_ERR_UNSUPPORTED). */
 tasp_status tasp_tree_step(tasp_plan plan, const int8_t* embed, const float* embed_scale,
                            const int32_t* tokens, const int32_t* parent, const float* u,

@@ -2222,8 +2222,9 @@ tasp_status check_verify(const float* logits, const int32_t* tokens, const float
   if (st) return st;
   if (!logits || !tokens || !ids || !path || !n)
     return fail(TASP_ERR_INVALID_ARG, "logits / tokens / ids / path / n is NULL");
-  if (!(temperature >= 0.0) || !std::isfinite(temperature) || (temperature > 0.0 && !std::isfinite(1.0 / temperature)))
-    return fail(TASP_ERR_INVALID_ARG, "temperature must be 0 or positive");
+  // (beyond these, what a temperature makes of the largest and smallest differences of two floats leaves 64 bits)
+  if (!(temperature == 0.0 || (temperature >= 1e-30 && temperature <= 1e30)))
+    return fail(TASP_ERR_INVALID_ARG, "temperature %g is neither 0 nor in 1e-30..1e30", temperature);
   if (temperature > 0.0 && !u) return fail(TASP_ERR_INVALID_ARG, "u is NULL");
   if (draft_logits && parent) return fail(TASP_ERR_INVALID_ARG, "draft_logits go with chains (parent NULL)");
   for (const void* p : {(const void*)logits, (const void*)tokens, (const void*)u, (const void*)parent,
@@ -2379,6 +2380,7 @@ tasp_status tasp_tree_forward(tasp_plan p, const float* x, const int32_t* parent
       (st = step_layout(p, cache, T, max_len, &attn, &total)))
     return st;
   if (!x || !out) return fail(TASP_ERR_INVALID_ARG, "x / out is NULL");
+  if (!aligned(x, 16) || !aligned(out, 16)) return fail(TASP_ERR_INVALID_ARG, "x / out is not 16-byte aligned");
   if (cache->plan_sig != p->sig)
     return fail(TASP_ERR_CACHE_PLAN_MISMATCH, "cache belongs to plan %016llx, not %016llx",
                 (unsigned long long)cache->plan_sig, (unsigned long long)p->sig);
@@ -2410,6 +2412,8 @@ tasp_status tasp_tree_step(tasp_plan p, const int8_t* embed, const float* embed_
       (st = check_tree(parent, T, false)))
     return st;
   if (!x_scratch) return fail(TASP_ERR_INVALID_ARG, "x_scratch is NULL");
+  if (!aligned(x_scratch, 16) || !aligned(logits, 16) || !aligned(embed, 4) || !aligned(embed_scale, 4))
+    return fail(TASP_ERR_INVALID_ARG, "x_scratch / logits (16 bytes) or the embedding (4) is not aligned");
   const size_t rows = size_t(T) * cache->batch;
   const char *xb = reinterpret_cast<const char*>(x_scratch), *ob = reinterpret_cast<const char*>(logits);
   if (ob < xb + rows * d.d_model * 4 && xb < ob + rows * d.vocab * 4)

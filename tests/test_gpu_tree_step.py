@@ -253,3 +253,27 @@ def test_step_refusals():
     headless.seq_bind(c)
     refused("TASP_ERR_UNSUPPORTED", lambda: headless.tree_step(emb[:0], sc[:0], tk, c))
     assert c.len.tolist() == [0, 0]
+
+
+def test_drafts_outside_the_vocabulary():
+    """Tokens outside the vocabulary in a branch: they are not accepted, and the other branch goes on as without them."""
+    flush("case drafts outside the vocabulary")
+    sh = Shape(2, 512, 8, 2, 64, 1536, vocab=512)
+    T0 = 30
+    plan, emb, sc, prompt, kv, text = request(sh, T0, 8)
+    kv2 = S.KVCache(plan.desc, 1, kv.k.shape[3])
+    x = (emb[prompt.long()].float() * sc[prompt.long(), None]).contiguous()
+    plan.prefill_last(x, T0, kv2, 0, torch.empty((sh.vocab,), device="cuda"))
+    parent = torch.tensor([[-1, 0, 0, 2, 3, 1]], dtype=torch.int32, device="cuda")      # 0 - 2 - 3 - 4 and 0 - 1 - 5
+    right = [int(t) for t in text[:4]]
+    outs = []
+    for kind in ("bf16", "int8"):
+        for wrong in ((7, 9), (-5, 512), (2 ** 31 - 1, -2 ** 31)):
+            cache = packed(plan, kv2, kind, T0, 1)
+            tokens = torch.tensor([[right[0], wrong[0], right[1], right[2], right[3], wrong[1]]], dtype=torch.int32, device="cuda")
+            ids, path, n = plan.tree_step(emb, sc, tokens, cache, parent=parent)
+            torch.cuda.synchronize()
+            k, v = S.seq_read(cache, 1, T0 + 6)
+            outs.append((ids.tolist(), path.tolist(), cache.len.item(), k[:, :, :T0 + 4].isfinite().all().item() and v[:, :, :T0 + 4].isfinite().all().item()))
+            assert path.tolist() == [[0, 2, 3, 4, -1, -1]] and outs[-1][3]
+        assert outs[-1] == outs[-2] == outs[-3]

@@ -129,3 +129,53 @@ def test_a_vocabulary_with_equal_shares():
     u = (k.double() / V).float()[:, None]
     ids, _, _ = run(torch.zeros((Bn, 1, V)), torch.zeros((Bn, 1), dtype=torch.int32), u, None, None, 1.0)
     assert ids[:, 0].tolist() == k.tolist()
+
+
+@pytest.mark.parametrize("draft", [False, True])
+def test_a_vocabulary_of_more_chunks_than_lanes(draft):
+    flush(f"case wide vocabulary {draft}")
+    V, T = 300001, 3
+    g = gen(21)
+    logits = torch.randn((3, T, V), generator=g)
+    logits[1] *= 0.01                   # nearly even: the last token lies anywhere
+    logits[2, :, :280000] = -math.inf
+    dl = logits[:, :2] + torch.randn((3, 2, V), generator=g) if draft else None
+    tokens = torch.tensor([[0, 5, 6], [0, 299999, 7], [0, 300000, 290000]], dtype=torch.int32)
+    u = torch.tensor([[0.3, 0.9, 0.1], [0.97, 0.9, 0.2], [0.999, 0.0, 0.9]])
+    check(run(logits, tokens, u, None, dl, 0.9), logits, tokens, u, None, dl, 0.9)
+    check(run(logits, tokens, u, None, dl, 0.0), logits, tokens, u, None, dl, 0.0)
+
+
+def test_ends_of_the_temperature():
+    """The coldest takes the largest logit whatever u; the hottest gives every finite logit the same share."""
+    flush("case temperatures")
+    V = 6000
+    logits = torch.randn((4, 1, V), generator=gen(22)) * 1e30
+    logits[:, :, 100:200] = -math.inf
+    logits[1, 0, 5999] = torch.finfo(torch.float32).max
+    u = torch.tensor([[0.0], [0.5], [0.25], [0.999]])
+    tokens = torch.zeros((4, 1), dtype=torch.int32)
+    ids, _, _ = run(logits, tokens, u, None, None, 1e-30)
+    assert ids[:, 0].tolist() == logits[:, 0].argmax(-1).tolist()
+    flat = logits / 1e30
+    ids, _, _ = run(flat, tokens, u, None, None, 1e30)
+    ok = torch.cat([torch.arange(100), torch.arange(200, V)])
+    want = [int(ok[int(x * 5900)]) for x in u[:, 0].double().tolist()]
+    # differences of 1 weigh 1e-30 at this temperature: shares are equal to all of 64 bits; u on a border takes the token behind it
+    assert ids[:, 0].tolist() == want
+
+
+def test_two_calls_at_once():
+    """Calls on two streams with a workspace each, a raw stream among them, give what they give alone."""
+    flush("case two streams")
+    a, b = (inputs(4, 9, 20000, 30 + k, False, True, 0.8) for k in range(2))
+    alone = [run(*x, 0.8) for x in (a, b)]
+    dev = [[None if t is None else t.cuda() for t in x] for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [S.verify(*x, 0.8, stream=s.cuda_stream) for x, s in zip(dev, streams)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, alone):
+            for p, q in zip(g, w):
+                assert np.array_equal(p.cpu().numpy(), q)

@@ -167,3 +167,25 @@ def test_session_refuses_tensors_before_the_library():
     assert (r.p, r.seq, r.token, r.head) == (k.data_ptr(), 1024, 64, 512)
     assert B.tasp_rows.from_buffer_copy(S._rows(k[0, :, :1], (2, 1, 8, 64), torch.bfloat16, "k")).token == 0
     assert C.sizeof(B.tasp_rows) == 32 and C.sizeof(B.tasp_seq_cache) == 72 and C.sizeof(B.tasp_rope) == 56
+
+
+@pytest.mark.parametrize("t", [1e-31, 1e31, -1e-30, 5e-324])
+def test_temperatures_out_of_range(t):
+    B.load()
+    nb = B.tasp_verify_workspace_bytes(1, 1, 100)
+    refused("TASP_ERR_INVALID_ARG", B.tasp_verify, FAKE, FAKE, FAKE, None, None, 1, 1, 100, t, FAKE, FAKE, FAKE, FAKE, nb, None)
+
+
+def test_types_that_are_no_activations():
+    k = torch.zeros((1, 2, 2, 8, 64), dtype=torch.float16)
+    with pytest.raises(ValueError, match="float16"):
+        S._SEQ_TYPES[k.dtype]
+
+
+def test_plan_steps_refuse_no_plan():
+    c = cache()
+    refused("TASP_ERR_INVALID_ARG", B.tasp_seq_bind, None, c)
+    refused("TASP_ERR_INVALID_ARG", B.tasp_tree_step_workspace_bytes, None, c, 4, 100)
+    refused("TASP_ERR_INVALID_ARG", B.tasp_tree_forward, None, FAKE, None, 4, c, 100, FAKE, FAKE, 1 << 30, None)
+    refused("TASP_ERR_INVALID_ARG", B.tasp_tree_step, None, FAKE, FAKE, FAKE, None, FAKE, None, 1.0, 4, 100, c, FAKE, FAKE,
+            FAKE, FAKE, FAKE, FAKE, 1 << 30, None)
