@@ -67,7 +67,7 @@ struct TreeAttnArgs {
   unsigned short q_start[65];
   float scale2;                        // scale * log2(e)
   int max_len;                         // largest length expected (sizes the grid; any length is served)
-  float* ws;                           // records, tree_attn_workspace_bytes
+  float* ws;                           // tree_attn_workspace_bytes
 };
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a);
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s);

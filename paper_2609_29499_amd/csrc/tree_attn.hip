@@ -324,7 +324,7 @@ struct Place {
   int b, g, rb;                        // sequence, slot, block of query rows
   int h0, group, R;                    // the slot's first query head, its heads, its query rows
   size_t unit;                         // its cache head among those of all sequences
-  int n_ch, rec;                       // chunks or pieces of the sequence, and this one's record
+  int n_ch, ch, before, rec;           // chunks or pieces of the sequence, this one, those of the sequences before, its record
   int L, Lr, end;                      // length (-1: passed over), rows cached, rows that may be read
   int s0, s1;                          // steps
   bool more;                           // another piece follows
@@ -344,7 +344,6 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   p.group = a.q_start[p.g + 1] - p.h0;
   p.R = a.T * p.group;
   if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
-  int ch;
   p.more = false;
   if (SPAN && y.span) {
     // sequences that end before the slot come first; the slot's own follow one another
@@ -356,7 +355,7 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
     auto starts = [&](int b) { return b < a.c.batch && pick(d.slot, b >> 2, b & 3) <= all; };
     if (!starts(p.b)) return false;
     p.more = starts(p.b + 1);
-    ch = all - pick(d.slot, p.b >> 2, p.b & 3);
+    p.ch = all - pick(d.slot, p.b >> 2, p.b & 3);
   } else {
     int hit = -1;
 #pragma unroll
@@ -364,11 +363,12 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
       if (all >= d.before[i] && all < d.before[i] + d.mine[i]) hit = i;
     const int owner = __ffsll((long long)__ballot(hit >= 0)) - 1;
     p.b = 4 * owner + __builtin_amdgcn_readlane(hit, owner);
-    ch = all - pick(d.before, owner, p.b & 3);
+    p.ch = all - pick(d.before, owner, p.b & 3);
   }
   const int owner = p.b >> 2, sub = p.b & 3;
   p.n_ch = pick(d.mine, owner, sub);
-  p.rec = ((pick(d.before, owner, sub) + ch) * a.slots + p.g) * y.rb + p.rb;
+  p.before = pick(d.before, owner, sub);
+  p.rec = ((p.before + p.ch) * a.slots + p.g) * y.rb + p.rb;
   p.unit = size_t(p.b) * a.c.n_kv + a.kv_map[p.g];
   p.L = pick(d.len, owner, sub);
   p.Lr = max(p.L, 0);
@@ -381,8 +381,8 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   } else {
     // the last chunk of a sequence takes what is left (with `most` chunks that may be more than a chunk)
     const int per = p.n_ch * d.chunk >= steps ? d.chunk : ((steps + p.n_ch - 1) / p.n_ch + 3) / 4 * 4;
-    p.s0 = ch * per;
-    p.s1 = ch == p.n_ch - 1 ? steps : min(steps, p.s0 + per);
+    p.s0 = p.ch * per;
+    p.s1 = p.ch == p.n_ch - 1 ? steps : min(steps, p.s0 + per);
   }
   return true;
 }
@@ -408,9 +408,15 @@ __device__ __forceinline__ void put_output(const TreeAttnArgs& a, int b, int t, 
 // A record: [RB][DH] outputs, then [RB] (maximum, sum).
 template <int DH, int RB>
 constexpr size_t kRecFloats = size_t(RB) * (DH + 2);
+// The workspace starts with (chunks, chunks of the sequences before) of each sequence, for the join, which then has no
+// lengths to read and nothing to deal (0.7 us).
+constexpr size_t kHeadFloats = 2 * 256;
+__device__ __forceinline__ void put_head(const TreeAttnArgs& a, const Place& p) {
+  if (p.ch == 0 && p.g == 0 && p.rb == 0 && threadIdx.x == 0) reinterpret_cast<int2*>(a.ws)[p.b] = make_int2(p.n_ch, p.before);
+}
 template <int DH, int RB, int N>
 __device__ __forceinline__ void put_record(const TreeAttnArgs& a, int rec, int row, int d0, float m, float l, const float (&v)[N]) {
-  float* po = a.ws + size_t(rec) * kRecFloats<DH, RB>;
+  float* po = a.ws + kHeadFloats + size_t(rec) * kRecFloats<DH, RB>;
 #pragma unroll
   for (int e = 0; e < N; e += 4)
     *reinterpret_cast<float4*>(po + row * DH + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
@@ -481,6 +487,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
   Place p;
   if (!place<false>(a, y, lane, 0, p)) return;
   const int b = p.b, rb = p.rb, L = p.L, Lr = p.Lr, end = p.end, s0 = p.s0, s1 = p.s1;
+  if (y.most > 1) put_head(a, p);
   // steps from s_edge on hold rows of the tree: at most three, so a wave has one at most
   const int s_edge = min(Lr / kStep, s1);
 
@@ -724,6 +731,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
     if (!place<true>(a, y, lane, piece, p)) return;
     if (piece > 0) __syncthreads();      // (LDS is read no more)
     const int Lr = p.Lr, end = p.end;
+    if (y.most > 1) put_head(a, p);
     const size_t unit = p.unit;
     const uint32_t row_bytes = DH * ES;
     const bool for_v = wave < 2;         // this wave brings V (32 rows), or K
@@ -964,8 +972,8 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   __shared__ float s_m[ROWS][PARTS], s_l[ROWS][PARTS];
   __shared__ float4 s_o[ROWS][PARTS][LPR];
   const int tid = threadIdx.x, b = blockIdx.y;
-  const Deal d = deal<true>(a, y, tid & 63);
-  const int n = pick(d.mine, b >> 2, b & 3), before = pick(d.before, b >> 2, b & 3);
+  const int2 head = reinterpret_cast<const int2*>(a.ws)[b];
+  const int n = head.x, before = head.y;
   if (n <= 1) return;                  // written already
   const int mine = tid / (LPR * PARTS), q_row = blockIdx.x * ROWS + mine;
   const int th = quot(min(q_row, a.T * a.slots * a.group - 1), a.group), t = quot(th, a.slots), g = th - t * a.slots;
@@ -974,7 +982,7 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   const bool there = own < group;      // (others repeat a row, and store nothing)
   const int row = t * group + hh, rows = y.rows, rb = row >> y.rows_log, in = row & (rows - 1);
   const size_t rec = size_t(rows) * (DH + 2), stride = rec * a.slots * y.rb;
-  const float* first = a.ws + before * stride + (size_t(g) * y.rb + rb) * rec;
+  const float* first = a.ws + kHeadFloats + before * stride + (size_t(g) * y.rb + rb) * rec;
   const int part = tid / LPR % PARTS, d0 = 4 * (tid % LPR);
   float m = -INFINITY, l = 0.0f;
   float v[4] = {};
@@ -1043,7 +1051,7 @@ TreeShape shape(const TreeAttnArgs& a) {
 
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a) {
   const TreeShape y = shape(a);
-  return y.most == 1 ? 0 : size_t(y.room) * y.rows * (a.c.dh + 2) * 4;
+  return y.most == 1 ? 0 : (kHeadFloats + size_t(y.room) * y.rows * (a.c.dh + 2)) * 4;
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s) {
