@@ -2115,8 +2115,7 @@ tasp_status tree_attn_args(const tasp_seq_cache* c, int32_t n_q, int32_t T, int3
     return fail(TASP_ERR_SHAPE, "%d query heads over %d KV heads (1..8 per KV head)", n_q, c->n_kv_heads);
   if (max_len < 0 || max_len > c->max_seq) return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_seq);
   a->T = T; a->max_len = max_len; a->slots = c->n_kv_heads; a->group = n_q / c->n_kv_heads;
-  for (int j = 0; j < a->slots; ++j) a->kv_map[j] = (unsigned char)j;
-  for (int j = 0; j <= a->slots; ++j) a->q_start[j] = (unsigned short)(j * a->group);
+  for (int j = 0; j < a->slots; ++j) a->slot[j] = tasp::tree_slot(j, j * a->group, a->group);
   return TASP_OK;
 }
 
@@ -2338,11 +2337,10 @@ tasp_status tree_forward(tasp_plan p, const float* x, const int32_t* parent, int
     tasp::TreeAttnArgs t{};
     t.c = layer; t.parent = parent; t.T = T; t.act = TASP_F32; t.max_len = max_len; t.slots = P.m_kv;
     for (int j = 0; j < P.m_kv; ++j) {
-      t.kv_map[j] = (unsigned char)P.kv_idx[j];
-      t.q_start[j] = (unsigned short)P.slot_start[j];
-      t.group = std::max(t.group, P.slot_start[j + 1] - P.slot_start[j]);
+      const int heads = P.slot_start[j + 1] - P.slot_start[j];
+      t.slot[j] = tasp::tree_slot(P.kv_idx[j], P.slot_start[j], heads);
+      t.group = std::max(t.group, heads);
     }
-    t.q_start[P.m_kv] = (unsigned short)P.m_q;
     t.q = a.q_out;
     t.o = {p->pxw, long(T) * p->ld_xw, p->ld_xw, dh};
     t.scale2 = float(1.44269504088896340736 / std::sqrt(double(dh)));

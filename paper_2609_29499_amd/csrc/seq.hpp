@@ -60,17 +60,20 @@ struct TreeAttnArgs {
   const int* parent; int T;
   int act;
   SeqRows q, o;
-  // slots: cache heads that are read; slot j reads head kv_map[j] for query heads q_start[j] .. q_start[j + 1] - 1,
+  // slots: cache heads that are read, slot[j] (tree_slot) says which and for which query heads,
   // 1 .. group of them
   int slots, group;
-  unsigned char kv_map[64];
-  unsigned short q_start[65];
+  int slot[64];
   float scale2;                        // scale * log2(e)
   int max_len;                         // largest length expected (sizes the grid; any length is served)
   float* ws;                           // tree_attn_workspace_bytes
 };
 size_t tree_attn_workspace_bytes(const TreeAttnArgs& a);
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t s);
+
+// a cache head, its first query head and their number in one word (a scalar load; one byte of an array is a vector's,
+// 1 us where nothing else is on its way)
+inline int tree_slot(int head, int first, int count) { return head | first << 8 | count << 20; }
 
 struct VerifyArgs {
   const float* logits; const float* draft;   // [B][T][V], [B][T - 1][V] or null

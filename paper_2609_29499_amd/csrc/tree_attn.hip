@@ -332,16 +332,16 @@ struct Place {
 // piece: 0, 1, .. of the workgroup's
 template <bool SPAN>
 __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y, int lane, int piece, Place& p) {
-  const Deal d = deal<SPAN>(a, y, lane);
   // Grid (8, row blocks, items / 8): row blocks of one chunk and head read the same rows, and are eight workgroups
   // apart (one XCD, one L2) and next to each other in time. Item: chunk of a sequence x slot.
   p.rb = blockIdx.y;
-  const int item = blockIdx.z * 8 + blockIdx.x;
-  if (item >= d.total * a.slots) return false;
-  const int all = quot(item, a.slots);                 // chunk, or slot of the row
+  const int item = blockIdx.z * 8 + blockIdx.x, all = quot(item, a.slots);     // chunk, or slot of the row
   p.g = item - all * a.slots;
-  p.h0 = a.q_start[p.g];
-  p.group = a.q_start[p.g + 1] - p.h0;
+  const int slot = a.slot[p.g];                        // (on its way with the lengths)
+  const Deal d = deal<SPAN>(a, y, lane);
+  if (item >= d.total * a.slots) return false;
+  p.h0 = slot >> 8 & 0xfff;
+  p.group = slot >> 20;
   p.R = a.T * p.group;
   if (p.rb * y.rows >= p.R) return false;              // (a slot with fewer heads than the largest)
   p.more = false;
@@ -369,7 +369,7 @@ __device__ __forceinline__ bool place(const TreeAttnArgs& a, const TreeShape& y,
   p.n_ch = pick(d.mine, owner, sub);
   p.before = pick(d.before, owner, sub);
   p.rec = ((p.before + p.ch) * a.slots + p.g) * y.rb + p.rb;
-  p.unit = size_t(p.b) * a.c.n_kv + a.kv_map[p.g];
+  p.unit = size_t(p.b) * a.c.n_kv + (slot & 0xff);
   p.L = pick(d.len, owner, sub);
   p.Lr = max(p.L, 0);
   p.end = p.L < 0 ? 0 : min(p.L + a.T, a.c.S);
@@ -977,7 +977,7 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
   if (n <= 1) return;                  // written already
   const int mine = tid / (LPR * PARTS), q_row = blockIdx.x * ROWS + mine;
   const int th = quot(min(q_row, a.T * a.slots * a.group - 1), a.group), t = quot(th, a.slots), g = th - t * a.slots;
-  const int h0 = a.q_start[g], group = a.q_start[g + 1] - h0;
+  const int slot = a.slot[g], h0 = slot >> 8 & 0xfff, group = slot >> 20;
   const int own = q_row - th * a.group, hh = min(own, group - 1);
   const bool there = own < group;      // (others repeat a row, and store nothing)
   const int row = t * group + hh, rows = y.rows, rb = row >> y.rows_log, in = row & (rows - 1);
