@@ -17,10 +17,10 @@
 // Softmax with a running maximum per query row, raised only when a score passes it by 8 powers of two (sums
 // are float32, so the slack costs no accuracy): most steps exchange nothing between lanes.
 //
-// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 166 + 12 us,
+// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 170 + 10 us,
 // bound by instructions: 560 of a wave's per step of 64 rows, 64 of them matrix products, two waves per SIMD; a tree of 16
-// over 4 BF16 sequences of 4096 .. 2560 rows (55 MB) 20 + 6.5 us and 8 tokens over 131072 E4M3 rows (277 MB) 56 + 6 us,
-// bound by memory (5 TB/s behind the first 5 us); one token over 2047 INT8 rows 7 + 4.6 us, latency.
+// over 4 BF16 sequences of 4096 .. 2560 rows (55 MB) 20 + 5 us and 8 tokens over 131072 E4M3 rows (277 MB) 56 + 5 us,
+// bound by memory (5 TB/s behind the first 4 us); one token over 2047 INT8 rows 7 + 4 us, latency.
 //
 // Two kernels. Up to 32 query rows (tree_attn_kernel) a wave keeps all of them and walks every fourth step
 // straight from memory in the operands' layout, the next step's loads in flight; no LDS is used before
