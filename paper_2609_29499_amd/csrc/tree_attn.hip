@@ -46,7 +46,8 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 constexpr int kStep = 32;              // cache rows per step
-constexpr int kMinSteps = 4;           // steps of a chunk at least: one per wave
+constexpr int kMinSteps = 4;           // steps of a chunk at least, and its granule: one per wave
+constexpr int kMinWide = 2;            // and in the wide kernel: 64 rows that all waves share
 constexpr float kSlack = 8.0f;         // powers of two a score may pass the running maximum by
 
 // ---- which rows a workgroup serves
@@ -126,7 +127,8 @@ __device__ __forceinline__ Deal deal(const TreeAttnArgs& a, const TreeShape& y, 
     }
   } else {
     const int units = a.slots * y.rb;
-    d.chunk = max(kMinSteps, (int((long(sum) * units + kTarget - 1) / kTarget) + 3) / 4 * 4);
+    const int least = y.wide ? kMinWide : kMinSteps;
+    d.chunk = max(least, (int((long(sum) * units + kTarget - 1) / kTarget) + least - 1) / least * least);
     if (a.c.batch > 1 && 2 * a.c.batch <= y.quota) {
       // Sequences are rounded up to whole chunks: the shortest chunk that keeps all workgroups within the target is
       // looked for, a candidate per lane (workgroups beyond it would make a second round)
@@ -1033,9 +1035,9 @@ TreeShape shape(const TreeAttnArgs& a) {
   y.rows = 16 * block;
   y.rows_log = 31 - __builtin_clz(y.rows);
   y.rb = (tiles + block - 1) / block;
-  const int units = a.slots * y.rb;
+  const int units = a.slots * y.rb, least = y.wide ? kMinWide : kMinSteps;
   const long steps = (std::min<long>(std::max(a.max_len, 0) + long(a.T), a.c.S) + kStep - 1) / kStep;
-  y.most = int(std::max<long>(1, std::min<long>((steps + kMinSteps - 1) / kMinSteps, (kTarget + units - 1) / units)));
+  y.most = int(std::max<long>(1, std::min<long>((steps + least - 1) / least, (kTarget + units - 1) / units)));
   // chunks of all sequences: their steps over the chunk's, rounded up per sequence
   const long chunks = std::min<long>(long(a.c.batch) * y.most, kTarget / units + 1 + a.c.batch);
   y.room = int(chunks) * a.slots * y.rb;
