@@ -2076,8 +2076,8 @@ tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
     return fail(TASP_ERR_SHAPE, "rot_dim %d (a multiple of 16 up to %d)", r->rot_dim, dh);
   if (r->scaling < TASP_ROPE_NONE || r->scaling > TASP_ROPE_INDEX)
     return fail(TASP_ERR_INVALID_ARG, "rope scaling %d", r->scaling);
-  if (!(r->theta > 1.0) || !std::isfinite(r->theta) || !std::isfinite(r->mscale))
-    return fail(TASP_ERR_INVALID_ARG, "rope theta must be above 1, mscale finite");
+  if (!(r->theta > 1.0) || !std::isfinite(r->theta) || !std::isfinite(float(r->mscale)))
+    return fail(TASP_ERR_INVALID_ARG, "rope theta must be above 1, mscale finite in 32 bits");
   if (r->scaling != TASP_ROPE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
     return fail(TASP_ERR_INVALID_ARG, "rope factor must be positive");
   if (r->scaling >= TASP_ROPE_WAVELENGTH &&
@@ -2087,23 +2087,21 @@ tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
   const int n = r->rot_dim;
   a->rot = n;
   a->interleaved = r->layout == TASP_ROPE_INTERLEAVED;
-  a->mscale = r->mscale;
-  double lo = 0.0, hi = 0.0;
-  if (r->scaling == TASP_ROPE_INDEX) {
-    auto index = [&](double turns) { return n * std::log(r->orig_len / (kTurn * turns)) / (2.0 * std::log(r->theta)); };
-    lo = std::max(std::floor(index(r->high)), 0.0);
-    hi = std::min(std::ceil(index(r->low)), double(n - 1));
+  a->mscale = float(r->mscale);
+  const double log_theta = std::log(r->theta);
+  for (int k = 0; k < 6; ++k) a->power[k] = n ? std::exp(-2.0 * (1 << k) * log_theta / n) : 1.0;
+  // share of the unscaled frequency
+  a->mul = 0.0; a->add = r->scaling == TASP_ROPE_NONE ? 1.0 : 0.0; a->keep = r->scaling == TASP_ROPE_NONE ? 1.0 : 1.0 / r->factor;
+  a->by_index = r->scaling == TASP_ROPE_INDEX;
+  if (r->scaling == TASP_ROPE_WAVELENGTH) {
+    a->mul = r->orig_len / (kTurn * (r->high - r->low));
+    a->add = -r->low / (r->high - r->low);
   }
-  // f_i by repeated multiplication: 64 roundings of 1e-16 at most, and no power function per call and pair
-  const double step = n ? std::exp(-2.0 * std::log(r->theta) / n) : 1.0;
-  double f = 1.0;
-  for (int i = 0; i < n / 2; ++i, f *= step) {
-    double g = 1.0;                    // share of the unscaled frequency
-    if (r->scaling == TASP_ROPE_LINEAR) g = 0.0;
-    if (r->scaling == TASP_ROPE_WAVELENGTH) g = (r->orig_len * f / kTurn - r->low) / (r->high - r->low);
-    if (r->scaling == TASP_ROPE_INDEX) g = 1.0 - (i - lo) / std::max(hi - lo, 0.001);
-    g = std::min(1.0, std::max(0.0, g));
-    a->inv_freq[i] = r->scaling == TASP_ROPE_NONE ? f : f * (g + (1.0 - g) / r->factor);
+  if (r->scaling == TASP_ROPE_INDEX) {
+    auto index = [&](double turns) { return n * std::log(r->orig_len / (kTurn * turns)) / (2.0 * log_theta); };
+    const double lo = std::max(std::floor(index(r->high)), 0.0), hi = std::min(std::ceil(index(r->low)), double(n - 1));
+    a->mul = -1.0 / std::max(hi - lo, 0.001);
+    a->add = 1.0 - lo * a->mul;
   }
   return TASP_OK;
 }

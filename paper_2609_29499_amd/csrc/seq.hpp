@@ -33,8 +33,12 @@ struct SeqAppendArgs {
   int n_q, n_kv;                       // head rows of q; of k and v
   const int* kv_map;                   // host: cache head of k / v head j (null: j), used by the launch
   int rot, interleaved;                // rotated dimensions of a head; pair layout
-  double mscale;
-  double inv_freq[64];                 // of the rot / 2 pairs
+  // Pair i's frequency: f = theta^(-2 i / rot), the product of power[k] = theta^(-2 2^k / rot) over the bits of i, times
+  // g + (1 - g) keep, g = (by_index ? i : f) mul + add cut to 0 .. 1. (64 frequencies as arguments cost a launch 0.6 us.)
+  double power[6];
+  double mul, add, keep;
+  float mscale;
+  int by_index;
 };
 hipError_t launch_seq_append(const SeqAppendArgs& a, hipStream_t s);
 

@@ -8,7 +8,7 @@
 // head rows of one token: a lane holds eight elements of a head, so the row's maximum stays inside 8
 // or 16 lanes and every access is 16 or 32 bytes wide; the token's sines and cosines go through LDS.
 // Bound by memory: q, k and v are read once, q and the rows written once (2 x 8192 tokens of 32 + 2 x 8 heads of 128 in
-// float32 into INT8, 705 MB: 145 us, 4.9 TB/s; 8 trees of 32, 10 MB: 6.2 us, of which 2 us are the launch).
+// float32 into INT8, 705 MB: 139 us, 5.1 TB/s; 8 trees of 32, 10 MB: 6.5 us, latency: lengths and tree, then sines).
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -70,15 +70,22 @@ __device__ __forceinline__ void store8(void* p, long at, const Vec8& x) {
 
 // Sine and cosine of pos * freq: turns = pos freq / 2 pi is formed and cut to [-1/2, 1/2] in 64 bits;
 // what a 32-bit angle loses of it (d) is put back to first order.
-__device__ __forceinline__ float2 turn(double pos, double freq, double mscale) {
+__device__ __forceinline__ float2 turn(double pos, double freq, float m) {
   double a = pos * (freq * 0.15915494309189533577);
   a -= rint(a);
   a *= 6.28318530717958647693;
   const float x = float(a), d = float(a - double(x));
   float s, c;
   sincosf(x, &s, &c);
-  const float m = float(mscale);
   return make_float2(fmaf(-s, d, c) * m, fmaf(c, d, s) * m);
+}
+
+__device__ __forceinline__ double pair_freq(const SeqAppendArgs& a, int i) {
+  double f = 1.0;
+#pragma unroll
+  for (int k = 0; k < 6; ++k) f *= (i >> k) & 1 ? a.power[k] : 1.0;
+  const double g = fmin(fmax(fma(a.by_index ? double(i) : f, a.mul, a.add), 0.0), 1.0);
+  return f * fma(1.0 - g, a.keep, g);
 }
 
 struct KvMap {
@@ -94,6 +101,29 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
   __shared__ int s_pos, s_row;
   const int tid = threadIdx.x;
   const int b = blockIdx.x / a.T, t = blockIdx.x % a.T;
+  const int total = a.n_q + 2 * a.n_kv;
+  const int r0 = blockIdx.y * rows, r1 = min(total, r0 + rows);
+  const int e0 = kE * (tid % LPR);
+  // A pass's elements, and their partners where pairs lie apart: asked for a pass ahead, the first ahead of the token's
+  // place in its tree. (Rows of absent nodes are read like others; whole rows are in or out, reductions stay inside a row.)
+  struct Pass {
+    Vec8 x, y;
+    int kind, h, head;                 // q, k, v; head; cache head
+  };
+  auto fetch = [&](int r, Pass& p) __attribute__((always_inline)) {
+    const bool in = r < r1;
+    p.kind = !in || r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
+    const SeqRows& src = p.kind == 0 ? a.q : p.kind == 1 ? a.k : a.v;
+    p.h = !in ? 0 : p.kind == 0 ? r : p.kind == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
+    if (!in) return;
+    p.head = p.kind > 0 ? map.h[p.h] : 0;
+    const long row = b * src.seq + t * src.token + p.h * src.head;
+    p.x = load8<ACT>(src.p, row + e0, a);
+    if (p.kind < 2 && e0 < a.rot && !a.interleaved)
+      p.y = load8<ACT>(src.p, row + (e0 < a.rot / 2 ? e0 + a.rot / 2 : e0 - a.rot / 2), a);
+  };
+  Pass next;
+  fetch(r0 + tid / LPR, next);
   if (tid < kWave) {
     const int L = seq_len(a.c.len, b, a.c.S);
     int depth = t, there = 1;
@@ -103,7 +133,7 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
       there = depth >= 0;
     }
     there = there && L >= 0 && L + t < a.c.S;
-    for (int i = tid; i < a.rot / 2; i += kWave) cs[i] = turn(double(L + depth), a.inv_freq[i], a.mscale);
+    for (int i = tid; i < a.rot / 2; i += kWave) cs[i] = turn(double(L + depth), pair_freq(a, i), a.mscale);
     if (tid == 0) {
       s_pos = there ? L + depth : -1;
       s_row = L + t;
@@ -111,18 +141,14 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
   }
   __syncthreads();
   const bool there = s_pos >= 0;
-  const int total = a.n_q + 2 * a.n_kv;
-  const int r0 = blockIdx.y * rows, r1 = min(total, r0 + rows);
-  const int e0 = kE * (tid % LPR);
   for (int r = r0 + tid / LPR; r - tid / LPR < r1; r += RPP) {
-    const bool in = r < r1;            // (whole rows are in or out; reductions stay inside a row)
-    const int kind = !in || r < a.n_q ? 0 : r < a.n_q + a.n_kv ? 1 : 2;
-    const SeqRows& src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-    const int h = !in ? 0 : kind == 0 ? r : kind == 1 ? r - a.n_q : r - a.n_q - a.n_kv;
+    const bool in = r < r1;
+    const Pass now = next;
+    if (r - tid / LPR + RPP < r1) fetch(r + RPP, next);
+    const int kind = now.kind, h = now.h;
     Vec8 x{};
     if (in && there) {
-      const long row = b * src.seq + t * src.token + h * src.head;
-      x = load8<ACT>(src.p, row + e0, a);
+      x = now.x;
       if (kind < 2 && e0 < a.rot) {
         if (a.interleaved) {           // pairs (2 i, 2 i + 1)
 #pragma unroll
@@ -135,11 +161,10 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
         } else {                       // pairs (i, i + rot / 2): the partner's eight elements
           const int half = a.rot / 2;
           const bool first = e0 < half;
-          const Vec8 y = load8<ACT>(src.p, row + (first ? e0 + half : e0 - half), a);
 #pragma unroll
           for (int i = 0; i < kE; ++i) {
             const float2 w = cs[(first ? e0 : e0 - half) + i];
-            x.v[i] = first ? x.v[i] * w.x - y.v[i] * w.y : x.v[i] * w.x + y.v[i] * w.y;
+            x.v[i] = first ? x.v[i] * w.x - now.y.v[i] * w.y : x.v[i] * w.x + now.y.v[i] * w.y;
           }
         }
       }
@@ -149,7 +174,7 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
     }
     if constexpr (TYPE == SEQ_BF16) {
       if (in && there && kind > 0) {
-        const size_t at = (size_t(b) * a.c.n_kv + map.h[h]) * a.c.S + s_row;
+        const size_t at = (size_t(b) * a.c.n_kv + now.head) * a.c.S + s_row;
         store8<SEQ_BF16>(kind == 1 ? a.c.k : a.c.v, long(at * DH + e0), x);
       }
     } else {
@@ -189,7 +214,7 @@ __global__ __launch_bounds__(kBlock) void seq_append_kernel(SeqAppendArgs a, KvM
             w[j] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * j + 2], q[4 * j + 3], o, true));
           }
         }
-        const size_t at = (size_t(b) * a.c.n_kv + map.h[h]) * a.c.S + s_row;
+        const size_t at = (size_t(b) * a.c.n_kv + now.head) * a.c.S + s_row;
         *reinterpret_cast<uint2*>(static_cast<uint8_t*>(kind == 1 ? a.c.k : a.c.v) + at * DH + e0) = make_uint2(w[0], w[1]);
         // a row with an infinity or a NaN has no scale: it reads back as NaN
         if (e0 == 0) (kind == 1 ? a.c.ks : a.c.vs)[at] = top >= 0x7f800000u ? __builtin_nanf("") : amax / QMAX;
