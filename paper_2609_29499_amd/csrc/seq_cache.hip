@@ -330,8 +330,8 @@ hipError_t launch_seq_append(const SeqAppendArgs& a, hipStream_t s) {
   KvMap map{};
   for (int j = 0; j < a.n_kv; ++j) map.h[j] = (unsigned char)(a.kv_map ? a.kv_map[j] : j);
   const int rpp = kBlock / (a.c.dh / kE);
-  // few tokens: one pass of head rows per workgroup (latency); many: a workgroup walks its token's rows, so
-  // that its sines and cosines are formed once
+  // few tokens: one pass of head rows per workgroup (latency: 8 x 32 tokens 6.5 us, 9.4 the other way); many: a
+  // workgroup walks its token's rows, so that its sines and cosines are formed once (2 x 8192 tokens 139 us, 151)
   const int rows = long(a.c.batch) * a.T < 1024 ? rpp : total;
   const dim3 grid(a.c.batch * a.T, (total + rows - 1) / rows);
 #define APPEND(DH, ACT, TYPE) hipLaunchKernelGGL((seq_append_kernel<DH, ACT, TYPE>), grid, dim3(kBlock), 0, s, a, map, rows)
@@ -377,7 +377,8 @@ hipError_t launch_seq_read(const SeqReadArgs& a, hipStream_t s) {
 
 hipError_t launch_seq_commit(const SeqCommitArgs& a, hipStream_t s) {
   const int units = a.n_layers * a.c.batch * a.c.n_kv;
-  // four heads per workgroup where that leaves four workgroups per CU
+  // four heads per workgroup where that leaves four workgroups per CU (5120 heads 11 us, 16.7 the other way; 256 heads
+  // one each 3.5 us, 3.8)
   const bool four = a.c.n_kv % 4 == 0 && units >= 2048;
   const dim3 grid(four ? units / 4 : units, 2);
   const int rb = a.c.dh * (a.c.type == SEQ_BF16 ? 2 : 1);

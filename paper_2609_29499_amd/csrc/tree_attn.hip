@@ -1029,6 +1029,9 @@ __global__ __launch_bounds__(kBlock) void tree_join_kernel(TreeAttnArgs a, TreeS
 TreeShape shape(const TreeAttnArgs& a) {
   TreeShape y;
   const int tiles = (a.T * a.group + 15) / 16;
+  // One or two tiles stay in every wave (8 tokens over 131072 E4M3 rows 57 us, 93 through LDS; one token 7.2, 8.5); more go
+  // through LDS (a tree of 16 with four tiles 20 us, 27 with four in every wave), two tiles per wave where there are
+  // eight and registers for them (64 nodes x 64 heads 232 us when it was tried, 262 with one)
   y.wide = tiles > 2;
   y.mt = y.wide ? (tiles > 4 && a.act == SEQ_BF16 ? 2 : 1) : tiles;
   const int block = (y.wide ? 4 : 1) * y.mt;           // tiles of a workgroup

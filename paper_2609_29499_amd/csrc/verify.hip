@@ -349,8 +349,9 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
 
 // The token of a chunk whose cumulative weight first exceeds `target`, the weights before it being
 // `base`; also the chunk's last token with a weight. w(k, read(k)): weight of token k; the reads of all of a thread's
-// tokens are in flight together. A wave holds consecutive groups of 64 tokens (16 consecutive tokens per thread:
-// 15000 cycles for two rows of logits, for their strided loads), so sums run in token order. found: -1 none, else the token; tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
+// tokens are in flight together. A wave holds consecutive groups of 64 tokens, so sums run in token order (16
+// consecutive tokens per thread: 15000 cycles for two rows of logits, for their strided loads). found: -1 none, else the
+// token; tail: the last token with a weight, -1 none; returns base plus the chunk's weight.
 template <class R, class W>
 __device__ __forceinline__ double scan_chunk(const VerifyArgs& a, int c, double base, double target, WalkSmem& sm, R&& read, W&& w,
                                              int* found, int* tail) {
