@@ -369,7 +369,8 @@ def _ref(struct):
 
 def tasp_seq_append(cache, layer, rope, parent_ptr, T, act_type, q, k, v, n_q_heads, q_out, stream):
     """``cache``, ``rope`` (or None) and the ``tasp_rows`` q, k, v, q_out are structs, their bytes or their addresses."""
-    if type(k) is not bytes:           # (bytes, as the tensor wrappers pass them, are told apart once: a call each costs 0.1 us)
+    # (bytes, as the tensor wrappers pass them, are told apart at once: a call each costs 0.1 us)
+    if not (type(k) is type(v) is bytes and (q is None or type(q) is type(q_out) is bytes)):
         q, k, v, q_out = _ref(q), _ref(k), _ref(v), _ref(q_out)
     st = (_lib or load()).tasp_seq_append(_ref(cache), layer, _ref(rope), parent_ptr, T, act_type, q, k, v, n_q_heads,
                                           q_out, stream)
