@@ -12,13 +12,14 @@
 //     neighbours, so rows are stored whole.
 // Rows in 8 bits become BF16 exactly; their scales multiply scores and probabilities in 32 bits. P is
 // carried as two BF16 terms (16 bits; one alone would double the error of a BF16 output), float32 q and P
-// as three (24 bits, as exact as the products' float32 sums). Over rows in 8 bits under wide trees P is one FP16 term (below).
+// as three (24 bits, as exact as the products' float32 sums). (One FP16 term has 11 bits, and not the range of a
+// probability times a scale; it took 170 us instead of 192 for the 64-node case below, three BF16 terms 225.)
 //
 // Softmax with a running maximum per query row, raised only when a score passes it by 8 powers of two (sums
 // are float32, so the slack costs no accuracy): most steps exchange nothing between lanes.
 //
-// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 170 + 10 us,
-// bound by instructions: 560 of a wave's per step of 64 rows, 64 of them matrix products, two waves per SIMD; a tree of 16
+// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 201 + 10 us,
+// bound by instructions: about 640 of a wave's per step of 64 rows, 96 of them matrix products, two waves per SIMD; a tree of 16
 // over 4 BF16 sequences of 4096 .. 2560 rows (55 MB) 20 + 5 us and 8 tokens over 131072 E4M3 rows (277 MB) 56 + 5 us,
 // bound by memory (5 TB/s behind the first 4 us); one token over 2047 INT8 rows 7 + 4 us, latency.
 //
@@ -178,26 +179,10 @@ __device__ __forceinline__ f32x4 mfma(const uint32_t (&a)[4], const uint32_t (&b
       __builtin_bit_cast(bf16x8, make_uint4(b[0], b[1], b[2], b[3])), acc, 0, 0, 0);
 }
 
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
-// two floats -> packed FP16 (round to nearest even)
-__device__ __forceinline__ uint32_t pack_half(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_seq{a, b}, half2v));
-}
-__device__ __forceinline__ f32x4 mfma_half(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 acc) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(
-      __builtin_bit_cast(f16x8, make_uint4(a[0], a[1], a[2], a[3])),
-      __builtin_bit_cast(f16x8, make_uint4(b[0], b[1], b[2], b[3])), acc, 0, 0, 0);
-}
-
-// four codes of a word -> two words of BF16 pairs (HALF: FP16 pairs); either is exact
-template <int TYPE, bool HALF = false>
+// four codes of a word -> two words of BF16 pairs (exact)
+template <int TYPE>
 __device__ __forceinline__ void widen(uint32_t w, uint32_t* o) {
-  if constexpr (HALF) {
-    static_assert(TYPE == SEQ_E4M3, "");
-    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
-    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
-  } else if constexpr (TYPE == SEQ_INT8) {
+  if constexpr (TYPE == SEQ_INT8) {
     const float f0 = float(int8_t(w)), f1 = float(int8_t(w >> 8)), f2 = float(int8_t(w >> 16)), f3 = float(int8_t(w >> 24));
     o[0] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
     o[1] = __builtin_amdgcn_perm(__float_as_uint(f3), __float_as_uint(f2), 0x07060302u);
@@ -221,17 +206,9 @@ __device__ __forceinline__ void terms(float v0, float v1, uint32_t* o, int strid
 // One query row's scores of a step (lane (r, c): cache rows 4 c + i of both tiles) to the terms of P.
 // t0: the step's first row minus the cached rows, i.e. rows from 0 on are the tree's; EDGE: there are
 // such rows (or rows behind them), of which the row sees those in anc.
-//
-// HALF (rows in 8 bits): P times the rows' scales is one FP16 term. FP16 has the bits (half a step is 2^-11, next to 2^-8 of a
-// BF16 output), but not the range: outputs and sums are carried times 2^lift per query row, which holds the largest scale
-// that the row has seen between 2^4 and 2^7 (x 2^8 for the maximum's slack: below 2^15). What 2^-18 of the largest scale
-// leaves of a probability is a subnormal, off by 2^-29 of the largest value at most.
-struct Lift {
-  float by, limit;                     // lift, and the scale that raises it: 2^(7 - lift); -1: nothing was seen
-};
-template <int NDT, int PT, bool SCALED, bool EDGE, bool HALF>
+template <int NDT, int PT, bool SCALED, bool EDGE>
 __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks)[8], const float (&vs)[8], float scale2, int t0, int c,
-                                          unsigned long long anc, float& m_run, float& l_run, Lift& lift, f32x4 (&o)[NDT], uint32_t (&pf)[PT][4]) {
+                                          unsigned long long anc, float& m_run, float& l_run, f32x4 (&o)[NDT], uint32_t (&pf)[PT][4]) {
   float p[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) p[i] = sc[i >> 2][i & 3] * (SCALED ? ks[i] : scale2);
@@ -246,33 +223,12 @@ __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks
     }
   }
   const float top = fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
-  float w[8], wide = 0.0f;             // the scales of rows that the query row sees, and the largest
-  if constexpr (SCALED) {
+  float w[8];                          // the scales of rows that the query row sees (others' may be anything)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w[i] = !EDGE || ((seen >> i) & 1) ? vs[i] : 0.0f;
-      if constexpr (HALF) wide = fmaxf(wide, w[i]);
-    }
-  }
-  if (__ballot(top > m_run + kSlack || (HALF && wide > lift.limit))) {     // (also the first rows: m_run is -inf)
+  for (int i = 0; i < 8; ++i) w[i] = !SCALED ? 1.0f : !EDGE || ((seen >> i) & 1) ? vs[i] : 0.0f;
+  if (__ballot(top > m_run + kSlack)) {                // (also the first rows: m_run is -inf)
     const float mn = fmaxf(m_run, quad_max(top));
-    float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
-    if constexpr (HALF) {
-      wide = 0.0f;                     // (a scale that is not finite has no part in it)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float x = w[i];
-        asm volatile("" : "+v"(x));    // (or all of this is done ahead of the branch)
-        wide = fmaxf(wide, x < INFINITY ? x : 0.0f);
-      }
-      wide = quad_max(wide);
-      if (wide > lift.limit) {
-        const float by = wide > 0.0f ? float(min(max(5 - __builtin_amdgcn_frexp_expf(wide), -123), 110)) : 0.0f;
-        alpha *= __builtin_amdgcn_exp2f(by - lift.by);
-        lift.by = by;
-        lift.limit = wide > 0.0f ? __builtin_amdgcn_exp2f(7.0f - by) : 0.0f;
-      }
-    }
+    const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run - mn);
     m_run = mn;
     l_run *= alpha;
 #pragma unroll
@@ -282,7 +238,7 @@ __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks
       for (int e = 0; e < NDT; ++e) o[e][i] *= f;
     }
   }
-  const float base = (m_run == -INFINITY ? 0.0f : m_run) - (HALF ? lift.by : 0.0f);
+  const float base = m_run == -INFINITY ? 0.0f : m_run;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     p[i] = __builtin_amdgcn_exp2f(p[i] - base);
@@ -290,17 +246,12 @@ __device__ __forceinline__ void soft_step(const f32x4 (&sc)[2], const float (&ks
     if constexpr (SCALED) p[i] *= w[i];
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (HALF) pf[0][e] = pack_half(p[2 * e], p[2 * e + 1]);
-    else terms<PT>(p[2 * e], p[2 * e + 1], &pf[0][e], 4);
-  }
+  for (int e = 0; e < 4; ++e) terms<PT>(p[2 * e], p[2 * e + 1], &pf[0][e], 4);
 }
 
-// Non-finite halves of V words (BF16, HALF: FP16) become zeros; returns a non-zero word if there are any.
-template <bool HALF = false>
+// Non-finite halves of V words become zeros; returns a non-zero word if there are any.
 __device__ __forceinline__ uint32_t drop_odd(uint32_t& v) {
-  constexpr uint32_t EXP = HALF ? 0x7c007c00u : 0x7f807f80u, ONE = HALF ? 0x04000400u : 0x00800080u;
-  const uint32_t top = ((v & EXP) + ONE) & 0x80008000u;                      // a half's exponent is full
+  const uint32_t top = ((v & 0x7f807f80u) + 0x00800080u) & 0x80008000u;      // a half's exponent is full
   v &= ~((top >> 15) * 0xffffu);
   return top;
 }
@@ -595,12 +546,11 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void tr
     }
     uint32_t pf[MT][PT][4];
     float ks[8];
-    Lift none;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ks[i] = TYPE == SEQ_BF16 ? 0.0f : x.ks[i] * a.scale2;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
-      soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE, false>(sc[mt], ks, x.vs, a.scale2, s * kStep - Lr, c, anc[mt], m_run[mt], l_run[mt], none, o[mt], pf[mt]);
+      soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, x.vs, a.scale2, s * kStep - Lr, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
     // V: eight rows of NDT dimensions as BF16 pairs
     uint32_t v[8][NDT / 2];
 #pragma unroll
@@ -708,8 +658,7 @@ template <int DH, int TYPE, int ACT, int MT>
 __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs a, TreeShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
   constexpr int NKC = DH / 32, NDT = DH / 16, RB = 64 * MT;
-  constexpr bool HALF = TYPE != SEQ_BF16 && ACT == SEQ_BF16;         // P and V in FP16
-  constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : HALF ? 1 : 2;
+  constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 2;
   constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a K row as loaded
   constexpr int KL = 32 * PPR / kWave; // K loads per thread: 32 rows per wave
   constexpr int VW = NDT * ES / 4;     // words of V per lane and row
@@ -788,7 +737,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float f0 = float(int8_t(x.w[2 * i * VW + e / 4] >> (8 * (e & 3)))), f1 = float(int8_t(x.w[(2 * i + 1) * VW + e / 4] >> (8 * (e & 3))));
-              q[i] = HALF ? pack_half(f0, f1) : __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
+              q[i] = __builtin_amdgcn_perm(__float_as_uint(f1), __float_as_uint(f0), 0x07060302u);
             }
             z.v[wave][e][lane] = make_uint4(q[0], q[1], q[2], q[3]);
           }
@@ -801,7 +750,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
               for (int e = 0; e < NDT / 2; ++e) v[i][e] = x.w[i * VW + e];
             } else {
 #pragma unroll
-              for (int e = 0; e < NDT / 4; ++e) widen<TYPE, HALF>(x.w[i * VW + e], &v[i][2 * e]);
+              for (int e = 0; e < NDT / 4; ++e) widen<TYPE>(x.w[i * VW + e], &v[i][2 * e]);
             }
           }
           const int new_row = Lr - s * kStep - half;     // the first of the wave's rows that is the tree's
@@ -811,7 +760,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
             for (int i = 0; i < 8; ++i)
               if (16 * (i >> 2) + 4 * c + (i & 3) >= new_row)
 #pragma unroll
-                for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd<HALF>(v[i][e]);
+                for (int e = 0; e < NDT / 2; ++e) bad |= drop_odd(v[i][e]);
             if (bad) s_odd = 1;
           }
 #pragma unroll
@@ -864,12 +813,10 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
       load_q<DH, ACT, QT, false>(a, p.b * a.q.seq + t * a.q.token + h * a.q.head + 8 * c, qf[mt]);
     }
     float m_run[MT], l_run[MT];          // of query row r; l of this lane's cache rows
-    Lift lift[MT];
     f32x4 o[MT][NDT];                    // lane (r, c): query rows 4 c + i, dimension NDT r + d
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       m_run[mt] = -INFINITY;
-      lift[mt] = {0.0f, -1.0f};
       l_run[mt] = 0.0f;
 #pragma unroll
       for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -919,7 +866,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
         uint32_t pf[MT][PT][4];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE, HALF>(sc[mt], ks, vs, a.scale2, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], lift[mt], o[mt], pf[mt]);
+          soft_step<NDT, PT, TYPE != SEQ_BF16, EDGE>(sc[mt], ks, vs, a.scale2, t0 + 32 * half_, c, anc[mt], m_run[mt], l_run[mt], o[mt], pf[mt]);
 #pragma unroll
         for (int e = 0; e < NDT; e += 2) {
           uint4 vb[2];
@@ -931,8 +878,7 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int mt = 0; mt < MT; ++mt)
-                o[mt][e + i] = HALF ? mfma_half(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i])
-                                    : mfma(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i]);
+                o[mt][e + i] = mfma(pf[mt][k], {vb[i].x, vb[i].y, vb[i].z, vb[i].w}, o[mt][e + i]);
         }
       }
     };
@@ -944,7 +890,6 @@ __global__ __launch_bounds__(kBlock, 2) void tree_attn_wide_kernel(TreeAttnArgs 
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const float l_all = quad_sum(l_run[mt]);
-      if constexpr (HALF) m_run[mt] -= lift[mt].by;      // (sums and outputs are times 2^lift)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int in = (wave * MT + mt) * 16 + 4 * c + i, row = p.rb * RB + in;
