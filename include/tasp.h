@@ -558,6 +558,7 @@ tasp_status tasp_tree_attention(const tasp_seq_cache* cache, int32_t layer, cons
  * tokens are distributed as the target's own samples. temperature 0: p_v is the lowest index of the
  * largest logit, draft_logits are not read. T = 1 samples one token from logits. NaN logits count as -inf;
  * a row without a finite or +inf logit yields token -1; drafted tokens outside the vocabulary are never accepted.
+ * It knows no cache: nodes whose rows did not fit one have to be absent in `parent` (tasp_tree_step sees to that itself).
  *   n (device int32 [batch]): tokens emitted, the accepted ones and one more; ids (device int32 [batch][T]): those
  *   tokens, then -1; path (device int32 [batch][T]): the nodes 0, ... of the accepted path (n entries), then -1.
  * All sums in float64. workspace: device, 256-byte aligned, at least tasp_verify_workspace_bytes, needs no clearing;
@@ -600,7 +601,9 @@ tasp_status tasp_tree_forward(tasp_plan plan, const float* x, const int32_t* par
 /* One step of decoding with drafted tokens: embeds tokens (device int32 [batch][T]; node 0 the last token of the
  * text, whose row is not in the cache yet), runs tasp_tree_forward, verifies the drafts (tasp_verify; arguments as
  * there) and keeps the accepted path (tasp_seq_commit, cache->len grows by n). The next step's node 0 is
- * ids[b][n[b] - 1]. Nothing waits for the host: lengths, tokens and acceptance stay on the device, and a step can be
+ * ids[b][n[b] - 1]. Nodes whose rows do not fit max_seq are absent for the verification too: they are never accepted, and a
+ * sequence whose node 0 is absent (no row left, a length outside 0..max_seq, or parent[b][0] other than -1) emits nothing:
+ * n[b] = 0, ids and path -1, its length and rows as they were. Nothing waits for the host: lengths, tokens and acceptance stay on the device, and a step can be
  * captured into a HIP graph and replayed with new tokens in the same arrays (max_len then is an upper bound for the
  * replays). embed, embed_scale as tasp_generate; x_scratch float32 [batch][T][d_model]; logits float32
  * [batch][T][vocab] receive the target's logits (both 16-byte aligned). A drafted token outside the vocabulary is not

@@ -2230,6 +2230,19 @@ tasp_status check_verify(const float* logits, const int32_t* tokens, const float
   return check_workspace(workspace, workspace_bytes, tasp::verify_workspace_bytes(batch, T, vocab));
 }
 
+// (checked before) len, S: as in VerifyArgs
+tasp_status run_verify(const float* logits, const int32_t* tokens, const float* u, const int32_t* parent,
+                       const float* draft_logits, const int32_t* len, int32_t S, int32_t batch, int32_t T,
+                       int32_t vocab, double temperature, int32_t* ids, int32_t* path, int32_t* n, void* workspace,
+                       void* stream) {
+  tasp::VerifyArgs a{};
+  a.logits = logits; a.draft = draft_logits; a.tokens = tokens; a.u = u; a.parent = parent; a.len = len; a.S = S;
+  a.B = batch; a.T = T; a.V = vocab; a.inv_temp = temperature > 0.0 ? 1.0 / temperature : 0.0;
+  a.ids = ids; a.path = path; a.n = n; a.ws = workspace;
+  HIP_TRY(tasp::launch_verify(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
 }  // namespace
 
 tasp_status tasp_verify_workspace_bytes(int32_t batch, int32_t T, int32_t vocab, size_t* bytes) {
@@ -2247,12 +2260,8 @@ tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float*
   tasp_status st = check_verify(logits, tokens, u, parent, draft_logits, batch, T, vocab, temperature, ids, path, n,
                                 workspace, workspace_bytes);
   if (st) return st;
-  tasp::VerifyArgs a{};
-  a.logits = logits; a.draft = draft_logits; a.tokens = tokens; a.u = u; a.parent = parent;
-  a.B = batch; a.T = T; a.V = vocab; a.inv_temp = temperature > 0.0 ? 1.0 / temperature : 0.0;
-  a.ids = ids; a.path = path; a.n = n; a.ws = workspace;
-  HIP_TRY(tasp::launch_verify(a, static_cast<hipStream_t>(stream)));
-  return TASP_OK;
+  return run_verify(logits, tokens, u, parent, draft_logits, nullptr, 0, batch, T, vocab, temperature, ids, path, n,
+                    workspace, stream);
 }
 
 tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, const int32_t* n,
@@ -2420,8 +2429,8 @@ tasp_status tasp_tree_step(tasp_plan p, const int8_t* embed, const float* embed_
   hipStream_t s = static_cast<hipStream_t>(stream);
   HIP_TRY(tasp::launch_embed(embed, embed_scale, d.vocab, d.d_model, tokens, T * cache->batch, x_scratch, s));
   if ((st = tasp_tree_forward(p, x_scratch, parent, T, cache, max_len, logits, workspace, workspace_bytes, stream)) ||
-      (st = tasp_verify(logits, tokens, u, parent, draft_logits, cache->batch, T, d.vocab, temperature, ids, path, n,
-                        ws + attn, total - attn, stream)))
+      (st = run_verify(logits, tokens, u, parent, draft_logits, cache->len, cache->max_seq, cache->batch, T, d.vocab,
+                       temperature, ids, path, n, ws + attn, stream)))
     return st;
   return tasp_seq_commit(cache, path, n, T, cache->len, stream);
 }

@@ -82,6 +82,9 @@ inline int tree_slot(int head, int first, int count) { return head | first << 8 
 struct VerifyArgs {
   const float* logits; const float* draft;   // [B][T][V], [B][T - 1][V] or null
   const int* tokens; const float* u; const int* parent;
+  // rows that the sequences hold, of at most S (null: every node fits): nodes whose row does not fit are absent, and a
+  // sequence whose node 0 is absent emits nothing
+  const int* len; int S;
   int B, T, V;
   double inv_temp;                     // 0: greedy
   int* ids; int* path; int* n;         // [B][T], [B][T], [B]

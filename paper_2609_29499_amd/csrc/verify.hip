@@ -274,7 +274,12 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
   float lx = 0.0f, dx = 0.0f;
   if (tid < kWave) {
     sm.kids[t] = 0;
-    nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, T, t);
+    int t_end = T;
+    if (a.len) {
+      const int L = seq_len(a.len, b, a.S);
+      t_end = L < 0 ? 0 : a.S - L;
+    }
+    nd = tree_node(a.parent ? a.parent + size_t(b) * T : nullptr, T, t_end, t);
     node = nd.anc != 0 && nd.parent >= 0;
     up = node ? nd.parent : -1;
     x = t < T ? a.tokens[size_t(b) * T + t] : -1;
@@ -323,8 +328,9 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
     const unsigned long long taken = __ballot(chosen) | 1ull;
     const bool on = nd.anc != 0 && (nd.anc & 1) && !(nd.anc & ~taken);
     const unsigned long long path = __ballot(on);
-    // node 0 absent (its parent is not -1): nothing is on the path and the last node is 0
-    const int n = max(1, __popcll(path)), last = path ? 63 - __clzll(path) : 0;
+    // node 0 absent (its parent is not -1, or it does not fit): nothing is on the path. Without lengths it is the last node
+    // all the same, with them nothing is emitted.
+    const int n = a.len ? __popcll(path) : max(1, __popcll(path)), last = path ? 63 - __clzll(path) : 0;
     const unsigned long long kids = draft ? __ballot(node && up == last) : sm.kids[last];
     if (t == 0) {
       sm.n = n;
@@ -335,7 +341,7 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, const Exp& ex, const C
       const int before = __popcll(path & ((1ull << t) - 1));
       int* po = a.path + size_t(b) * T;
       int* io = a.ids + size_t(b) * T;
-      if (on || (t == 0 && !path)) po[before] = t;
+      if (on || (t == 0 && n > 0)) po[before] = t;
       if (on && t > 0) io[before - 1] = x;
       if (t >= n) {
         po[t] = -1;
@@ -477,6 +483,7 @@ __global__ __launch_bounds__(kWalk) void verify_walk_kernel(VerifyArgs a, const 
   const bool greedy = a.inv_temp == 0.0;
   const Exp ex = exp_table(sm.table, a.inv_temp);
   walk(a, ex, stat, b, chunks, sm, blockIdx.x == 0);
+  if (sm.n == 0) return;
   const int last = sm.last, slot = sm.n - 1;
   int* out = a.ids + size_t(b) * T + slot;
   const RowStat rs = sm.row[last];

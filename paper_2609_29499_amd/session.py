@@ -278,8 +278,8 @@ class Plan:
     def tree_step(self, embed, embed_scale, tokens, cache, u=None, parent=None, draft_logits=None, temperature=0.0,
                   max_len=None, out=None, scratch=None, workspace=None, stream=None):
         """One step over drafted tokens int32 [B][T] (node 0: the text's last token): returns (ids, path, n) as
-        ``verify`` does, and the cache has grown by the accepted rows. ``out``: those three; ``scratch``: (x [B][T][d],
-        logits [B][T][V])."""
+        ``verify`` does, and the cache has grown by n rows (0 where it has none left for node 0). ``out``: those three;
+        ``scratch``: (x [B][T][d], logits [B][T][V])."""
         dev = _device(cache.k, embed, embed_scale, tokens, u, parent, draft_logits)
         nb, T = tokens.shape
         D, V = self.desc.d_model, self.desc.vocab
