@@ -488,7 +488,7 @@ typedef struct {
 } tasp_rows;
 
 /* Rotary positions. layout: pairs (i, i + rot_dim / 2) or (2 i, 2 i + 1) of a head's first rot_dim values (a
- * multiple of 16, up to head_dim; the others pass unchanged), turned by pos * f_i, f_i = theta^(-2 i / rot_dim),
+ * multiple of 16, up to head_dim; the others pass unchanged), turned by pos * f_i, f_i = theta^(-2 i / rot_dim) (theta above 1),
  * and multiplied by mscale. For contexts beyond orig_len positions the frequencies are scaled:
  *   LINEAR      f / factor
  *   WAVELENGTH  by the turns n = orig_len f / 2 pi: f for n >= high, f / factor for n <= low, between them

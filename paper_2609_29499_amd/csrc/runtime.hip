@@ -2067,8 +2067,7 @@ tasp_status check_tree(const int32_t* parent, int32_t T, bool chains) {
   return TASP_OK;
 }
 
-// rotation of the append kernel from a tasp_rope (checked); NULL: none
-tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
+tasp_status check_rope(const tasp_rope* r, int dh) {
   if (!r) return TASP_OK;
   if (r->layout != TASP_ROPE_HALF && r->layout != TASP_ROPE_INTERLEAVED)
     return fail(TASP_ERR_INVALID_ARG, "rope layout %d", r->layout);
@@ -2083,6 +2082,12 @@ tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
   if (r->scaling >= TASP_ROPE_WAVELENGTH &&
       (!(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high) || r->orig_len < 1))
     return fail(TASP_ERR_INVALID_ARG, "rope scaling needs 0 < low < high and orig_len >= 1");
+  return TASP_OK;
+}
+
+// rotation of the append kernel from a checked tasp_rope, or a plan's (any theta above 0); NULL: none
+void rope_args(const tasp_rope* r, tasp::SeqAppendArgs* a) {
+  if (!r) return;
   constexpr double kTurn = 6.28318530717958647693;
   const int n = r->rot_dim;
   a->rot = n;
@@ -2103,6 +2108,11 @@ tasp_status rope_args(const tasp_rope* r, int dh, tasp::SeqAppendArgs* a) {
     a->mul = -1.0 / std::max(hi - lo, 0.001);
     a->add = 1.0 - lo * a->mul;
   }
+}
+
+tasp_status check_commit_grid(const tasp_seq_cache* c) {
+  if (int64_t(c->n_layers) * c->batch * c->n_kv_heads > kMaxGrid)
+    return fail(TASP_ERR_SHAPE, "%d layers of %d sequences", c->n_layers, c->batch);
   return TASP_OK;
 }
 
@@ -2143,7 +2153,8 @@ tasp_status tasp_seq_append(const tasp_seq_cache* cache, int32_t layer, const ta
   } else if ((q && q->p) || (q_out && q_out->p)) {
     return fail(TASP_ERR_INVALID_ARG, "q given with 0 query heads");
   }
-  if ((st = rope_args(rope, cache->head_dim, &a))) return st;
+  if ((st = check_rope(rope, cache->head_dim))) return st;
+  rope_args(rope, &a);
   a.c = seq_layer(cache, layer);
   a.parent = parent; a.T = T; a.act = act_type; a.n_q = n_q_heads; a.n_kv = cache->n_kv_heads;
   HIP_TRY(tasp::launch_seq_append(a, static_cast<hipStream_t>(stream)));
@@ -2272,8 +2283,7 @@ tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, co
   if (!path || !n || !len_out) return fail(TASP_ERR_INVALID_ARG, "path / n / len_out is NULL");
   if (!aligned(path, 4) || !aligned(n, 4) || !aligned(len_out, 4))
     return fail(TASP_ERR_INVALID_ARG, "path / n / len_out is not 4-byte aligned");
-  if (int64_t(cache->n_layers) * cache->batch * cache->n_kv_heads > kMaxGrid)
-    return fail(TASP_ERR_SHAPE, "%d layers of %d sequences", cache->n_layers, cache->batch);
+  if ((st = check_commit_grid(cache))) return st;
   tasp::SeqCommitArgs a{};
   a.c = seq_layer(cache, 0); a.n_layers = cache->n_layers;
   a.path = path; a.ld = T; a.n = n; a.len_out = len_out;
@@ -2326,14 +2336,14 @@ tasp_status tree_forward(tasp_plan p, const float* x, const int32_t* parent, int
                          int32_t max_len, float* out, float* ws, hipStream_t s) {
   const tasp_model_desc& d = p->desc;
   const int dh = d.head_dim, n = c->batch * T;
-  tasp_rope rope{TASP_ROPE_HALF, dh, TASP_ROPE_NONE, 0, d.rope_theta, 1.0, 1.0, 2.0, 1.0};
+  const tasp_rope rope{TASP_ROPE_HALF, dh, TASP_ROPE_NONE, 0, d.rope_theta, 1.0, 1.0, 2.0, 1.0};
+  tasp::SeqAppendArgs turned{};
+  rope_args(&rope, &turned);
   float* q = reinterpret_cast<float*>(p->pq);          // [batch][T][m_q][dh] (as wide as the prefill's two BF16 planes)
   auto attend = [&](int l, const float* qkv, int ld, int ks) -> tasp_status {
     const LayerPlan& P = p->layers[l];
     const tasp::SeqLayer layer = seq_layer(c, l);
-    tasp::SeqAppendArgs a{};
-    tasp_status st = rope_args(&rope, dh, &a);
-    if (st) return st;
+    tasp::SeqAppendArgs a = turned;
     a.c = layer; a.parent = parent; a.T = T; a.act = TASP_F32; a.n_q = P.m_q; a.n_kv = P.m_kv; a.kv_map = P.kv_idx.data();
     a.ks = ks; a.split = long(n) * ld;
     float* base = const_cast<float*>(qkv);             // (read only)
@@ -2414,7 +2424,7 @@ tasp_status tasp_tree_step(tasp_plan p, const int8_t* embed, const float* embed_
   // everything that the later calls would refuse is refused here, before the first launch
   if ((st = check_verify(logits, tokens, u, parent, draft_logits, cache->batch, T, d.vocab, temperature, ids, path, n,
                          ws + attn, total - attn)) ||
-      (st = check_tree(parent, T, false)))
+      (st = check_tree(parent, T, false)) || (st = check_commit_grid(cache)))
     return st;
   if (!x_scratch) return fail(TASP_ERR_INVALID_ARG, "x_scratch is NULL");
   if (!aligned(x_scratch, 16) || !aligned(logits, 16) || !aligned(embed, 4) || !aligned(embed_scale, 4))
