@@ -518,7 +518,8 @@ tasp_status tasp_seq_append(const tasp_seq_cache* cache, int32_t layer, const ta
                             const tasp_rows* q_out, void* stream);
 
 /* Read rows first[b]..first[b] + n - 1 (device int32 [batch]; NULL: 0) of layer `layer` back as out_type
- * TASP_BF16 or TASP_F32 values (token stride: from row to row); rows outside 0..max_seq - 1 read as zeros.
+ * TASP_BF16 or TASP_F32 values (token stride: from row to row); rows outside 0..max_seq - 1 read as zeros. n is at least
+ * 1 and n * head_dim at most 2^35 - 2^11.
  * Stream-ordered, capturable. Errors as tasp_seq_append. */
 tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int32_t* first,
                           int32_t n, int32_t out_type, const tasp_rows* k_out,

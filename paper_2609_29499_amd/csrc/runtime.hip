@@ -2169,7 +2169,8 @@ tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int3
   if ((st = check_seq_cache(cache, layer)) || (st = check_seq_buffers(cache)) ||
       (st = check_rows(k_out, out_type, "k_out", &a.k)) || (st = check_rows(v_out, out_type, "v_out", &a.v)))
     return st;
-  if (n < 1) return fail(TASP_ERR_SHAPE, "%d rows", n);
+  const int64_t per = 8 * tasp::kBlock / cache->head_dim;    // rows of a workgroup
+  if (n < 1 || n > kMaxGrid * per) return fail(TASP_ERR_SHAPE, "%d rows (1..%lld)", n, (long long)(kMaxGrid * per));
   if (!aligned(first, 4)) return fail(TASP_ERR_INVALID_ARG, "first is not 4-byte aligned");
   a.c = seq_layer(cache, layer);
   a.first = first; a.n = n; a.out_type = out_type;
