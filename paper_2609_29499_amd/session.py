@@ -460,7 +460,13 @@ def _workspace(nbytes, device, stream=None):
 
 class SeqCache:
     """A cache whose sequences have their own lengths: k, v ``[L][B][Hkv][S][dh]`` as bfloat16, int8 or
-    float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch."""
+    float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch. They stay the
+    tensors that the cache was made of, whose addresses ``struct`` holds: new values are copied into them."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:  # (c.len += 1 sets the same tensor again)
+            raise AttributeError(f"{name} of a cache stays what it is: copy into it, or make another cache")
+        super().__setattr__(name, value)
 
     def __init__(self, k, v, length, k_scale=None, v_scale=None):
         if k.dtype not in (torch.bfloat16, torch.int8, torch.float8_e4m3fn) or k.dim() != 5:

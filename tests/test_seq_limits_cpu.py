@@ -1,7 +1,9 @@
 """Limits of the drafted-token entry points that are checked before any GPU work."""
 import pytest
+import torch
 
 from paper_2609_29499_amd import binding as B
+from paper_2609_29499_amd import session as S
 from tests.test_seq_cpu import cache, refused, rows
 
 
@@ -9,3 +11,16 @@ from tests.test_seq_cpu import cache, refused, rows
 def test_reads_of_more_rows_than_a_launch_has(dh, n):
     """A workgroup reads 2048 / dh rows, and a launch has fewer than 2^24 of them in a dimension."""
     refused("TASP_ERR_SHAPE", B.tasp_seq_read, cache(head_dim=dh), 0, None, n, B.BF16, rows(), rows(), None)
+
+
+def test_a_cache_keeps_the_tensors_that_it_names():
+    """Another tensor under a cache's name would leave the library with the address of one that torch frees."""
+    c = S.SeqCache.__new__(S.SeqCache)
+    for name in ("k", "v", "len", "k_scale", "v_scale", "struct", "max_seq", "batch"):
+        setattr(c, name, torch.zeros(3))
+        with pytest.raises(AttributeError, match=name):
+            setattr(c, name, torch.ones(3))
+        assert not getattr(c, name).any()
+    kept = c.len
+    c.len += 1                                         # (in place)
+    assert c.len is kept and c.len.tolist() == [1, 1, 1]
