@@ -573,7 +573,7 @@ tasp_status tasp_verify(const float* logits, const int32_t* tokens, const float*
 
 /* Keep an accepted path: in every layer, sequence and KV head, row len + path[b][i] moves to row len + i for
  * i < n[b] (entries of path outside 0..T - 1 and rows past max_seq stay where they are), and len_out[b] = len[b] + n[b],
- * cut to max_seq (device int32 [batch]; cache->len itself is allowed). path [batch][T] and n as tasp_verify
+ * cut to max_seq (device int32 [batch]; it may lie over cache->len, n or path). path [batch][T] and n as tasp_verify
  * returns them, T <= TASP_TREE_MAX. Stream-ordered, capturable. Errors as tasp_seq_append. */
 tasp_status tasp_seq_commit(const tasp_seq_cache* cache, const int32_t* path, const int32_t* n,
                             int32_t T, int32_t* len_out, void* stream);

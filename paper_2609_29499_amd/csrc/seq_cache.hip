@@ -317,9 +317,13 @@ __global__ __launch_bounds__(kBlock) void seq_commit_kernel(SeqCommitArgs a) {
 }
 
 __global__ __launch_bounds__(kBlock) void seq_length_kernel(SeqCommitArgs a) {
+  // (len_out may share memory with the lengths or counts, shifted too: all are read, and here, before any is written)
   const int b = threadIdx.x;
-  if (b >= a.c.batch) return;
-  a.len_out[b] = next_len(a, b);
+  static_assert(kSeqMaxBatch <= kBlock, "one workgroup");
+  int L = b < a.c.batch ? next_len(a, b) : 0;
+  asm volatile("" : "+v"(L));
+  __syncthreads();
+  if (b < a.c.batch) a.len_out[b] = L;
 }
 
 }  // namespace
@@ -394,7 +398,7 @@ hipError_t launch_seq_commit(const SeqCommitArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.apart) return hipSuccess;
-  // a launch of its own: every workgroup above reads the lengths that this one replaces
+  // a launch of its own, of one workgroup (a batch has as many sequences at most): all above read what this one replaces
   hipLaunchKernelGGL(seq_length_kernel, dim3(1), dim3(kBlock), 0, s, a);
   return hipGetLastError();
 }
