@@ -264,13 +264,13 @@ class Plan:
 
     def tree_forward(self, x, cache, parent=None, max_len=None, out=None, workspace=None, stream=None):
         """The plan over trees of nodes: x float32 [B][T][d] -> logits [B][T][V] (or residuals [B][T][d])."""
-        dev = _device(cache.k, x, parent, out)
+        dev = _device(cache.k, self.ws, x, parent, out)
         nb, T = x.shape[:2]
         width = self.desc.vocab or self.desc.d_model
         if out is None:
             out = _empty((nb, T, width), torch.float32, x.device, stream)
         ml = cache.max_seq if max_len is None else max_len
-        ws = workspace if workspace is not None else self.tree_workspace(cache, T, ml, stream)
+        ws = _on(dev, workspace) if workspace is not None else self.tree_workspace(cache, T, ml, stream)
         _launch(B.tasp_tree_forward, dev, stream, self.handle, _ptr(x, (cache.batch, T, self.desc.d_model), torch.float32, "x"),
                 cache._parent(parent, T), T, cache.struct, ml, _ptr(out, (nb, T, width), torch.float32, "out"), ws[1], ws[2])
         return out
@@ -280,7 +280,7 @@ class Plan:
         """One step over drafted tokens int32 [B][T] (node 0: the text's last token): returns (ids, path, n) as
         ``verify`` does, and the cache has grown by n rows (0 where it has none left for node 0). ``out``: those three;
         ``scratch``: (x [B][T][d], logits [B][T][V])."""
-        dev = _device(cache.k, embed, embed_scale, tokens, u, parent, draft_logits)
+        dev = _device(cache.k, self.ws, embed, embed_scale, tokens, u, parent, draft_logits)
         nb, T = tokens.shape
         D, V = self.desc.d_model, self.desc.vocab
         if scratch is None:
@@ -290,7 +290,7 @@ class Plan:
             ids, path = _empty((2, nb, T), torch.int32, tokens.device, stream)
             out = ids, path, _empty((nb,), torch.int32, tokens.device, stream)
         ml = cache.max_seq if max_len is None else max_len
-        ws = workspace if workspace is not None else self.tree_workspace(cache, T, ml, stream)
+        ws = _on(dev, workspace) if workspace is not None else self.tree_workspace(cache, T, ml, stream)
         _device(cache.k, *out, *scratch)
         _launch(B.tasp_tree_step, dev, stream, self.handle, _ptr(embed, (V, D), torch.int8, "embed"),
                 _ptr(embed_scale, (V,), torch.float32, "embed_scale"), _ptr(tokens, (cache.batch, T), torch.int32, "tokens"),
@@ -458,6 +458,14 @@ def _workspace(nbytes, device, stream=None):
     return t, t.data_ptr() + (-t.data_ptr()) % 256, nbytes
 
 
+def _on(dev, workspace):
+    """A call's workspace, refused where its tensor lies on another device than the call's."""
+    t = workspace[0]
+    if t is not None and t.get_device() != dev:
+        raise ValueError(f"the workspace lies on {t.device}, the call's tensors on cuda:{dev}")
+    return workspace
+
+
 class SeqCache:
     """A cache whose sequences have their own lengths: k, v ``[L][B][Hkv][S][dh]`` as bfloat16, int8 or
     float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch. They stay the
@@ -563,7 +571,7 @@ def tree_attention(cache, layer, q, parent=None, scale=None, max_len=None, out=N
         ro = _rows(out, shape, dt, "out")
     if max_len is None:
         max_len = cache.max_seq
-    ws = workspace if workspace is not None else tree_attention_workspace(cache, n_q, T, max_len, stream)
+    ws = _on(dev, workspace) if workspace is not None else tree_attention_workspace(cache, n_q, T, max_len, stream)
     _launch(B.tasp_tree_attention, dev, stream, cache.struct, layer, cache._parent(parent, T), T, _SEQ_TYPES[dt],
             rq, n_q, cache.dh ** -0.5 if scale is None else scale, max_len, ro, ws[1], ws[2])
     return out
@@ -581,7 +589,7 @@ def verify(logits, tokens, u, parent=None, draft_logits=None, temperature=1.0, w
     nb, T, V = logits.shape
     ids, path = _like(tokens, stream), _like(tokens, stream)
     n = _empty((nb,), torch.int32, tokens.device, stream)
-    ws = workspace if workspace is not None else verify_workspace(nb, T, V, logits.device, stream)
+    ws = _on(dev, workspace) if workspace is not None else verify_workspace(nb, T, V, logits.device, stream)
     _launch(B.tasp_verify, dev, stream, _ptr(logits, (nb, T, V), torch.float32, "logits"),
             _ptr(tokens, (nb, T), torch.int32, "tokens"), _ptr(u, (nb, T), torch.float32, "u"),
             _ptr(parent, (nb, T), torch.int32, "parent"), _ptr(draft_logits, (nb, T - 1, V), torch.float32, "draft_logits"),

@@ -24,3 +24,10 @@ def test_a_cache_keeps_the_tensors_that_it_names():
     kept = c.len
     c.len += 1                                         # (in place)
     assert c.len is kept and c.len.tolist() == [1, 1, 1]
+
+
+def test_workspaces_of_another_device():
+    ws = S._workspace(512, "cpu")
+    with pytest.raises(ValueError, match="workspace"):
+        S._on(0, ws)
+    assert S._on(-1, ws) is ws and S._on(0, (None, 256, 16)) == (None, 256, 16)
