@@ -419,7 +419,7 @@ struct Rows32 {                        // a step's K and V as loaded
 
 // Waves per SIMD that the registers of MT tiles leave room for
 template <int DH, int TYPE, int ACT, int MT>
-constexpr int kWavesPerSimd = MT == 4 || (MT == 2 && DH == 128 && (TYPE == SEQ_BF16 || ACT == SEQ_F32)) ? 1 : 2;
+constexpr int kWavesPerSimd = MT == 2 && DH == 128 && (TYPE == SEQ_BF16 || ACT == SEQ_F32) ? 1 : 2;
 
 // MT: tiles of 16 query rows per wave. (Lambdas here are inlined by order: called, they would keep what they
 // capture in memory, descriptors among it.)
