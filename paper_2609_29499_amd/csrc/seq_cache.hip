@@ -8,7 +8,7 @@
 // head rows of one token: a lane holds eight elements of a head, so the row's maximum stays inside 8
 // or 16 lanes and every access is 16 or 32 bytes wide; the token's sines and cosines go through LDS.
 // Bound by memory: q, k and v are read once, q and the rows written once (2 x 8192 tokens of 32 + 2 x 8 heads of 128 in
-// float32 into INT8, 705 MB: 139 us, 5.1 TB/s; 8 trees of 32, 10 MB: 6.5 us, latency: lengths and tree, then sines).
+// float32 into INT8, 705 MB: 141 us, 5.0 TB/s; 8 trees of 32, 10 MB: 6.7 us, latency: lengths and tree, then sines).
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -267,7 +267,7 @@ __device__ __forceinline__ int next_len(const SeqCommitArgs& a, int b) {
 // sequence, k / v). The workgroup reads every row that moves before it writes the first (path may
 // name rows that earlier entries replace). Rows that stay are not touched. Bound by three latencies in a row
 // (length and count, path, rows), which HEADS heads share: 80 layers of 8 x 8 heads, 9 of 64 nodes (42 MB moved):
-// 16.2 us with one head per workgroup, 12.0 with four.
+// 16.7 us with one head per workgroup, 11 with four.
 template <int RB, int HEADS>           // bytes of a row
 __global__ __launch_bounds__(kBlock) void seq_commit_kernel(SeqCommitArgs a) {
   constexpr int LPR = RB / 16, RPP = kBlock / LPR, NP = kTreeMax / RPP;

@@ -13,15 +13,16 @@
 // Rows in 8 bits become BF16 exactly; their scales multiply scores and probabilities in 32 bits. P is
 // carried as two BF16 terms (16 bits; one alone would double the error of a BF16 output), float32 q and P
 // as three (24 bits, as exact as the products' float32 sums). (One FP16 term has 11 bits, and not the range of a
-// probability times a scale; it took 170 us instead of 192 for the 64-node case below, three BF16 terms 225.)
+// probability times a scale; calls of the 64-node case below took 170 us with it, 192 with two BF16 terms, 225 with three.)
 //
 // Softmax with a running maximum per query row, raised only when a score passes it by 8 powers of two (sums
 // are float32, so the slack costs no accuracy): most steps exchange nothing between lanes.
 //
-// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 201 + 10 us,
-// bound by instructions: about 640 of a wave's per step of 64 rows, 96 of them matrix products, two waves per SIMD; a tree of 16
-// over 4 BF16 sequences of 4096 .. 2560 rows (55 MB) 20 + 5 us and 8 tokens over 131072 E4M3 rows (277 MB) 56 + 5 us,
-// bound by memory (5 TB/s behind the first 4 us); one token over 2047 INT8 rows 7 + 4 us, latency.
+// Measured, first launch + join: 64 nodes x 64 heads over 8 INT8 sequences of 8192 .. 4608 rows (108 GFLOP) 199 + 10 us,
+// bound by instructions: some 640 of a wave's per step of 64 rows, 96 of them matrix products, two waves per SIMD; a tree of 16
+// over 4 BF16 sequences of 4096 .. 2560 rows 20 + 5 us: 4 us until rows arrive, then 55 MB of them read and 15 MB of records
+// written at 4.4 TB/s; 8 tokens over 131072 E4M3 rows (277 MB) 57 + 5 us, bound by memory (4.9 TB/s); one token over 2047
+// INT8 rows 7 + 4 us, latency.
 //
 // Two kernels. Up to 32 query rows (tree_attn_kernel) a wave keeps all of them and walks every fourth step
 // straight from memory in the operands' layout, the next step's loads in flight; no LDS is used before

@@ -17,8 +17,8 @@
 // max(p - q, 0), and the last to finish takes the token.
 //
 // Bound by the read of the logits, and nearly as much by the exponentials: 16 trees of 32 over 128256 tokens, 263 MB, take
-// 63 us in the first launch (4.2 TB/s; 20 instructions per logit are 40 us of every SIMD) and 12 in the second, which is
-// latency: records from other dies' caches, the tree, a chunk of logits. Chains of 9 x 8 with drafts, 70 MB: 20 + 14 us;
+// 63 .. 72 us in the first launch (4.2 .. 3.7 TB/s; 20 instructions per logit are 40 us of every SIMD) and 13 in the second,
+// which is latency: records from other dies' caches, the tree, a chunk of logits. Chains of 9 x 8 with drafts, 70 MB: 20 + 14 us;
 // one row: 4 + 7.
 #include <algorithm>
 
