@@ -529,7 +529,8 @@ tasp_status tasp_seq_read(const tasp_seq_cache* cache, int32_t layer, const int3
  * 0..len - 1, its ancestors' rows and its own, with scores scale * q . k. q, out: n_q_heads heads (a multiple
  * of n_kv_heads, at most 8 per KV head; query head h reads KV head h / (n_q_heads / n_kv_heads)) of act_type;
  * out must not overlap q or the cache. Outputs of absent nodes are zeros, and what absent or unseen
- * rows hold (NaN, infinities) reaches no output. TASP_BF16: q and V exact, probabilities in 16 bits, sums in float32;
+ * rows hold (NaN, infinities) reaches no output (in a row that is seen they leave nothing finite in their dimension: an
+ * infinite v of a node's row comes out as it is, of a cached row perhaps as NaN). TASP_BF16: q and V exact, probabilities in 16 bits, sums in float32;
  * TASP_F32: everything to 24 bits. The ends of float32: rows seen times the largest |v| stay below 2^120 (sums are divided
  * at the end, a row's share in them is up to 2^8), and of a probability times a row's scale what lies below 2^-126
  * may be lost. max_len: the largest length expected (0..max_seq): it sizes launches and

@@ -2077,8 +2077,8 @@ tasp_status check_rope(const tasp_rope* r, int dh) {
     return fail(TASP_ERR_INVALID_ARG, "rope scaling %d", r->scaling);
   if (!(r->theta > 1.0) || !std::isfinite(r->theta) || !std::isfinite(float(r->mscale)))
     return fail(TASP_ERR_INVALID_ARG, "rope theta must be above 1, mscale finite in 32 bits");
-  if (r->scaling != TASP_ROPE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
-    return fail(TASP_ERR_INVALID_ARG, "rope factor must be positive");
+  if (r->scaling != TASP_ROPE_NONE && (!(r->factor > 0.0) || !std::isfinite(r->factor) || !std::isfinite(1.0 / r->factor)))
+    return fail(TASP_ERR_INVALID_ARG, "rope factor and its reciprocal must be positive and finite");
   if (r->scaling >= TASP_ROPE_WAVELENGTH &&
       (!(r->low > 0.0) || !(r->high > r->low) || !std::isfinite(r->high) || r->orig_len < 1))
     return fail(TASP_ERR_INVALID_ARG, "rope scaling needs 0 < low < high and orig_len >= 1");
@@ -2204,10 +2204,11 @@ tasp_status tasp_tree_attention(const tasp_seq_cache* cache, int32_t layer, cons
       (st = check_rows(q, act_type, "q", &a.q)) || (st = check_rows(out, act_type, "out", &a.o)) ||
       (st = tree_attn_args(cache, n_q_heads, T, max_len, &a)))
     return st;
-  if (!(scale > 0.0) || !std::isfinite(scale)) return fail(TASP_ERR_INVALID_ARG, "scale must be positive");
+  a.scale2 = float(scale * 1.44269504088896340736);
+  if (!(scale > 0.0) || !std::isfinite(a.scale2))
+    return fail(TASP_ERR_INVALID_ARG, "scale must be positive, and finite in 32 bits");
   a.c = seq_layer(cache, layer);
   a.parent = parent; a.act = act_type;
-  a.scale2 = float(scale * 1.44269504088896340736);
   if ((st = check_workspace(workspace, workspace_bytes, tasp::tree_attn_workspace_bytes(a)))) return st;
   a.ws = static_cast<float*>(workspace);
   HIP_TRY(tasp::launch_tree_attn(a, static_cast<hipStream_t>(stream)));

@@ -4,7 +4,7 @@ import torch
 
 from paper_2609_29499_amd import binding as B
 from paper_2609_29499_amd import session as S
-from tests.test_seq_cpu import cache, refused, rows
+from tests.test_seq_cpu import FAKE, cache, refused, rope, rows
 
 
 @pytest.mark.parametrize("dh,n", [(128, ((1 << 24) - 1) * 16 + 1), (64, ((1 << 24) - 1) * 32 + 1), (128, 2 ** 31 - 1), (64, 2 ** 31 - 1)])
@@ -31,3 +31,13 @@ def test_workspaces_of_another_device():
     with pytest.raises(ValueError, match="workspace"):
         S._on(0, ws)
     assert S._on(-1, ws) is ws and S._on(0, (None, 256, 16)) == (None, 256, 16)
+
+
+def test_numbers_that_leave_their_types():
+    """A scale that is infinite in 32 bits, a factor whose reciprocal is infinite in 64."""
+    c = cache(batch=1)
+    for s in (1e300, 3e38, 2.0 ** 128):
+        refused("TASP_ERR_INVALID_ARG", B.tasp_tree_attention, c, 0, None, 1, B.BF16, rows(), 8, s, 100, rows(), FAKE, 1 << 40, None)
+    for scaling in (1, 2, 3):
+        refused("TASP_ERR_INVALID_ARG", B.tasp_seq_append, c, 0, rope(scaling=scaling, factor=1e-310), None, 1, B.BF16, None,
+                rows(), rows(), 0, None, None)
