@@ -618,6 +618,103 @@ tasp_status tasp_tree_step(tasp_plan plan, const int8_t* embed, const float* emb
                            float* x_scratch, float* logits, void* workspace, size_t workspace_bytes,
                            void* stream);
 
+/* ---- caches in pages: many conversations of one pool (paper, Sec. "Dependency-Closed Masks and Cache-Consistent
+ * Routing": a plan's prefill and decode over its own cache rows; here for any mixture of prompts, chunks of
+ * prompts and single tokens of several sequences in one call).
+ *
+ * A pool holds, per layer, n_pages pages of page_rows rows of every KV head, in BF16 or in 8 bits (INT8 or E4M3: value =
+ * code * scale, one float32 scale per page and head). Row r of sequence b lies in page table[b][r / page_rows] at r % page_rows.
+ * A table entry outside 0..n_pages - 1 is no page: its rows are not written, not seen and read as zeros. len (device) is
+ * the number of rows each sequence holds; as for a tasp_seq_cache no call needs it on the host, and a sequence with a length
+ * outside 0..max_pages * page_rows is passed over. Sequences may share pages that are read (a common prefix); a page
+ * that a call writes rows of must be one sequence's only, and in its table once (else its contents are undefined).
+ *
+ * Scales: a page and head's scale is the largest magnitude / 127 or 448 of what was written into it since its row 0 was
+ * (rows given up by a smaller len still count). A call whose rows raise it rounds the page's older codes again, code' = round(code *
+ * old / new); new rows are round(x / scale), ties to even. A page and head that was given an infinity or a NaN has
+ * the scale NaN: all of it reads as NaN until its row 0 is written again.
+ *
+ * Packed tokens: a call's n_tokens new tokens (1..TASP_PAGE_MAX_TOKENS) lie one after the other, those of sequence b at
+ * start[b]..start[b + 1] - 1 (device int32 [batch + 1]; a pair that falls or leaves 0..n_tokens: no tokens; ranges must not
+ * overlap). start NULL: one token for every sequence (n_tokens = batch). The i-th token of a sequence is cache row and
+ * position len + i; one beyond the table's pages is absent. Rows of tokens that are no sequence's (in front of start[0], behind
+ * start[batch]) are neither read nor written. */
+#define TASP_PAGE_MAX_TOKENS 262143
+typedef struct {
+  void* k;                /* (device) [n_layers][n_pages][n_kv_heads][page_rows][head_dim], 16-byte aligned */
+  void* v;
+  float* k_scale;         /* (device) [n_layers][n_pages][n_kv_heads]; NULL for TASP_BF16 */
+  float* v_scale;
+  const int32_t* table;   /* (device) [batch][max_pages] */
+  int32_t* len;           /* (device) [batch] */
+  int32_t type;           /* TASP_BF16, TASP_INT8 or TASP_E4M3 */
+  int32_t n_layers, n_pages, n_kv_heads, page_rows, head_dim, batch, max_pages;   /* heads 1..64 of 64 or 128,
+                             page_rows 16, 32, 64 or 128, batch 1..TASP_SEQ_MAX_BATCH, max_pages * page_rows at most 2^23 */
+  uint64_t plan_sig;      /* the plan the rows belong to (tasp_page_forward), 0: none */
+} tasp_page_cache;
+
+/* Write the tokens' k and v into their sequences' pages of layer `layer` (len itself stays) and rotate q: q and k are
+ * turned by the tokens' positions (rope NULL: not at all), v is taken as it is. k, v: rows of n_kv_heads heads; q, q_out:
+ * n_q_heads (0: no queries, both NULL), neither q_out overlapping q, k or v; all of act_type TASP_BF16 or TASP_F32 (seq
+ * strides are not used). q_out of absent tokens are zeros. Arithmetic in float32, angles in float64.
+ * Stream-ordered, asynchronous, capturable, no workspace. Errors: TASP_ERR_INVALID_ARG (NULL, types, misaligned rows),
+ * TASP_ERR_SHAPE (cache fields, layer, n_tokens, head counts, rot_dim). */
+tasp_status tasp_page_append(const tasp_page_cache* cache, int32_t layer, const tasp_rope* rope,
+                             const int32_t* start, int32_t n_tokens, int32_t act_type, const tasp_rows* q,
+                             const tasp_rows* k, const tasp_rows* v, int32_t n_q_heads,
+                             const tasp_rows* q_out, void* stream);
+
+/* Read rows first[b]..first[b] + n - 1 (device int32 [batch]; NULL: 0) of layer `layer` back as out_type
+ * TASP_BF16 or TASP_F32 values, [batch][n_kv_heads][n] by the strides (token stride: from row to row); rows outside the table
+ * read as zeros. n as for tasp_seq_read. Stream-ordered, capturable. Errors as tasp_page_append. */
+tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const int32_t* first,
+                           int32_t n, int32_t out_type, const tasp_rows* k_out,
+                           const tasp_rows* v_out, void* stream);
+
+/* Causal attention of packed tokens (their rows already appended): token i of a sequence sees its rows 0..len + i that have
+ * pages, with scores scale * q . k. q, out: rows of n_q_heads heads (a multiple of n_kv_heads, at most 8 per KV head; query head
+ * h reads KV head h / (n_q_heads / n_kv_heads)) of act_type; out must not overlap q or the cache. Outputs of absent tokens and of
+ * tokens that see no row are zeros, and what unseen rows hold (NaN, infinities) reaches no output (a page's scale belongs to all
+ * of its rows). TASP_BF16: q and V exact, probabilities in 16 bits, sums in float32; TASP_F32: everything to 24 bits. The ends
+ * of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
+ * that are expected (max_len 0..max_pages * page_rows, max_new 1..n_tokens): they size launches and workspace; more is served too.
+ * workspace: device, 256-byte aligned, at least tasp_page_attention_workspace_bytes for the same cache shape, n_q_heads,
+ * n_tokens, max_len and max_new; its contents need no clearing; calls that overlap need one each. Stream-ordered,
+ * capturable. Errors as tasp_page_append, TASP_ERR_WORKSPACE. */
+tasp_status tasp_page_attention_workspace_bytes(const tasp_page_cache* cache, int32_t n_q_heads,
+                                                int32_t n_tokens, int32_t max_len, int32_t max_new,
+                                                size_t* bytes);
+tasp_status tasp_page_attention(const tasp_page_cache* cache, int32_t layer, const int32_t* start,
+                                int32_t n_tokens, int32_t act_type, const tasp_rows* q,
+                                int32_t n_q_heads, double scale, int32_t max_len, int32_t max_new,
+                                const tasp_rows* out, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* Scores of given tokens. logits (device): `rows` rows of vocab values, TASP_F32 or TASP_BF16, row_stride elements from
+ * one to the next; tokens (device int32 [rows]); p = softmax(row / temperature). Per row:
+ *   logprob (float32 [rows])   log p(token); 0 for a token outside the vocabulary (padding)
+ *   entropy (float32 [rows])   of p in nats; may be NULL
+ *   rank (int32 [rows])        tokens before this one in the order of logits, equal ones by id (0: the most likely); -1 for
+ *                              padding; may be NULL
+ *   top_ids, top_logprobs      ([rows][n_top], n_top 0..TASP_TOP_MAX) the n_top first tokens in that order with their log
+ *                              probabilities; -1 and -inf behind the last token above -inf
+ * mean (float32 [n_seqs], with start device int32 [n_seqs + 1]; both may be NULL): the mean logprob of rows start[i]..start[i + 1] - 1
+ * whose tokens lie in the vocabulary (0 where there are none; bounds are cut to 0..rows): what tasp_route takes as
+ * proxy_logprob, over a prompt's rows of logits and next tokens.
+ * NaN logits count as -inf, magnitudes of 2^126 / max(1, log2(e) / temperature) and more as infinite; infinite logits share the
+ * whole probability evenly. A row without a logit above -inf has logprob -inf and entropy 0. Terms in float32, sums joined in float64.
+ * workspace: device, 256-byte aligned, at least tasp_token_logprobs_workspace_bytes, needs no clearing; calls that overlap need
+ * one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, types, a temperature outside 1e-30..1e30),
+ * TASP_ERR_SHAPE (rows, vocab 1..2^24, n_top, n_seqs), TASP_ERR_WORKSPACE. */
+#define TASP_TOP_MAX 32
+tasp_status tasp_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes);
+tasp_status tasp_token_logprobs(const void* logits, int32_t logits_type, int64_t row_stride,
+                                const int32_t* tokens, int32_t rows, int32_t vocab, double temperature,
+                                int32_t n_top, float* logprob, float* entropy, int32_t* rank,
+                                int32_t* top_ids, float* top_logprobs, const int32_t* start,
+                                int32_t n_seqs, float* mean, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 /* Plain streaming copy of `bytes` (multiple of 16) from src to dst (device, not overlapping):
  * the reference kernel whose counter readings calibrate memory-traffic measurements (the byte
  * ledger of appendix "FLOP and storage validation" checked against hardware counters).

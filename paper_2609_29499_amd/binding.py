@@ -36,6 +36,8 @@ EXPORTS = ["tasp_plan_workspace_bytes", "tasp_compile_plan", "tasp_plan_counts",
            "tasp_seq_append", "tasp_seq_read", "tasp_tree_attention_workspace_bytes", "tasp_tree_attention",
            "tasp_verify_workspace_bytes", "tasp_verify", "tasp_seq_commit",
            "tasp_seq_bind", "tasp_tree_step_workspace_bytes", "tasp_tree_forward", "tasp_tree_step",
+           "tasp_page_append", "tasp_page_read", "tasp_page_attention_workspace_bytes", "tasp_page_attention",
+           "tasp_token_logprobs_workspace_bytes", "tasp_token_logprobs",
            "tasp_status_string", "tasp_last_error"]
 
 
@@ -105,6 +107,13 @@ class tasp_seq_cache(C.Structure):
                 ("plan_sig", C.c_uint64)]
 
 
+class tasp_page_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("type", C.c_int32), ("n_layers", C.c_int32),
+                ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_rows", C.c_int32), ("head_dim", C.c_int32),
+                ("batch", C.c_int32), ("max_pages", C.c_int32), ("plan_sig", C.c_uint64)]
+
+
 class tasp_rows(C.Structure):
     _fields_ = [("p", C.c_void_p), ("seq", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
@@ -120,6 +129,7 @@ BF16, F32, INT8, E4M3 = 0, 1, 2, 3
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "wavelength": 2, "index": 3}
 TREE_MAX, SEQ_MAX_BATCH = 64, 256
+PAGE_MAX_TOKENS, TOP_MAX = 262143, 32
 
 _lib = None
 
@@ -179,6 +189,12 @@ def load(path: str = LIB_PATH):
         "tasp_tree_step_workspace_bytes": [P, P, I32, I32, C.POINTER(SZ)],
         "tasp_tree_forward": [P, P, P, I32, P, I32, P, P, SZ, P],
         "tasp_tree_step": [P, P, P, P, P, P, P, C.c_double, I32, I32, P, P, P, P, P, P, P, SZ, P],
+        "tasp_page_append": [P, I32, P, P, I32, I32, P, P, P, I32, P, P],
+        "tasp_page_read": [P, I32, P, I32, I32, P, P, P],
+        "tasp_page_attention_workspace_bytes": [P, I32, I32, I32, I32, C.POINTER(SZ)],
+        "tasp_page_attention": [P, I32, P, I32, I32, P, I32, C.c_double, I32, I32, P, P, SZ, P],
+        "tasp_token_logprobs_workspace_bytes": [I32, I32, I32, C.POINTER(SZ)],
+        "tasp_token_logprobs": [P, I32, C.c_int64, P, I32, I32, C.c_double, I32, P, P, P, P, P, P, I32, P, P, SZ, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -437,3 +453,48 @@ def tasp_tree_step(plan, embed_ptr, scale_ptr, tokens_ptr, parent_ptr, u_ptr, dr
     _check(load().tasp_tree_step(plan, embed_ptr, scale_ptr, tokens_ptr, parent_ptr, u_ptr, draft_ptr, temperature, T,
                                  max_len, _ref(cache), ids_ptr, path_ptr, n_ptr, x_ptr, logits_ptr, ws_ptr, ws_bytes,
                                  stream))
+
+
+def tasp_page_append(cache, layer, rope, start_ptr, n_tokens, act_type, q, k, v, n_q_heads, q_out, stream):
+    """As tasp_seq_append: structs, their bytes or their addresses."""
+    if not (type(k) is type(v) is bytes and (q is None or type(q) is type(q_out) is bytes)):
+        q, k, v, q_out = _ref(q), _ref(k), _ref(v), _ref(q_out)
+    st = (_lib or load()).tasp_page_append(_ref(cache), layer, _ref(rope), start_ptr, n_tokens, act_type, q, k, v, n_q_heads,
+                                           q_out, stream)
+    if st:
+        _check(st)
+
+
+def tasp_page_read(cache, layer, first_ptr, n, out_type, k_out, v_out, stream):
+    st = (_lib or load()).tasp_page_read(_ref(cache), layer, first_ptr, n, out_type, _ref(k_out), _ref(v_out), stream)
+    if st:
+        _check(st)
+
+
+def tasp_page_attention_workspace_bytes(cache, n_q_heads, n_tokens, max_len, max_new):
+    n = C.c_size_t()
+    _check(load().tasp_page_attention_workspace_bytes(_ref(cache), n_q_heads, n_tokens, max_len, max_new, C.byref(n)))
+    return n.value
+
+
+def tasp_page_attention(cache, layer, start_ptr, n_tokens, act_type, q, n_q_heads, scale, max_len, max_new, out, ws_ptr,
+                        ws_bytes, stream):
+    st = (_lib or load()).tasp_page_attention(_ref(cache), layer, start_ptr, n_tokens, act_type, _ref(q), n_q_heads, scale,
+                                              max_len, max_new, _ref(out), ws_ptr, ws_bytes, stream)
+    if st:
+        _check(st)
+
+
+def tasp_token_logprobs_workspace_bytes(rows, vocab, n_top):
+    n = C.c_size_t()
+    _check(load().tasp_token_logprobs_workspace_bytes(rows, vocab, n_top, C.byref(n)))
+    return n.value
+
+
+def tasp_token_logprobs(logits_ptr, logits_type, row_stride, tokens_ptr, rows, vocab, temperature, n_top, logprob_ptr,
+                        entropy_ptr, rank_ptr, ids_ptr, top_ptr, start_ptr, n_seqs, mean_ptr, ws_ptr, ws_bytes, stream):
+    st = (_lib or load()).tasp_token_logprobs(logits_ptr, logits_type, row_stride, tokens_ptr, rows, vocab, temperature,
+                                              n_top, logprob_ptr, entropy_ptr, rank_ptr, ids_ptr, top_ptr, start_ptr,
+                                              n_seqs, mean_ptr, ws_ptr, ws_bytes, stream)
+    if st:
+        _check(st)

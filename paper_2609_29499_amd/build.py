@@ -20,6 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["plan_kernels.hip", "gemv_kernels.hip", "mfma_kernels.hip", "attn_kernels.hip",
            "prefill_kernels.hip", "prefill_i8.hip", "prefill_attn.hip", "mask_kernels.hip", "token_kernels.hip",
            "router_kernels.hip", "shared_kernels.hip", "seq_cache.hip", "tree_attn.hip", "verify.hip",
+           "page_cache.hip", "page_attn.hip", "logprob.hip",
            "runtime.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -14,6 +14,8 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "logprob.hpp"
+#include "page.hpp"
 #include "seq.hpp"
 #include "tasp.h"
 
@@ -2085,8 +2087,9 @@ tasp_status check_rope(const tasp_rope* r, int dh) {
   return TASP_OK;
 }
 
-// rotation of the append kernel from a checked tasp_rope, or a plan's (any theta above 0); NULL: none
-void rope_args(const tasp_rope* r, tasp::SeqAppendArgs* a) {
+// rotation of an append kernel from a checked tasp_rope, or a plan's (any theta above 0); NULL: none
+template <class Args>
+void rope_args(const tasp_rope* r, Args* a) {
   if (!r) return;
   constexpr double kTurn = 6.28318530717958647693;
   const int n = r->rot_dim;
@@ -2445,6 +2448,199 @@ tasp_status tasp_tree_step(tasp_plan p, const int8_t* embed, const float* embed_
                        temperature, ids, path, n, ws + attn, stream)))
     return st;
   return tasp_seq_commit(cache, path, n, T, cache->len, stream);
+}
+
+// ---- caches in pages, scores of given tokens
+
+namespace {
+
+tasp_status check_page_cache(const tasp_page_cache* c, int32_t layer) {
+  if (!c) return fail(TASP_ERR_INVALID_ARG, "cache is NULL");
+  if (c->type != TASP_BF16 && c->type != TASP_INT8 && c->type != TASP_E4M3)
+    return fail(TASP_ERR_INVALID_ARG, "cache type %d", c->type);
+  if (c->page_rows != 16 && c->page_rows != 32 && c->page_rows != 64 && c->page_rows != 128)
+    return fail(TASP_ERR_SHAPE, "pages of %d rows (16, 32, 64 or 128)", c->page_rows);
+  if (c->n_layers < 1 || c->n_pages < 1 || c->batch < 1 || c->batch > TASP_SEQ_MAX_BATCH || c->n_kv_heads < 1 ||
+      c->n_kv_heads > 64 || c->max_pages < 1 || (c->head_dim != 64 && c->head_dim != 128) ||
+      int64_t(c->max_pages) * c->page_rows > (int64_t(1) << 23))
+    return fail(TASP_ERR_SHAPE, "cache of %d layers, %d pages of %d rows, %d heads of %d, batch %d of %d pages", c->n_layers,
+                c->n_pages, c->page_rows, c->n_kv_heads, c->head_dim, c->batch, c->max_pages);
+  if (layer < 0 || layer >= c->n_layers) return fail(TASP_ERR_SHAPE, "layer %d of %d", layer, c->n_layers);
+  return TASP_OK;
+}
+
+tasp_status check_page_buffers(const tasp_page_cache* c) {
+  if (!c->k || !c->v || !c->table || !c->len) return fail(TASP_ERR_INVALID_ARG, "cache k / v / table / len is NULL");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(TASP_ERR_INVALID_ARG, "cache k / v is not 16-byte aligned");
+  if (c->type != TASP_BF16 && (!c->k_scale || !c->v_scale))
+    return fail(TASP_ERR_INVALID_ARG, "an 8-bit cache needs k_scale and v_scale");
+  if (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4) || !aligned(c->table, 4) || !aligned(c->len, 4))
+    return fail(TASP_ERR_INVALID_ARG, "scales / table / len are not 4-byte aligned");
+  return TASP_OK;
+}
+
+tasp_status check_packed(const tasp_page_cache* c, const int32_t* start, int32_t n_tokens) {
+  if (n_tokens < 1 || n_tokens > TASP_PAGE_MAX_TOKENS)
+    return fail(TASP_ERR_SHAPE, "%d tokens (1..%d)", n_tokens, TASP_PAGE_MAX_TOKENS);
+  if (!start && n_tokens != c->batch) return fail(TASP_ERR_SHAPE, "%d tokens of %d sequences without start", n_tokens, c->batch);
+  if (!aligned(start, 4)) return fail(TASP_ERR_INVALID_ARG, "start is not 4-byte aligned");
+  return TASP_OK;
+}
+
+tasp::PageLayer page_layer(const tasp_page_cache* c, int layer) {
+  const size_t units = size_t(layer) * c->n_pages * c->n_kv_heads;
+  const size_t at = units * c->page_rows * c->head_dim * (c->type == TASP_BF16 ? 2 : 1);
+  tasp::PageLayer y{};
+  y.k = static_cast<char*>(c->k) + at;
+  y.v = static_cast<char*>(c->v) + at;
+  if (c->type != TASP_BF16) {
+    y.ks = c->k_scale + units;
+    y.vs = c->v_scale + units;
+  }
+  y.table = c->table; y.len = c->len; y.type = c->type; y.batch = c->batch; y.n_kv = c->n_kv_heads; y.n_pages = c->n_pages;
+  y.width = c->max_pages; y.P = c->page_rows; y.P_log = __builtin_ctz(unsigned(c->page_rows)); y.dh = c->head_dim;
+  y.cap = c->max_pages * c->page_rows;
+  return y;
+}
+
+tasp_status page_attn_args(const tasp_page_cache* c, int32_t n_q, int32_t n_tokens, int32_t max_len, int32_t max_new,
+                           tasp::PageAttnArgs* a) {
+  if (n_q < 1 || n_q % c->n_kv_heads || n_q / c->n_kv_heads > 8)
+    return fail(TASP_ERR_SHAPE, "%d query heads over %d KV heads (1..8 per KV head)", n_q, c->n_kv_heads);
+  if (n_tokens < 1 || n_tokens > TASP_PAGE_MAX_TOKENS)
+    return fail(TASP_ERR_SHAPE, "%d tokens (1..%d)", n_tokens, TASP_PAGE_MAX_TOKENS);
+  if (max_len < 0 || max_len > c->max_pages * c->page_rows)
+    return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_pages * c->page_rows);
+  if (max_new < 1 || max_new > n_tokens) return fail(TASP_ERR_SHAPE, "max_new %d outside 1..%d", max_new, n_tokens);
+  a->c = page_layer(c, 0);
+  a->N = n_tokens; a->max_len = max_len; a->max_new = max_new; a->slots = c->n_kv_heads; a->group = n_q / c->n_kv_heads;
+  for (int j = 0; j < a->slots; ++j) a->slot[j] = tasp::tree_slot(j, j * a->group, a->group);
+  return TASP_OK;
+}
+
+}  // namespace
+
+tasp_status tasp_page_append(const tasp_page_cache* cache, int32_t layer, const tasp_rope* rope,
+                             const int32_t* start, int32_t n_tokens, int32_t act_type, const tasp_rows* q,
+                             const tasp_rows* k, const tasp_rows* v, int32_t n_q_heads,
+                             const tasp_rows* q_out, void* stream) {
+  tasp_status st;
+  tasp::PageAppendArgs a{};
+  if ((st = check_page_cache(cache, layer)) || (st = check_page_buffers(cache)) || (st = check_packed(cache, start, n_tokens)) ||
+      (st = check_rows(k, act_type, "k", &a.k)) || (st = check_rows(v, act_type, "v", &a.v)))
+    return st;
+  if (n_q_heads < 0 || n_q_heads > 512) return fail(TASP_ERR_SHAPE, "%d query heads", n_q_heads);
+  if (n_q_heads > 0) {
+    if ((st = check_rows(q, act_type, "q", &a.q)) || (st = check_rows(q_out, act_type, "q_out", &a.q_out))) return st;
+  } else if ((q && q->p) || (q_out && q_out->p)) {
+    return fail(TASP_ERR_INVALID_ARG, "q given with 0 query heads");
+  }
+  if ((st = check_rope(rope, cache->head_dim))) return st;
+  rope_args(rope, &a);
+  a.c = page_layer(cache, layer);
+  a.start = start; a.N = n_tokens; a.act = act_type; a.n_q = n_q_heads; a.n_kv = cache->n_kv_heads;
+  HIP_TRY(tasp::launch_page_append(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const int32_t* first, int32_t n,
+                           int32_t out_type, const tasp_rows* k_out, const tasp_rows* v_out, void* stream) {
+  tasp_status st;
+  tasp::PageReadArgs a{};
+  if ((st = check_page_cache(cache, layer)) || (st = check_page_buffers(cache)) ||
+      (st = check_rows(k_out, out_type, "k_out", &a.k)) || (st = check_rows(v_out, out_type, "v_out", &a.v)))
+    return st;
+  const int64_t per = 8 * tasp::kBlock / cache->head_dim;    // rows of a workgroup
+  if (n < 1 || n > kMaxGrid * per) return fail(TASP_ERR_SHAPE, "%d rows (1..%lld)", n, (long long)(kMaxGrid * per));
+  if (!aligned(first, 4)) return fail(TASP_ERR_INVALID_ARG, "first is not 4-byte aligned");
+  a.c = page_layer(cache, layer);
+  a.first = first; a.n = n; a.out_type = out_type;
+  HIP_TRY(tasp::launch_page_read(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+tasp_status tasp_page_attention_workspace_bytes(const tasp_page_cache* cache, int32_t n_q_heads, int32_t n_tokens,
+                                                int32_t max_len, int32_t max_new, size_t* bytes) {
+  tasp_status st = check_page_cache(cache, 0);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  tasp::PageAttnArgs a{};
+  if ((st = page_attn_args(cache, n_q_heads, n_tokens, max_len, max_new, &a))) return st;
+  *bytes = 0;
+  for (int act : {TASP_BF16, TASP_F32}) {              // launched in blocks of other sizes
+    a.act = act;
+    *bytes = std::max(*bytes, tasp::page_attn_workspace_bytes(a));
+  }
+  return TASP_OK;
+}
+
+tasp_status tasp_page_attention(const tasp_page_cache* cache, int32_t layer, const int32_t* start, int32_t n_tokens,
+                                int32_t act_type, const tasp_rows* q, int32_t n_q_heads, double scale,
+                                int32_t max_len, int32_t max_new, const tasp_rows* out, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  tasp_status st;
+  tasp::PageAttnArgs a{};
+  if ((st = check_page_cache(cache, layer)) || (st = check_page_buffers(cache)) || (st = check_packed(cache, start, n_tokens)) ||
+      (st = check_rows(q, act_type, "q", &a.q)) || (st = check_rows(out, act_type, "out", &a.o)) ||
+      (st = page_attn_args(cache, n_q_heads, n_tokens, max_len, max_new, &a)))
+    return st;
+  a.scale2 = float(scale * 1.44269504088896340736);
+  if (!(scale > 0.0) || !std::isfinite(a.scale2))
+    return fail(TASP_ERR_INVALID_ARG, "scale must be positive, and finite in 32 bits");
+  a.c = page_layer(cache, layer);
+  a.start = start; a.act = act_type;
+  if ((st = check_workspace(workspace, workspace_bytes, tasp::page_attn_workspace_bytes(a)))) return st;
+  a.ws = static_cast<float*>(workspace);
+  HIP_TRY(tasp::launch_page_attn(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+namespace {
+
+tasp_status check_logprob_shape(int32_t rows, int32_t vocab, int32_t n_top) {
+  if (rows < 1 || rows > kMaxGrid || vocab < 1 || vocab > (1 << 24) || n_top < 0 || n_top > TASP_TOP_MAX)
+    return fail(TASP_ERR_SHAPE, "%d rows, vocabulary %d (1..2^24), %d alternatives (0..%d)", rows, vocab, n_top, TASP_TOP_MAX);
+  return TASP_OK;
+}
+
+}  // namespace
+
+tasp_status tasp_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes) {
+  tasp_status st = check_logprob_shape(rows, vocab, n_top);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = tasp::logprob_workspace_bytes(rows, vocab, n_top);
+  return TASP_OK;
+}
+
+tasp_status tasp_token_logprobs(const void* logits, int32_t logits_type, int64_t row_stride, const int32_t* tokens,
+                                int32_t rows, int32_t vocab, double temperature, int32_t n_top, float* logprob,
+                                float* entropy, int32_t* rank, int32_t* top_ids, float* top_logprobs,
+                                const int32_t* start, int32_t n_seqs, float* mean, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  tasp_status st = check_logprob_shape(rows, vocab, n_top);
+  if (st) return st;
+  if (logits_type != TASP_BF16 && logits_type != TASP_F32) return fail(TASP_ERR_INVALID_ARG, "type %d of logits", logits_type);
+  if (!logits || !tokens || !logprob) return fail(TASP_ERR_INVALID_ARG, "logits / tokens / logprob is NULL");
+  if (n_top > 0 && (!top_ids || !top_logprobs)) return fail(TASP_ERR_INVALID_ARG, "top_ids / top_logprobs is NULL");
+  if (!start != !mean) return fail(TASP_ERR_INVALID_ARG, "start and mean go together");
+  if (start && (n_seqs < 1 || n_seqs > kMaxGrid)) return fail(TASP_ERR_SHAPE, "%d sequences", n_seqs);
+  if (row_stride < vocab) return fail(TASP_ERR_SHAPE, "rows of %d logits %lld apart", vocab, (long long)row_stride);
+  if (!(temperature >= 1e-30 && temperature <= 1e30))
+    return fail(TASP_ERR_INVALID_ARG, "temperature %g outside 1e-30..1e30", temperature);
+  for (const void* p : {(const void*)tokens, (const void*)logprob, (const void*)entropy, (const void*)rank, (const void*)top_ids,
+                        (const void*)top_logprobs, (const void*)start, (const void*)mean})
+    if (!aligned(p, 4)) return fail(TASP_ERR_INVALID_ARG, "an array is not 4-byte aligned");
+  if (!aligned(logits, logits_type == TASP_F32 ? 4 : 2)) return fail(TASP_ERR_INVALID_ARG, "logits are not aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, tasp::logprob_workspace_bytes(rows, vocab, n_top)))) return st;
+  tasp::LogprobArgs a{};
+  a.logits = logits; a.f32 = logits_type == TASP_F32; a.ld = long(row_stride); a.tokens = tokens; a.rows = rows; a.V = vocab;
+  a.c = float(1.44269504088896340736 / temperature);
+  a.lim = float(std::ldexp(1.0, 126) / std::max(1.0, double(a.c)));
+  a.top = n_top; a.logprob = logprob; a.entropy = entropy; a.rank = rank; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  a.start = start; a.seqs = n_seqs; a.mean = mean; a.ws = workspace;
+  HIP_TRY(tasp::launch_logprob(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
 }
 
 tasp_status tasp_copy_probe(void* dst, const void* src, size_t bytes, void* stream) {

@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -466,15 +467,17 @@ def _on(dev, workspace):
     return workspace
 
 
-class SeqCache:
-    """A cache whose sequences have their own lengths: k, v ``[L][B][Hkv][S][dh]`` as bfloat16, int8 or
-    float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch. They stay the
-    tensors that the cache was made of, whose addresses ``struct`` holds: new values are copied into them."""
-
+class _Fixed:
     def __setattr__(self, name, value):
         if self.__dict__.get(name, value) is not value:  # (c.len += 1 sets the same tensor again)
             raise AttributeError(f"{name} of a cache stays what it is: copy into it, or make another cache")
         super().__setattr__(name, value)
+
+
+class SeqCache(_Fixed):
+    """A cache whose sequences have their own lengths: k, v ``[L][B][Hkv][S][dh]`` as bfloat16, int8 or
+    float8_e4m3fn (8 bits with float32 scales ``[L][B][Hkv][S]``), len int32 ``[B]``, all owned by torch. They stay the
+    tensors that the cache was made of, whose addresses ``struct`` holds: new values are copied into them."""
 
     def __init__(self, k, v, length, k_scale=None, v_scale=None):
         if k.dtype not in (torch.bfloat16, torch.int8, torch.float8_e4m3fn) or k.dim() != 5:
@@ -605,3 +608,167 @@ def seq_commit(cache, path, n, len_out=None, stream=None):
     _launch(B.tasp_seq_commit, dev, stream, cache.struct, _ptr(path, (nb, T), torch.int32, "path"),
             _ptr(n, (nb,), torch.int32, "n"), T, _ptr(len_out, (nb,), torch.int32, "len_out"))
     return len_out
+
+
+# ------------------------------------------- caches in pages, scores of given tokens
+
+class PageCache(_Fixed):
+    """A cache in pages: k, v ``[L][pages][Hkv][rows][dh]`` as bfloat16, int8 or float8_e4m3fn (8 bits with float32 scales
+    ``[L][pages][Hkv]``), table int32 ``[B][max_pages]``, len int32 ``[B]``, all owned by torch. They stay the tensors that the
+    cache was made of, whose addresses ``struct`` holds: new values are copied into them."""
+
+    def __init__(self, k, v, table, length, k_scale=None, v_scale=None):
+        if k.dtype not in (torch.bfloat16, torch.int8, torch.float8_e4m3fn) or k.dim() != 5:
+            raise ValueError(f"k must be a bfloat16, int8 or float8_e4m3fn tensor [L][pages][Hkv][rows][dh], not {k.dtype} {tuple(k.shape)}")
+        if table.dim() != 2:
+            raise ValueError(f"table must be [B][max_pages], not {tuple(table.shape)}")
+        self.dev = _device(k, v, table, length, k_scale, v_scale)
+        self.k, self.v, self.table, self.len, self.k_scale, self.v_scale = k, v, table, length, k_scale, v_scale
+        wide = k.dtype == torch.bfloat16
+        if wide == (k_scale is not None) or wide == (v_scale is not None):
+            raise ValueError("scales go with caches in 8 bits, and only with them")
+        self.n_layers, self.n_pages, self.n_kv, self.page_rows, self.dh = k.shape
+        self.batch, self.max_pages = table.shape
+        self.max_seq = self.max_pages * self.page_rows
+        self.struct = B.tasp_page_cache(
+            _ptr(k, k.shape, k.dtype, "k"), _ptr(v, k.shape, k.dtype, "v"),
+            _ptr(k_scale, k.shape[:3], torch.float32, "k_scale"), _ptr(v_scale, k.shape[:3], torch.float32, "v_scale"),
+            _ptr(table, table.shape, torch.int32, "table"), _ptr(length, (self.batch,), torch.int32, "len"), _SEQ_TYPES[k.dtype],
+            *k.shape, self.batch, self.max_pages, 0)
+
+    @classmethod
+    def empty(cls, n_layers, n_pages, n_kv_heads, page_rows, head_dim, batch, max_pages, dtype=torch.int8, device="cuda"):
+        """A pool of pages that no sequence has yet (table -1, lengths 0)."""
+        shape = (n_layers, n_pages, n_kv_heads, page_rows, head_dim)
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        sc = [None, None] if dtype == torch.bfloat16 else [torch.zeros(shape[:3], device=device) for _ in range(2)]
+        return cls(k, v, torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(batch, dtype=torch.int32, device=device), *sc)
+
+    def _start(self, start):
+        return None if start is None else _ptr(start, (self.batch + 1,), torch.int32, "start")
+
+
+def _packed(t, shape, dtype, what):
+    """The tasp_rows (as bytes) of a tensor [N][heads][dh]."""
+    st = t.stride()
+    if t.shape != shape or t.dtype != dtype or st[2] != 1:
+        raise ValueError(f"{what} must be a {dtype} tensor of {tuple(shape)} with contiguous heads, not {t.dtype} {tuple(t.shape)}")
+    return _pack_rows(t.data_ptr(), 0, st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0)
+
+
+def page_append(cache, layer, q, k, v, start=None, rope=None, q_out=None, stream=None):
+    """Write packed k, v ``[N][Hkv][dh]`` into the pages of their sequences (lengths stay) and return q ``[N][Hq][dh]``
+    rotated (None without queries). start int32 ``[B + 1]``: tokens start[b] .. start[b + 1] - 1 are sequence b's; None:
+    one token of each. Any strides whose rows are 16-byte aligned; bfloat16 or float32."""
+    dev = _device(cache.k, q, k, v, start, q_out)
+    N, dt = k.shape[0], k.dtype
+    kv = (N, cache.n_kv, cache.dh)
+    rq = ro = None
+    n_q = 0
+    if q is not None:
+        n_q = q.shape[1]
+        shape = (N, n_q, cache.dh)
+        rq = _packed(q, shape, dt, "q")
+        if q_out is None:
+            q_out = _like(q, stream) if q.is_contiguous() else _empty(shape, dt, q.device, stream)
+            ro = _dense(q_out, 0, n_q * cache.dh, cache.dh)
+        else:
+            ro = _packed(q_out, shape, dt, "q_out")
+    _launch(B.tasp_page_append, dev, stream, cache.struct, layer, None if rope is None else rope.struct, cache._start(start),
+            N, _SEQ_TYPES[dt], rq, _packed(k, kv, dt, "k"), _packed(v, kv, dt, "v"), n_q, ro)
+    return q_out
+
+
+def page_read(cache, layer, n, first=None, dtype=torch.bfloat16, out=None, stream=None):
+    """(k, v) ``[B][Hkv][n][dh]``: rows first .. first + n - 1 (device int32 [B]; None: 0) as values."""
+    shape = (cache.batch, cache.n_kv, n, cache.dh)
+    if out is not None:
+        k, v = out
+        dev, dt = _device(cache.k, first, k, v), k.dtype
+        rk, rv = _rows(k, shape, dt, "k", 2, 1), _rows(v, shape, dt, "v", 2, 1)
+    else:
+        dev, dt = _device(cache.k, first), dtype
+        k = _empty(shape, dt, cache.k.device, stream)
+        v = _like(k, stream)
+        strides = cache.n_kv * n * cache.dh, cache.dh, n * cache.dh
+        rk, rv = _dense(k, *strides), _dense(v, *strides)
+    _launch(B.tasp_page_read, dev, stream, cache.struct, layer, _ptr(first, (cache.batch,), torch.int32, "first"), n,
+            _SEQ_TYPES[dt], rk, rv)
+    return k, v
+
+
+def page_attention_workspace(cache, n_q_heads, n_tokens, max_len=None, max_new=None, stream=None):
+    """A workspace for page_attention calls of this shape (any layer)."""
+    n = B.tasp_page_attention_workspace_bytes(cache.struct, n_q_heads, n_tokens, cache.max_seq if max_len is None else max_len,
+                                              n_tokens if max_new is None else max_new)
+    return _workspace(n, cache.k.device, stream)
+
+
+def page_attention(cache, layer, q, start=None, scale=None, max_len=None, max_new=None, out=None, workspace=None, stream=None):
+    """Causal attention of the appended tokens' queries ``[N][Hq][dh]`` over their sequences' pages; start as page_append.
+    max_len, max_new: the largest length and number of new tokens of a sequence that are expected; workspace: of
+    page_attention_workspace with the same arguments (else one of the call's own). Rows of tokens that are no sequence's are
+    not written."""
+    dev, dt = _device(cache.k, q, start, out), q.dtype
+    N, n_q = q.shape[:2]
+    shape = (N, n_q, cache.dh)
+    rq = _packed(q, shape, dt, "q")
+    if out is None:
+        out = _like(q, stream) if q.is_contiguous() else _empty(shape, dt, q.device, stream)
+        ro = _dense(out, 0, n_q * cache.dh, cache.dh)
+    else:
+        ro = _packed(out, shape, dt, "out")
+    if max_len is None:
+        max_len = cache.max_seq
+    if max_new is None:
+        max_new = 1 if start is None else N
+    ws = _on(dev, workspace) if workspace is not None else page_attention_workspace(cache, n_q, N, max_len, max_new, stream)
+    _launch(B.tasp_page_attention, dev, stream, cache.struct, layer, cache._start(start), N, _SEQ_TYPES[dt], rq, n_q,
+            cache.dh ** -0.5 if scale is None else scale, max_len, max_new, ro, ws[1], ws[2])
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    """Of every row: the token's log probability, the entropy, the token's rank, the first tokens in the order of logits and
+    their log probabilities; of every sequence of rows the mean log probability (None without ``start``)."""
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    rank: torch.Tensor
+    top_ids: torch.Tensor
+    top_logprobs: torch.Tensor
+    mean: Optional[torch.Tensor]
+
+
+def token_logprobs_workspace(rows, vocab, n_top=0, device="cuda", stream=None):
+    """A workspace for token_logprobs calls of this shape."""
+    return _workspace(B.tasp_token_logprobs_workspace_bytes(rows, vocab, n_top), device, stream)
+
+
+def token_logprobs(logits, tokens, n_top=0, temperature=1.0, start=None, workspace=None, stream=None):
+    """Scores of tokens int32 ``[R]`` (outside the vocabulary: padding) against logits ``[R][V]`` (float32 or bfloat16, rows
+    of any stride). start int32 ``[S + 1]``: rows start[i] .. start[i + 1] - 1 are sequence i's."""
+    dev = _device(logits, tokens, start)
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits must be a float32 or bfloat16 tensor [R][V] with contiguous rows, not {logits.dtype} {tuple(logits.shape)}")
+    R, V = logits.shape
+    S = 0
+    mean = None
+    if start is not None:
+        if start.dim() != 1 or start.shape[0] < 2:
+            raise ValueError(f"start must be [S + 1], not {tuple(start.shape)}")
+        S = start.shape[0] - 1
+    # one allocation of 32-bit numbers for all outputs
+    top = R * n_top
+    buf = _empty((3 * R + 2 * top + S,), torch.float32, logits.device, stream)
+    whole = buf.view(torch.int32)
+    logprob, entropy, rank = buf[:R], buf[R:2 * R], whole[2 * R:3 * R]
+    ids, top_lp = whole[3 * R:3 * R + top].view(R, n_top), buf[3 * R + top:3 * R + 2 * top].view(R, n_top)
+    if S:
+        mean = buf[3 * R + 2 * top:]
+    at = buf.data_ptr()
+    ws = _on(dev, workspace) if workspace is not None else token_logprobs_workspace(R, V, n_top, logits.device, stream)
+    _launch(B.tasp_token_logprobs, dev, stream, logits.data_ptr(), _SEQ_TYPES[logits.dtype], logits.stride(0) if R > 1 else V,
+            _ptr(tokens, (R,), torch.int32, "tokens"), R, V, temperature, n_top, at, at + 4 * R, at + 8 * R, at + 12 * R,
+            at + 12 * R + 4 * top, _ptr(start, (S + 1,), torch.int32, "start"), S, at + 12 * R + 8 * top if S else None, ws[1], ws[2])
+    return TokenLogprobs(logprob, entropy, rank, ids, top_lp, mean)
