@@ -8,8 +8,8 @@
 //
 // The largest: elements above a bound go to a list in LDS as 64-bit keys (the logit as an integer that keeps its order,
 // then the complement of the index: equal logits are in the order of their indices). The bound of the first 4096 elements is
-// the smallest of 32 groups' maxima: at least 32 elements reach it, about 130 do. When the list has grown by 512 it is cut to
-// its first `top`, and the last of them is the new bound: of 128256 logits in no particular order some 200 enter it.
+// the `top`-th largest of 64 groups' maxima, which at least `top` elements reach (some 44 for 32, 6 for 5). When the list has
+// grown by 64 it is cut to its first `top`, and the last of them is the new bound.
 //
 // Bound by memory: a row is read once. Few rows are cut into pieces whose records a second launch joins.
 #include <algorithm>
@@ -23,10 +23,11 @@ namespace {
 
 constexpr int kPer = 16;               // elements of a thread and tile
 constexpr int kTile = kBlock * kPer;
-constexpr int kLimit = 512;            // keys that are ranked by comparing each with each
-constexpr int kKeys = kLimit + kTile;  // the list has room for a whole tile more
-constexpr int kTarget = 1024;          // workgroups aimed at
-constexpr int kPieces = kKeys / kTopMax;          // of a row at most: the join's list holds all their keys
+constexpr int kGrown = 64;             // keys that the list may grow by before it is cut to its first
+constexpr int kLimit = 256;            // keys that are ranked by comparing each with each: one per thread
+constexpr int kKeys = kTopMax + kGrown + kTile;        // the list has room for a whole tile more
+constexpr int kTarget = 512;           // workgroups aimed at
+constexpr int kPieces = kKeys / kTopMax;               // of a row at most: the join's list holds all their keys
 
 struct Sums {
   float m, s, w;                       // maximum; sums of 2^t and of t 2^t, t = (x - m) c
@@ -52,7 +53,7 @@ __device__ __forceinline__ unsigned long long key_of(float x, int i) {
 }
 
 struct List {
-  unsigned long long key[kKeys];
+  __align__(16) unsigned long long key[kKeys + 2];
   unsigned long long best[kTopMax];
   int count, found;
   int part[4];
@@ -63,7 +64,8 @@ __device__ __forceinline__ int block_count(List& z, int v) {   // sum over the w
   __syncthreads();
   return z.part[0] + z.part[1] + z.part[2] + z.part[3];
 }
-// The list's `top` largest keys to its front, in order. All keys are different. Ends behind a barrier; returns their number.
+// The list's `top` largest keys to its front, in order. All keys are different. Begins and ends with a barrier; returns
+// their number.
 __device__ __forceinline__ int rank_list(List& z, int top) {
   const int tid = threadIdx.x;
   __syncthreads();
@@ -88,12 +90,18 @@ __device__ __forceinline__ int rank_list(List& z, int top) {
     if (tid < n) z.key[tid] = z.best[tid];
     __syncthreads();
   }
-  for (int i = tid; i < n; i += kBlock) {
-    const unsigned long long mine = z.key[i];
-    int before = 0;
-    for (int j = 0; j < n; ++j) before += z.key[j] > mine;
-    if (before < out) z.best[before] = mine;
+  if (tid == 0) z.key[n] = 0;          // (pairs are compared)
+  __syncthreads();
+  const unsigned long long mine = tid < n ? z.key[tid] : 0;
+  int before = 0;
+  if ((tid & ~63) < n) {
+#pragma unroll 4
+    for (int j = 0; j < n; j += 2) {
+      const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(&z.key[j]);
+      before += (k.x > mine) + (k.y > mine);
+    }
   }
+  if (tid < n && before < out) z.best[before] = mine;
   __syncthreads();
   if (tid < out) z.key[tid] = z.best[tid];
   if (tid == 0) z.count = out;
@@ -101,35 +109,51 @@ __device__ __forceinline__ int rank_list(List& z, int top) {
   return out;
 }
 
-// Of a row (or a piece of it): sums, elements that come before the token, and its largest keys
+// Of a row (or a piece of it): sums under the maximum m, and elements that come before the token
 struct Record {
   double s, w;
   float m;
   int before;
 };
+// q's sums under the maximum m (a float32 factor: its 2^-22 is what the terms have)
+__device__ __forceinline__ void add_to(Record& rec, const Record& q, float c) {
+  const double d = (double(q.m) - double(rec.m)) * double(c);
+  const double f = double(__builtin_amdgcn_exp2f(float(d)));
+  rec.before += q.before;
+  if (f == 0.0) return;
+  rec.s += q.s * f;
+  rec.w += (q.w + d * q.s) * f;
+}
 
-// Results of a row from its joined record; keys: `n` of them in order. All threads of a wave at least.
+// A token's log probability under a row's record
+struct Scale {
+  double log_s;
+  float m, c, lim;
+  __device__ __forceinline__ Scale(const LogprobArgs& a, const Record& z) : log_s(z.m <= -a.lim ? 0.0 : log2(z.s)), m(z.m), c(a.c), lim(a.lim) {}
+  // (an infinite logit leaves nothing to finite ones; a row without a logit above -inf nothing at all)
+  __device__ __forceinline__ float operator()(float x) const {
+    return m <= -lim || x <= -lim || (m >= lim && x < m) ? -INFINITY
+                                                         : float(((double(x) - double(m)) * double(c) - log_s) * 0.693147180559945309417);
+  }
+};
+// a row's token's logit; false: the token is padding
+__device__ __forceinline__ bool token_logit(const LogprobArgs& a, int row, int t, float& x) {
+  if (t < 0 || t >= a.V) return false;
+  const size_t at = size_t(row) * a.ld + t;
+  x = a.f32 ? static_cast<const float*>(a.logits)[at] : bf16_to_f32(static_cast<const uint16_t*>(a.logits)[at]);
+  x = fminf(fmaxf(x, -a.lim), a.lim);
+  return true;
+}
+// Results of a row from its joined record; keys: `n` of them in order. Of one wave.
 __device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Record& z, const unsigned long long* key, int n) {
   const int tid = threadIdx.x;
-  const bool empty = z.m <= -a.lim;              // no logit above -inf
-  const double log_s = empty ? 0.0 : log2(z.s);
-  constexpr double kLn2 = 0.693147180559945309417;
-  auto lp = [&](float x) {
-    // (an infinite logit leaves nothing to finite ones)
-    return empty || x <= -a.lim || (z.m >= a.lim && x < z.m) ? -INFINITY : float(((double(x) - double(z.m)) * double(a.c) - log_s) * kLn2);
-  };
+  const Scale lp(a, z);
   if (tid == 0) {
-    const int t = a.tokens[row];
-    const bool there = t >= 0 && t < a.V;
-    float x = 0.0f;
-    if (there) {
-      const size_t at = size_t(row) * a.ld + t;
-      x = a.f32 ? static_cast<const float*>(a.logits)[at] : bf16_to_f32(static_cast<const uint16_t*>(a.logits)[at]);
-      x = fminf(fmaxf(x, -a.lim), a.lim);
-    }
+    float x;
+    const bool there = token_logit(a, row, a.tokens[row], x);
     a.logprob[row] = there ? lp(x) : 0.0f;
     if (a.rank) a.rank[row] = there ? z.before : -1;
-    if (a.entropy) a.entropy[row] = empty ? 0.0f : float((log_s - z.w / z.s) * kLn2);
+    if (a.entropy) a.entropy[row] = z.m <= -a.lim ? 0.0f : float((lp.log_s - z.w / z.s) * 0.693147180559945309417);
   }
   if (tid < a.top) {
     const bool in = tid < n;
@@ -146,89 +170,101 @@ __device__ __forceinline__ unsigned long long* keys(const LogprobArgs& a, int pi
 
 // A piece of a row: tiles blockIdx.x * per .. of row blockIdx.y.
 template <bool F32, bool TOP>
-__global__ __launch_bounds__(kBlock) void logprob_kernel(LogprobArgs a, int per) {
+__global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int per) {
+  constexpr int RAW = F32 ? 16 : 8;    // words of a tile's elements per thread
+  constexpr int AHEAD = F32 ? 1 : 2;   // tiles on their way: 16 words either way
   __shared__ List z;
-  __shared__ float s_group[32];
+  __shared__ __align__(16) float s_group[kWave];
   __shared__ Sums s_sums[4];
   __shared__ int s_before[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const char* base = static_cast<const char*>(a.logits) + size_t(row) * a.ld * (F32 ? 4 : 2);
-    const int first = blockIdx.x * per * kTile, end = min(long(a.V), long(first) + long(per) * kTile);
-    // the token: the smallest key that comes before it in order is one more than its own
-    const int token = a.tokens[row];
-    const bool there = token >= 0 && token < a.V;
-    float xt = INFINITY;
-    if (there) {
-      xt = F32 ? reinterpret_cast<const float*>(base)[token] : bf16_to_f32(reinterpret_cast<const uint16_t*>(base)[token]);
-      xt = fminf(fmaxf(xt, -a.lim), a.lim);
-    }
-    // element j of this thread: index i0 + at(j)
-    float x[kPer], nx[kPer];
-    auto index = [&](int tile, int j, bool whole) {
-      return !whole ? tile + j * kBlock + tid : F32 ? tile + (j >> 2) * 4 * kBlock + 4 * tid + (j & 3) : tile + (j >> 3) * 8 * kBlock + 8 * tid + (j & 7);
+    const int first = blockIdx.x * per * kTile, end = int(min(long(a.V), long(first) + long(per) * kTile));
+    // element j of this thread in a tile
+    auto index = [&](int tile, int j) {
+      return tile + kTile > end ? tile + j * kBlock + tid : F32 ? tile + (j >> 2) * 4 * kBlock + 4 * tid + (j & 3) : tile + (j >> 3) * 8 * kBlock + 8 * tid + (j & 7);
     };
-    auto load = [&](int tile, float (&v)[kPer]) {
+    auto load = [&](int tile, uint32_t (&v)[RAW]) __attribute__((always_inline)) {
       if (tile + kTile <= end) {
-        if constexpr (F32) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float4 q;
-            __builtin_memcpy(&q, base + (size_t(tile) + j * 4 * kBlock + 4 * tid) * 4, 16);
-            v[4 * j] = q.x; v[4 * j + 1] = q.y; v[4 * j + 2] = q.z; v[4 * j + 3] = q.w;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t q[4];
-            __builtin_memcpy(q, base + (size_t(tile) + j * 8 * kBlock + 8 * tid) * 2, 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              v[8 * j + 2 * i] = bf16_lo(q[i]);
-              v[8 * j + 2 * i + 1] = bf16_hi(q[i]);
-            }
-          }
-        }
-      } else {                         // the row's last elements, one by one
+        for (int j = 0; j < RAW / 4; ++j) __builtin_memcpy(&v[4 * j], base + size_t(tile) * (F32 ? 4 : 2) + j * 16 * kBlock + 16 * tid, 16);
+      } else if (tile < end) {         // the row's last elements, one by one
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
           const int i = tile + j * kBlock + tid;
-          v[j] = i >= end ? -INFINITY : F32 ? reinterpret_cast<const float*>(base)[i] : bf16_to_f32(reinterpret_cast<const uint16_t*>(base)[i]);
+          if constexpr (F32) {
+            v[j] = i < end ? reinterpret_cast<const uint32_t*>(base)[i] : 0xff800000u;
+          } else {
+            const uint32_t u = i < end ? reinterpret_cast<const uint16_t*>(base)[i] : 0xff80u;
+            v[j / 2] = j & 1 ? v[j / 2] | u << 16 : u;
+          }
         }
       }
     };
+    uint32_t raw[AHEAD][RAW];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) load(first + k * kTile, raw[k]);
+    const int token = a.tokens[row];
+    float xt = INFINITY;               // (padding: nothing comes before it)
+    token_logit(a, row, token, xt);
     Sums sum{-INFINITY, 0.0f, 0.0f};
-    int before = 0;
+    int before = 0, n = 0;
     float bound = -a.lim;              // elements above it enter the list
     __syncthreads();                   // (the row before has been read)
     if (tid == 0) z.count = 0;
-    load(first, nx);
     for (int tile = first; tile < end; tile += kTile) {
-      const bool whole = tile + kTile <= end;
+      float x[kPer];
+      if constexpr (F32) {
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) x[j] = fminf(fmaxf(nx[j], -a.lim), a.lim);      // (NaN is -lim)
-      if (tile + kTile < end) load(tile + kTile, nx);
-      float top = x[0];
+        for (int j = 0; j < kPer; ++j) x[j] = __uint_as_float(raw[0][j]);
+      } else {
 #pragma unroll
-      for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
+        for (int j = 0; j < RAW; ++j) {
+          x[2 * j] = bf16_lo(raw[0][j]);
+          x[2 * j + 1] = bf16_hi(raw[0][j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) x[j] = fmaxf(x[j], -a.lim);                         // (NaN is -lim)
+      float top = fmaxf(x[0], x[1]);
+#pragma unroll
+      for (int j = 2; j < kPer; ++j) top = fmaxf(top, x[j]);
+      if (__ballot(top > a.lim)) {
+        top = fminf(top, a.lim);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = fminf(x[j], a.lim);
+      }
+#pragma unroll
+      for (int k = 0; k + 1 < AHEAD; ++k)
+#pragma unroll
+        for (int j = 0; j < RAW; ++j) raw[k][j] = raw[k + 1][j];
+      load(tile + AHEAD * kTile, raw[AHEAD - 1]);
+      // (places behind the row's end hold -lim: their terms are 0, or the row is empty)
       if (top > sum.m) move_to(sum, top, a.c);
+      float s2 = 0.0f, w2 = 0.0f;
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
         const float t = (x[j] - sum.m) * a.c, e = __builtin_amdgcn_exp2f(t);
-        const bool in = whole || index(tile, j, whole) < end;
-        sum.s += in ? e : 0.0f;
-        sum.w = fmaf(in ? e : 0.0f, t, sum.w);
+        float& s = j & 1 ? s2 : sum.s;
+        float& w = j & 1 ? w2 : sum.w;
+        s += e;
+        w = fmaf(e, t, w);
       }
-      if (token < tile || token >= tile + kTile) {     // (before the token equal ones come first too)
-        const bool equal = token >= tile + kTile;
+      sum.s += s2;
+      sum.w += w2;
+      // before the token equal logits come first too
+      if (token < tile || token >= tile + kTile) {
+        if (token >= tile + kTile) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) before += __popcll(__ballot((x[j] > xt || (equal && x[j] == xt)) && (whole || index(tile, j, whole) < end)));
+          for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] >= xt));
+        } else {
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt));
+        }
       } else {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          const int i = index(tile, j, whole);
-          before += __popcll(__ballot((x[j] > xt || (i < token && x[j] == xt)) && i < end));
-        }
+        for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt || (x[j] == xt && index(tile, j) < token)));
       }
       if constexpr (TOP) {
         bool least = false;            // the bound itself is enough
@@ -236,41 +272,55 @@ __global__ __launch_bounds__(kBlock) void logprob_kernel(LogprobArgs a, int per)
           float g = top;
           g = fmaxf(g, dpp<kQuadXor1>(g));
           g = fmaxf(g, dpp<kQuadXor2>(g));
-          g = fmaxf(g, dpp<kRowHalfMirror>(g));
-          if ((lane & 7) == 0) s_group[tid >> 3] = g;
+          if ((lane & 3) == 0) s_group[tid >> 2] = g;
           __syncthreads();
-          g = s_group[lane & 31];
-          bound = -wave_max(-g);
+          g = s_group[lane];           // 64 groups' maxima, and those that are larger
+          if (a.top > 1) {
+            int larger = 0;
+#pragma unroll
+            for (int j = 0; j < kWave; j += 4) {
+              const float4 q = *reinterpret_cast<const float4*>(&s_group[j]);
+              larger += (q.x > g) + (q.y > g) + (q.z > g) + (q.w > g);
+            }
+            bound = -wave_max(larger < a.top ? -g : -INFINITY);
+          } else {
+            bound = wave_max(g);
+          }
           least = bound > -a.lim;
         }
         if (__ballot(top > bound || (least && top == bound))) {
+          unsigned long long who[kPer];
+          int found = 0;
 #pragma unroll
           for (int j = 0; j < kPer; ++j) {
-            const bool take = x[j] > bound || (least && x[j] == bound);
-            const unsigned long long who = __ballot(take);
-            if (who) {
-              int at = 0;
-              if (lane == 0) at = atomicAdd(&z.count, __popcll(who));
-              at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0));
-              if (take) z.key[at] = key_of(x[j], index(tile, j, whole));
+            who[j] = least ? __ballot(x[j] >= bound) : __ballot(x[j] > bound);
+            found += __popcll(who[j]);
+          }
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&z.count, found);
+          at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) {
+            if (who[j]) {
+              if ((who[j] >> lane) & 1)
+                z.key[at + __builtin_amdgcn_mbcnt_hi(uint32_t(who[j] >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who[j]), 0))] = key_of(x[j], index(tile, j));
+              at += __popcll(who[j]);
             }
           }
         }
         __syncthreads();
         const int count = z.count;
         __syncthreads();               // (read by all before the next tile adds to it)
-        if (count > kLimit) {
-          rank_list(z, a.top);
-          bound = fmaxf(bound, unordered(uint32_t(z.key[a.top - 1] >> 32)));
+        if (count > a.top + kGrown || tile + kTile >= end) {
+          n = rank_list(z, a.top);
+          if (n == a.top) bound = fmaxf(bound, unordered(uint32_t(z.key[a.top - 1] >> 32)));
         }
       }
     }
-    int n = 0;
-    if constexpr (TOP) n = rank_list(z, a.top);
     // the workgroup's sums
     {
       const float m = wave_max(sum.m);
-      if (sum.m > -INFINITY) move_to(sum, m, a.c);
+      move_to(sum, m, a.c);
       const float s = wave_sum(sum.s), w = wave_sum(sum.w);
       if (lane == 0) {
         s_sums[wave] = {m, s, w};
@@ -278,18 +328,12 @@ __global__ __launch_bounds__(kBlock) void logprob_kernel(LogprobArgs a, int per)
       }
       __syncthreads();
     }
+    if (wave > 0) continue;
     Record rec{0.0, 0.0, -INFINITY, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) rec.m = fmaxf(rec.m, s_sums[i].m);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const Sums q = s_sums[i];
-      rec.before += s_before[i];
-      if (q.m == -INFINITY) continue;
-      const double d = (double(q.m) - double(rec.m)) * double(a.c), f = exp2(d);
-      rec.s += double(q.s) * f;
-      rec.w += (double(q.w) + d * double(q.s)) * f;
-    }
+    for (int i = 0; i < 4; ++i) add_to(rec, Record{double(s_sums[i].s), double(s_sums[i].w), s_sums[i].m, s_before[i]}, a.c);
     if (gridDim.x == 1) {
       finish(a, row, rec, z.key, n);
     } else {
@@ -300,51 +344,17 @@ __global__ __launch_bounds__(kBlock) void logprob_kernel(LogprobArgs a, int per)
   }
 }
 
-// Joins the pieces of a row: a workgroup each.
-__global__ __launch_bounds__(kBlock) void logprob_join_kernel(LogprobArgs a, int pieces) {
-  __shared__ List z;
-  __shared__ Record s_rec[kBlock];
-  const int row = blockIdx.x, tid = threadIdx.x;
-  if (tid < pieces) s_rec[tid] = records(a)[size_t(row) * pieces + tid];
-  if (tid == 0) z.count = 0;
-  __syncthreads();
-  const unsigned long long* from = keys(a, pieces) + size_t(row) * pieces * a.top;
-  // a piece's last key has `top` keys at or above it: what lies below the largest of them is out
-  unsigned long long least = 1;
-  for (int i = 0; i < pieces && a.top > 0; ++i) least = max(least, from[i * a.top + a.top - 1]);
-  for (int i = tid; i < pieces * a.top; i += kBlock) {
-    const unsigned long long k = from[i];
-    if (k >= least) z.key[atomicAdd(&z.count, 1)] = k;
-  }
-  int n = 0;
-  if (a.top > 0) n = rank_list(z, a.top);
+// A row's record of its pieces', in their order
+__device__ __forceinline__ Record join(const LogprobArgs& a, const Record* of, int pieces) {
   Record rec{0.0, 0.0, -INFINITY, 0};
-  for (int i = 0; i < pieces; ++i) rec.m = fmaxf(rec.m, s_rec[i].m);
-  for (int i = 0; i < pieces; ++i) {
-    const Record q = s_rec[i];
-    rec.before += q.before;
-    if (q.m == -INFINITY) continue;
-    const double d = (double(q.m) - double(rec.m)) * double(a.c), f = exp2(d);
-    rec.s += q.s * f;
-    rec.w += (q.w + d * q.s) * f;
-  }
-  finish(a, row, rec, z.key, n);
+  for (int i = 0; i < pieces; ++i) rec.m = fmaxf(rec.m, of[i].m);
+  for (int i = 0; i < pieces; ++i) add_to(rec, of[i], a.c);
+  return rec;
 }
-
-// Mean log probability of the rows of a sequence that have a token (0 where none has): a workgroup each.
-__global__ __launch_bounds__(kBlock) void logprob_mean_kernel(LogprobArgs a) {
+__device__ __forceinline__ void put_mean(const LogprobArgs& a, int b, double sum, int n) {
   __shared__ double s_sum[kBlock];
   __shared__ int s_n[kBlock];
-  const int tid = threadIdx.x, b = blockIdx.x;
-  const int lo = max(a.start[b], 0), hi = min(a.start[b + 1], a.rows);
-  double sum = 0.0;
-  int n = 0;
-  for (int i = lo + tid; i < hi; i += kBlock) {
-    const int t = a.tokens[i];
-    if (t < 0 || t >= a.V) continue;
-    sum += double(a.logprob[i]);
-    ++n;
-  }
+  const int tid = threadIdx.x;
   s_sum[tid] = sum;
   s_n[tid] = n;
   for (int k = kBlock / 2; k > 0; k /= 2) {
@@ -357,10 +367,95 @@ __global__ __launch_bounds__(kBlock) void logprob_mean_kernel(LogprobArgs a) {
   if (tid == 0) a.mean[b] = s_n[0] ? float(s_sum[0] / s_n[0]) : 0.0f;
 }
 
+// Joins the pieces of a row: a workgroup each, and behind them one for each sequence's mean, which forms the log
+// probabilities that it needs by itself (a third launch would cost 4 us).
+__global__ __launch_bounds__(kBlock) void logprob_join_kernel(LogprobArgs a, int pieces) {
+  constexpr int kRecords = 1024;       // of several rows at a time, for the means
+  __shared__ union {
+    List z;
+    Record rec[kRecords];
+  } u;
+  __shared__ Record s_rec[kPieces];
+  __shared__ unsigned long long s_least[4];
+  __shared__ __align__(16) unsigned long long s_key[kWave];
+  List& z = u.z;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  if (row >= a.rows) {
+    const int b = row - a.rows, lo = max(a.start[b], 0), hi = min(a.start[b + 1], a.rows), per = min(kBlock, kRecords / pieces);
+    double sum = 0.0;
+    int n = 0;
+    for (int i0 = lo; i0 < hi; i0 += per) {
+      const int here = min(per, hi - i0);
+      float x = 0.0f;
+      const bool mine = tid < here && token_logit(a, i0 + tid, a.tokens[i0 + tid], x);
+      __syncthreads();
+      for (int k = tid; k < here * pieces; k += kBlock) u.rec[k] = records(a)[size_t(i0) * pieces + k];
+      __syncthreads();
+      if (mine) {
+        sum += double(Scale(a, join(a, &u.rec[tid * pieces], pieces))(x));
+        ++n;
+      }
+    }
+    put_mean(a, b, sum, n);
+    return;
+  }
+  const unsigned long long* from = keys(a, pieces) + size_t(row) * pieces * a.top;
+  // What lies below a key that `top` keys reach is out: the largest of the pieces' last keys is one, and, the j-th keys of the
+  // pieces being taken, that of them which ceil(top / j) reach (j = 1 for as many pieces as alternatives)
+  unsigned long long least = 1;
+  const int j = (a.top + pieces - 1) / pieces;
+  if (tid < pieces) {
+    s_rec[tid] = records(a)[size_t(row) * pieces + tid];
+    if (a.top > 0) least = max(least, from[tid * a.top + a.top - 1]);
+  }
+  if (a.top > 0 && tid < kWave) s_key[tid] = tid < pieces ? from[tid * a.top + j - 1] : 0;
+#pragma unroll
+  for (int k = 1; k < kWave; k *= 2) {
+    const unsigned long long o = __shfl_xor(least, k, kWave);
+    least = max(least, o);
+  }
+  if (tid == 0) z.count = 0;
+  if ((tid & 63) == 0) s_least[tid >> 6] = least;
+  __syncthreads();
+  least = max(max(s_least[0], s_least[1]), max(s_least[2], s_least[3]));
+  if (a.top > 0) {
+    const unsigned long long mine = s_key[tid & 63];
+    int larger = 0;
+#pragma unroll 8
+    for (int k = 0; k < kWave; k += 2) {
+      const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s_key[k]);
+      larger += (q.x > mine) + (q.y > mine);
+    }
+    const unsigned long long who = __ballot(mine > 0 && larger == (a.top + j - 1) / j - 1);      // (keys are different)
+    if (who) least = max(least, s_key[__ffsll((long long)who) - 1]);
+  }
+  for (int i = tid; i < pieces * a.top; i += kBlock) {
+    const unsigned long long k = from[i];
+    if (k >= least) z.key[atomicAdd(&z.count, 1)] = k;
+  }
+  int n = 0;
+  if (a.top > 0) n = rank_list(z, a.top);
+  if (tid < kWave) finish(a, row, join(a, s_rec, pieces), z.key, n);
+}
+
+// Mean log probability of the rows of a sequence that have a token (0 where none has): a workgroup each.
+__global__ __launch_bounds__(kBlock) void logprob_mean_kernel(LogprobArgs a) {
+  const int b = blockIdx.x, lo = max(a.start[b], 0), hi = min(a.start[b + 1], a.rows);
+  double sum = 0.0;
+  int n = 0;
+  for (int i = lo + threadIdx.x; i < hi; i += kBlock) {
+    const int t = a.tokens[i];
+    if (t < 0 || t >= a.V) continue;
+    sum += double(a.logprob[i]);
+    ++n;
+  }
+  put_mean(a, b, sum, n);
+}
+
 // pieces of a row: tiles of each, such that there are about kTarget workgroups
 int tiles_per_piece(int rows, int V) {
   const int tiles = (V + kTile - 1) / kTile;
-  const int pieces = std::min({std::max(1, kTarget / rows), tiles, kPieces});
+  const int pieces = std::min({(kTarget + rows - 1) / rows, tiles, kPieces});
   return (tiles + pieces - 1) / pieces;
 }
 int pieces_of(int rows, int V) {
@@ -385,8 +480,8 @@ hipError_t launch_logprob(const LogprobArgs& a, hipStream_t s) {
     if (a.top) hipLaunchKernelGGL((logprob_kernel<false, true>), grid, dim3(kBlock), 0, s, a, per);
     else hipLaunchKernelGGL((logprob_kernel<false, false>), grid, dim3(kBlock), 0, s, a, per);
   }
-  if (pieces > 1) hipLaunchKernelGGL(logprob_join_kernel, dim3(a.rows), dim3(kBlock), 0, s, a, pieces);
-  if (a.start) hipLaunchKernelGGL(logprob_mean_kernel, dim3(a.seqs), dim3(kBlock), 0, s, a);
+  if (pieces > 1) hipLaunchKernelGGL(logprob_join_kernel, dim3(a.rows + (a.start ? a.seqs : 0)), dim3(kBlock), 0, s, a, pieces);
+  else if (a.start) hipLaunchKernelGGL(logprob_mean_kernel, dim3(a.seqs), dim3(kBlock), 0, s, a);
   return hipGetLastError();
 }
 
