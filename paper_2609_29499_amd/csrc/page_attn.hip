@@ -14,9 +14,15 @@
 // Softmax with a running maximum per query row, raised only when a score passes it by 8 powers of two (sums are
 // float32, so the slack costs no accuracy): most steps exchange nothing between lanes.
 //
-// The cache rows of all sequences are cut into chunks of equal length (from the lengths on the device: no host knows
-// them); a workgroup takes one chunk of one cache head. A sequence of one chunk is written at once; the others leave
-// (maximum, sum, unnormalised output) per query row in the workspace, which a second launch joins in chunk order.
+// Two kernels. Up to 32 query rows of a sequence and cache head (page_attn_kernel): a wave keeps all of them and walks every
+// fourth step straight from memory in the operands' layout, the next step's loads in flight. More
+// (page_attn_wide_kernel): blocks of 64 or 128 rows are dealt to the four waves, which share steps of 64 cache rows
+// through LDS (below).
+//
+// A workgroup takes one chunk of the cache rows of one block of query rows and cache head. Chunks have equal lengths, found
+// from the lengths on the device (no host knows them) such that there are about two workgroups per CU. A block of one
+// chunk is written at once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which
+// another launch joins in chunk order.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,59 +34,65 @@ namespace tasp {
 namespace {
 
 constexpr int kStep = 32;              // cache rows per step
+constexpr int kWideStep = 64;          // and in the wide kernel
 constexpr int kMinSteps = 4;           // steps of a chunk at least, and its granule: one per wave
 constexpr float kSlack = 8.0f;         // powers of two a score may pass the running maximum by
 constexpr int kTarget = 512;           // workgroups aimed at: two per CU
+constexpr int kFew = 32;               // query rows of a sequence and cache head that the first kernel serves
 
-// How a call is launched: query rows in blocks of `rows`, at most rb of them in a sequence that is cut; chunks of all
-// sequences, `room` at most; items: of the grid
+// How a kernel is launched. Sequences with least .. most query rows per cache head, in blocks of `rows` = 2^rows_log; steps of
+// `step` rows; items: chunks of all blocks, at most; cut: there may be several chunks of a block
 struct PageShape {
-  int mt, rows, rows_log, rb, room, items, cut;
+  int least, most, mt, rows, rows_log, step, items, cut;
+  size_t ws;                           // floats of the workspace in front of its records
 };
 struct Deal {
-  int chunk, total;                    // steps per chunk; chunks of all sequences
-  int mine[4], before[4];              // of the lane's sequences: chunks, and those of the sequences before them
+  int chunk, total;                    // steps per chunk; items of all sequences
+  int nch[4], mine[4], before[4];      // of the lane's sequences: chunks of a block, items, items of the sequences before them
   int first[4], n[4], len[4];
 };
-// A lane holds four sequences. The chunk is the shortest multiple of kMinSteps that leaves at most `room` chunks.
+// A lane holds four sequences. The chunk is the shortest multiple of kMinSteps that leaves at most `items` items.
 __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, int lane) {
   Deal d;
-  int steps[4], sum = 0, most = 0;
+  int steps[4], blocks[4], sum = 0, most = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const PageSeq q = page_seq(a.start, a.N, a.c, min(4 * lane + i, a.c.batch - 1));
     d.first[i] = q.first; d.len[i] = q.L;
-    d.n[i] = 4 * lane + i < a.c.batch ? q.n : 0;
+    const int rows = q.n * a.group;
+    d.n[i] = 4 * lane + i < a.c.batch && rows >= y.least && rows <= y.most ? q.n : 0;
     const int end = q.L < 0 ? 0 : min(q.L + d.n[i], a.c.cap);
-    steps[i] = d.n[i] == 0 ? 0 : max(1, (end + kStep - 1) / kStep);
-    sum += steps[i];
+    steps[i] = d.n[i] == 0 ? 0 : max(1, (end + y.step - 1) / y.step);
+    blocks[i] = (d.n[i] * a.group + y.rows - 1) >> y.rows_log;
+    sum += steps[i] * min(blocks[i], kTarget);
     most = max(most, steps[i]);
   }
-  sum = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
-  most = int(wave_max(float(most)));   // (below 2^24)
-  auto count = [&](int chunk, int i, float inv) {
-    return d.n[i] * a.group > y.rb * y.rows || !y.cut ? min(steps[i], 1) : quot_steps(steps[i] + chunk - 1, chunk, inv);
-  };
-  auto total = [&](int chunk) {
-    const float inv = __builtin_amdgcn_rcpf(float(chunk));
-    int own = 0;
+  d.chunk = 1 << 24;
+  if (y.cut) {
+    auto total = [&](int chunk) {
+      const float inv = __builtin_amdgcn_rcpf(float(chunk));
+      int own = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) own += count(chunk, i, inv);
-    return __builtin_amdgcn_readlane(wave_scan(own), kWave - 1);
-  };
-  // in units of kMinSteps: lo may do, hi does
-  int lo = max(1, ((sum + y.room - 1) / y.room + kMinSteps - 1) / kMinSteps), hi = max(lo, (most + kMinSteps - 1) / kMinSteps);
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (total(mid * kMinSteps) <= y.room) hi = mid;
-    else lo = mid + 1;
+      for (int i = 0; i < 4; ++i) own += blocks[i] * quot_steps(steps[i] + chunk - 1, chunk, inv);
+      return __builtin_amdgcn_readlane(wave_scan(own), kWave - 1);
+    };
+    sum = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
+    most = int(wave_max(float(most)));                 // (below 2^24)
+    // in units of kMinSteps: lo may do, hi does
+    int lo = max(1, ((sum + y.items - 1) / y.items + kMinSteps - 1) / kMinSteps), hi = max(lo, (most + kMinSteps - 1) / kMinSteps);
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (total(mid * kMinSteps) <= y.items) hi = mid;
+      else lo = mid + 1;
+    }
+    d.chunk = lo * kMinSteps;
   }
-  d.chunk = lo * kMinSteps;
   const float inv = __builtin_amdgcn_rcpf(float(d.chunk));
   int own = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    d.mine[i] = count(d.chunk, i, inv);
+    d.nch[i] = y.cut ? quot_steps(steps[i] + d.chunk - 1, d.chunk, inv) : min(steps[i], 1);
+    d.mine[i] = blocks[i] * d.nch[i];
     d.before[i] = own;
     own += d.mine[i];
   }
@@ -95,20 +107,25 @@ __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, 
 struct Place {
   int b, g, head;                      // sequence, slot, its cache head
   int h0, group, R;                    // the slot's first query head, its heads, its query rows
-  int n_ch, ch, before;                // chunks of the sequence, this one, those of the sequences before
-  int first, n, L, end;                // its tokens, rows it held (-1: passed over), rows that may be read
+  int item, nch, ch, block;            // among all items; chunks of the block, this one; block of query rows
+  int first, n, L;                     // the sequence's tokens, rows it held (-1: passed over)
+  int common, end;                     // rows that all of the block's tokens see, and that any does
   int s0, s1;                          // steps
 };
+// false: nothing to do. Grid (slots, kItems, items / kItems): slots take turns, so that with eight of them a cache head's
+// workgroups run on one XCD and share its L2.
+constexpr int kItems = 1024;
+__device__ __forceinline__ void note_tokens(const PageAttnArgs& a, const PageShape& y, const Place& p);
 __device__ __forceinline__ bool place(const PageAttnArgs& a, const PageShape& y, int lane, Place& p) {
-  const int item = blockIdx.z * 8 + blockIdx.x, all = quot(item, a.slots);
-  p.g = item - all * a.slots;
+  p.item = blockIdx.z * kItems + blockIdx.y;
+  p.g = blockIdx.x;
   const int slot = a.slot[p.g];
   const Deal d = deal(a, y, lane);
-  if (all >= d.total) return false;
+  if (p.item >= d.total) return false;
   int hit = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (all >= d.before[i] && all < d.before[i] + d.mine[i]) hit = i;
+    if (p.item >= d.before[i] && p.item < d.before[i] + d.mine[i]) hit = i;
   const int owner = __builtin_amdgcn_readfirstlane(__ffsll((long long)__ballot(hit >= 0)) - 1), sub = __builtin_amdgcn_readlane(hit, owner);
   p.b = 4 * owner + sub;
   p.head = slot & 0xff;
@@ -118,13 +135,20 @@ __device__ __forceinline__ bool place(const PageAttnArgs& a, const PageShape& y,
   p.n = pick(d.n, owner, sub);
   p.L = pick(d.len, owner, sub);
   p.R = p.n * p.group;
-  p.n_ch = pick(d.mine, owner, sub);
-  p.before = pick(d.before, owner, sub);
-  p.ch = all - p.before;
-  p.end = p.L < 0 ? 0 : min(p.L + p.n, a.c.cap);
-  const int steps = (p.end + kStep - 1) / kStep;
-  p.s0 = p.ch * d.chunk;
-  p.s1 = p.n_ch == 1 ? steps : min(steps, p.s0 + d.chunk);
+  p.nch = pick(d.nch, owner, sub);
+  const int local = p.item - pick(d.before, owner, sub), k = quot(local, p.nch), blocks = quot(pick(d.mine, owner, sub), p.nch);
+  p.ch = local - k * p.nch;
+  p.block = blocks - 1 - k;            // the last rows, which see the most, first
+  const int r0 = p.block << y.rows_log;
+  if (y.cut && p.ch == 0 && p.g == 0) note_tokens(a, y, p);
+  if (r0 >= p.R) return false;         // (a slot with fewer heads than the largest)
+  const int t_first = quot(r0, p.group), t_last = quot(min(p.R, r0 + y.rows) - 1, p.group);
+  const int most = p.L < 0 ? 0 : min(p.L + p.n, a.c.cap);
+  p.common = p.L < 0 ? 0 : min(p.L + t_first + 1, most);
+  p.end = p.L < 0 ? 0 : min(p.L + t_last + 1, most);
+  const int steps = (p.end + y.step - 1) / y.step;
+  p.s0 = p.ch * min(d.chunk, 1 << 20);
+  p.s1 = p.nch == 1 ? steps : min(steps, p.s0 + d.chunk);
   return true;
 }
 
@@ -146,11 +170,18 @@ __device__ __forceinline__ void put_output(const PageAttnArgs& a, int t, int h, 
   }
 }
 
-// The workspace: of each sequence (chunks, chunks of the sequences before, its first token, its tokens), then records of
-// [rows][DH] outputs and [rows] (maximum, sum), [chunk][slot][block].
-constexpr size_t kHeadFloats = 4 * kSeqMaxBatch;
-__device__ __forceinline__ float* record(const PageAttnArgs& a, const PageShape& y, int chunk, int g, int rb) {
-  return a.ws + kHeadFloats + ((size_t(chunk) * a.slots + g) * y.rb + rb) * (size_t(y.rows) * (a.c.dh + 2));
+// The workspace: of each token (its sequence, the sequence's first item, chunks of a block), then of each item and slot a
+// record: [rows] (maximum, sum), [rows][DH] outputs. Both kernels' records lie behind each other.
+__device__ __forceinline__ int4* token_notes(const PageAttnArgs& a) { return reinterpret_cast<int4*>(a.ws); }
+__device__ __forceinline__ float* record(const PageAttnArgs& a, const PageShape& y, int item, int g) {
+  return a.ws + y.ws + (size_t(item) * a.slots + g) * (size_t(y.rows) * (a.c.dh + 2));
+}
+// of the tokens whose first row (of the largest slot) lies in the block
+__device__ __forceinline__ void note_tokens(const PageAttnArgs& a, const PageShape& y, const Place& p) {
+  const int r0 = p.block << y.rows_log, blocks = (p.n * a.group + y.rows - 1) >> y.rows_log;
+  const int t0 = quot(r0 + a.group - 1, a.group), t1 = min(p.n, quot(r0 + y.rows + a.group - 1, a.group));
+  const int4 note = make_int4(p.b, p.item - (blocks - 1 - p.block) * p.nch, p.nch, 0);
+  for (int t = t0 + int(threadIdx.x); t < t1; t += kBlock) token_notes(a)[p.first + t] = note;
 }
 
 template <int DH, int TYPE>
@@ -261,7 +292,7 @@ template <int DH, int TYPE, int ACT, int MT>
 constexpr int kWavesPerSimd = MT == 2 && DH == 128 && (TYPE == SEQ_BF16 || ACT == SEQ_F32) ? 1 : 2;
 
 // MT: tiles of 16 query rows per wave; every wave holds all of the block's query rows and takes every fourth step of the
-// chunk, the next step's loads in flight. Grid (8, row blocks, items / 8).
+// chunk, the next step's loads in flight.
 template <int DH, int TYPE, int ACT, int MT>
 __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void page_attn_kernel(PageAttnArgs a, PageShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
@@ -279,17 +310,10 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
   const int r = lane & 15, c = lane >> 4;
   Place p;
   if (!place(a, y, lane, p)) return;
-  if (y.cut && p.ch == 0 && p.g == 0 && blockIdx.y == 0 && tid == 0)
-    reinterpret_cast<int4*>(a.ws)[p.b] = make_int4(p.n_ch, p.before, p.first, p.n);
-  const int pages = (p.end + a.c.P - 1) >> a.c.P_log;
   const size_t page_bytes = size_t(row_bytes) << a.c.P_log;
-
-  for (int rb = blockIdx.y; rb * RB < p.R; rb += gridDim.y) {
-    // rows that all of the block's tokens see, and that any of them does
-    const int t_first = quot(rb * RB, p.group), t_last = quot(min(p.R, rb * RB + RB) - 1, p.group);
-    const int common = p.L < 0 ? 0 : min(p.L + t_first + 1, p.end), end = p.L < 0 ? 0 : min(p.L + t_last + 1, p.end);
-    const int s1 = min(p.s1, (end + kStep - 1) / kStep);
-
+  const int common = p.common, end = p.end, s1 = p.s1, r0 = p.block * RB;
+  const int pages = (end + a.c.P - 1) >> a.c.P_log;
+  {
     // steps from s_edge on hold rows that some tokens do not see: at most three, so a wave has one at most
     const int s_own = p.s0 + wave;     // this wave's steps: s_own, s_own + 4, ..
     const int s_edge = min(common / kStep, s1), s_late = s_own + max(0, (s_edge - s_own + 3) / 4) * 4;
@@ -362,7 +386,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
     uint32_t qf[MT][QT][NKC][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int row = min(rb * RB + mt * 16 + r, p.R - 1);     // (rows past the last one repeat it and are not stored)
+      const int row = min(r0 + mt * 16 + r, p.R - 1);     // (rows past the last one repeat it and are not stored)
       const int t = quot(row, p.group), h = p.h0 + row - t * p.group;
       lim[mt] = p.L >= 0 && p.L + t < a.c.cap ? p.L + t + 1 : 0;
       load_q<DH, ACT, QT, ES == 1>(a.q.p, (p.first + t) * a.q.token + h * a.q.head + (ES == 2 ? 8 : 16) * c, qf[mt]);
@@ -449,7 +473,6 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
             for (int mt = 0; mt < MT; ++mt) o[mt][e + i] = mfma(pf[mt][k], vb[i], o[mt][e + i]);
       }
     };
-    __syncthreads();                   // (the block of query rows before has been read)
     if (tid == 0) s_odd = 0;
     __syncthreads();
 #pragma unroll
@@ -472,7 +495,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
         s_l[wave][16 * mt + r] = l_all;
       }
     }
-    float* rec = p.n_ch > 1 ? record(a, y, p.before + p.ch, p.g, rb) : nullptr;
+    float* rec = p.nch > 1 ? record(a, y, p.item, p.g) : nullptr;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if (mt > 0) __syncthreads();
@@ -499,7 +522,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[e] += s_o[k][qr][d0 + e] * f[k];
       }
-      const int in = mt * 16 + qr, row = rb * RB + in;
+      const int in = mt * 16 + qr, row = r0 + in;
       if (row >= p.R) continue;
       const int t = quot(row, p.group);
       const int mine = p.L >= 0 && p.L + t < a.c.cap ? p.L + t + 1 : 0;
@@ -507,44 +530,458 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
       if constexpr (TYPE != SEQ_INT8) {
         if (s_odd) add_odd<DH, TYPE>(a, p.b, p.head, max(common, p.s0 * kStep), min(mine, s1 * kStep), d0, v);
       }
-      if (p.n_ch == 1) {
+      if (p.nch == 1) {
         put_output<DH, ACT>(a, p.first + t, p.h0 + row - t * p.group, d0, l, there, v);
       } else {
 #pragma unroll
         for (int e = 0; e < NDT; e += 4)
-          *reinterpret_cast<float4*>(rec + in * DH + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-        if (d0 == 0) *reinterpret_cast<float2*>(rec + RB * DH + 2 * in) = make_float2(m, there ? l : 0.0f);
+          *reinterpret_cast<float4*>(rec + 2 * RB + in * DH + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * in) = make_float2(m, there ? l : 0.0f);
       }
     }
   }
 }
 
-// Joins the chunks' records: dh / 4 lanes over a query row's dimensions, PARTS such groups of lanes over its
-// chunks, the rest of the workgroup over rows. Grid (query rows of a sequence / rows, sequences).
+// ---- more query rows
+//
+// A workgroup's four waves hold MT tiles of 16 query rows each. Steps of 64 cache rows go through LDS, two of them in turn: all
+// threads bring K and V of the next one (16 bytes a thread and row piece; loads in flight while the present step is computed),
+// widen 8 bits and write rows of 16-bit values; chunks of 16 bytes change places by the row, so that no reader meets a
+// bank twice. K rows are read as they lie (operand A of S^T = K Q^T); V is turned on its way from LDS
+// (ds_read_b64_tr_b16: four rows of 16 dimensions, one per lane), cache rows 4 c .. 4 c + 3 of two tiles being the eight of
+// operand B that meet the lane's P. So P stays in registers.
+//   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries: P is one FP16 term (11 bits; half the matrix
+// products of two BF16 terms), lifted by 2^kLift, so that what falls below FP16's range is 2^-30 of a probability of 1, and V is
+// FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below the largest scale seen)
+// goes into P; BF16 values are multiplied by a power of two that brings the largest seen below 2^15 (lowered when a step has a
+// larger one), exact but for what lies 2^-37 below it.
+constexpr float kLift = 6.0f;
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {         // round to nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, f16x2_t));
+}
+__device__ __forceinline__ f32x4 mfma_f16(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(a[0], a[1], a[2], a[3])),
+                                                __builtin_bit_cast(f16x8, make_uint4(b[0], b[1], b[2], b[3])), acc, 0, 0, 0);
+}
+// four codes -> two words of FP16 pairs (exact)
+template <int TYPE>
+__device__ __forceinline__ void widen_f16(uint32_t w, uint32_t* o) {
+  if constexpr (TYPE == SEQ_INT8) {
+    // 1024 + (code + 128) as an FP16 number is the byte under 0x64
+    const uint32_t u = w ^ 0x80808080u;
+    const f16x2_t bias = {_Float16(1152.0f), _Float16(1152.0f)};
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias);
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias);
+  } else {
+    o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+    o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  }
+}
+// E4M3 codes that are NaN become zeros; non-zero if there are any
+__device__ __forceinline__ uint32_t drop_nan_codes(uint32_t& w) {
+  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  w &= ~((top >> 7) * 0xffu);
+  return top;
+}
+// the power of two that brings a largest magnitude to 2^11 .. 2^12
+__device__ __forceinline__ float scale_for(float top) {
+  const int e = int(__float_as_uint(top) >> 23);       // (0 for zero and what is next to it)
+  return __uint_as_float(uint32_t(min(127 + 11 + 127 - e, 253)) << 23);
+}
+
+template <int DH, int TYPE, int ACT, int MT>
+__global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs a, PageShape y) {
+  constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
+  constexpr int NKC = DH / 32, NDT = DH / 16, RB = 64 * MT;
+  constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 1;
+  constexpr bool HALF = ACT == SEQ_BF16;               // P and V in FP16
+  constexpr int CPR = DH / 8;          // chunks (eight 16-bit values) of a row in LDS
+  constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a row as loaded
+  constexpr int RPI = kBlock / PPR;    // rows per load of the workgroup
+  constexpr int NL = kWideStep / RPI;  // loads of K, and of V, per thread and step
+  constexpr uint32_t row_bytes = DH * ES;
+  constexpr int LDO = DH + 4;
+  union Lds {
+    struct {
+      uint4 k[kWideStep][CPR], v[kWideStep][CPR];
+    } step[2];
+    float o[4][16][LDO];
+  };
+  __shared__ Lds z;
+  __shared__ float s_top[4];
+  __shared__ uint32_t s_raise[3];      // a step's largest finite V where one does not fit (as its bits)
+  __shared__ int s_odd;                // a row that some query rows do not see holds something not finite
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, c = lane >> 4;
+  Place p;
+  if (!place(a, y, lane, p)) return;
+  const int common = p.common, end = p.end, s1 = p.s1, r0 = p.block * RB;
+  float* rec = p.nch > 1 ? record(a, y, p.item, p.g) : nullptr;
+  if (p.s0 >= s1 && p.nch > 1) {       // (a block that ends before this chunk)
+    if (tid < RB) *reinterpret_cast<float2*>(rec + 2 * tid) = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+  const size_t page_bytes = size_t(row_bytes) << a.c.P_log;
+  const int pages = (end + a.c.P - 1) >> a.c.P_log;
+
+  int base = p.s0 * kWideStep >> a.c.P_log;
+  PageLane<TYPE> now, next;
+  now.fetch(a, p.b, p.head, base + lane, pages);
+  next.fetch(a, p.b, p.head, base + kWave + lane, pages);
+  struct Raw {
+    uint32_t k[NL][4], v[NL][4];
+    float ks[4], vs[4], bias[4];       // of the step's tiles of 16 rows
+  };
+  Raw x;
+  const int piece = tid % PPR, row_in = tid / PPR;     // of its first load; the others are RPI rows on
+  auto load = [&](int s) __attribute__((always_inline)) {
+    if ((s * kWideStep >> a.c.P_log) - base >= kWave) {
+      base += kWave;
+      now = next;
+      next.fetch(a, p.b, p.head, base + kWave + lane, pages);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int at = ((s * kWideStep + 16 * t) >> a.c.P_log) - base, id = __builtin_amdgcn_readlane(now.id, at);
+      x.bias[t] = id >= 0 ? 0.0f : -INFINITY;
+      x.ks[t] = id >= 0 ? a.scale2 : 0.0f;
+      x.vs[t] = 0.0f;
+      if constexpr (TYPE != SEQ_BF16) {
+        x.ks[t] = id >= 0 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(now.ks), at)) * a.scale2 : 0.0f;
+        x.vs[t] = id >= 0 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(now.vs), at)) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = s * kWideStep + 16 * (i * (RPI / 16) + wave * 4 / PPR);      // of the wave's tile
+      const int id = __builtin_amdgcn_readlane(now.id, (row >> a.c.P_log) - base);
+      const size_t at = (size_t(max(id, 0)) * a.c.n_kv + p.head) * page_bytes + size_t(row & (a.c.P - 1)) * row_bytes;
+      const uint32_t bytes = id >= 0 && s < s1 ? uint32_t(min(max(end - row, 0), 16)) * row_bytes : 0u;
+      const uint32_t off = uint32_t(row_in & 15) * row_bytes + 16u * piece;
+      const int4 k = buf_load16(make_rsrc(static_cast<const char*>(a.c.k) + at, bytes), off);
+      const int4 v = buf_load16(make_rsrc(static_cast<const char*>(a.c.v) + at, bytes), off);
+      x.k[i][0] = k.x; x.k[i][1] = k.y; x.k[i][2] = k.z; x.k[i][3] = k.w;
+      x.v[i][0] = v.x; x.v[i][1] = v.y; x.v[i][2] = v.z; x.v[i][3] = v.w;
+    }
+  };
+  auto k_place = [](int row, int j) { return j ^ (DH == 128 ? row & 15 : row >> 1 & 7); };
+  auto v_place = [](int row, int j) { return j ^ (DH == 128 ? 2 * (row & 7) : 2 * (row >> 1 & 3)); };
+  float mul = 1.0f;                    // BF16: V's power of two
+  // V into buffer buf; returns the largest magnitude (BF16)
+  auto commit_v = [&](int buf) __attribute__((always_inline)) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = row_in + i * RPI;
+      if constexpr (TYPE == SEQ_BF16) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (!HALF) {
+            w[e] = x.v[i][e];
+            continue;
+          }
+          const float f0 = bf16_lo(x.v[i][e]) * mul, f1 = bf16_hi(x.v[i][e]) * mul;
+          top = fmaxf(fmaxf(fabsf(f0), fabsf(f1)), top);
+          w[e] = pack_f16(f0, f1);
+        }
+        z.step[buf].v[row][v_place(row, piece)] = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) HALF ? widen_f16<TYPE>(x.v[i][e], &w[2 * e]) : widen<TYPE>(x.v[i][e], &w[2 * e]);
+        z.step[buf].v[row][v_place(row, 2 * piece)] = make_uint4(w[0], w[1], w[2], w[3]);
+        z.step[buf].v[row][v_place(row, 2 * piece + 1)] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    }
+    return top;
+  };
+  auto commit_k = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = row_in + i * RPI;
+      if constexpr (TYPE == SEQ_BF16) {
+        z.step[buf].k[row][k_place(row, piece)] = make_uint4(x.k[i][0], x.k[i][1], x.k[i][2], x.k[i][3]);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) widen<TYPE>(x.k[i][e], &w[2 * e]);
+        z.step[buf].k[row][k_place(row, 2 * piece)] = make_uint4(w[0], w[1], w[2], w[3]);
+        z.step[buf].k[row][k_place(row, 2 * piece + 1)] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    }
+  };
+  // the largest finite magnitude of the step's V in this wave
+  auto top_v = [&]() __attribute__((always_inline)) {
+    float top = 0.0f;
+    if constexpr (TYPE == SEQ_BF16) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float f0 = fabsf(bf16_lo(x.v[i][e])), f1 = fabsf(bf16_hi(x.v[i][e]));
+          top = fmaxf(top, f0 < INFINITY ? f0 : 0.0f);
+          top = fmaxf(top, f1 < INFINITY ? f1 : 0.0f);
+        }
+    }
+    return wave_max(top);
+  };
+
+  load(p.s0);
+  // this lane's query rows, as rows of Q (B operand): token t, head h; the cache rows below `lim` are seen
+  int lim[MT];
+  uint32_t qf[MT][QT][NKC][4];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int row = min(r0 + (wave * MT + mt) * 16 + r, p.R - 1);      // (rows past the last one repeat it and are not stored)
+    const int t = quot(row, p.group), h = p.h0 + row - t * p.group;
+    lim[mt] = p.L >= 0 && p.L + t < a.c.cap ? p.L + t + 1 : 0;
+    load_q<DH, ACT, QT, false>(a.q.p, (p.first + t) * a.q.token + h * a.q.head + 8 * c, qf[mt]);
+  }
+  float m_run[MT], l_run[MT];          // of query row r; l of this lane's cache rows
+  f32x4 o[MT][NDT];                    // lane (r, c): query rows 4 c + i, dimension 16 d + r
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m_run[mt] = -INFINITY;
+    l_run[mt] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  float ref = 0.0f, inv_ref = 0.0f;    // 8 bits: the power of two that V's scales are divided by
+  if (tid == 0) s_odd = 0;
+  if (tid < 3) s_raise[tid] = 0;
+  if constexpr (TYPE == SEQ_BF16 && HALF) {
+    const float top = top_v();
+    if (lane == 0) s_top[wave] = top;
+    __syncthreads();
+    mul = scale_for(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) arrived(qf[mt]);
+  __syncthreads();                     // s_odd, s_raise
+  // everything that has been added up is multiplied by f
+  auto rescale = [&](float f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int e = 0; e < NDT; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[mt][e][i] *= f;
+  };
+  // lane constants of the reads from LDS
+  uint32_t k_at[NKC], v_at;
+#pragma unroll
+  for (int kk = 0; kk < NKC; ++kk) k_at[kk] = uint32_t(r * CPR + k_place(r, 4 * kk + c));
+  const int v_row = 4 * c + (r >> 2);
+  v_at = uint32_t(v_row * CPR + v_place(v_row, r >> 1 & 1)) * 16 + 8 * (r & 1);
+
+  // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
+  auto step = [&](int s, int buf, int turn, auto edge_) __attribute__((always_inline)) {
+    constexpr bool EDGE = decltype(edge_)::value;
+    // A row that some query rows do not see must not reach them through 0 * inf: its non-finite values are left out
+    // of the product, and added at the end to the outputs that see them
+    if constexpr (EDGE && TYPE != SEQ_INT8) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (s * kWideStep + row_in + i * RPI >= common)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad |= TYPE == SEQ_BF16 ? drop_odd(x.v[i][e]) : drop_nan_codes(x.v[i][e]);
+      if (bad) s_odd = 1;
+    }
+    commit_k(buf);
+    const float top = commit_v(buf);
+    if constexpr (TYPE == SEQ_BF16 && HALF) {
+      if (__ballot(top >= 0x1p15f)) {                  // (an infinity too, each time)
+        const float t = top_v();
+        if (lane == 0) atomicMax(&s_raise[turn], __float_as_uint(t));
+      }
+    }
+    __syncthreads();
+    if constexpr (TYPE == SEQ_BF16 && HALF) {
+      if (tid == 0) s_raise[turn == 0 ? 2 : turn - 1] = 0;             // (the step after the next one's)
+      const float most = __uint_as_float(__builtin_amdgcn_readfirstlane(s_raise[turn]));
+      if (most * mul >= 0x1p15f) {
+        const float to = scale_for(most);
+        rescale(to / mul);
+        mul = to;
+        commit_v(buf);
+        __syncthreads();
+      }
+    }
+    float ks[4], f[4], bias[4];
+    if constexpr (TYPE != SEQ_BF16 && HALF) {
+      float most = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) most = fmaxf(most, x.vs[t] < INFINITY ? x.vs[t] : 0.0f);
+      if (most >= 2.0f * ref && most > 0.0f) {
+        const float to = __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u));
+        rescale(ref / to);
+        ref = to;
+        inv_ref = 1.0f / to;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      ks[t] = x.ks[t]; bias[t] = x.bias[t];
+      f[t] = TYPE == SEQ_BF16 ? 1.0f : HALF ? x.vs[t] * inv_ref : x.vs[t];
+    }
+    load(s + 1);
+    const char* kz = reinterpret_cast<const char*>(&z.step[buf].k[0][0]);
+    f32x4 sc[MT][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) sc[mt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int kk = 0; kk < NKC; ++kk) {
+        const uint4 w = *reinterpret_cast<const uint4*>(kz + 16 * k_at[kk] + t * 16 * CPR * 16);
+        const uint32_t kf[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < QT; ++q)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) sc[mt][t] = mfma(kf, qf[mt][q][kk], sc[mt][t]);
+      }
+    uint32_t pf[MT][PT][2][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const int seen = lim[mt] - s * kWideStep - 4 * c;                // rows 16 t + i below it are
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if constexpr (EDGE) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, 16 * t + i < seen ? fmaf(sc[mt][t][i], ks[t], bias[t]) : -INFINITY);
+        } else {
+          const float q = fmaxf(fmaxf(sc[mt][t][0], sc[mt][t][1]), fmaxf(sc[mt][t][2], sc[mt][t][3]));
+          top = fmaxf(top, fmaf(q, ks[t], bias[t]));
+        }
+      }
+      if (__ballot(top > m_run[mt] + kSlack)) {        // (also the first rows: m_run is -inf)
+        const float mn = fmaxf(m_run[mt], quad_max(top));
+        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[mt] - mn);
+        m_run[mt] = mn;
+        l_run[mt] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float g = __shfl(alpha, 4 * c + i, kWave);
+#pragma unroll
+          for (int e = 0; e < NDT; ++e) o[mt][e][i] *= g;
+        }
+      }
+      const float low = (HALF ? kLift : 0.0f) - (m_run[mt] == -INFINITY ? 0.0f : m_run[mt]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = __builtin_amdgcn_exp2f(fmaf(sc[mt][t][i], ks[t], bias[t] + low));
+          if constexpr (EDGE) v[i] = 16 * t + i < seen ? v[i] : 0.0f;
+          l_run[mt] += v[i];
+          if constexpr (TYPE != SEQ_BF16) {
+            v[i] *= f[t];
+            if constexpr (EDGE) v[i] = 16 * t + i < seen ? v[i] : 0.0f;            // (a hidden row's scale may be anything)
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if constexpr (HALF) pf[mt][0][t >> 1][2 * (t & 1) + e] = pack_f16(v[2 * e], v[2 * e + 1]);
+          else terms<PT>(v[2 * e], v[2 * e + 1], &pf[mt][0][t >> 1][2 * (t & 1) + e], 8);
+        }
+      }
+    }
+    typedef __attribute__((address_space(3))) s16x4* lds_p;
+    __attribute__((address_space(3))) char* vz = (__attribute__((address_space(3))) char*)(&z.step[buf].v[0][0]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < NDT; ++e) {
+        __attribute__((address_space(3))) char* at = vz + (v_at ^ (32u * e)) + h * 32 * CPR * 16;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_p(at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_p(at + 16 * CPR * 16));
+        const uint2 w0 = __builtin_bit_cast(uint2, lo), w1 = __builtin_bit_cast(uint2, hi);
+        const uint32_t vf[4] = {w0.x, w0.y, w1.x, w1.y};
+#pragma unroll
+        for (int k = 0; k < PT; ++k)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) o[mt][e] = HALF ? mfma_f16(pf[mt][k][h], vf, o[mt][e]) : mfma(pf[mt][k][h], vf, o[mt][e]);
+      }
+  };
+  const int s_edge = min(s1, common / kWideStep);
+  int s = p.s0, buf = 0, turn = 0;
+  for (; s < s_edge; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::false_type{});
+  for (; s < s1; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::true_type{});
+
+  // every wave holds its rows' results; through LDS, 16 rows at a time, they become whole rows
+  const float unit = !HALF ? 1.0f : TYPE == SEQ_BF16 ? 1.0f / mul : ref;
+  __syncthreads();
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l_all = quad_sum(l_run[mt]);
+#pragma unroll
+    for (int e = 0; e < NDT; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z.o[wave][4 * c + i][16 * e + r] = o[mt][e][i] * unit;
+#pragma unroll
+    for (int k = 0; k < DH / 16; ++k) {
+      const int in = (k * kWave + lane) / (DH / 4), d0 = 4 * (lane % (DH / 4));
+      const float4 q = *reinterpret_cast<const float4*>(&z.o[wave][in][d0]);
+      float v[4] = {q.x, q.y, q.z, q.w};
+      const float m = __shfl(m_run[mt], in, kWave), l = __shfl(l_all, in, kWave);
+      const int place = (wave * MT + mt) * 16 + in, row = r0 + place;
+      if (row >= p.R) continue;
+      const int t = quot(row, p.group);
+      const int mine = p.L >= 0 && p.L + t < a.c.cap ? p.L + t + 1 : 0;
+      if constexpr (TYPE != SEQ_INT8) {
+        if (s_odd) add_odd<DH, TYPE>(a, p.b, p.head, max(common, p.s0 * kWideStep), min(mine, s1 * kWideStep), d0, v);
+      }
+      if (p.nch == 1) {
+        put_output<DH, ACT>(a, p.first + t, p.h0 + row - t * p.group, d0, l, mine > 0, v);
+      } else {
+        *reinterpret_cast<float4*>(rec + 2 * RB + place * DH + d0) = make_float4(v[0], v[1], v[2], v[3]);
+        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * place) = make_float2(m, mine > 0 ? l : 0.0f);
+      }
+    }
+  }
+}
+
+// Joins the chunks' records: dh / 4 lanes over a query row's dimensions, PARTS such groups of lanes over its chunks, the
+// rest of the workgroup over rows. Query rows of all tokens in a row; few, wide: the kernels' shapes.
 template <int DH, int ACT, int PARTS>
-__global__ __launch_bounds__(kBlock) void page_join_kernel(PageAttnArgs a, PageShape y) {
+__global__ __launch_bounds__(kBlock) void page_join_kernel(PageAttnArgs a, PageShape few, PageShape wide) {
   constexpr int LPR = DH / 4, ROWS = kBlock / (LPR * PARTS);
   __shared__ float s_m[ROWS][PARTS], s_l[ROWS][PARTS];
   __shared__ float4 s_o[ROWS][PARTS][LPR];
-  const int tid = threadIdx.x, b = blockIdx.y;
-  if (page_seq(a.start, a.N, a.c, b).n == 0) return;   // (its entry of the workspace is not written)
-  const int4 head = reinterpret_cast<const int4*>(a.ws)[b];
-  const int n = head.x, before = head.y;
-  if (n <= 1) return;                  // written already
+  const int tid = threadIdx.x;
   const int mine = tid / (LPR * PARTS), q_row = blockIdx.x * ROWS + mine;
-  const int last = head.w * a.slots * a.group - 1;
-  if (blockIdx.x * ROWS > last) return;
-  const int th = quot(min(q_row, last), a.group), t = quot(th, a.slots), g = th - t * a.slots;
-  const int slot = a.slot[g], h0 = slot >> 8 & 0xfff, group = slot >> 20;
-  const int own = q_row - th * a.group, hh = min(own, group - 1);
-  const bool there = own < group;      // (others repeat a row, and store nothing)
-  const int row = t * group + hh, rows = y.rows, rb = row >> y.rows_log, in = row & (rows - 1);
-  const size_t stride = size_t(rows) * (DH + 2) * a.slots * y.rb;
-  const float* first = record(a, y, before, g, rb);
+  const int total = a.N * a.slots * a.group;           // (at most 2^17)
+  const int th = quot(min(q_row, total - 1), a.group), token = quot(th, a.slots), g = th - token * a.slots;
+  const int slot = a.slot[g], h0 = slot >> 8 & 0xfff, group = slot >> 20, own = q_row - th * a.group, hh = min(own, group - 1);
+  // whose token it is: a note that names a sequence with this token, of a kernel that cuts blocks, was left by this call
+  // (others may hold anything)
+  const int4 note = token_notes(a)[token];
+  const PageSeq seq = page_seq(a.start, a.N, a.c, min(max(note.x, 0), a.c.batch - 1));
+  const int rows_all = seq.n * a.group;
+  const PageShape& y = rows_all >= wide.least && rows_all <= wide.most ? wide : few;
+  // (rows past a slot's last one repeat it, and store nothing; one chunk: written already)
+  const bool there = own < group && q_row < total && token >= seq.first && token < seq.first + seq.n && y.cut && note.z > 1;
+  if (!__syncthreads_or(there)) return;
+  const int n = there ? note.z : 1, row = there ? (token - seq.first) * group + hh : 0;
+  const int blocks = (rows_all + y.rows - 1) >> y.rows_log, in = row & (y.rows - 1);
+  const size_t stride = size_t(y.rows) * (DH + 2) * a.slots;
+  const float* first = there ? record(a, y, note.y + (blocks - 1 - (row >> y.rows_log)) * n, g) : a.ws;
   const int part = tid / LPR % PARTS, d0 = 4 * (tid % LPR);
   float m = -INFINITY, l = 0.0f;
   float v[4] = {};
   auto add = [&](float mk, float lk, const float4& x) {
+    if (mk == -INFINITY && lk == 0.0f) return;         // (rows that were not seen, or a chunk behind the block's end: x is not written)
     const float mn = fmaxf(m, mk);
     const float fa = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
     const float fb = mk == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mk - mn);
@@ -559,8 +996,8 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(PageAttnArgs a, PageS
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float* po = first + min(k0 + i * PARTS, n - 1) * stride;
-      q[i] = *reinterpret_cast<const float2*>(po + rows * DH + 2 * in);
-      x[i] = *reinterpret_cast<const float4*>(po + in * DH + d0);
+      q[i] = *reinterpret_cast<const float2*>(po + 2 * in);
+      x[i] = *reinterpret_cast<const float4*>(po + 2 * y.rows + in * DH + d0);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -579,42 +1016,56 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(PageAttnArgs a, PageS
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) add(s_m[mine][k], s_l[mine][k], s_o[mine][k][tid % LPR]);
   }
-  if (there) put_output<DH, ACT>(a, head.z + t, h0 + hh, d0, l, true, v);
+  if (there) put_output<DH, ACT>(a, token, h0 + hh, d0, l, true, v);
 }
 
-PageShape shape(const PageAttnArgs& a) {
-  PageShape y;
-  const int tiles = int(std::min<long>(long(std::max(a.max_new, 1)) * a.group + 15, 1 << 21) / 16);
-  y.mt = std::min(tiles, 2);
-  y.rows = 16 * y.mt;
-  y.rows_log = 31 - __builtin_clz(y.rows);
-  const int blocks = std::min((tiles + y.mt - 1) / y.mt, 65535);
-  y.rb = std::min(blocks, kTarget);
-  const int units = a.slots * y.rb, seqs = std::min(a.c.batch, a.N);
-  const long steps = (std::min<long>(std::max(a.max_len, 0) + long(std::max(a.max_new, 1)), a.c.cap) + kStep - 1) / kStep;
-  y.room = std::max(seqs, (kTarget + units - 1) / units);
-  y.cut = steps > kMinSteps && y.room > seqs;
-  y.items = (y.room * a.slots + 7) / 8 * 8;
-  y.rb = std::min(blocks, kTarget);
-  return y;
+struct Shapes {
+  PageShape few, wide;
+  size_t floats;                       // of the workspace
+};
+Shapes shapes(const PageAttnArgs& a) {
+  Shapes z{};
+  const int seqs = std::min(a.c.batch, a.N), expected = std::max(a.max_new, 1);
+  const long rows = long(expected) * a.group;
+  const long most = std::min<long>(std::max(a.max_len, 0) + long(expected), a.c.cap);
+  // One kernel for all where it is what the expected number of tokens asks for, or where there is one sequence
+  const bool use_wide = rows > kFew, use_few = !use_wide || (a.c.batch > 1 && a.N > 1);
+  constexpr int kAll = 1 << 30;
+  auto fill = [&](PageShape& y, bool use, int least, int limit, int step, int mt, int block) {
+    y.least = use ? least : 1;
+    y.most = use ? limit : 0;
+    y.mt = mt; y.step = step; y.rows = block; y.rows_log = 31 - __builtin_clz(block);
+    if (!use) return;
+    const long blocks = std::min<long>(long(a.N) * a.group, limit == kFew ? long(seqs) * kFew : kAll) / block + seqs;    // of all sequences, at most
+    const int quota = (kTarget + a.slots - 1) / a.slots;
+    // (the join looks at every token's rows)
+    y.cut = blocks < quota && most > kMinSteps * step && long(a.N) * a.slots * a.group <= 1 << 17;
+    y.items = int(std::max<long>(blocks, y.cut ? quota : 0));
+  };
+  const int mt = rows > 16 || use_wide ? 2 : 1;
+  fill(z.few, use_few, 1, use_wide ? kFew : kAll, kStep, mt, 16 * mt);
+  const int wt = a.act == SEQ_BF16 ? 2 : 1;
+  fill(z.wide, use_wide, use_few ? kFew + 1 : 1, kAll, kWideStep, wt, 64 * wt);
+  z.floats = z.few.cut || z.wide.cut ? (size_t(a.N) * 4 + 63) / 64 * 64 : 0;
+  for (PageShape* y : {&z.few, &z.wide}) {
+    y->ws = z.floats;
+    if (y->cut) z.floats += size_t(y->items) * a.slots * y->rows * (a.c.dh + 2);
+  }
+  return z;
 }
 
 }  // namespace
 
-size_t page_attn_workspace_bytes(const PageAttnArgs& a) {
-  const PageShape y = shape(a);
-  return y.cut ? (kHeadFloats + size_t(y.room) * a.slots * y.rb * y.rows * (a.c.dh + 2)) * 4 : 0;
-}
+size_t page_attn_workspace_bytes(const PageAttnArgs& a) { return shapes(a).floats * 4; }
 
 hipError_t launch_page_attn(const PageAttnArgs& a, hipStream_t s) {
-  const PageShape y = shape(a);
-  const int blocks = int(std::min<long>((long(std::max(a.max_new, 1)) * a.group + y.rows - 1) / y.rows, 65535));
-#define ATTN(DH, TYPE, ACT, MT) \
-  hipLaunchKernelGGL((page_attn_kernel<DH, TYPE, ACT, MT>), dim3(8, blocks, y.items / 8), dim3(kBlock), 0, s, a, y)
-#define ATTN_MT(DH, TYPE, ACT)                   \
-  do {                                           \
-    if (y.mt == 1) ATTN(DH, TYPE, ACT, 1);       \
-    else ATTN(DH, TYPE, ACT, 2);                 \
+  const Shapes z = shapes(a);
+#define ATTN(KERNEL, Y, DH, TYPE, ACT, MT) hipLaunchKernelGGL((KERNEL<DH, TYPE, ACT, MT>), dim3(a.slots, std::min(Y.items, kItems), (Y.items + kItems - 1) / kItems), dim3(kBlock), 0, s, a, Y)
+#define ATTN_MT(DH, TYPE, ACT)                                                                      \
+  do {                                                                                              \
+    if (z.wide.items) ATTN(page_attn_wide_kernel, z.wide, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1)); \
+    if (z.few.items && z.few.mt == 1) ATTN(page_attn_kernel, z.few, DH, TYPE, ACT, 1);              \
+    else if (z.few.items) ATTN(page_attn_kernel, z.few, DH, TYPE, ACT, 2);                          \
   } while (0)
 #define ATTN_TYPE(DH, ACT)                                      \
   do {                                                          \
@@ -633,17 +1084,16 @@ hipError_t launch_page_attn(const PageAttnArgs& a, hipStream_t s) {
 #undef ATTN_MT
 #undef ATTN
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !y.cut) return e;
-  const int rows = y.rb * y.rows * a.slots;
-  const int seqs = std::min(a.c.batch, a.N);
-#define JOIN_PARTS(DH, ACT, PARTS)                                                                                        \
-  hipLaunchKernelGGL((page_join_kernel<DH, ACT, PARTS>), dim3((rows * PARTS + 4 * kBlock / DH - 1) / (4 * kBlock / DH), a.c.batch), \
-                     dim3(kBlock), 0, s, a, y)
-#define JOIN(DH, ACT)                                                        \
-  do {                                                                       \
-    if (rows * seqs < 2048) JOIN_PARTS(DH, ACT, 4 * kBlock / DH);            \
-    else if (rows * seqs < 8192) JOIN_PARTS(DH, ACT, 4);                     \
-    else JOIN_PARTS(DH, ACT, 1);                                             \
+  if (e != hipSuccess || z.floats == 0) return e;
+  const int rows = a.N * a.slots * a.group;
+#define JOIN_PARTS(DH, ACT, PARTS)                                                                                      \
+  hipLaunchKernelGGL((page_join_kernel<DH, ACT, PARTS>), dim3(int((long(rows) * PARTS + 4 * kBlock / DH - 1) / (4 * kBlock / DH))), \
+                     dim3(kBlock), 0, s, a, z.few, z.wide)
+#define JOIN(DH, ACT)                                                 \
+  do {                                                                \
+    if (rows < 2048) JOIN_PARTS(DH, ACT, 4 * kBlock / DH);            \
+    else if (rows < 8192) JOIN_PARTS(DH, ACT, 4);                     \
+    else JOIN_PARTS(DH, ACT, 1);                                      \
   } while (0)
   if (a.c.dh == 128 && a.act == SEQ_BF16) JOIN(128, SEQ_BF16);
   else if (a.c.dh == 128) JOIN(128, SEQ_F32);

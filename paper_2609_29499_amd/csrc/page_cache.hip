@@ -128,12 +128,18 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
       int state = 0, pos = 0;
       if (t < a.N) {
         int b = t;
-        if (a.start) {                 // sequences that end at or before the token
-          b = 0;
+        if (a.start) {                 // the sequence that has the token
+          b = a.c.batch;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 3; i >= 0; --i) {
             const int at = 64 * i + lane;
-            b += __popcll(__ballot(at < a.c.batch && t >= a.start[at + 1]));
+            bool mine = false;
+            if (at < a.c.batch) {
+              const int lo = a.start[at], hi = a.start[at + 1];
+              mine = lo >= 0 && hi <= a.N && t >= lo && t < hi;
+            }
+            const unsigned long long who = __ballot(mine);
+            if (who) b = 64 * i + __ffsll((long long)who) - 1;
           }
         }
         if (b < a.c.batch) {

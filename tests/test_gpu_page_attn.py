@@ -3,12 +3,11 @@
 Tolerance of one output: with A = sum of p |v| over the rows seen, n their number,
   scores: a float32 dot product of dh exact products, |error| <= (dh + 4) 2^-24 scale sum |q_i k_i| = d, which
   moves p by a factor within exp(2 d);
-  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in float32 calls 2^-21 (two FP16 terms, half a step of the second) or
-  better; more than 32 BF16 query rows of a sequence and cache head: one FP16 term, half a step 2^-11, and where P times the page's scale
+  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; more than 32 BF16 query rows of a sequence and cache head: one FP16 term, half a step 2^-11, and where P times the page's scale
   falls below 2^-18 of the largest scale M, a subnormal's half step 2^-25 in units of 2^-4 M or less: n 2^-29 max |v| together;
   float32 sums n 2^-24;
   the output's rounding 2^-8 of the value in BF16, 2^-24 in float32.
-|error| <= A (2 d + 2^-21 + 2^-11, 2^-16 or 2^-21 + n 2^-24) + (n 2^-29 max |v|) + |o| 2^-8 or 2^-24."""
+|error| <= A (2 d + 2^-21 + 2^-11, 2^-16 or 2^-24 + n 2^-24) + (n 2^-29 max |v|) + |o| 2^-8 or 2^-24."""
 import math
 
 import numpy as np
@@ -42,7 +41,7 @@ def check(got, q, rows, lens, counts, P, act, scale, first=0, cap=None, gone=lam
                 k, v = rows[b][0][:, h // G], rows[b][1][:, h // G]
                 o, A = O.attention(q[t, h], k, v, seen, scale)
                 d = (dh + 4) * 2.0 ** -24 * scale * np.max(np.abs(k[seen]) @ np.abs(q[t, h]))
-                tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -11 if half else 2.0 ** -16 if act == "bf16" else 2.0 ** -21) + len(seen) * 2.0 ** -24)
+                tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -11 if half else 2.0 ** -16 if act == "bf16" else 2.0 ** -24) + len(seen) * 2.0 ** -24)
                 tol = tol + half * len(seen) * 2.0 ** -29 * np.max(np.abs(v[seen]))
                 tol = tol + np.abs(o) * (2.0 ** -8 if act == "bf16" else 2.0 ** -24)
                 err = np.abs(got[t, h] - o)
