@@ -336,7 +336,8 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
           x.vs[tt] = id >= 0 ? vs : 0.0f;
         }
         const size_t place = (size_t(max(id, 0)) * a.c.n_kv + p.head) * page_bytes + size_t(in_page) * row_bytes;
-        const uint32_t bytes = id >= 0 && s < stop ? uint32_t(min(max(end - row, 0), 16)) * row_bytes : 0u;
+        // (said to be the same in all lanes: a descriptor that the compiler takes for divergent becomes a loop around every load)
+        const uint32_t bytes = __builtin_amdgcn_readfirstlane(id >= 0 && s < stop ? min(max(end - row, 0), 16) * int(row_bytes) : 0);
         const __amdgpu_buffer_rsrc_t rk = make_rsrc(static_cast<const char*>(a.c.k) + place, bytes);
         const __amdgpu_buffer_rsrc_t rv = make_rsrc(static_cast<const char*>(a.c.v) + place, bytes);
 #pragma unroll
@@ -662,7 +663,8 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
       const int row = s * kWideStep + 16 * (i * (RPI / 16) + wave * 4 / PPR);      // of the wave's tile
       const int id = __builtin_amdgcn_readlane(now.id, (row >> a.c.P_log) - base);
       const size_t at = (size_t(max(id, 0)) * a.c.n_kv + p.head) * page_bytes + size_t(row & (a.c.P - 1)) * row_bytes;
-      const uint32_t bytes = id >= 0 && s < s1 ? uint32_t(min(max(end - row, 0), 16)) * row_bytes : 0u;
+      // (said to be the same in all lanes: a descriptor that the compiler takes for divergent becomes a loop around every load)
+      const uint32_t bytes = __builtin_amdgcn_readfirstlane(id >= 0 && s < s1 ? min(max(end - row, 0), 16) * int(row_bytes) : 0);
       const uint32_t off = uint32_t(row_in & 15) * row_bytes + 16u * piece;
       const int4 k = buf_load16(make_rsrc(static_cast<const char*>(a.c.k) + at, bytes), off);
       const int4 v = buf_load16(make_rsrc(static_cast<const char*>(a.c.v) + at, bytes), off);
@@ -832,24 +834,35 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
       ks[t] = x.ks[t]; bias[t] = x.bias[t];
       f[t] = TYPE == SEQ_BF16 ? 1.0f : HALF ? x.vs[t] * inv_ref : x.vs[t];
     }
-    load(s + 1);
+    // K's operands are read two tiles ahead of their products: at most eight reads are on their way
     const char* kz = reinterpret_cast<const char*>(&z.step[buf].k[0][0]);
+    uint4 kf[2][NKC];
+    auto read_k = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kk = 0; kk < NKC; ++kk) kf[t & 1][kk] = *reinterpret_cast<const uint4*>(kz + 16 * k_at[kk] + t * 16 * CPR * 16);
+    };
+    read_k(0);
+    read_k(1);
+    __builtin_amdgcn_sched_barrier(0);
+    load(s + 1);
     f32x4 sc[MT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) sc[mt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
 #pragma unroll
       for (int kk = 0; kk < NKC; ++kk) {
-        const uint4 w = *reinterpret_cast<const uint4*>(kz + 16 * k_at[kk] + t * 16 * CPR * 16);
-        const uint32_t kf[4] = {w.x, w.y, w.z, w.w};
+        const uint32_t kw[4] = {kf[t & 1][kk].x, kf[t & 1][kk].y, kf[t & 1][kk].z, kf[t & 1][kk].w};
 #pragma unroll
         for (int q = 0; q < QT; ++q)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) sc[mt][t] = mfma(kf, qf[mt][q][kk], sc[mt][t]);
+          for (int mt = 0; mt < MT; ++mt) sc[mt][t] = mfma(kw, qf[mt][q][kk], sc[mt][t]);
       }
+      if (t < 2) read_k(t + 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     uint32_t pf[MT][PT][2][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -1042,7 +1055,7 @@ Shapes shapes(const PageAttnArgs& a) {
     y.cut = blocks < quota && most > kMinSteps * step && long(a.N) * a.slots * a.group <= 1 << 17;
     y.items = int(std::max<long>(blocks, y.cut ? quota : 0));
   };
-  const int mt = rows > 16 || use_wide ? 2 : 1;
+  const int mt = rows > 16 && !use_wide ? 2 : 1;       // (beside the other kernel it has single tokens, mostly)
   fill(z.few, use_few, 1, use_wide ? kFew : kAll, kStep, mt, 16 * mt);
   const int wt = a.act == SEQ_BF16 ? 2 : 1;
   fill(z.wide, use_wide, use_few ? kFew + 1 : 1, kAll, kWideStep, wt, 64 * wt);
