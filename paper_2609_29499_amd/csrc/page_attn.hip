@@ -326,15 +326,6 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
       for (int tt = 0; tt < 2; ++tt) {
         const int row = s * kStep + 16 * tt, at = (row >> a.c.P_log) - from, in_page = row & (a.c.P - 1);
         const int id = __builtin_amdgcn_readlane(ids.id, at);
-        x.bias[tt] = id >= 0 ? 0.0f : -INFINITY;
-        x.ks[tt] = id >= 0 ? a.scale2 : 0.0f;
-        x.vs[tt] = 0.0f;
-        if constexpr (TYPE != SEQ_BF16) {
-          const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ids.ks), at));
-          const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ids.vs), at));
-          x.ks[tt] = id >= 0 ? ks * a.scale2 : 0.0f;
-          x.vs[tt] = id >= 0 ? vs : 0.0f;
-        }
         const size_t place = (size_t(max(id, 0)) * a.c.n_kv + p.head) * page_bytes + size_t(in_page) * row_bytes;
         // (said to be the same in all lanes: a descriptor that the compiler takes for divergent becomes a loop around every load)
         const uint32_t bytes = __builtin_amdgcn_readfirstlane(id >= 0 && s < stop ? min(max(end - row, 0), 16) * int(row_bytes) : 0);
@@ -358,6 +349,20 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
           } else {
             v[0] = __builtin_amdgcn_raw_buffer_load_b32(rv, int(off), 0, kCpolStream);
           }
+        }
+      }
+      // (behind the rows' loads: the scales' own, which follow the page ids', are waited for here)
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const int at = ((s * kStep + 16 * tt) >> a.c.P_log) - from, id = __builtin_amdgcn_readlane(ids.id, at);
+        x.bias[tt] = id >= 0 ? 0.0f : -INFINITY;
+        x.ks[tt] = id >= 0 ? a.scale2 : 0.0f;
+        x.vs[tt] = 0.0f;
+        if constexpr (TYPE != SEQ_BF16) {
+          const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ids.ks), at));
+          const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ids.vs), at));
+          x.ks[tt] = id >= 0 ? ks * a.scale2 : 0.0f;
+          x.vs[tt] = id >= 0 ? vs : 0.0f;
         }
       }
     };
@@ -783,7 +788,9 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
   const int v_row = 4 * c + (r >> 2);
   v_at = uint32_t(v_row * CPR + v_place(v_row, r >> 1 & 1)) * 16 + 8 * (r & 1);
 
-  // one barrier per step: whoever writes a buffer has passed the barrier that followed its last use
+  // Bringing a step goes first (priority 2: all waves wait for it), then scores (1: the matrix cores, while another wave's
+  // softmax has the vector unit): 512 tokens behind 8191 rows 129.6 us, 140.8 without.
+  // One barrier per step: whoever writes a buffer has passed the barrier that followed its last use
   auto step = [&](int s, int buf, int turn, auto edge_) __attribute__((always_inline)) {
     constexpr bool EDGE = decltype(edge_)::value;
     // A row that some query rows do not see must not reach them through 0 * inf: its non-finite values are left out
@@ -797,8 +804,10 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
           for (int e = 0; e < 4; ++e) bad |= TYPE == SEQ_BF16 ? drop_odd(x.v[i][e]) : drop_nan_codes(x.v[i][e]);
       if (bad) s_odd = 1;
     }
+    __builtin_amdgcn_s_setprio(2);
     commit_k(buf);
     const float top = commit_v(buf);
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (TYPE == SEQ_BF16 && HALF) {
       if (__ballot(top >= 0x1p15f)) {                  // (an infinity too, each time)
         const float t = top_v();
@@ -841,6 +850,7 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
 #pragma unroll
       for (int kk = 0; kk < NKC; ++kk) kf[t & 1][kk] = *reinterpret_cast<const uint4*>(kz + 16 * k_at[kk] + t * 16 * CPR * 16);
     };
+    __builtin_amdgcn_s_setprio(1);
     read_k(0);
     read_k(1);
     __builtin_amdgcn_sched_barrier(0);
@@ -863,6 +873,7 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
       if (t < 2) read_k(t + 2);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     uint32_t pf[MT][PT][2][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
