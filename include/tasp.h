@@ -678,7 +678,7 @@ tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const in
  * of its rows). TASP_BF16: q exact, sums in float32, probabilities in 16 bits, or, with more than 32 query rows of a sequence and
  * cache head, in 11 bits (and what probability and |v| leave below 2^-29 of the largest |v| may be lost); TASP_F32: everything to 24 bits. The ends
  * of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
- * that are expected (max_len 0..max_pages * page_rows, max_new 1..n_tokens): they size launches and workspace; more is served too.
+ * that are expected (max_len 0..max_pages * page_rows, max_new at least 1): they size launches and workspace; more is served too.
  * workspace: device, 256-byte aligned, at least tasp_page_attention_workspace_bytes for the same cache shape, n_q_heads,
  * n_tokens, max_len and max_new; its contents need no clearing; calls that overlap need one each. Stream-ordered,
  * capturable. Errors as tasp_page_append, TASP_ERR_WORKSPACE. */
@@ -690,6 +690,27 @@ tasp_status tasp_page_attention(const tasp_page_cache* cache, int32_t layer, con
                                 int32_t n_q_heads, double scale, int32_t max_len, int32_t max_new,
                                 const tasp_rows* out, void* workspace, size_t workspace_bytes,
                                 void* stream);
+
+/* Lengths grow by the call's tokens, cut to the table's pages: len[b] += start[b + 1] - start[b] (a sequence that is passed
+ * over keeps its length). Behind the last layer of a step. Stream-ordered, capturable. Errors as tasp_page_append. */
+tasp_status tasp_page_advance(const tasp_page_cache* cache, const int32_t* start, int32_t n_tokens, void* stream);
+
+/* A plan over packed tokens of many sequences: prompts, chunks of prompts and single tokens in one call. tasp_page_bind
+ * adopts a pool for a plan as tasp_seq_bind does. tasp_page_forward runs the plan's layers (any plan format; projections as
+ * tasp_prefill, attention as tasp_page_attention with TASP_F32 over the retained groups): x (device) float32
+ * [n_tokens][d_model], out (device, not overlapping x; both 16-byte aligned) float32 [n_tokens][vocab], or
+ * [n_tokens][d_model] without an LM head. It appends the tokens' k and v to every layer (rotate-half RoPE with the plan's base; only
+ * retained groups' rows are written); the lengths stay (tasp_page_advance). Rows of out of absent tokens and of tokens
+ * that are no sequence's hold values of no meaning. n_tokens <= max_prefill (TASP_ERR_SHAPE; TASP_ERR_UNSUPPORTED for max_prefill 0):
+ * the step runs in the plan's prefill scratch. The cache must be bound to the plan (else TASP_ERR_CACHE_PLAN_MISMATCH).
+ * max_len, max_new, workspace: as for tasp_page_attention. Stream-ordered, capturable; calls on one plan must be ordered. */
+tasp_status tasp_page_bind(tasp_plan plan, tasp_page_cache* cache);
+tasp_status tasp_page_forward_workspace_bytes(tasp_plan plan, const tasp_page_cache* cache,
+                                              int32_t n_tokens, int32_t max_len, int32_t max_new,
+                                              size_t* bytes);
+tasp_status tasp_page_forward(tasp_plan plan, const float* x, const int32_t* start, int32_t n_tokens,
+                              const tasp_page_cache* cache, int32_t max_len, int32_t max_new,
+                              float* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Scores of given tokens. logits (device): `rows` rows of vocab values, TASP_F32 or TASP_BF16, row_stride elements from
  * one to the next; tokens (device int32 [rows]); p = softmax(row / temperature). Per row:

@@ -37,6 +37,7 @@ EXPORTS = ["tasp_plan_workspace_bytes", "tasp_compile_plan", "tasp_plan_counts",
            "tasp_verify_workspace_bytes", "tasp_verify", "tasp_seq_commit",
            "tasp_seq_bind", "tasp_tree_step_workspace_bytes", "tasp_tree_forward", "tasp_tree_step",
            "tasp_page_append", "tasp_page_read", "tasp_page_attention_workspace_bytes", "tasp_page_attention",
+           "tasp_page_advance", "tasp_page_bind", "tasp_page_forward_workspace_bytes", "tasp_page_forward",
            "tasp_token_logprobs_workspace_bytes", "tasp_token_logprobs",
            "tasp_status_string", "tasp_last_error"]
 
@@ -193,6 +194,10 @@ def load(path: str = LIB_PATH):
         "tasp_page_read": [P, I32, P, I32, I32, P, P, P],
         "tasp_page_attention_workspace_bytes": [P, I32, I32, I32, I32, C.POINTER(SZ)],
         "tasp_page_attention": [P, I32, P, I32, I32, P, I32, C.c_double, I32, I32, P, P, SZ, P],
+        "tasp_page_advance": [P, P, I32, P],
+        "tasp_page_bind": [P, P],
+        "tasp_page_forward_workspace_bytes": [P, P, I32, I32, I32, C.POINTER(SZ)],
+        "tasp_page_forward": [P, P, P, I32, P, I32, I32, P, P, SZ, P],
         "tasp_token_logprobs_workspace_bytes": [I32, I32, I32, C.POINTER(SZ)],
         "tasp_token_logprobs": [P, I32, C.c_int64, P, I32, I32, C.c_double, I32, P, P, P, P, P, P, I32, P, P, SZ, P],
     }
@@ -483,6 +488,27 @@ def tasp_page_attention(cache, layer, start_ptr, n_tokens, act_type, q, n_q_head
                                               max_len, max_new, _ref(out), ws_ptr, ws_bytes, stream)
     if st:
         _check(st)
+
+
+def tasp_page_advance(cache, start_ptr, n_tokens, stream):
+    st = (_lib or load()).tasp_page_advance(_ref(cache), start_ptr, n_tokens, stream)
+    if st:
+        _check(st)
+
+
+def tasp_page_bind(plan, cache):
+    _check(load().tasp_page_bind(plan, _ref(cache)))
+
+
+def tasp_page_forward_workspace_bytes(plan, cache, n_tokens, max_len, max_new):
+    n = C.c_size_t()
+    _check(load().tasp_page_forward_workspace_bytes(plan, _ref(cache), n_tokens, max_len, max_new, C.byref(n)))
+    return n.value
+
+
+def tasp_page_forward(plan, x_ptr, start_ptr, n_tokens, cache, max_len, max_new, out_ptr, ws_ptr, ws_bytes, stream):
+    _check(load().tasp_page_forward(plan, x_ptr, start_ptr, n_tokens, _ref(cache), max_len, max_new, out_ptr, ws_ptr,
+                                    ws_bytes, stream))
 
 
 def tasp_token_logprobs_workspace_bytes(rows, vocab, n_top):

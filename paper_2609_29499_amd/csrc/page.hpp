@@ -21,6 +21,7 @@ struct PageAppendArgs {
   const int* start; int N;             // [batch + 1] or null: token b is sequence b's
   int act;                             // SEQ_BF16 or SEQ_F32: type of q, k, v and q_out
   SeqRows q, k, v, q_out;              // (seq is not used)
+  SeqRows rest;                        // p not null: rows like q_out's; tokens of no sequence get zeros here and in q_out
   int ks; long split;                  // as SeqAppendArgs, and so on to the end
   int n_q, n_kv;
   const int* kv_map;
@@ -31,6 +32,13 @@ struct PageAppendArgs {
   int by_index;
 };
 hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s);
+
+struct PageAdvanceArgs {
+  PageLayer c;                         // any layer
+  const int* start; int N;
+  int* len;                            // c.len
+};
+hipError_t launch_page_advance(const PageAdvanceArgs& a, hipStream_t s);
 
 struct PageReadArgs {
   PageLayer c;

@@ -1049,7 +1049,7 @@ struct Shapes {
 };
 Shapes shapes(const PageAttnArgs& a) {
   Shapes z{};
-  const int seqs = std::min(a.c.batch, a.N), expected = std::max(a.max_new, 1);
+  const int seqs = std::min(a.c.batch, a.N), expected = std::min(a.max_new, a.N);
   const long rows = long(expected) * a.group;
   const long most = std::min<long>(std::max(a.max_len, 0) + long(expected), a.c.cap);
   // One kernel for all where it is what the expected number of tokens asks for, or where there is one sequence

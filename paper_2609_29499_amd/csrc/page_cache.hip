@@ -158,7 +158,13 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
     const float inv = 1.0f / float(a.n_q);
     for (int r = blockIdx.y * y.rows + own; r < r1; r += RPP) {
       const int w = int((float(r) + 0.5f) * inv), h = r - w * a.n_q;      // (r < 4 * 512)
-      if (s_state[w] == 0) continue;
+      if (s_state[w] == 0) {
+        if (a.rest.p && t0 + w < a.N) {
+          store8<ACT>(a.q_out.p, (t0 + w) * a.q_out.token + h * a.q_out.head + e0, Vec8{});
+          store8<ACT>(a.rest.p, (t0 + w) * a.rest.token + h * a.rest.head + e0, Vec8{});
+        }
+        continue;
+      }
       Vec8 x{}, z{};
       if (s_state[w] == 2) {
         const long at = (t0 + w) * a.q.token + h * a.q.head + e0;
@@ -296,7 +302,21 @@ __global__ __launch_bounds__(kBlock) void page_read_kernel(PageReadArgs a) {
   store8<OUT>(dst.p, b * dst.seq + i * dst.token + h * dst.head + e0, x);
 }
 
+// Lengths grow by the sequences' new tokens: a thread each.
+__global__ __launch_bounds__(kBlock) void page_advance_kernel(PageAdvanceArgs a) {
+  static_assert(kSeqMaxBatch <= kBlock, "one workgroup");
+  const int b = threadIdx.x;
+  if (b >= a.c.batch) return;
+  const PageSeq q = page_seq(a.start, a.N, a.c, b);
+  if (q.L >= 0 && q.n > 0) a.len[b] = min(q.L + min(q.n, a.c.cap), a.c.cap);
+}
+
 }  // namespace
+
+hipError_t launch_page_advance(const PageAdvanceArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(page_advance_kernel, dim3(1), dim3(kBlock), 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s) {
   if (a.N < 1 || a.n_kv < 1 || a.n_kv > 64 || a.n_q < 0 || a.n_q > 512) return hipErrorInvalidValue;

@@ -2511,7 +2511,7 @@ tasp_status page_attn_args(const tasp_page_cache* c, int32_t n_q, int32_t n_toke
     return fail(TASP_ERR_SHAPE, "%d tokens (1..%d)", n_tokens, TASP_PAGE_MAX_TOKENS);
   if (max_len < 0 || max_len > c->max_pages * c->page_rows)
     return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_pages * c->page_rows);
-  if (max_new < 1 || max_new > n_tokens) return fail(TASP_ERR_SHAPE, "max_new %d outside 1..%d", max_new, n_tokens);
+  if (max_new < 1) return fail(TASP_ERR_SHAPE, "max_new %d", max_new);
   a->c = page_layer(c, 0);
   a->N = n_tokens; a->max_len = max_len; a->max_new = max_new; a->slots = c->n_kv_heads; a->group = n_q / c->n_kv_heads;
   for (int j = 0; j < a->slots; ++j) a->slot[j] = tasp::tree_slot(j, j * a->group, a->group);
@@ -2593,6 +2593,125 @@ tasp_status tasp_page_attention(const tasp_page_cache* cache, int32_t layer, con
   a.ws = static_cast<float*>(workspace);
   HIP_TRY(tasp::launch_page_attn(a, static_cast<hipStream_t>(stream)));
   return TASP_OK;
+}
+
+tasp_status tasp_page_advance(const tasp_page_cache* cache, const int32_t* start, int32_t n_tokens, void* stream) {
+  tasp_status st;
+  if ((st = check_page_cache(cache, 0)) || (st = check_page_buffers(cache)) || (st = check_packed(cache, start, n_tokens))) return st;
+  tasp::PageAdvanceArgs a{};
+  a.c = page_layer(cache, 0);
+  a.start = start; a.N = n_tokens; a.len = cache->len;
+  HIP_TRY(tasp::launch_page_advance(a, static_cast<hipStream_t>(stream)));
+  return TASP_OK;
+}
+
+namespace {
+
+// The cache of a plan's step: the plan's shape, and its rows the plan's.
+tasp_status check_plan_pages(const tasp_plan_s* p, const tasp_page_cache* c) {
+  tasp_status st;
+  if (!p) return fail(TASP_ERR_INVALID_ARG, "plan is NULL");
+  if ((st = check_page_cache(c, 0)) || (st = check_page_buffers(c))) return st;
+  const tasp_model_desc& d = p->desc;
+  if (c->n_layers != d.n_layers || c->n_kv_heads != d.n_kv_heads || c->head_dim != d.head_dim)
+    return fail(TASP_ERR_SHAPE, "cache of %d layers, %d heads of %d; the plan has %d, %d of %d", c->n_layers,
+                c->n_kv_heads, c->head_dim, d.n_layers, d.n_kv_heads, d.head_dim);
+  return TASP_OK;
+}
+
+// The attention's arguments over the retained groups of a layer.
+tasp::PageAttnArgs plan_attn_args(const tasp_plan_s* p, const tasp_page_cache* c, int l, const int32_t* start, int32_t n_tokens,
+                                  int32_t max_len, int32_t max_new) {
+  const LayerPlan& P = p->layers[l];
+  tasp::PageAttnArgs t{};
+  t.c = page_layer(c, l);
+  t.start = start; t.N = n_tokens; t.act = TASP_F32; t.max_len = max_len; t.max_new = max_new; t.slots = P.m_kv;
+  for (int j = 0; j < P.m_kv; ++j) {
+    const int heads = P.slot_start[j + 1] - P.slot_start[j];
+    t.slot[j] = tasp::tree_slot(P.kv_idx[j], P.slot_start[j], heads);
+    t.group = std::max(t.group, heads);
+  }
+  return t;
+}
+
+tasp_status page_step_bytes(const tasp_plan_s* p, const tasp_page_cache* c, int32_t n_tokens, int32_t max_len, int32_t max_new,
+                            size_t* bytes) {
+  const tasp_model_desc& d = p->desc;
+  if (d.max_prefill < 1) return fail(TASP_ERR_UNSUPPORTED, "plan compiled with max_prefill 0");
+  if (n_tokens < 1 || n_tokens > d.max_prefill || n_tokens > TASP_PAGE_MAX_TOKENS)
+    return fail(TASP_ERR_SHAPE, "%d tokens outside 1..max_prefill %d", n_tokens, d.max_prefill);
+  if (max_len < 0 || max_len > c->max_pages * c->page_rows)
+    return fail(TASP_ERR_SHAPE, "max_len %d outside 0..%d", max_len, c->max_pages * c->page_rows);
+  if (max_new < 1) return fail(TASP_ERR_SHAPE, "max_new %d", max_new);
+  *bytes = 0;
+  for (size_t l = 0; l < p->layers.size(); ++l)
+    if (p->layers[l].m_kv > 0)
+      *bytes = std::max(*bytes, tasp::page_attn_workspace_bytes(plan_attn_args(p, c, int(l), nullptr, n_tokens, max_len, max_new)));
+  return TASP_OK;
+}
+
+}  // namespace
+
+tasp_status tasp_page_bind(tasp_plan p, tasp_page_cache* cache) {
+  tasp_status st = check_plan_pages(p, cache);
+  if (st) return st;
+  cache->plan_sig = p->sig;
+  return TASP_OK;
+}
+
+tasp_status tasp_page_forward_workspace_bytes(tasp_plan p, const tasp_page_cache* cache, int32_t n_tokens, int32_t max_len,
+                                              int32_t max_new, size_t* bytes) {
+  tasp_status st = check_plan_pages(p, cache);
+  if (st) return st;
+  if (!bytes) return fail(TASP_ERR_INVALID_ARG, "bytes is NULL");
+  return page_step_bytes(p, cache, n_tokens, max_len, max_new, bytes);
+}
+
+tasp_status tasp_page_forward(tasp_plan p, const float* x, const int32_t* start, int32_t n_tokens, const tasp_page_cache* cache,
+                              int32_t max_len, int32_t max_new, float* out, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  tasp_status st;
+  size_t need = 0;
+  if ((st = check_plan_pages(p, cache)) || (st = check_packed(cache, start, n_tokens)) ||
+      (st = page_step_bytes(p, cache, n_tokens, max_len, max_new, &need)))
+    return st;
+  if (!x || !out) return fail(TASP_ERR_INVALID_ARG, "x / out is NULL");
+  if (!aligned(x, 16) || !aligned(out, 16)) return fail(TASP_ERR_INVALID_ARG, "x / out is not 16-byte aligned");
+  if (cache->plan_sig != p->sig)
+    return fail(TASP_ERR_CACHE_PLAN_MISMATCH, "cache belongs to plan %016llx, not %016llx",
+                (unsigned long long)cache->plan_sig, (unsigned long long)p->sig);
+  const tasp_model_desc& d = p->desc;
+  const size_t width = d.vocab ? d.vocab : d.d_model;
+  const char *xb = reinterpret_cast<const char*>(x), *ob = reinterpret_cast<const char*>(out);
+  if (ob < xb + size_t(n_tokens) * d.d_model * 4 && xb < ob + size_t(n_tokens) * width * 4)
+    return fail(TASP_ERR_INVALID_ARG, "x and out overlap");
+  if ((st = check_workspace(workspace, workspace_bytes, need))) return st;
+  const int dh = d.head_dim;
+  const tasp_rope rope{TASP_ROPE_HALF, dh, TASP_ROPE_NONE, 0, d.rope_theta, 1.0, 1.0, 2.0, 1.0};
+  tasp::PageAppendArgs turned{};
+  rope_args(&rope, &turned);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  float* q = reinterpret_cast<float*>(p->pq);          // [n_tokens][m_q][dh] (as wide as the prefill's two BF16 planes)
+  auto attend = [&](int l, const float* qkv, int ld, int ks) -> tasp_status {
+    const LayerPlan& P = p->layers[l];
+    tasp::PageAttnArgs t = plan_attn_args(p, cache, l, start, n_tokens, max_len, max_new);
+    tasp::PageAppendArgs a = turned;
+    a.c = t.c; a.start = start; a.N = n_tokens; a.act = TASP_F32; a.n_q = P.m_q; a.n_kv = P.m_kv; a.kv_map = P.kv_idx.data();
+    a.ks = ks; a.split = long(n_tokens) * ld;
+    float* base = const_cast<float*>(qkv);             // (read only)
+    auto rows = [&](int first) { return tasp::SeqRows{base + size_t(first) * dh, 0, ld, dh}; };
+    a.q = rows(0); a.k = rows(P.m_q); a.v = rows(P.m_q + P.m_kv);
+    a.q_out = {q, 0, long(P.m_q) * dh, dh};
+    t.q = a.q_out;
+    t.o = {p->pxw, 0, p->ld_xw, dh};
+    a.rest = t.o;                                      // (the next projection reads every token's row)
+    t.scale2 = float(1.44269504088896340736 / std::sqrt(double(dh)));
+    t.ws = static_cast<float*>(workspace);
+    HIP_TRY(tasp::launch_page_append(a, s));
+    HIP_TRY(tasp::launch_page_attn(t, s));
+    return TASP_OK;
+  };
+  return prefill_layers(p, x, n_tokens, out, s, nullptr, false, attend);
 }
 
 namespace {

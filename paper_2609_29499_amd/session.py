@@ -303,6 +303,31 @@ class Plan:
         return out
 
 
+    def page_bind(self, cache):
+        B.tasp_page_bind(self.handle, cache.struct)
+
+    def page_workspace(self, cache, n_tokens, max_len=None, max_new=None, stream=None):
+        """A workspace for page_forward calls of this shape."""
+        n = B.tasp_page_forward_workspace_bytes(self.handle, cache.struct, n_tokens, cache.max_seq if max_len is None else max_len,
+                                                n_tokens if max_new is None else max_new)
+        return _workspace(n, cache.k.device, stream)
+
+    def page_forward(self, x, cache, start=None, max_len=None, max_new=None, out=None, workspace=None, stream=None):
+        """The plan over packed tokens x float32 [N][d] (start as page_append) -> logits [N][V] (or residuals [N][d]). The
+        lengths stay: page_advance."""
+        dev = _device(cache.k, self.ws, x, start, out)
+        N = x.shape[0]
+        width = self.desc.vocab or self.desc.d_model
+        if out is None:
+            out = _empty((N, width), torch.float32, x.device, stream)
+        ml = cache.max_seq if max_len is None else max_len
+        mn = max_new if max_new is not None else 1 if start is None else N
+        ws = _on(dev, workspace) if workspace is not None else self.page_workspace(cache, N, ml, mn, stream)
+        _launch(B.tasp_page_forward, dev, stream, self.handle, _ptr(x, (N, self.desc.d_model), torch.float32, "x"),
+                cache._start(start), N, cache.struct, ml, mn, _ptr(out, (N, width), torch.float32, "out"), ws[1], ws[2])
+        return out
+
+
 def build_mask(desc, head_scores, chan_scores, granule, target, stream=None):
     """Greedy dependency-closed mask from device float32 scores ([L][Hq], [L][d_ffn/granule]).
     Returns (q_keep, kv_keep, ffn_keep) as device uint8 tensors and the FLOPs spent."""
@@ -729,6 +754,13 @@ def page_attention(cache, layer, q, start=None, scale=None, max_len=None, max_ne
     return out
 
 
+def page_advance(cache, n_tokens, start=None, stream=None):
+    """Lengths grow by the tokens of a step (start as page_append), behind its last layer. Returns them."""
+    dev = _device(cache.k, start)
+    _launch(B.tasp_page_advance, dev, stream, cache.struct, cache._start(start), n_tokens)
+    return cache.len
+
+
 class TokenLogprobs(NamedTuple):
     """Of every row: the token's log probability, the entropy, the token's rank, the first tokens in the order of logits and
     their log probabilities; of every sequence of rows the mean log probability (None without ``start``)."""
@@ -753,22 +785,18 @@ def token_logprobs(logits, tokens, n_top=0, temperature=1.0, start=None, workspa
         raise ValueError(f"logits must be a float32 or bfloat16 tensor [R][V] with contiguous rows, not {logits.dtype} {tuple(logits.shape)}")
     R, V = logits.shape
     S = 0
-    mean = None
     if start is not None:
         if start.dim() != 1 or start.shape[0] < 2:
             raise ValueError(f"start must be [S + 1], not {tuple(start.shape)}")
         S = start.shape[0] - 1
-    # one allocation of 32-bit numbers for all outputs
+    # one allocation for the outputs of a type
     top = R * n_top
-    buf = _empty((3 * R + 2 * top + S,), torch.float32, logits.device, stream)
-    whole = buf.view(torch.int32)
-    logprob, entropy, rank = buf[:R], buf[R:2 * R], whole[2 * R:3 * R]
-    ids, top_lp = whole[3 * R:3 * R + top].view(R, n_top), buf[3 * R + top:3 * R + 2 * top].view(R, n_top)
-    if S:
-        mean = buf[3 * R + 2 * top:]
-    at = buf.data_ptr()
+    numbers, whole = _empty((2 * R + top + S,), torch.float32, logits.device, stream), _empty((R + top,), torch.int32, logits.device, stream)
+    logprob, entropy, top_lp, mean = numbers.split((R, R, top, S))
+    rank, ids = whole.split((R, top))
+    at, to = numbers.data_ptr(), whole.data_ptr()
     ws = _on(dev, workspace) if workspace is not None else token_logprobs_workspace(R, V, n_top, logits.device, stream)
     _launch(B.tasp_token_logprobs, dev, stream, logits.data_ptr(), _SEQ_TYPES[logits.dtype], logits.stride(0) if R > 1 else V,
-            _ptr(tokens, (R,), torch.int32, "tokens"), R, V, temperature, n_top, at, at + 4 * R, at + 8 * R, at + 12 * R,
-            at + 12 * R + 4 * top, _ptr(start, (S + 1,), torch.int32, "start"), S, at + 12 * R + 8 * top if S else None, ws[1], ws[2])
-    return TokenLogprobs(logprob, entropy, rank, ids, top_lp, mean)
+            _ptr(tokens, (R,), torch.int32, "tokens"), R, V, temperature, n_top, at, at + 4 * R, to, to + 4 * R,
+            at + 8 * R, _ptr(start, (S + 1,), torch.int32, "start"), S, at + 8 * R + 4 * top if S else None, ws[1], ws[2])
+    return TokenLogprobs(logprob, entropy, rank, ids.view(R, n_top), top_lp.view(R, n_top), mean if S else None)

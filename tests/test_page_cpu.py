@@ -117,7 +117,7 @@ def test_attention_refusals():
     bad("TASP_ERR_SHAPE", _8=-1)
     bad("TASP_ERR_SHAPE", _8=321)
     bad("TASP_ERR_SHAPE", _9=0)
-    bad("TASP_ERR_SHAPE", _9=6)
+    bad("TASP_ERR_SHAPE", _9=-4)
     long = dict(_0=cache(max_pages=1000), _8=30000)
     bad("TASP_ERR_INVALID_ARG", _11=None, **long)
     bad("TASP_ERR_WORKSPACE", _11=FAKE + 16, **long)
