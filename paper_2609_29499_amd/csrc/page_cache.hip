@@ -5,7 +5,7 @@
 // s per page and KV head: s = max(|y|) / qmax (127 or 448) over all that was written there since row 0 was. A call whose rows
 // raise it rounds the older rows' codes again, code' = round(code s_old / s); new rows are round(y / s). The rotated
 // rows of a page and head must all be known before the first code is, so a workgroup holds them in registers: a lane eight
-// elements of a head for each of NP rows, in float32. The page's sines and cosines go through LDS and serve all the heads
+// elements of a head (both halves of four pairs) for each of NP rows, in float32. The page's sines and cosines go through LDS and serve all the heads
 // that the workgroup walks.
 #include <algorithm>
 
@@ -34,25 +34,85 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return max(max(at(0), at(16)), max(at(32), at(48)));
 }
 
-// eight elements rotated by the sines and cosines of their pairs; y: the partners' where pairs lie apart
-__device__ __forceinline__ void rotate8(Vec8& x, const Vec8& y, const float2* cs, int e0, int rot, bool interleaved) {
-  if (interleaved) {                   // pairs (2 i, 2 i + 1)
+// A lane's eight elements of a head: two pieces of four that hold both halves of four pairs, so that a row is read
+// once. Rows of interleaved pairs, and what is not rotated: neighbours.
+struct Pieces {
+  int at[2];
+  __device__ __forceinline__ Pieces(int lane, int rot, bool interleaved) {
+    const int e0 = kE * lane;
+    const bool apart = !interleaved && e0 < rot;
+    at[0] = apart ? 4 * lane : e0;
+    at[1] = apart ? rot / 2 + 4 * lane : e0 + 4;
+  }
+};
+// the elements as they lie
+template <int ACT>
+struct Raw8 {
+  uint32_t w[ACT == SEQ_BF16 ? 4 : 8];
+};
+template <int ACT>
+__device__ __forceinline__ Raw8<ACT> load_raw(const void* p, long row, const Pieces& e) {
+  Raw8<ACT> x;
 #pragma unroll
-    for (int i = 0; i < kE; i += 2) {
-      const float2 w = cs[(e0 + i) / 2];
-      const float p = x.v[i], q = x.v[i + 1];
-      x.v[i] = p * w.x - q * w.y;
-      x.v[i + 1] = q * w.x + p * w.y;
-    }
-  } else {                             // pairs (i, i + rot / 2)
-    const int half = rot / 2;
-    const bool first = e0 < half;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) {
-      const float2 w = cs[(first ? e0 : e0 - half) + i];
-      x.v[i] = first ? x.v[i] * w.x - y.v[i] * w.y : x.v[i] * w.x + y.v[i] * w.y;
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (ACT == SEQ_BF16) {
+      const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + row + e.at[k]);
+      x.w[2 * k] = q.x; x.w[2 * k + 1] = q.y;
+    } else {
+      const uint4 q = *reinterpret_cast<const uint4*>(static_cast<const uint32_t*>(p) + row + e.at[k]);
+      x.w[4 * k] = q.x; x.w[4 * k + 1] = q.y; x.w[4 * k + 2] = q.z; x.w[4 * k + 3] = q.w;
     }
   }
+  return x;
+}
+template <int ACT>
+__device__ __forceinline__ Vec8 values_of(const Raw8<ACT>& x) {
+  Vec8 v;
+#pragma unroll
+  for (int i = 0; i < kE; ++i) {
+    if constexpr (ACT == SEQ_BF16) v.v[i] = i & 1 ? bf16_hi(x.w[i / 2]) : bf16_lo(x.w[i / 2]);
+    else v.v[i] = __uint_as_float(x.w[i]);
+  }
+  return v;
+}
+// the same of a sum of arrays (a projection's splits, a.split floats apart), in their order
+template <int ACT>
+__device__ __forceinline__ void add_splits(Vec8& x, const PageAppendArgs& a, const void* p, long row, const Pieces& e) {
+  if constexpr (ACT == SEQ_F32)
+    for (int z = 1; z < a.ks; ++z) {
+      const Vec8 y = values_of<ACT>(load_raw<ACT>(p, row + z * a.split, e));
+#pragma unroll
+      for (int i = 0; i < kE; ++i) x.v[i] += y.v[i];
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void store_pieces(void* p, long row, const Pieces& e, const Vec8& x) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float* v = x.v + 4 * k;
+    if constexpr (ACT == SEQ_BF16)
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + row + e.at[k]) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    else
+      *reinterpret_cast<float4*>(static_cast<float*>(p) + row + e.at[k]) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+// cs: the sines and cosines of the lane's four pairs
+__device__ __forceinline__ void rotate_pieces(Vec8& x, const float2* cs, bool interleaved) {
+  Vec8 y = x;
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y.v[2 * i] = x.v[2 * i] * cs[i].x - x.v[2 * i + 1] * cs[i].y;
+      y.v[2 * i + 1] = x.v[2 * i + 1] * cs[i].x + x.v[2 * i] * cs[i].y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y.v[i] = x.v[i] * cs[i].x - x.v[4 + i] * cs[i].y;
+      y.v[4 + i] = x.v[i] * cs[i].y + x.v[4 + i] * cs[i].x;
+    }
+  }
+  x = y;
 }
 
 // x / s for |x| up to qmax s about, by a refined reciprocal: s is brought near 1 by a power of two first
@@ -114,15 +174,31 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
   __shared__ float2 cs[NP * RPP][DH / 2];
   __shared__ uint32_t s_top[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int e0 = kE * (tid % LPR), own = tid / LPR, half = a.rot / 2;
-  const bool apart = !a.interleaved && e0 < a.rot;     // its pairs' other halves are another lane's
-  const int far = e0 < half ? half : -half;
+  const int own = tid / LPR, half = a.rot / 2, pair0 = 4 * (tid % LPR);
+  const Pieces e(tid % LPR, a.rot, a.interleaved);
+  const bool turns = kE * (tid % LPR) < a.rot;
 
   if (int(blockIdx.x) >= y.items) {
     // ---- q of a token group
     if (int(blockIdx.y) >= y.q_slices) return;
     const int t0 = (blockIdx.x - y.items) * y.tokens;
     __shared__ int s_state[4];         // of a token: 0 no sequence's, 1 absent, 2 there
+    // a pass's elements, asked for a pass ahead, the first ahead of the tokens' places
+    struct Row {
+      Raw8<ACT> x;
+      int w, h;                        // token of the group, head
+      bool in;
+    };
+    const int r0 = blockIdx.y * y.rows, r1 = min(min(y.tokens, a.N - t0) * a.n_q, r0 + y.rows);
+    const float inv = 1.0f / float(a.n_q);
+    auto fetch = [&](int r, Row& p) __attribute__((always_inline)) {
+      p.in = r < r1;
+      p.w = int((float(r) + 0.5f) * inv);              // (r < 4 * 512)
+      p.h = r - p.w * a.n_q;
+      if (p.in) p.x = load_raw<ACT>(a.q.p, (t0 + p.w) * a.q.token + p.h * a.q.head, e);
+    };
+    Row next;
+    fetch(r0 + own, next);
     if (wave < y.tokens) {
       const int t = t0 + wave;
       int state = 0, pos = 0;
@@ -154,27 +230,26 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
       if (lane == 0) s_state[wave] = state;
     }
     __syncthreads();
-    const int total = y.tokens * a.n_q, r1 = min(total, int(blockIdx.y + 1) * y.rows);
-    const float inv = 1.0f / float(a.n_q);
-    for (int r = blockIdx.y * y.rows + own; r < r1; r += RPP) {
-      const int w = int((float(r) + 0.5f) * inv), h = r - w * a.n_q;      // (r < 4 * 512)
-      if (s_state[w] == 0) {
-        if (a.rest.p && t0 + w < a.N) {
-          store8<ACT>(a.q_out.p, (t0 + w) * a.q_out.token + h * a.q_out.head + e0, Vec8{});
-          store8<ACT>(a.rest.p, (t0 + w) * a.rest.token + h * a.rest.head + e0, Vec8{});
+    for (int r = r0 + own; r - own < r1; r += RPP) {
+      const Row now = next;
+      if (r - own + RPP < r1) fetch(r + RPP, next);
+      if (!now.in) continue;
+      const int state = s_state[now.w];
+      const long to = (t0 + now.w) * a.q_out.token + now.h * a.q_out.head;
+      if (state == 0) {
+        if (a.rest.p) {
+          store_pieces<ACT>(a.q_out.p, to, e, Vec8{});
+          store_pieces<ACT>(a.rest.p, (t0 + now.w) * a.rest.token + now.h * a.rest.head, e, Vec8{});
         }
         continue;
       }
-      Vec8 x{}, z{};
-      if (s_state[w] == 2) {
-        const long at = (t0 + w) * a.q.token + h * a.q.head + e0;
-        x = load8<ACT>(a.q.p, at, a);
-        if (e0 < a.rot) {
-          if (apart) z = load8<ACT>(a.q.p, at + far, a);
-          rotate8(x, z, cs[w], e0, a.rot, a.interleaved);
-        }
+      Vec8 x{};
+      if (state == 2) {
+        x = values_of<ACT>(now.x);
+        add_splits<ACT>(x, a, a.q.p, (t0 + now.w) * a.q.token + now.h * a.q.head, e);
+        if (turns) rotate_pieces(x, &cs[now.w][pair0], a.interleaved);
       }
-      store8<ACT>(a.q_out.p, (t0 + w) * a.q_out.token + h * a.q_out.head + e0, x);
+      store_pieces<ACT>(a.q_out.p, to, e, x);
     }
     return;
   }
@@ -220,22 +295,21 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
     float* scale = TYPE == SEQ_BF16 ? nullptr : (is_v ? a.c.vs : a.c.ks) + unit;
     float was = TYPE != SEQ_BF16 && lo > 0 ? *scale : 0.0f;
     const size_t base = (unit << a.c.P_log) * DH;      // elements
+    Raw8<ACT> raw[NP];                 // (a branch around a load would wait for it: rows that are not new read the last one)
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      raw[p] = load_raw<ACT>(src.p, long(first + row0 + min(max(p * RPP + own, lo), hi - 1) - L) * src.token + (c >> 1) * src.head, e);
     Vec8 x[NP];
     uint32_t top = 0;                  // magnitudes as integers: infinities and NaN on top
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int r = p * RPP + own;
-      x[p] = Vec8{};
+      x[p] = values_of<ACT>(raw[p]);
       if (r >= lo && r < hi) {
-        const long at = long(first + row0 + r - L) * src.token + (c >> 1) * src.head + e0;
-        x[p] = load8<ACT>(src.p, at, a);
-        if (!is_v && e0 < a.rot) {
-          Vec8 z{};
-          if (apart) z = load8<ACT>(src.p, at + far, a);
-          rotate8(x[p], z, cs[r], e0, a.rot, a.interleaved);
-        }
+        add_splits<ACT>(x[p], a, src.p, long(first + row0 + r - L) * src.token + (c >> 1) * src.head, e);
+        if (!is_v && turns) rotate_pieces(x[p], &cs[r][pair0], a.interleaved);
         if constexpr (TYPE == SEQ_BF16) {
-          store8<SEQ_BF16>(is_v ? a.c.v : a.c.k, long(base + size_t(r) * DH + e0), x[p]);
+          store_pieces<SEQ_BF16>(is_v ? a.c.v : a.c.k, long(base + size_t(r) * DH), e, x[p]);
         } else {
 #pragma unroll
           for (int i = 0; i < kE; ++i) top = max(top, __float_as_uint(x[p].v[i]) & 0x7fffffffu);
@@ -257,20 +331,24 @@ __global__ __launch_bounds__(kBlock) void page_append_kernel(PageAppendArgs a, K
       const Quotient by(some ? now : 1.0f);
       const bool again = some && now > was;            // older rows' codes change
       const float f = again ? was / now : 0.0f;
-      uint8_t* out = static_cast<uint8_t*>(is_v ? a.c.v : a.c.k) + base + e0;
+      uint8_t* out = static_cast<uint8_t*>(is_v ? a.c.v : a.c.k) + base;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
         const int r = p * RPP + own;
+        uint32_t* w0 = reinterpret_cast<uint32_t*>(out + r * DH + e.at[0]);
+        uint32_t* w1 = reinterpret_cast<uint32_t*>(out + r * DH + e.at[1]);
         float q[kE];
         if (r >= lo && r < hi) {
 #pragma unroll
           for (int i = 0; i < kE; ++i) q[i] = some ? by(x[p].v[i]) : 0.0f;
         } else if (again && r < lo) {
-          values8<TYPE>(*reinterpret_cast<const uint2*>(out + r * DH), f, q);
+          values8<TYPE>(make_uint2(*w0, *w1), f, q);
         } else {
           continue;
         }
-        *reinterpret_cast<uint2*>(out + r * DH) = codes8<TYPE>(q);
+        const uint2 w = codes8<TYPE>(q);
+        *w0 = w.x;
+        *w1 = w.y;
       }
       if (tid == 0) *scale = now;
     }
@@ -332,14 +410,22 @@ hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s) {
   y.groups = a.n_q ? (a.N + y.tokens - 1) / y.tokens : 0;
   y.rows = a.N >= 1024 ? y.tokens * a.n_q : rpp;
   y.q_slices = a.n_q ? (y.tokens * a.n_q + y.rows - 1) / y.rows : 0;
-  const dim3 grid(y.items + y.groups, std::max(y.slices, y.q_slices));
-#define APPEND(DH, ACT, TYPE, NP) hipLaunchKernelGGL((page_append_kernel<DH, ACT, TYPE, NP>), grid, dim3(kBlock), 0, s, a, map, y)
-#define APPEND_NP(DH, ACT, TYPE)                                      \
-  do {                                                                \
-    if (a.c.P <= kBlock * kE / DH) APPEND(DH, ACT, TYPE, 1);          \
-    else if (a.c.P <= 2 * kBlock * kE / DH) APPEND(DH, ACT, TYPE, 2); \
-    else if (a.c.P <= 4 * kBlock * kE / DH) APPEND(DH, ACT, TYPE, 4); \
-    else if constexpr (DH == 128) APPEND(DH, ACT, TYPE, 8);           \
+  // Many tokens: q in a launch of its own, which has the LDS of a small page, and so more workgroups per CU
+  AppendShape q = y;
+  const bool apart = a.N >= 1024 && y.groups > 0;
+  if (apart) {
+    y.groups = y.q_slices = 0;
+    q.items = q.slices = 0;
+  }
+#define APPEND(DH, ACT, TYPE, NP, Y) \
+  hipLaunchKernelGGL((page_append_kernel<DH, ACT, TYPE, NP>), dim3(Y.items + Y.groups, std::max(Y.slices, Y.q_slices)), dim3(kBlock), 0, s, a, map, Y)
+#define APPEND_NP(DH, ACT, TYPE)                                         \
+  do {                                                                   \
+    if (apart) APPEND(DH, ACT, TYPE, 1, q);                              \
+    if (a.c.P <= kBlock * kE / DH) APPEND(DH, ACT, TYPE, 1, y);          \
+    else if (a.c.P <= 2 * kBlock * kE / DH) APPEND(DH, ACT, TYPE, 2, y); \
+    else if (a.c.P <= 4 * kBlock * kE / DH) APPEND(DH, ACT, TYPE, 4, y); \
+    else if constexpr (DH == 128) APPEND(DH, ACT, TYPE, 8, y);           \
   } while (0)
 #define APPEND_TYPE(DH, ACT)                                      \
   do {                                                            \
