@@ -556,12 +556,15 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 // bank twice. K rows are read as they lie (operand A of S^T = K Q^T); V is turned on its way from LDS
 // (ds_read_b64_tr_b16: four rows of 16 dimensions, one per lane), cache rows 4 c .. 4 c + 3 of two tiles being the eight of
 // operand B that meet the lane's P. So P stays in registers.
-//   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries: P is one FP16 term (11 bits; half the matrix
-// products of two BF16 terms), lifted by 2^kLift, so that what falls below FP16's range is 2^-30 of a probability of 1, and V is
+//   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries: P is one FP16 term: 11 bits, an eighth of the
+// output's rounding, and half the matrix products of two BF16 terms (8192 tokens x 64 heads 1302 us, 1573 with two terms). V is
 // FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below the largest scale seen)
-// goes into P; BF16 values are multiplied by a power of two that brings the largest seen below 2^15 (lowered when a step has a
-// larger one), exact but for what lies 2^-37 below it.
-constexpr float kLift = 6.0f;
+// goes into P, below 2; BF16 values are multiplied by a power of two that brings the largest seen below 2^15 (lowered when a
+// step has a larger one). P is at most 2^kWideSlack, and lifted by 2^kLift to just below FP16's end, so that half a step of its
+// least numbers is 2^-35 of the row with the running maximum; the lift is taken out of the sums at the end. (Slack of
+// 2: 1320 us, of 8: 1303.) Lost at most: 2^-35 of the largest |v| for each row, and 2^-36 for V's own least numbers.
+constexpr float kWideSlack = 4.0f;     // in place of kSlack
+constexpr float kLift = 10.0f, kUnlift = 0x1p-10f;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
@@ -889,7 +892,7 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
           top = fmaxf(top, fmaf(q, ks[t], bias[t]));
         }
       }
-      if (__ballot(top > m_run[mt] + kSlack)) {        // (also the first rows: m_run is -inf)
+      if (__ballot(top > m_run[mt] + kWideSlack)) {        // (also the first rows: m_run is -inf)
         const float mn = fmaxf(m_run[mt], quad_max(top));
         const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[mt] - mn);
         m_run[mt] = mn;
@@ -944,11 +947,11 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
   for (; s < s1; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::true_type{});
 
   // every wave holds its rows' results; through LDS, 16 rows at a time, they become whole rows
-  const float unit = !HALF ? 1.0f : TYPE == SEQ_BF16 ? 1.0f / mul : ref;
+  const float unit = !HALF ? 1.0f : (TYPE == SEQ_BF16 ? 1.0f / mul : ref) * kUnlift;
   __syncthreads();
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const float l_all = quad_sum(l_run[mt]);
+    const float l_all = quad_sum(l_run[mt]) * (HALF ? kUnlift : 1.0f);
 #pragma unroll
     for (int e = 0; e < NDT; ++e)
 #pragma unroll
@@ -995,7 +998,8 @@ __global__ __launch_bounds__(kBlock) void page_join_kernel(PageAttnArgs a, PageS
   const int rows_all = seq.n * a.group;
   const PageShape& y = rows_all >= wide.least && rows_all <= wide.most ? wide : few;
   // (rows past a slot's last one repeat it, and store nothing; one chunk: written already)
-  const bool there = own < group && q_row < total && token >= seq.first && token < seq.first + seq.n && y.cut && note.z > 1;
+  const bool there = own < group && q_row < total && token >= seq.first && token < seq.first + seq.n && y.cut && note.z > 1 &&
+                     note.y >= 0 && note.z <= y.items && note.y <= y.items - ((rows_all + y.rows - 1) >> y.rows_log) * note.z;
   if (!__syncthreads_or(there)) return;
   const int n = there ? note.z : 1, row = there ? (token - seq.first) * group + hh : 0;
   const int blocks = (rows_all + y.rows - 1) >> y.rows_log, in = row & (y.rows - 1);

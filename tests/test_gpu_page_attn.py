@@ -3,11 +3,12 @@
 Tolerance of one output: with A = sum of p |v| over the rows seen, n their number,
   scores: a float32 dot product of dh exact products, |error| <= (dh + 4) 2^-24 scale sum |q_i k_i| = d, which
   moves p by a factor within exp(2 d);
-  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; more than 32 BF16 query rows of a sequence and cache head: one FP16 term, half a step 2^-11, and where P times the page's scale
-  falls below 2^-18 of the largest scale M, a subnormal's half step 2^-25 in units of 2^-4 M or less: n 2^-29 max |v| together;
+  exp2 and the rescaling by powers: 2^-21; P in two BF16 terms 2^-16, in three 2^-24; more than 32 BF16 query rows of a sequence and cache head: one FP16 term, half a step 2^-11, and half a step
+  of FP16's least numbers, 2^-25, of P (lifted by 2^10; V times it is in units of the largest |v| or less) and of V (the largest at
+  2^11 or more): n (2^-35 + 2^-36) max |v|, less than n 2^-34 max |v| together;
   float32 sums n 2^-24;
   the output's rounding 2^-8 of the value in BF16, 2^-24 in float32.
-|error| <= A (2 d + 2^-21 + 2^-11, 2^-16 or 2^-24 + n 2^-24) + (n 2^-29 max |v|) + |o| 2^-8 or 2^-24."""
+|error| <= A (2 d + 2^-21 + 2^-11, 2^-16 or 2^-24 + n 2^-24) + (n 2^-34 max |v|) + |o| 2^-8 or 2^-24."""
 import math
 
 import numpy as np
@@ -42,7 +43,7 @@ def check(got, q, rows, lens, counts, P, act, scale, first=0, cap=None, gone=lam
                 o, A = O.attention(q[t, h], k, v, seen, scale)
                 d = (dh + 4) * 2.0 ** -24 * scale * np.max(np.abs(k[seen]) @ np.abs(q[t, h]))
                 tol = A * (2 * d + 2.0 ** -21 + (2.0 ** -11 if half else 2.0 ** -16 if act == "bf16" else 2.0 ** -24) + len(seen) * 2.0 ** -24)
-                tol = tol + half * len(seen) * 2.0 ** -29 * np.max(np.abs(v[seen]))
+                tol = tol + half * len(seen) * 2.0 ** -34 * np.max(np.abs(v[seen]))
                 tol = tol + np.abs(o) * (2.0 ** -8 if act == "bf16" else 2.0 ** -24)
                 err = np.abs(got[t, h] - o)
                 worst = max(worst, float(np.max(np.divide(err, tol, out=np.zeros_like(err), where=tol > 0))))
