@@ -40,6 +40,11 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 constexpr int kTarget = 512;           // workgroups aimed at: two per CU
 constexpr int kFew = 32;               // query rows of a sequence and cache head that the first kernel serves
 
+// Steps of 64 cache rows, in all slots, of short sequences that the wide kernel takes beside its own, in place of a second launch:
+// for float32, whose bits are the same in both kernels. (3 x 37 tokens x 24 heads behind 1001 rows: 16.5 us, 19.3 with both
+// kernels. Three single tokens behind 8191 rows are 3072 steps: in BF16 beside 512 tokens 137.6 us, 131.7 with both.)
+constexpr int kAside = 2048;
+
 // How a kernel is launched. Sequences with least .. most query rows per cache head, in blocks of `rows` = 2^rows_log; steps of
 // `step` rows; items: chunks of all blocks, at most; cut: there may be several chunks of a block
 struct PageShape {
@@ -1056,8 +1061,10 @@ Shapes shapes(const PageAttnArgs& a) {
   const int seqs = std::min(a.c.batch, a.N), expected = std::min(a.max_new, a.N);
   const long rows = long(expected) * a.group;
   const long most = std::min<long>(std::max(a.max_len, 0) + long(expected), a.c.cap);
-  // One kernel for all where it is what the expected number of tokens asks for, or where there is one sequence
-  const bool use_wide = rows > kFew, use_few = !use_wide || (a.c.batch > 1 && a.N > 1);
+  // One kernel for all where it is what the expected number of tokens asks for, where there is one sequence, or where the
+  // others' steps take the wide kernel less time than a second launch
+  const long aside = (seqs - 1) * ((most + kWideStep - 1) / kWideStep) * a.slots;
+  const bool use_wide = rows > kFew, use_few = !use_wide || aside > (a.act == SEQ_F32 ? kAside : 0);
   constexpr int kAll = 1 << 30;
   auto fill = [&](PageShape& y, bool use, int least, int limit, int step, int mt, int block) {
     y.least = use ? least : 1;
