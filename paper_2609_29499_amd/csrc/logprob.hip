@@ -6,12 +6,16 @@
 // thread has a maximum and sums of its own in float32 (some 500 terms); they meet in float64. (x c - m c, one instruction less,
 // loses all digits at small temperatures.)
 //
-// The largest: elements above a bound go to a list in LDS as 64-bit keys (the logit as an integer that keeps its order,
-// then the complement of the index: equal logits are in the order of their indices). The bound of the first 4096 elements is
-// the `top`-th largest of 64 groups' maxima, which at least `top` elements reach (some 44 for 32, 6 for 5). When the list has
-// grown by 64 it is cut to its first `top`, and the last of them is the new bound.
+// The largest: every wave keeps a list in LDS of the elements that reach a bound, without a barrier: the `top`-th largest of its
+// 64 lanes' maxima, which at least `top` elements reach (some 44 for 32), looked at again behind 1, 2, 4, .. tiles and where the list
+// is full. At the end what reaches the largest of the four bounds becomes 64-bit keys (the logit as an integer that keeps
+// its order, then the complement of the index: equal logits are in the order of their indices), and each is ranked against all. (One
+// list of the workgroup, cut to its first as it grew, has two barriers per tile: 2048 rows of 128256 BF16, top 1 / 5 / 32,
+// 154 / 157 / 182 us; this way 121 / 133 / 161; without alternatives 110.)
 //
-// Bound by memory: a row is read once. Few rows are cut into pieces whose records a second launch joins.
+// Bound by memory: a row is read once (float32: 2048 rows of 128256 with 20 alternatives 190 us, 5.5 TB/s), BF16 with many alternatives by
+// the instructions that enter elements into lists. Few rows are cut into pieces whose records a second launch joins: such that
+// there are 512 workgroups (513 x 32003 BF16 in one piece each 30.6 us, cut in two for 1024 workgroups 41).
 #include <algorithm>
 #include <cmath>
 
@@ -23,9 +27,10 @@ namespace {
 
 constexpr int kPer = 16;               // elements of a thread and tile
 constexpr int kTile = kBlock * kPer;
-constexpr int kGrown = 64;             // keys that the list may grow by before it is cut to its first
+constexpr int kGrown = 96;             // elements that a wave's list may hold beyond `top` before it is cut
 constexpr int kLimit = 256;            // keys that are ranked by comparing each with each: one per thread
-constexpr int kKeys = kTopMax + kGrown + kTile;        // the list has room for a whole tile more
+constexpr int kKeys = 4192;            // of the join's list
+constexpr int kWaveKeys = kTopMax + kGrown + kWave * kPer + 8; // a wave's list has room for its next elements, all of them
 constexpr int kTarget = 512;           // workgroups aimed at
 constexpr int kPieces = kKeys / kTopMax;               // of a row at most: the join's list holds all their keys
 
@@ -109,6 +114,72 @@ __device__ __forceinline__ int rank_list(List& z, int top) {
   return out;
 }
 
+// The least number above x (finite, or the largest)
+__device__ __forceinline__ float above(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return __uint_as_float(u & 0x80000000u ? u - 1 : u + 1);
+}
+// what lanes have written to LDS is what other lanes of the wave read
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ int lanes_before(unsigned long long who) {
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0));
+}
+// The top-th largest of a wave's 64 values g: that many lanes' reach it. z: 64 values of LDS.
+__device__ __forceinline__ float nth_of_lanes(float g, int top, float* z, int lane) {
+  if (top == 1) return wave_max(g);
+  z[lane] = g;
+  wave_sync();
+  int larger = 0;
+#pragma unroll
+  for (int j = 0; j < kWave; j += 4) {
+    const float4 q = *reinterpret_cast<const float4*>(&z[j]);
+    larger += (q.x > g) + (q.y > g) + (q.z > g) + (q.w > g);
+  }
+  wave_sync();
+  return -wave_max(larger < top ? -g : -INFINITY);
+}
+// A wave's candidates, as they come: logits and indexes
+struct Found {
+  float x[kWaveKeys];
+  int i[kWaveKeys];
+};
+// Those that `stays` says true of to the front. Returns their number.
+template <class Pred>
+__device__ __forceinline__ int keep(Found& z, int n, int lane, Pred stays) {
+  int kept = 0;
+  wave_sync();
+  for (int k = 0; k < n; k += kWave) {
+    const bool in = k + lane < n;
+    const float x = in ? z.x[k + lane] : 0.0f;
+    const int i = in ? z.i[k + lane] : 0;
+    const unsigned long long who = __ballot(in && stays(x, i));
+    wave_sync();
+    if ((who >> lane) & 1) {
+      z.x[kept + lanes_before(who)] = x;
+      z.i[kept + lanes_before(who)] = i;
+    }
+    kept += __popcll(who);
+    wave_sync();
+  }
+  return kept;
+}
+// The top-th largest of a wave's n keys (n >= top), bit by bit: the largest value that `top` keys reach
+__device__ __forceinline__ unsigned long long nth_key(const Found& z, int n, int top, int lane) {
+  unsigned long long at = 0;
+  wave_sync();
+  for (int bit = 63; bit >= 0; --bit) {
+    const unsigned long long with = at | 1ull << bit;
+    int reach = 0;
+    for (int k = lane; k - lane < n; k += kWave) reach += __popcll(__ballot(k < n && key_of(z.x[min(k, n - 1)], z.i[min(k, n - 1)]) >= with));
+    if (reach >= top) at = with;
+  }
+  return at;
+}
+
 // Of a row (or a piece of it): sums under the maximum m, and elements that come before the token
 struct Record {
   double s, w;
@@ -144,14 +215,12 @@ __device__ __forceinline__ bool token_logit(const LogprobArgs& a, int row, int t
   x = fminf(fmaxf(x, -a.lim), a.lim);
   return true;
 }
-// Results of a row from its joined record; keys: `n` of them in order. Of one wave.
-__device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Record& z, const unsigned long long* key, int n) {
+// Results of a row from its joined record; xt: the token's logit (there: it has one); keys: `n` of them in order. Of one wave.
+__device__ __forceinline__ void finish(const LogprobArgs& a, int row, const Record& z, bool there, float xt, const unsigned long long* key, int n) {
   const int tid = threadIdx.x;
   const Scale lp(a, z);
   if (tid == 0) {
-    float x;
-    const bool there = token_logit(a, row, a.tokens[row], x);
-    a.logprob[row] = there ? lp(x) : 0.0f;
+    a.logprob[row] = there ? lp(xt) : 0.0f;
     if (a.rank) a.rank[row] = there ? z.before : -1;
     if (a.entropy) a.entropy[row] = z.m <= -a.lim ? 0.0f : float((lp.log_s - z.w / z.s) * 0.693147180559945309417);
   }
@@ -173,8 +242,11 @@ template <bool F32, bool TOP>
 __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int per) {
   constexpr int RAW = F32 ? 16 : 8;    // words of a tile's elements per thread
   constexpr int AHEAD = F32 ? 1 : 2;   // tiles on their way: 16 words either way
-  __shared__ List z;
-  __shared__ __align__(16) float s_group[kWave];
+  __shared__ __align__(16) Found s_found[TOP ? 4 : 1];
+  __shared__ unsigned long long s_best[kTopMax];
+  __shared__ __align__(16) float s_group[TOP ? 4 : 1][kWave];
+  __shared__ float s_bound[4];
+  __shared__ int s_n;
   __shared__ Sums s_sums[4];
   __shared__ int s_before[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -183,7 +255,9 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
     const int first = blockIdx.x * per * kTile, end = int(min(long(a.V), long(first) + long(per) * kTile));
     // element j of this thread in a tile
     auto index = [&](int tile, int j) {
-      return tile + kTile > end ? tile + j * kBlock + tid : F32 ? tile + (j >> 2) * 4 * kBlock + 4 * tid + (j & 3) : tile + (j >> 3) * 8 * kBlock + 8 * tid + (j & 7);
+      const bool whole = tile + kTile <= end;
+      constexpr int W = F32 ? 4 : 8;
+      return tile + (whole ? W * tid : tid) + (whole ? j / W * W * kBlock + j % W : j * kBlock);
     };
     auto load = [&](int tile, uint32_t (&v)[RAW]) __attribute__((always_inline)) {
       if (tile + kTile <= end) {
@@ -207,12 +281,13 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
     for (int k = 0; k < AHEAD; ++k) load(first + k * kTile, raw[k]);
     const int token = a.tokens[row];
     float xt = INFINITY;               // (padding: nothing comes before it)
-    token_logit(a, row, token, xt);
+    const bool there = token_logit(a, row, token, xt);
     Sums sum{-INFINITY, 0.0f, 0.0f};
     int before = 0, n = 0;
-    float bound = -a.lim;              // elements above it enter the list
+    Found& found = s_found[TOP ? wave : 0];
+    float bound = above(-a.lim);       // elements from it on enter the wave's list
+    float g = -a.lim;                  // the `top`-th largest of its lanes' maxima when last looked at
     __syncthreads();                   // (the row before has been read)
-    if (tid == 0) z.count = 0;
     for (int tile = first; tile < end; tile += kTile) {
       float x[kPer];
       if constexpr (F32) {
@@ -267,55 +342,45 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
         for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt || (x[j] == xt && index(tile, j) < token)));
       }
       if constexpr (TOP) {
-        bool least = false;            // the bound itself is enough
-        if (tile == first) {
-          float g = top;
-          g = fmaxf(g, dpp<kQuadXor1>(g));
-          g = fmaxf(g, dpp<kQuadXor2>(g));
-          if ((lane & 3) == 0) s_group[tid >> 2] = g;
-          __syncthreads();
-          g = s_group[lane];           // 64 groups' maxima, and those that are larger
-          if (a.top > 1) {
-            int larger = 0;
-#pragma unroll
-            for (int j = 0; j < kWave; j += 4) {
-              const float4 q = *reinterpret_cast<const float4*>(&s_group[j]);
-              larger += (q.x > g) + (q.y > g) + (q.z > g) + (q.w > g);
-            }
-            bound = -wave_max(larger < a.top ? -g : -INFINITY);
-          } else {
-            bound = wave_max(g);
-          }
-          least = bound > -a.lim;
+        // The `top`-th largest of the lanes' maxima so far: that many elements reach it, and later ones lose to equal ones.
+        // Raised behind 1, 2, 4, .. tiles
+        float from = bound;
+        const int k = (tile - first) / kTile;
+        if ((k & (k + 1)) == 0) {
+          g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
+          from = fmaxf(from, g);
+          if (g > -a.lim) bound = fmaxf(bound, above(g));
         }
-        if (__ballot(top > bound || (least && top == bound))) {
-          unsigned long long who[kPer];
-          int found = 0;
+        if (__ballot(top >= from)) {
 #pragma unroll
           for (int j = 0; j < kPer; ++j) {
-            who[j] = least ? __ballot(x[j] >= bound) : __ballot(x[j] > bound);
-            found += __popcll(who[j]);
-          }
-          int at = 0;
-          if (lane == 0) at = atomicAdd(&z.count, found);
-          at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            if (who[j]) {
-              if ((who[j] >> lane) & 1)
-                z.key[at + __builtin_amdgcn_mbcnt_hi(uint32_t(who[j] >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(who[j]), 0))] = key_of(x[j], index(tile, j));
-              at += __popcll(who[j]);
+            const unsigned long long who = __ballot(x[j] >= from);
+            if (who) {
+              if (x[j] >= from) {
+                found.x[n + lanes_before(who)] = x[j];
+                found.i[n + lanes_before(who)] = index(tile, j);
+              }
+              n += __popcll(who);
             }
           }
         }
-        __syncthreads();
-        const int count = z.count;
-        __syncthreads();               // (read by all before the next tile adds to it)
-        if (count > a.top + kGrown || tile + kTile >= end) {
-          n = rank_list(z, a.top);
-          if (n == a.top) bound = fmaxf(bound, unordered(uint32_t(z.key[a.top - 1] >> 32)));
+        if (n > a.top + kGrown) {
+          g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
+          n = keep(found, n, lane, [&](float x, int) { return x >= g; });
+          if (g > -a.lim) bound = fmaxf(bound, above(g));
+        }
+        if (n > a.top + kGrown) {      // (many equal ones, or in few lanes)
+          const unsigned long long least = nth_key(found, n, a.top, lane);
+          n = keep(found, n, lane, [&](float x, int i) { return key_of(x, i) >= least; });
+          bound = fmaxf(bound, above(unordered(uint32_t(least >> 32))));
         }
       }
+    }
+    if constexpr (TOP) {
+      const int tiles = (end - first + kTile - 1) / kTile;
+      if (tiles & (tiles - 1)) g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
+      if (lane == 0) s_bound[wave] = g;
+      if (tid == 0) s_n = 0;
     }
     // the workgroup's sums
     {
@@ -328,6 +393,34 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
       }
       __syncthreads();
     }
+    if constexpr (TOP) {
+      // what reaches the largest of the four waves' bounds, in one list (where the first wave's next elements had room)
+      constexpr int kUsed = kTopMax + kGrown;
+      static_assert((4 * kUsed + 1) * 8 <= (kWaveKeys - kUsed) * 4 && kUsed % 4 == 0);
+      unsigned long long* const s_all = reinterpret_cast<unsigned long long*>(&s_found[0].x[kUsed]);
+      const float g = fmaxf(fmaxf(s_bound[0], s_bound[1]), fmaxf(s_bound[2], s_bound[3]));
+      n = keep(found, n, lane, [&](float x, int) { return x >= g; });
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s_n, n);
+      at = __builtin_amdgcn_readfirstlane(at);
+      for (int i = lane; i < n; i += kWave) s_all[at + i] = key_of(found.x[i], found.i[i]);
+      __syncthreads();
+      n = s_n;
+      if (tid == 0) s_all[n] = 0;      // (pairs are compared)
+      __syncthreads();
+      for (int i = tid; (i & ~63) < n; i += kBlock) {
+        const unsigned long long mine = i < n ? s_all[i] : 0;
+        int larger = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; j += 2) {
+          const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(&s_all[j]);
+          larger += (q.x > mine) + (q.y > mine);
+        }
+        if (i < n && larger < a.top) s_best[larger] = mine;
+      }
+      n = min(n, a.top);
+      __syncthreads();
+    }
     if (wave > 0) continue;
     Record rec{0.0, 0.0, -INFINITY, 0};
 #pragma unroll
@@ -335,11 +428,11 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
 #pragma unroll
     for (int i = 0; i < 4; ++i) add_to(rec, Record{double(s_sums[i].s), double(s_sums[i].w), s_sums[i].m, s_before[i]}, a.c);
     if (gridDim.x == 1) {
-      finish(a, row, rec, z.key, n);
+      finish(a, row, rec, there, xt, s_best, n);
     } else {
       const size_t at = size_t(row) * gridDim.x + blockIdx.x;
       if (tid == 0) records(a)[at] = rec;
-      if (TOP && tid < a.top) keys(a, gridDim.x)[at * a.top + tid] = tid < n ? z.key[tid] : 0;
+      if (TOP && tid < a.top) keys(a, gridDim.x)[at * a.top + tid] = tid < n ? s_best[tid] : 0;
     }
   }
 }
@@ -399,11 +492,14 @@ __global__ __launch_bounds__(kBlock) void logprob_join_kernel(LogprobArgs a, int
     put_mean(a, b, sum, n);
     return;
   }
+  float xt = 0.0f;                     // (asked for before the keys are ranked)
+  const bool there = token_logit(a, row, a.tokens[row], xt);
   const unsigned long long* from = keys(a, pieces) + size_t(row) * pieces * a.top;
   // What lies below a key that `top` keys reach is out: the largest of the pieces' last keys is one, and, the j-th keys of the
-  // pieces being taken, that of them which ceil(top / j) reach (j = 1 for as many pieces as alternatives)
+  // pieces being taken, that of them which ceil(top / j) reach: half of the pieces' (of 32 pieces of 32 keys some 54 stay; with
+  // j = 1 it was the least of the pieces' largest, which 256 keys and more may reach)
   unsigned long long least = 1;
-  const int j = (a.top + pieces - 1) / pieces;
+  const int j = max(1, min(a.top, (2 * a.top + pieces - 1) / pieces));
   if (tid < pieces) {
     s_rec[tid] = records(a)[size_t(row) * pieces + tid];
     if (a.top > 0) least = max(least, from[tid * a.top + a.top - 1]);
@@ -435,7 +531,7 @@ __global__ __launch_bounds__(kBlock) void logprob_join_kernel(LogprobArgs a, int
   }
   int n = 0;
   if (a.top > 0) n = rank_list(z, a.top);
-  if (tid < kWave) finish(a, row, join(a, s_rec, pieces), z.key, n);
+  if (tid < kWave) finish(a, row, join(a, s_rec, pieces), there, xt, z.key, n);
 }
 
 // Mean log probability of the rows of a sequence that have a token (0 where none has): a workgroup each.

@@ -92,6 +92,29 @@ def test_orders_and_ties(V, R, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("R", [1, 520])
+def test_largest_logits_in_few_places(R, kind):
+    """All large logits where one thread, one wave or one tile reads them, in both orders, and rows of one value but for these: lists
+    that fill up again and again, for rows in one piece and in many."""
+    flush(f"case few places {R} {kind}")
+    V = 40000
+    i = torch.arange(V)
+    rows = [torch.where(i % 256 == 7, i / 64.0, -5.0), torch.where(i % 256 == 7, -i / 64.0, -900.0),
+            torch.where((i // 4) % 256 < 8, i % 97 / 8.0, 0.0), torch.where(i // 4096 == 3, 2.0, 1.0), torch.where(i % 1024 == 9, 1.0, 0.0),
+            torch.where(i > V - 50, 3.0, -1.0), (i // 3000).float(), -(i // 3000).float()]
+    x = torch.stack([rows[k % len(rows)] for k in range(R)] if R > 1 else rows).to(DTYPES[kind])
+    for k in range(len(rows)):
+        one = x[k:k + 1] if R == 1 else x
+        tokens = torch.randint(0, V, (one.shape[0],), generator=gen(k)).to(torch.int32)
+        for top in (1, 5, 32):
+            got = S.token_logprobs(one.cuda(), tokens.cuda(), top)
+            torch.cuda.synchronize()
+            check(got, one, tokens, 1.0, top, rows=None if R == 1 else range(len(rows)))
+        if R > 1:
+            break
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [5, 6000])
 def test_rows_with_infinities_and_nan(V, kind):
     flush(f"case infinities {V} {kind}")
