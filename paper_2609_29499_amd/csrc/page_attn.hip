@@ -23,6 +23,12 @@
 // from the lengths on the device (no host knows them) such that there are about two workgroups per CU. A block of one
 // chunk is written at once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which
 // another launch joins in chunk order.
+//
+// What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 77 us and a join of 5: 5.6 TB/s; 32 tokens over 8190
+// INT8 rows, 79: 4.3 TB/s, with a common prefix read by each sequence); one token is latency (8.5 us and a join of 4.5 for
+// 2047 rows). The second, matrix products and the softmax's vector instructions, of which each waits for the other:
+// a prompt of 8192 tokens x 64 heads in BF16 1302 us, 844 TFLOP/s of visible pairs, 68 % of what a library product of 8192^3
+// reaches (1243); 512 tokens behind 8191 INT8 rows 114 us, 620 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -37,12 +43,16 @@ constexpr int kStep = 32;              // cache rows per step
 constexpr int kWideStep = 64;          // and in the wide kernel
 constexpr int kMinSteps = 4;           // steps of a chunk at least, and its granule: one per wave
 constexpr float kSlack = 8.0f;         // powers of two a score may pass the running maximum by
-constexpr int kTarget = 512;           // workgroups aimed at: two per CU
-constexpr int kFew = 32;               // query rows of a sequence and cache head that the first kernel serves
+// workgroups aimed at: two per CU. (512 / 1024 / 2048, first version: 4 tokens x 64 heads over 65,530 rows 82 / 90 / 106 us, 32 tokens over
+// 8190 rows 88 / 89 / 103, 512 tokens behind 8191 rows 153 / 163 / 177: more of them leave more records to join)
+constexpr int kTarget = 512;
+// query rows of a sequence and cache head that the first kernel serves: what a wave's registers hold. (Serving all, it took 262 us for 512
+// tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 131 and 1302)
+constexpr int kFew = 32;
 
 // Steps of 64 cache rows, in all slots, of short sequences that the wide kernel takes beside its own, in place of a second launch:
 // for float32, whose bits are the same in both kernels. (3 x 37 tokens x 24 heads behind 1001 rows: 16.5 us, 19.3 with both
-// kernels. Three single tokens behind 8191 rows are 3072 steps: in BF16 beside 512 tokens 137.6 us, 131.7 with both.)
+// kernels. Three single tokens behind 8191 rows, 384 steps in each of 8 slots: in BF16 beside 512 tokens 137.6 us, 131.7 with both.)
 constexpr int kAside = 2048;
 
 // How a kernel is launched. Sequences with least .. most query rows per cache head, in blocks of `rows` = 2^rows_log; steps of
