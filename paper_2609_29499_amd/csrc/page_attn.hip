@@ -16,7 +16,7 @@
 //
 // Two kernels. Up to 32 query rows of a sequence and cache head (page_attn_kernel): a wave keeps all of them and walks every
 // fourth step straight from memory in the operands' layout, the next step's loads in flight. More
-// (page_attn_wide_kernel): blocks of 64 or 128 rows are dealt to the four waves, which share steps of 64 cache rows
+// (page_attn_wide_kernel): blocks of 64 to 256 rows are dealt to four or eight waves, which share steps of 64 cache rows
 // through LDS (below).
 //
 // A workgroup takes one chunk of the cache rows of one block of query rows and cache head. Chunks have equal lengths, found
@@ -27,7 +27,7 @@
 // What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 77 us and a join of 5: 5.6 TB/s; 32 tokens over 8190
 // INT8 rows, 79: 4.3 TB/s, with a common prefix read by each sequence); one token is latency (8.5 us and a join of 4.5 for
 // 2047 rows). The second, matrix products and the softmax's vector instructions, of which each waits for the other:
-// a prompt of 8192 tokens x 64 heads in BF16 1302 us, 844 TFLOP/s of visible pairs, 68 % of what a library product of 8192^3
+// a prompt of 8192 tokens x 64 heads in BF16 1225 us, 898 TFLOP/s of visible pairs, 72 % of what a library product of 8192^3
 // reaches (1243); 512 tokens behind 8191 INT8 rows 114 us, 620 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
@@ -47,8 +47,13 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 // 8190 rows 88 / 89 / 103, 512 tokens behind 8191 rows 153 / 163 / 177: more of them leave more records to join)
 constexpr int kTarget = 512;
 // query rows of a sequence and cache head that the first kernel serves: what a wave's registers hold. (Serving all, it took 262 us for 512
-// tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 131 and 1302)
+// tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 130 and 1225)
 constexpr int kFew = 32;
+
+// Query rows from which eight waves, one workgroup per CU in place of two, share a step in LDS: bringing it (V to FP16 above all) takes
+// each of them half the instructions. (A prompt of 8192 tokens x 64 heads 1299 -> 1221 us, 512 tokens behind 8191 rows 131.3 -> 129.2;
+// for a block or less there are fewer workgroups: 30 tokens or so 12.8 -> 14.4)
+constexpr int kEight = 512;
 
 // Steps of 64 cache rows, in all slots, of short sequences that the wide kernel takes beside its own, in place of a second launch:
 // for float32, whose bits are the same in both kernels. (3 x 37 tokens x 24 heads behind 1001 rows: 16.5 us, 19.3 with both
@@ -196,7 +201,7 @@ __device__ __forceinline__ void note_tokens(const PageAttnArgs& a, const PageSha
   const int r0 = p.block << y.rows_log, blocks = (p.n * a.group + y.rows - 1) >> y.rows_log;
   const int t0 = quot(r0 + a.group - 1, a.group), t1 = min(p.n, quot(r0 + y.rows + a.group - 1, a.group));
   const int4 note = make_int4(p.b, p.item - (blocks - 1 - p.block) * p.nch, p.nch, 0);
-  for (int t = t0 + int(threadIdx.x); t < t1; t += kBlock) token_notes(a)[p.first + t] = note;
+  for (int t = t0 + int(threadIdx.x); t < t1; t += int(blockDim.x)) token_notes(a)[p.first + t] = note;
 }
 
 template <int DH, int TYPE>
@@ -565,14 +570,14 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 
 // ---- more query rows
 //
-// A workgroup's four waves hold MT tiles of 16 query rows each. Steps of 64 cache rows go through LDS, two of them in turn: all
+// A workgroup's four or eight waves (NW) hold MT tiles of 16 query rows each. Steps of 64 cache rows go through LDS, two of them in turn: all
 // threads bring K and V of the next one (16 bytes a thread and row piece; loads in flight while the present step is computed),
 // widen 8 bits and write rows of 16-bit values; chunks of 16 bytes change places by the row, so that no reader meets a
 // bank twice. K rows are read as they lie (operand A of S^T = K Q^T); V is turned on its way from LDS
 // (ds_read_b64_tr_b16: four rows of 16 dimensions, one per lane), cache rows 4 c .. 4 c + 3 of two tiles being the eight of
 // operand B that meet the lane's P. So P stays in registers.
 //   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries: P is one FP16 term: 11 bits, an eighth of the
-// output's rounding, and half the matrix products of two BF16 terms (8192 tokens x 64 heads 1302 us, 1573 with two terms). V is
+// output's rounding, and half the matrix products of two BF16 terms (with four waves, 8192 tokens x 64 heads 1302 us, 1573 with two terms). V is
 // FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below the largest scale seen)
 // goes into P, below 2; BF16 values are multiplied by a power of two that brings the largest seen below 2^15 (lowered when a
 // step has a larger one). P is at most 2^kWideSlack, and lifted by 2^kLift to just below FP16's end, so that half a step of its
@@ -618,15 +623,15 @@ __device__ __forceinline__ float scale_for(float top) {
   return __uint_as_float(uint32_t(min(127 + 11 + 127 - e, 253)) << 23);
 }
 
-template <int DH, int TYPE, int ACT, int MT>
-__global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs a, PageShape y) {
+template <int DH, int TYPE, int ACT, int MT, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnArgs a, PageShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
-  constexpr int NKC = DH / 32, NDT = DH / 16, RB = 64 * MT;
+  constexpr int NKC = DH / 32, NDT = DH / 16, RB = 16 * NW * MT;
   constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 1;
   constexpr bool HALF = ACT == SEQ_BF16;               // P and V in FP16
   constexpr int CPR = DH / 8;          // chunks (eight 16-bit values) of a row in LDS
   constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a row as loaded
-  constexpr int RPI = kBlock / PPR;    // rows per load of the workgroup
+  constexpr int RPI = NW * kWave / PPR;    // rows per load of the workgroup
   constexpr int NL = kWideStep / RPI;  // loads of K, and of V, per thread and step
   constexpr uint32_t row_bytes = DH * ES;
   constexpr int LDO = DH + 4;
@@ -634,10 +639,10 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
     struct {
       uint4 k[kWideStep][CPR], v[kWideStep][CPR];
     } step[2];
-    float o[4][16][LDO];
+    float o[NW][16][LDO];
   };
   __shared__ Lds z;
-  __shared__ float s_top[4];
+  __shared__ float s_top[NW];
   __shared__ uint32_t s_raise[3];      // a step's largest finite V where one does not fit (as its bits)
   __shared__ int s_odd;                // a row that some query rows do not see holds something not finite
 
@@ -785,7 +790,10 @@ __global__ __launch_bounds__(kBlock, 2) void page_attn_wide_kernel(PageAttnArgs 
     const float top = top_v();
     if (lane == 0) s_top[wave] = top;
     __syncthreads();
-    mul = scale_for(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])));
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) most = fmaxf(most, s_top[k]);
+    mul = scale_for(most);
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) arrived(qf[mt]);
@@ -1082,7 +1090,7 @@ Shapes shapes(const PageAttnArgs& a) {
     y.mt = mt; y.step = step; y.rows = block; y.rows_log = 31 - __builtin_clz(block);
     if (!use) return;
     const long blocks = std::min<long>(long(a.N) * a.group, limit == kFew ? long(seqs) * kFew : kAll) / block + seqs;    // of all sequences, at most
-    const int quota = (kTarget + a.slots - 1) / a.slots;
+    const int quota = ((block == 256 ? kTarget / 2 : kTarget) + a.slots - 1) / a.slots;      // (of eight waves: half)
     // (the join looks at every token's rows)
     y.cut = blocks < quota && most > kMinSteps * step && long(a.N) * a.slots * a.group <= 1 << 17;
     y.items = int(std::max<long>(blocks, y.cut ? quota : 0));
@@ -1090,7 +1098,8 @@ Shapes shapes(const PageAttnArgs& a) {
   const int mt = rows > 16 && !use_wide ? 2 : 1;       // (beside the other kernel it has single tokens, mostly)
   fill(z.few, use_few, 1, use_wide ? kFew : kAll, kStep, mt, 16 * mt);
   const int wt = a.act == SEQ_BF16 ? 2 : 1;
-  fill(z.wide, use_wide, use_few ? kFew + 1 : 1, kAll, kWideStep, wt, 64 * wt);
+  const int waves = a.act == SEQ_BF16 && a.c.dh == 128 && rows >= kEight ? 8 : 4;
+  fill(z.wide, use_wide, use_few ? kFew + 1 : 1, kAll, kWideStep, wt, 16 * waves * wt);
   z.floats = z.few.cut || z.wide.cut ? (size_t(a.N) * 4 + 63) / 64 * 64 : 0;
   for (PageShape* y : {&z.few, &z.wide}) {
     y->ws = z.floats;
@@ -1105,12 +1114,14 @@ size_t page_attn_workspace_bytes(const PageAttnArgs& a) { return shapes(a).float
 
 hipError_t launch_page_attn(const PageAttnArgs& a, hipStream_t s) {
   const Shapes z = shapes(a);
-#define ATTN(KERNEL, Y, DH, TYPE, ACT, MT) hipLaunchKernelGGL((KERNEL<DH, TYPE, ACT, MT>), dim3(a.slots, std::min(Y.items, kItems), (Y.items + kItems - 1) / kItems), dim3(kBlock), 0, s, a, Y)
+#define ATTN(KERNEL, Y, THREADS, ...) hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), dim3(a.slots, std::min(Y.items, kItems), (Y.items + kItems - 1) / kItems), dim3(THREADS), 0, s, a, Y)
 #define ATTN_MT(DH, TYPE, ACT)                                                                      \
   do {                                                                                              \
-    if (z.wide.items) ATTN(page_attn_wide_kernel, z.wide, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1)); \
-    if (z.few.items && z.few.mt == 1) ATTN(page_attn_kernel, z.few, DH, TYPE, ACT, 1);              \
-    else if (z.few.items) ATTN(page_attn_kernel, z.few, DH, TYPE, ACT, 2);                          \
+    constexpr bool EIGHT = DH == 128 && ACT == SEQ_BF16;                                            \
+    if (EIGHT && z.wide.items && z.wide.rows == 256) ATTN(page_attn_wide_kernel, z.wide, 8 * kWave, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1), (EIGHT ? 8 : 4)); \
+    else if (z.wide.items) ATTN(page_attn_wide_kernel, z.wide, 4 * kWave, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1), 4); \
+    if (z.few.items && z.few.mt == 1) ATTN(page_attn_kernel, z.few, kBlock, DH, TYPE, ACT, 1);      \
+    else if (z.few.items) ATTN(page_attn_kernel, z.few, kBlock, DH, TYPE, ACT, 2);                  \
   } while (0)
 #define ATTN_TYPE(DH, ACT)                                      \
   do {                                                          \

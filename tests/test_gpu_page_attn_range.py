@@ -114,6 +114,52 @@ def test_large_values_under_small_probabilities(kind, act, n, last):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("lens,n,hq,P", [([33, 0], [150, 64], 8, 16), ([2000, 700, 5], [130, 3, 65], 8, 64), ([0], [513], 1, 128), ([4001], [100], 7, 32)])
+def test_large_blocks_of_query_rows(kind, lens, n, hq, P):
+    """Heads of 128 with 512 query rows and more of a sequence: whole and partial blocks of 256, in one chunk and in several. Values
+    that grow along the cache by 20 powers of two; then NaN and infinities in the last tokens' rows, which earlier ones do not see."""
+    flush(f"case large blocks {kind} {lens} {n} {hq} {P}")
+    c, rows = paged(lens, n, 1, P, 128, kind, 33)
+    J = c.table.shape[1]
+    f = torch.exp2(torch.linspace(-10, 10, J).round())
+    for b in range(len(lens)):
+        for j in range(J):
+            page = int(c.table[b, j])
+            if page < 0:
+                continue
+            if kind == "bf16":
+                c.v[0, page] *= f[j].item()
+            else:
+                c.v_scale[0, page] *= f[j].item()
+            rows[0][b][1][j * P:(j + 1) * P] *= f[j].item()
+    q = randn((sum(n), hq, 128), torch.bfloat16, 34)
+    at = starts(n).cuda()
+    got = S.page_attention(c, 0, q.cuda(), at)
+    torch.cuda.synchronize()
+    check(got.double().cpu().numpy(), q.double().numpy(), rows[0], lens, n, P, "bf16", 128 ** -0.5,
+          some=lambda m: [0, 1, 31, 32, 63, 64, m // 2, m - 2, m - 1])
+    if kind == "int8":
+        return
+    t = 0
+    seen = []
+    for b, (L, m) in enumerate(zip(lens, n)):
+        r = L + m - 1                   # the last token's own row
+        page = int(c.table[b, r // P])
+        if kind == "bf16":
+            c.v[0, page, :, r % P, ::5], c.v[0, page, :, r % P, 1::5] = math.nan, math.inf
+        else:
+            c.v.view(torch.uint8)[0, page, :, r % P] = 0x7f
+        seen.append(torch.arange(t, t + m - 1))
+        t += m
+    seen = torch.cat(seen)
+    odd = S.page_attention(c, 0, q.cuda(), at)
+    torch.cuda.synchronize()
+    assert torch.equal(odd[seen], got[seen])
+    last = torch.tensor(n).cumsum(0) - 1
+    assert not torch.isfinite(odd[last][..., ::5]).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
 @pytest.mark.parametrize("n,hq,dh", [(40, 8, 64), (40, 8, 128), (64, 1, 64), (9, 8, 128)])
 def test_few_rows_keep_the_bits_of_the_probabilities(kind, n, hq, dh):
     """Sums that are often far smaller than their terms: the bound goes by the terms."""
