@@ -24,11 +24,11 @@
 // chunk is written at once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which
 // another launch joins in chunk order.
 //
-// What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 77 us and a join of 5: 5.6 TB/s; 32 tokens over 8190
-// INT8 rows, 79: 4.3 TB/s, with a common prefix read by each sequence); one token is latency (8.5 us and a join of 4.5 for
+// What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 75 us and a join of 5: 5.8 TB/s; 32 tokens over 8190
+// INT8 rows, a common prefix of 1024 read by each, 78: 5.2 TB/s); one token is latency (8.6 us and a join of 4.7 for
 // 2047 rows). The second, matrix products and the softmax's vector instructions, of which each waits for the other:
 // a prompt of 8192 tokens x 64 heads in BF16 1225 us, 898 TFLOP/s of visible pairs, 72 % of what a library product of 8192^3
-// reaches (1243); 512 tokens behind 8191 INT8 rows 114 us, 620 TFLOP/s.
+// reaches (1243); 512 tokens behind 8191 INT8 rows 108 us, 660 TFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
