@@ -674,10 +674,10 @@ tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const in
 /* Causal attention of packed tokens (their rows already appended): token i of a sequence sees its rows 0..len + i that have
  * pages, with scores scale * q . k. q, out: rows of n_q_heads heads (a multiple of n_kv_heads, at most 8 per KV head; query head
  * h reads KV head h / (n_q_heads / n_kv_heads)) of act_type; out must not overlap q or the cache. Outputs of absent tokens and of
- * tokens that see no row are zeros, and what unseen rows hold (NaN, infinities) reaches no output (a page's scale belongs to all
- * of its rows). TASP_BF16: q exact, sums in float32, probabilities in 16 bits, or, with more than 32 query rows of a sequence and
- * cache head (batch 1: of n_tokens tokens), in 11 bits, and up to 2^-34 of the largest |v| of each row; TASP_F32: everything to 24 bits. The ends
- * of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
+ * tokens that see no row are zeros, and what unseen rows hold (NaN, infinities, values of any size) reaches no output (a page's scale
+ * belongs to all of its rows). TASP_BF16: q exact, sums in float32, probabilities in 16 bits, or, with more than 32 query rows of a
+ * sequence and cache head (batch 1: of n_tokens tokens), in 11 to 16 bits, and up to 2^-34 of the largest |v| seen lost per row;
+ * TASP_F32: everything to 24 bits. The ends of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
  * that are expected (max_len 0..max_pages * page_rows, max_new at least 1): they size launches and workspace; more is served too.
  * workspace: device, 256-byte aligned, at least tasp_page_attention_workspace_bytes for the same cache shape, n_q_heads,
  * n_tokens, max_len and max_new; its contents need no clearing; calls that overlap need one each. Stream-ordered,

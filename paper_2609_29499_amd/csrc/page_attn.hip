@@ -576,13 +576,16 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 // bank twice. K rows are read as they lie (operand A of S^T = K Q^T); V is turned on its way from LDS
 // (ds_read_b64_tr_b16: four rows of 16 dimensions, one per lane), cache rows 4 c .. 4 c + 3 of two tiles being the eight of
 // operand B that meet the lane's P. So P stays in registers.
-//   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries: P is one FP16 term: 11 bits, an eighth of the
-// output's rounding, and half the matrix products of two BF16 terms (with four waves, 8192 tokens x 64 heads 1302 us, 1573 with two terms). V is
-// FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below the largest scale seen)
-// goes into P, below 2; BF16 values are multiplied by a power of two that brings the largest seen below 2^15 (lowered when a
-// step has a larger one). P is at most 2^kWideSlack, and lifted by 2^kLift to just below FP16's end, so that half a step of its
-// least numbers is 2^-35 of the row with the running maximum; the lift is taken out of the sums at the end. (Slack of
-// 2: 1320 us, of 8: 1303.) Lost at most: 2^-35 of the largest |v| for each row, and 2^-36 for V's own least numbers.
+//   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries, steps that all of the block's tokens see: P is one FP16
+// term: 11 bits, an eighth of the output's rounding, and half the matrix products of two BF16 terms (with four waves, 8192 tokens x 64
+// heads 1302 us, 1573 with two terms). V is FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below
+// the largest scale seen) goes into P, below 2; BF16 values are multiplied by a power of two that brings the largest seen
+// below 2^15 (lowered when a step has a larger one). P is at most 2^kWideSlack, and lifted by 2^kLift to just below FP16's end, so that
+// half a step of its least numbers is 2^-35 of the row with the running maximum. (Slack of 2: 1320 us, of 8: 1303.) Lost at most, for
+// each row: 2^-35 of the largest |v|, and 2^-36 for V's own least numbers.
+//   The units of V are the block's, so nothing that some of its tokens do not see may go into them: BF16 queries' last steps,
+// which hold such rows, have P in two BF16 terms and V as it is, as in the other kernel. Lift and units are taken out of the sums
+// in front of them.
 constexpr float kWideSlack = 4.0f;     // in place of kSlack
 constexpr float kLift = 10.0f, kUnlift = 0x1p-10f;
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
@@ -627,8 +630,8 @@ template <int DH, int TYPE, int ACT, int MT, int NW>
 __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnArgs a, PageShape y) {
   constexpr int ES = TYPE == SEQ_BF16 ? 2 : 1;
   constexpr int NKC = DH / 32, NDT = DH / 16, RB = 16 * NW * MT;
-  constexpr int QT = ACT == SEQ_F32 ? 3 : 1, PT = ACT == SEQ_F32 ? 3 : 1;
-  constexpr bool HALF = ACT == SEQ_BF16;               // P and V in FP16
+  constexpr int QT = ACT == SEQ_F32 ? 3 : 1;
+  constexpr bool HALF = ACT == SEQ_BF16;               // P and V in FP16 in most steps
   constexpr int CPR = DH / 8;          // chunks (eight 16-bit values) of a row in LDS
   constexpr int PPR = DH * ES / 16;    // 16-byte pieces of a row as loaded
   constexpr int RPI = NW * kWave / PPR;    // rows per load of the workgroup
@@ -703,8 +706,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
   auto k_place = [](int row, int j) { return j ^ (DH == 128 ? row & 15 : row >> 1 & 7); };
   auto v_place = [](int row, int j) { return j ^ (DH == 128 ? 2 * (row & 7) : 2 * (row >> 1 & 3)); };
   float mul = 1.0f;                    // BF16: V's power of two
-  // V into buffer buf; returns the largest magnitude (BF16)
-  auto commit_v = [&](int buf) __attribute__((always_inline)) {
+  // V into buffer buf, as FP16 or BF16; returns the largest magnitude (BF16 as FP16)
+  auto commit_v = [&](int buf, auto f16_) __attribute__((always_inline)) {
+    constexpr bool F16 = decltype(f16_)::value;
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -713,7 +717,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if constexpr (!HALF) {
+          if constexpr (!F16) {
             w[e] = x.v[i][e];
             continue;
           }
@@ -725,7 +729,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
       } else {
         uint32_t w[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) HALF ? widen_f16<TYPE>(x.v[i][e], &w[2 * e]) : widen<TYPE>(x.v[i][e], &w[2 * e]);
+        for (int e = 0; e < 4; ++e) F16 ? widen_f16<TYPE>(x.v[i][e], &w[2 * e]) : widen<TYPE>(x.v[i][e], &w[2 * e]);
         z.step[buf].v[row][v_place(row, 2 * piece)] = make_uint4(w[0], w[1], w[2], w[3]);
         z.step[buf].v[row][v_place(row, 2 * piece + 1)] = make_uint4(w[4], w[5], w[6], w[7]);
       }
@@ -783,10 +787,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
 #pragma unroll
     for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  const int s_edge = min(s1, common / kWideStep);      // steps from it on hold rows that some tokens do not see
   float ref = 0.0f, inv_ref = 0.0f;    // 8 bits: the power of two that V's scales are divided by
   if (tid == 0) s_odd = 0;
   if (tid < 3) s_raise[tid] = 0;
-  if constexpr (TYPE == SEQ_BF16 && HALF) {
+  if (TYPE == SEQ_BF16 && HALF && p.s0 < s_edge) {
     const float top = top_v();
     if (lane == 0) s_top[wave] = top;
     __syncthreads();
@@ -818,7 +823,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
   // softmax has the vector unit): 512 tokens behind 8191 rows 129.6 us, 140.8 without.
   // One barrier per step: whoever writes a buffer has passed the barrier that followed its last use
   auto step = [&](int s, int buf, int turn, auto edge_) __attribute__((always_inline)) {
-    constexpr bool EDGE = decltype(edge_)::value;
+    constexpr bool EDGE = decltype(edge_)::value, F16 = HALF && !EDGE;
+    constexpr int PT = ACT == SEQ_F32 ? 3 : F16 ? 1 : 2;
     // A row that some query rows do not see must not reach them through 0 * inf: its non-finite values are left out
     // of the product, and added at the end to the outputs that see them
     if constexpr (EDGE && TYPE != SEQ_INT8) {
@@ -832,28 +838,28 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
     }
     __builtin_amdgcn_s_setprio(2);
     commit_k(buf);
-    const float top = commit_v(buf);
+    const float top = commit_v(buf, std::bool_constant<F16>{});
     __builtin_amdgcn_s_setprio(0);
-    if constexpr (TYPE == SEQ_BF16 && HALF) {
+    if constexpr (TYPE == SEQ_BF16 && F16) {
       if (__ballot(top >= 0x1p15f)) {                  // (an infinity too, each time)
         const float t = top_v();
         if (lane == 0) atomicMax(&s_raise[turn], __float_as_uint(t));
       }
     }
     __syncthreads();
-    if constexpr (TYPE == SEQ_BF16 && HALF) {
+    if constexpr (TYPE == SEQ_BF16 && F16) {
       if (tid == 0) s_raise[turn == 0 ? 2 : turn - 1] = 0;             // (the step after the next one's)
       const float most = __uint_as_float(__builtin_amdgcn_readfirstlane(s_raise[turn]));
       if (most * mul >= 0x1p15f) {
         const float to = scale_for(most);
         rescale(to / mul);
         mul = to;
-        commit_v(buf);
+        commit_v(buf, std::true_type{});
         __syncthreads();
       }
     }
     float ks[4], f[4], bias[4];
-    if constexpr (TYPE != SEQ_BF16 && HALF) {
+    if constexpr (TYPE != SEQ_BF16 && F16) {
       float most = 0.0f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) most = fmaxf(most, x.vs[t] < INFINITY ? x.vs[t] : 0.0f);
@@ -867,7 +873,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       ks[t] = x.ks[t]; bias[t] = x.bias[t];
-      f[t] = TYPE == SEQ_BF16 ? 1.0f : HALF ? x.vs[t] * inv_ref : x.vs[t];
+      f[t] = TYPE == SEQ_BF16 ? 1.0f : F16 ? x.vs[t] * inv_ref : x.vs[t];
     }
     // K's operands are read two tiles ahead of their products: at most eight reads are on their way
     const char* kz = reinterpret_cast<const char*>(&z.step[buf].k[0][0]);
@@ -927,7 +933,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
           for (int e = 0; e < NDT; ++e) o[mt][e][i] *= g;
         }
       }
-      const float low = (HALF ? kLift : 0.0f) - (m_run[mt] == -INFINITY ? 0.0f : m_run[mt]);
+      const float low = (F16 ? kLift : 0.0f) - (m_run[mt] == -INFINITY ? 0.0f : m_run[mt]);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         float v[4];
@@ -943,7 +949,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          if constexpr (HALF) pf[mt][0][t >> 1][2 * (t & 1) + e] = pack_f16(v[2 * e], v[2 * e + 1]);
+          if constexpr (F16) pf[mt][0][t >> 1][2 * (t & 1) + e] = pack_f16(v[2 * e], v[2 * e + 1]);
           else terms<PT>(v[2 * e], v[2 * e + 1], &pf[mt][0][t >> 1][2 * (t & 1) + e], 8);
         }
       }
@@ -961,24 +967,27 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
 #pragma unroll
         for (int k = 0; k < PT; ++k)
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) o[mt][e] = HALF ? mfma_f16(pf[mt][k][h], vf, o[mt][e]) : mfma(pf[mt][k][h], vf, o[mt][e]);
+          for (int mt = 0; mt < MT; ++mt) o[mt][e] = F16 ? mfma_f16(pf[mt][k][h], vf, o[mt][e]) : mfma(pf[mt][k][h], vf, o[mt][e]);
       }
   };
-  const int s_edge = min(s1, common / kWideStep);
   int s = p.s0, buf = 0, turn = 0;
   for (; s < s_edge; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::false_type{});
+  if constexpr (HALF) {
+    rescale((TYPE == SEQ_BF16 ? 1.0f / mul : ref) * kUnlift);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) l_run[mt] *= kUnlift;
+  }
   for (; s < s1; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::true_type{});
 
   // every wave holds its rows' results; through LDS, 16 rows at a time, they become whole rows
-  const float unit = !HALF ? 1.0f : (TYPE == SEQ_BF16 ? 1.0f / mul : ref) * kUnlift;
   __syncthreads();
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const float l_all = quad_sum(l_run[mt]) * (HALF ? kUnlift : 1.0f);
+    const float l_all = quad_sum(l_run[mt]);
 #pragma unroll
     for (int e = 0; e < NDT; ++e)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) z.o[wave][4 * c + i][16 * e + r] = o[mt][e][i] * unit;
+      for (int i = 0; i < 4; ++i) z.o[wave][4 * c + i][16 * e + r] = o[mt][e][i];
 #pragma unroll
     for (int k = 0; k < DH / 16; ++k) {
       const int in = (k * kWave + lane) / (DH / 4), d0 = 4 * (lane % (DH / 4));
