@@ -676,7 +676,8 @@ tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const in
  * h reads KV head h / (n_q_heads / n_kv_heads)) of act_type; out must not overlap q or the cache. Outputs of absent tokens and of
  * tokens that see no row are zeros, and what unseen rows hold (NaN, infinities, values of any size) reaches no output (a page's scale
  * belongs to all of its rows). TASP_BF16: q exact, sums in float32, probabilities in 16 bits, or, with more than 32 query rows of a
- * sequence and cache head (batch 1: of n_tokens tokens), in 11 to 16 bits, and up to 2^-34 of the largest |v| seen lost per row;
+ * sequence and cache head (batch 1: of n_tokens tokens), in 11 to 16 bits, and lost per row up to 2^-34 of the largest |v|
+ * seen (8-bit pages: 2^-30 of the row's own);
  * TASP_F32: everything to 24 bits. The ends of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
  * that are expected (max_len 0..max_pages * page_rows, max_new at least 1): they size launches and workspace; more is served too.
  * workspace: device, 256-byte aligned, at least tasp_page_attention_workspace_bytes for the same cache shape, n_q_heads,

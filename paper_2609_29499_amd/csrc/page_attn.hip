@@ -579,15 +579,18 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 //   Float32 queries: three BF16 terms of q and of P, as above. BF16 queries, steps that all of the block's tokens see: P is one FP16
 // term: 11 bits, an eighth of the output's rounding, and half the matrix products of two BF16 terms (with four waves, 8192 tokens x 64
 // heads 1302 us, 1573 with two terms). V is FP16 too: codes are exact, and the page's scale over a reference (the power of two at or below
-// the largest scale seen) goes into P, below 2; BF16 values are multiplied by a power of two that brings the largest seen
+// the largest scale seen) goes into P, from 2^-kSpread to 2; BF16 values are multiplied by a power of two that brings the largest seen
 // below 2^15 (lowered when a step has a larger one). P is at most 2^kWideSlack, and lifted by 2^kLift to just below FP16's end, so that
 // half a step of its least numbers is 2^-35 of the row with the running maximum. (Slack of 2: 1320 us, of 8: 1303.) Lost at most, for
-// each row: 2^-35 of the largest |v|, and 2^-36 for V's own least numbers.
+// each row: of BF16 values 2^-35 of the largest |v|, and 2^-36 for V's own least numbers; of 8 bits 2^-31 of the row's own |v|.
 //   The units of V are the block's, so nothing that some of its tokens do not see may go into them: BF16 queries' last steps,
-// which hold such rows, have P in two BF16 terms and V as it is, as in the other kernel. Lift and units are taken out of the sums
-// in front of them.
+// which hold such rows, and all steps from one on whose pages' scales are further apart than 2^kSpread (a page's scale need not be
+// reached by the rows that are left in it), have P in two BF16 terms and V as it is, as in the other kernel. Lift and units are
+// taken out of the sums in front of them.
 constexpr float kWideSlack = 4.0f;     // in place of kSlack
 constexpr float kLift = 10.0f, kUnlift = 0x1p-10f;
+constexpr uint32_t kSpread = 4;        // 8 bits: powers of two between a scale and the largest one
+constexpr uint32_t kRise = 16;         // and between the first largest one and a later one: what was added up before stays far above 2^-126
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
@@ -788,7 +791,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
     for (int i = 0; i < NDT; ++i) o[mt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   const int s_edge = min(s1, common / kWideStep);      // steps from it on hold rows that some tokens do not see
-  float ref = 0.0f, inv_ref = 0.0f;    // 8 bits: the power of two that V's scales are divided by
+  uint32_t ref = 0, ref0 = 0;          // 8 bits: the exponent of the power of two that V's scales are divided by (0: none yet), the first one
+  float inv_ref = 0.0f;
   if (tid == 0) s_odd = 0;
   if (tid < 3) s_raise[tid] = 0;
   if (TYPE == SEQ_BF16 && HALF && p.s0 < s_edge) {
@@ -811,6 +815,27 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
       for (int e = 0; e < NDT; ++e)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[mt][e][i] *= f;
+  };
+  // 8 bits: whether the scales of the step that has been loaded are near enough to those before and to each other; ref then
+  // covers them
+  auto near = [&]() __attribute__((always_inline)) {
+    uint32_t hi = 0, lo = 0xffffffffu; // (integers of the same order; a scale of 0 has no say)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t u = __builtin_amdgcn_readfirstlane(__float_as_uint(x.vs[t]));
+      hi = max(hi, u);
+      lo = min(lo, u - 1);
+    }
+    if (hi == 0) return true;
+    const uint32_t e = max(ref, hi >> 23), least = max(e, kSpread + 1) - kSpread;
+    if (hi >= 0x7f000000u || (lo + 1) >> 23 < least || (ref0 > 0 && e > ref0 + kRise)) return false;
+    if (e > ref) {
+      if (ref > 0) rescale(__uint_as_float((127 + ref - e) << 23));
+      else ref0 = e;
+      ref = e;
+      inv_ref = __uint_as_float((254 - e) << 23);
+    }
+    return true;
   };
   // lane constants of the reads from LDS
   uint32_t k_at[NKC], v_at;
@@ -859,17 +884,6 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
       }
     }
     float ks[4], f[4], bias[4];
-    if constexpr (TYPE != SEQ_BF16 && F16) {
-      float most = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) most = fmaxf(most, x.vs[t] < INFINITY ? x.vs[t] : 0.0f);
-      if (most >= 2.0f * ref && most > 0.0f) {
-        const float to = __uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u));
-        rescale(ref / to);
-        ref = to;
-        inv_ref = 1.0f / to;
-      }
-    }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       ks[t] = x.ks[t]; bias[t] = x.bias[t];
@@ -971,9 +985,12 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
       }
   };
   int s = p.s0, buf = 0, turn = 0;
-  for (; s < s_edge; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) step(s, buf, turn, std::false_type{});
+  for (; s < s_edge; ++s, buf ^= 1, turn = turn == 2 ? 0 : turn + 1) {
+    if (TYPE != SEQ_BF16 && HALF && !near()) break;
+    step(s, buf, turn, std::false_type{});
+  }
   if constexpr (HALF) {
-    rescale((TYPE == SEQ_BF16 ? 1.0f / mul : ref) * kUnlift);
+    rescale((TYPE == SEQ_BF16 ? 1.0f / mul : __uint_as_float(ref << 23)) * kUnlift);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) l_run[mt] *= kUnlift;
   }

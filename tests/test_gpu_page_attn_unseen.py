@@ -1,4 +1,5 @@
-"""What a token does not see reaches nothing: finite values of any size in later rows and pages. Tolerances: those of test_gpu_page_attn.check."""
+"""What a token does not see reaches nothing: finite values of any size in later rows and pages, scales that the values seen do not
+reach. Tolerances: those of test_gpu_page_attn.check."""
 import pytest
 import torch
 
@@ -40,3 +41,24 @@ def test_large_values_of_later_tokens(kind, act, lens, n, hq, dh, P):
     torch.cuda.synchronize()
     check(got.double().cpu().numpy(), q.double().numpy(), rows[0], lens, n, P, act, dh ** -0.5, some=edges)
     assert torch.equal(got[kept], clean[kept])
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("power", [3, 5, 40])
+@pytest.mark.parametrize("lens,n,hq,dh,P", [([700, 5], [40, 40], 8, 128, 128), ([300], [600], 1, 128, 64), ([900, 300], [20, 33], 8, 64, 16)])
+def test_scales_above_the_values_seen(kind, power, lens, n, hq, dh, P):
+    """A page's scale goes by all that was written into it: here the rows that are left hold nothing but zeros, at the front or
+    in the middle, under scales of up to 2^40 times the others'."""
+    flush(f"case scales above {kind} {power} {lens} {n} {hq} {dh} {P}")
+    for j in (0, 1):
+        c, rows = paged(lens, n, 1, P, dh, kind, 73)
+        for b in range(len(lens)):
+            j_ = min(j, lens[b] // P)
+            page = int(c.table[b, j_])
+            c.v.view(torch.uint8 if kind == "e4m3" else torch.int8)[0, page] = 0
+            c.v_scale[0, page] = c.v_scale.max() * 2.0 ** power
+            rows[0][b][1][j_ * P:(j_ + 1) * P] = 0.0
+        q = randn((sum(n), hq, dh), torch.bfloat16, 74)
+        got = S.page_attention(c, 0, q.cuda(), starts(n).cuda())
+        torch.cuda.synchronize()
+        check(got.double().cpu().numpy(), q.double().numpy(), rows[0], lens, n, P, "bf16", dh ** -0.5, some=edges)
