@@ -291,6 +291,16 @@ __device__ __forceinline__ void add_odd(const PageAttnArgs& a, int b, int head, 
   }
 }
 
+// Whether any of the cache rows from .. to - 1 has a page. (Asked only of query rows whose sum is NaN: scores against missing rows
+// are NaN where the query is not finite, and a query row that sees none is zeros whatever it holds.)
+__device__ __forceinline__ bool any_page(const PageAttnArgs& a, int b, int from, int to) {
+  for (int j = from >> a.c.P_log; j << a.c.P_log < to; ++j) {
+    const int page = a.c.table[size_t(b) * a.c.width + j];
+    if (page >= 0 && page < a.c.n_pages) return true;
+  }
+  return false;
+}
+
 // Page ids and scales of a chunk: lane i holds those of page base + i, and of page base + 64 + i ahead of their use.
 template <int TYPE>
 struct PageLane {
@@ -552,7 +562,8 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
       if (row >= p.R) continue;
       const int t = quot(row, p.group);
       const int mine = p.L >= 0 && p.L + t < a.c.cap ? p.L + t + 1 : 0;
-      const bool there = mine > 0;     // (a row of an absent token is zeros)
+      // (a row of an absent token is zeros, as is one that sees nothing)
+      const bool there = mine > 0 && (l == l || any_page(a, p.b, p.s0 * kStep, min(mine, s1 * kStep)));
       if constexpr (TYPE != SEQ_INT8) {
         if (s_odd) add_odd<DH, TYPE>(a, p.b, p.head, max(common, p.s0 * kStep), min(mine, s1 * kStep), d0, v);
       }
@@ -562,7 +573,7 @@ __global__ __launch_bounds__(kBlock, (kWavesPerSimd<DH, TYPE, ACT, MT>)) void pa
 #pragma unroll
         for (int e = 0; e < NDT; e += 4)
           *reinterpret_cast<float4*>(rec + 2 * RB + in * DH + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * in) = make_float2(m, there ? l : 0.0f);
+        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * in) = there ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
       }
     }
   }
@@ -1000,7 +1011,11 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
   __syncthreads();
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const float l_all = quad_sum(l_run[mt]);
+    float l_all = quad_sum(l_run[mt]);
+    if (l_all != l_all && !any_page(a, p.b, p.s0 * kWideStep, min(lim[mt], s1 * kWideStep))) {
+      l_all = 0.0f;
+      m_run[mt] = -INFINITY;
+    }
 #pragma unroll
     for (int e = 0; e < NDT; ++e)
 #pragma unroll
@@ -1022,7 +1037,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void page_attn_wide_kernel(PageAttnA
         put_output<DH, ACT>(a, p.first + t, p.h0 + row - t * p.group, d0, l, mine > 0, v);
       } else {
         *reinterpret_cast<float4*>(rec + 2 * RB + place * DH + d0) = make_float4(v[0], v[1], v[2], v[3]);
-        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * place) = make_float2(m, mine > 0 ? l : 0.0f);
+        if (d0 == 0) *reinterpret_cast<float2*>(rec + 2 * place) = mine > 0 ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
       }
     }
   }

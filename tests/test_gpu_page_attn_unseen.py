@@ -1,5 +1,7 @@
 """What a token does not see reaches nothing: finite values of any size in later rows and pages, scales that the values seen do not
-reach. Tolerances: those of test_gpu_page_attn.check."""
+reach, queries of tokens without rows. Tolerances: those of test_gpu_page_attn.check."""
+import math
+
 import pytest
 import torch
 
@@ -62,3 +64,42 @@ def test_scales_above_the_values_seen(kind, power, lens, n, hq, dh, P):
         got = S.page_attention(c, 0, q.cuda(), starts(n).cuda())
         torch.cuda.synchronize()
         check(got.double().cpu().numpy(), q.double().numpy(), rows[0], lens, n, P, "bf16", dh ** -0.5, some=edges)
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("L,n,hq,what", [(3000, 20, 4, math.inf), (3000, 9, 2, -math.inf), (40, 30, 8, math.inf), (3005, 400, 4, math.nan)])
+def test_queries_of_absent_tokens(L, n, hq, what, kind, act):
+    """Tokens beyond the table's pages, in one chunk and in several, whose queries are not finite: zeros, and the others as they were."""
+    flush(f"case absent {L} {n} {hq} {what} {kind} {act}")
+    P, dh = 16, 64
+    c, rows = paged([L], [8], 1, P, dh, kind, 75)
+    q = randn((n, hq, dh), DTYPES[act], 76)
+    absent = c.max_seq - L
+    assert 0 < absent < n
+    clean = S.page_attention(c, 0, q.cuda(), starts([n]).cuda())
+    q[absent:, :, 0] = what             # (scores of one sign: the running maximum is infinite too)
+    got = S.page_attention(c, 0, q.cuda(), starts([n]).cuda())
+    torch.cuda.synchronize()
+    assert not got[absent:].any() and torch.equal(got[:absent], clean[:absent])
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("n", [1, 3, 40])
+@pytest.mark.parametrize("what", [math.inf, math.nan])
+def test_queries_that_see_no_row(what, n, kind, act):
+    """Sequences without any page (places of a step that no conversation has), whose queries hold anything: zeros."""
+    flush(f"case no row {what} {n} {kind} {act}")
+    P, dh, hq = 16, 64, 8
+    lens = [0, 50, 2500, 3000]
+    c, _ = paged(lens, [n] * 4, 1, P, dh, kind, 77)
+    q = randn((4 * n, hq, dh), DTYPES[act], 78)
+    at = None if n == 1 else starts([n] * 4).cuda()
+    clean = S.page_attention(c, 0, q.cuda(), at).view(4, n, hq, dh)
+    c.table[0] = -1
+    c.table[2] = c.n_pages
+    q.view(4, n, hq, dh)[::2, :, :, 1::2] = what
+    got = S.page_attention(c, 0, q.cuda(), at).view(4, n, hq, dh)
+    torch.cuda.synchronize()
+    assert not got[::2].any() and torch.equal(got[1::2], clean[1::2])
