@@ -725,7 +725,8 @@ tasp_status tasp_page_forward(tasp_plan plan, const float* x, const int32_t* sta
  * whose tokens lie in the vocabulary (0 where there are none; bounds are cut to 0..rows): what tasp_route takes as
  * proxy_logprob, over a prompt's rows of logits and next tokens.
  * NaN logits count as -inf, magnitudes of 2^126 / max(1, log2(e) / temperature) and more as infinite; infinite logits share the
- * whole probability evenly. A row without a logit above -inf has logprob -inf and entropy 0. Terms in float32, sums joined in float64.
+ * whole probability evenly. A row without a logit above -inf has logprob -inf and entropy 0. Terms in float32, sums joined in
+ * float64 behind every 512 terms of a thread.
  * workspace: device, 256-byte aligned, at least tasp_token_logprobs_workspace_bytes, needs no clearing; calls that overlap need
  * one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, types, a temperature outside 1e-30..1e30),
  * TASP_ERR_SHAPE (rows, vocab 1..2^24, n_top, n_seqs), TASP_ERR_WORKSPACE. */

@@ -3,8 +3,8 @@
 //
 // In one pass over a row, in powers of two: t = (x - m) c with c = log2(e) / temperature and m the running maximum,
 // s = sum 2^t, w = sum t 2^t. Then log p(x) = ln 2 ((x - m) c - log2 s) and the entropy is ln 2 (log2 s - w / s). Every
-// thread has a maximum and sums of its own in float32 (some 500 terms); they meet in float64. (x c - m c, one instruction less,
-// loses all digits at small temperatures.)
+// thread has a maximum and sums of its own in float32, of up to 512 terms; they meet in float64, behind every 32 tiles
+// of a piece that has more, and at its end. (x c - m c, one instruction less, loses all digits at small temperatures.)
 //
 // The largest: every wave keeps a list in LDS of the elements that reach a bound, without a barrier: the `top`-th largest of its
 // 64 lanes' maxima, which at least `top` elements reach (some 44 for 32), looked at again behind 1, 2, 4, .. tiles and where the list
@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kPer = 16;               // elements of a thread and tile
 constexpr int kTile = kBlock * kPer;
+constexpr int kFold = 32;              // tiles whose terms a thread adds up in float32
 constexpr int kGrown = 96;             // elements that a wave's list may hold beyond `top` before it is cut
 constexpr int kLimit = 256;            // keys that are ranked by comparing each with each: one per thread
 constexpr int kKeys = 4192;            // of the join's list
@@ -196,6 +197,21 @@ __device__ __forceinline__ void add_to(Record& rec, const Record& q, float c) {
   rec.w += (q.w + d * q.s) * f;
 }
 
+// The same where q's maximum may be above, by less than the range of 64 bits
+__device__ __forceinline__ void add_far(Record& rec, const Record& q, float c) {
+  const double d = (double(q.m) - double(rec.m)) * double(c), k = rint(d);
+  if (d < -1000.0) return;
+  const double f = ldexp(double(__builtin_amdgcn_exp2f(float(d - k))), int(k));
+  rec.s += q.s * f;
+  rec.w += (q.w + d * q.s) * f;
+}
+// A wave's sums into what it has of the tiles before. rec.m stays (and with it what has been added, to the bit) until a maximum is
+// 2^900 above it, which leaves nothing of the rest.
+__device__ __forceinline__ void fold(Record& rec, const Record& q, float c) {
+  if ((double(q.m) - double(rec.m)) * double(c) > 900.0) rec = Record{0.0, 0.0, q.m, 0};
+  add_far(rec, q, c);
+}
+
 // A token's log probability under a row's record
 struct Scale {
   double log_s;
@@ -248,6 +264,7 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
   __shared__ float s_bound[4];
   __shared__ int s_n;
   __shared__ Sums s_sums[4];
+  __shared__ Record s_fold[4];         // of pieces of more than kFold tiles: a wave's sums of whole kFold tiles
   __shared__ int s_before[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
@@ -287,97 +304,106 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
     Found& found = s_found[TOP ? wave : 0];
     float bound = above(-a.lim);       // elements from it on enter the wave's list
     float g = -a.lim;                  // the `top`-th largest of its lanes' maxima when last looked at
+    const int tiles = (end - first + kTile - 1) / kTile;
     __syncthreads();                   // (the row before has been read)
-    for (int tile = first; tile < end; tile += kTile) {
-      float x[kPer];
-      if constexpr (F32) {
+    if (lane == 0) s_fold[wave] = Record{0.0, 0.0, -INFINITY, 0};
+    for (int tile = first;;) {
+      for (const int to = min(end, tile + kFold * kTile); tile < to; tile += kTile) {
+        float x[kPer];
+        if constexpr (F32) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) x[j] = __uint_as_float(raw[0][j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < RAW; ++j) {
-          x[2 * j] = bf16_lo(raw[0][j]);
-          x[2 * j + 1] = bf16_hi(raw[0][j]);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) x[j] = fmaxf(x[j], -a.lim);                         // (NaN is -lim)
-      float top = fmaxf(x[0], x[1]);
-#pragma unroll
-      for (int j = 2; j < kPer; ++j) top = fmaxf(top, x[j]);
-      if (__ballot(top > a.lim)) {
-        top = fminf(top, a.lim);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) x[j] = fminf(x[j], a.lim);
-      }
-#pragma unroll
-      for (int k = 0; k + 1 < AHEAD; ++k)
-#pragma unroll
-        for (int j = 0; j < RAW; ++j) raw[k][j] = raw[k + 1][j];
-      load(tile + AHEAD * kTile, raw[AHEAD - 1]);
-      // (places behind the row's end hold -lim: their terms are 0, or the row is empty)
-      if (top > sum.m) move_to(sum, top, a.c);
-      float s2 = 0.0f, w2 = 0.0f;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const float t = (x[j] - sum.m) * a.c, e = __builtin_amdgcn_exp2f(t);
-        float& s = j & 1 ? s2 : sum.s;
-        float& w = j & 1 ? w2 : sum.w;
-        s += e;
-        w = fmaf(e, t, w);
-      }
-      sum.s += s2;
-      sum.w += w2;
-      // before the token equal logits come first too
-      if (token < tile || token >= tile + kTile) {
-        if (token >= tile + kTile) {
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] >= xt));
+          for (int j = 0; j < kPer; ++j) x[j] = __uint_as_float(raw[0][j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt));
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt || (x[j] == xt && index(tile, j) < token)));
-      }
-      if constexpr (TOP) {
-        // The `top`-th largest of the lanes' maxima so far: that many elements reach it, and later ones lose to equal ones.
-        // Raised behind 1, 2, 4, .. tiles
-        float from = bound;
-        const int k = (tile - first) / kTile;
-        if ((k & (k + 1)) == 0) {
-          g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
-          from = fmaxf(from, g);
-          if (g > -a.lim) bound = fmaxf(bound, above(g));
-        }
-        if (__ballot(top >= from)) {
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            const unsigned long long who = __ballot(x[j] >= from);
-            if (who) {
-              if (x[j] >= from) {
-                found.x[n + lanes_before(who)] = x[j];
-                found.i[n + lanes_before(who)] = index(tile, j);
-              }
-              n += __popcll(who);
-            }
+          for (int j = 0; j < RAW; ++j) {
+            x[2 * j] = bf16_lo(raw[0][j]);
+            x[2 * j + 1] = bf16_hi(raw[0][j]);
           }
         }
-        if (n > a.top + kGrown) {
-          g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
-          n = keep(found, n, lane, [&](float x, int) { return x >= g; });
-          if (g > -a.lim) bound = fmaxf(bound, above(g));
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = fmaxf(x[j], -a.lim);                         // (NaN is -lim)
+        float top = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int j = 2; j < kPer; ++j) top = fmaxf(top, x[j]);
+        if (__ballot(top > a.lim)) {
+          top = fminf(top, a.lim);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) x[j] = fminf(x[j], a.lim);
         }
-        if (n > a.top + kGrown) {      // (many equal ones, or in few lanes)
-          const unsigned long long least = nth_key(found, n, a.top, lane);
-          n = keep(found, n, lane, [&](float x, int i) { return key_of(x, i) >= least; });
-          bound = fmaxf(bound, above(unordered(uint32_t(least >> 32))));
+#pragma unroll
+        for (int k = 0; k + 1 < AHEAD; ++k)
+#pragma unroll
+          for (int j = 0; j < RAW; ++j) raw[k][j] = raw[k + 1][j];
+        load(tile + AHEAD * kTile, raw[AHEAD - 1]);
+        // (places behind the row's end hold -lim: their terms are 0, or the row is empty)
+        if (top > sum.m) move_to(sum, top, a.c);
+        float s2 = 0.0f, w2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const float t = (x[j] - sum.m) * a.c, e = __builtin_amdgcn_exp2f(t);
+          float& s = j & 1 ? s2 : sum.s;
+          float& w = j & 1 ? w2 : sum.w;
+          s += e;
+          w = fmaf(e, t, w);
+        }
+        sum.s += s2;
+        sum.w += w2;
+        // before the token equal logits come first too
+        if (token < tile || token >= tile + kTile) {
+          if (token >= tile + kTile) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] >= xt));
+          } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) before += __popcll(__ballot(x[j] > xt || (x[j] == xt && index(tile, j) < token)));
+        }
+        if constexpr (TOP) {
+          // The `top`-th largest of the lanes' maxima so far: that many elements reach it, and later ones lose to equal ones.
+          // Raised behind 1, 2, 4, .. tiles
+          float from = bound;
+          const int k = (tile - first) / kTile;
+          if ((k & (k + 1)) == 0) {
+            g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
+            from = fmaxf(from, g);
+            if (g > -a.lim) bound = fmaxf(bound, above(g));
+          }
+          if (__ballot(top >= from)) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+              const unsigned long long who = __ballot(x[j] >= from);
+              if (who) {
+                if (x[j] >= from) {
+                  found.x[n + lanes_before(who)] = x[j];
+                  found.i[n + lanes_before(who)] = index(tile, j);
+                }
+                n += __popcll(who);
+              }
+            }
+          }
+          if (n > a.top + kGrown) {
+            g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
+            n = keep(found, n, lane, [&](float x, int) { return x >= g; });
+            if (g > -a.lim) bound = fmaxf(bound, above(g));
+          }
+          if (n > a.top + kGrown) {      // (many equal ones, or in few lanes)
+            const unsigned long long least = nth_key(found, n, a.top, lane);
+            n = keep(found, n, lane, [&](float x, int i) { return key_of(x, i) >= least; });
+            bound = fmaxf(bound, above(unordered(uint32_t(least >> 32))));
+          }
         }
       }
+      if (tile >= end) break;
+      const float m = wave_max(sum.m), own = sum.m;
+      move_to(sum, m, a.c);
+      const float s = wave_sum(sum.s), w = wave_sum(sum.w);
+      if (lane == 0) fold(s_fold[wave], Record{double(s), double(w), m, 0}, a.c);
+      sum = {own, 0.0f, 0.0f};
     }
     if constexpr (TOP) {
-      const int tiles = (end - first + kTile - 1) / kTile;
       if (tiles & (tiles - 1)) g = nth_of_lanes(sum.m, a.top, s_group[wave], lane);
       if (lane == 0) s_bound[wave] = g;
       if (tid == 0) s_n = 0;
@@ -427,6 +453,9 @@ __global__ __launch_bounds__(kBlock, 4) void logprob_kernel(LogprobArgs a, int p
     for (int i = 0; i < 4; ++i) rec.m = fmaxf(rec.m, s_sums[i].m);
 #pragma unroll
     for (int i = 0; i < 4; ++i) add_to(rec, Record{double(s_sums[i].s), double(s_sums[i].w), s_sums[i].m, s_before[i]}, a.c);
+    if (tiles > kFold) {
+      for (int i = 0; i < 4; ++i) add_far(rec, s_fold[i], a.c);
+    }
     if (gridDim.x == 1) {
       finish(a, row, rec, there, xt, s_best, n);
     } else {
