@@ -50,10 +50,13 @@ constexpr int kTarget = 512;
 // tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 130 and 1225)
 constexpr int kFew = 32;
 
-// Query rows from which eight waves, one workgroup per CU in place of two, share a step in LDS: bringing it (V to FP16 above all) takes
-// each of them half the instructions. (A prompt of 8192 tokens x 64 heads 1299 -> 1221 us, 512 tokens behind 8191 rows 131.3 -> 129.2;
-// for a block or less there are fewer workgroups: 30 tokens or so 12.8 -> 14.4)
-constexpr int kEight = 512;
+// Eight waves, one workgroup per CU in place of two, may share a step in LDS: bringing it (BF16 V to FP16 above all) takes each of them
+// half the instructions, but a block's last steps and its empty waves take a whole CU. BF16 pages, from kEight query rows and
+// kEightRows rows seen on, four / eight waves, 32 heads: 512 tokens behind 0 rows 30 / 33 us, 1000 45 / 45, 2000 54 / 53, 4000 72 / 67,
+// 8191 113 / 103; 128 tokens behind 1000 29 / 33, 2000 35.4 / 34.5, 8191 51 / 48; a prompt of 1024 47.0 / 46.5, 2048 79 / 83, 4096
+// 190 / 178, 8192 698 / 645. 8 bits: 512 tokens behind 0 30 / 35, 2000 54 / 58, 8191 112 / 113, a prompt of 8192 694 / 700; they have four. Nor where
+// the other sequences, on average, fill less than a block and are not the first kernel's: a chunk of 512 beside 15 of 20 tokens behind 8191 207 / 316.
+constexpr int kEight = 512, kEightRows = 2048;
 
 // Steps of 64 cache rows, in all slots, of short sequences that the wide kernel takes beside its own, in place of a second launch:
 // for float32, whose bits are the same in both kernels. (3 x 37 tokens x 24 heads behind 1001 rows: 16.5 us, 19.3 with both
@@ -1139,7 +1142,9 @@ Shapes shapes(const PageAttnArgs& a) {
   const int mt = rows > 16 && !use_wide ? 2 : 1;       // (beside the other kernel it has single tokens, mostly)
   fill(z.few, use_few, 1, use_wide ? kFew : kAll, kStep, mt, 16 * mt);
   const int wt = a.act == SEQ_BF16 ? 2 : 1;
-  const int waves = a.act == SEQ_BF16 && a.c.dh == 128 && rows >= kEight ? 8 : 4;
+  const long rest = seqs > 1 ? long(a.N - expected) * a.group / (seqs - 1) : 0;          // query rows of another sequence on average
+  const bool eight = a.act == SEQ_BF16 && a.c.type == SEQ_BF16 && a.c.dh == 128 && rows >= kEight && most >= kEightRows && (rest <= kFew || rest >= 256);
+  const int waves = eight ? 8 : 4;
   fill(z.wide, use_wide, use_few ? kFew + 1 : 1, kAll, kWideStep, wt, 16 * waves * wt);
   z.floats = z.few.cut || z.wide.cut ? (size_t(a.N) * 4 + 63) / 64 * 64 : 0;
   for (PageShape* y : {&z.few, &z.wide}) {
@@ -1158,7 +1163,7 @@ hipError_t launch_page_attn(const PageAttnArgs& a, hipStream_t s) {
 #define ATTN(KERNEL, Y, THREADS, ...) hipLaunchKernelGGL((KERNEL<__VA_ARGS__>), dim3(a.slots, std::min(Y.items, kItems), (Y.items + kItems - 1) / kItems), dim3(THREADS), 0, s, a, Y)
 #define ATTN_MT(DH, TYPE, ACT)                                                                      \
   do {                                                                                              \
-    constexpr bool EIGHT = DH == 128 && ACT == SEQ_BF16;                                            \
+    constexpr bool EIGHT = DH == 128 && TYPE == SEQ_BF16 && ACT == SEQ_BF16;                        \
     if (EIGHT && z.wide.items && z.wide.rows == 256) ATTN(page_attn_wide_kernel, z.wide, 8 * kWave, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1), (EIGHT ? 8 : 4)); \
     else if (z.wide.items) ATTN(page_attn_wide_kernel, z.wide, 4 * kWave, DH, TYPE, ACT, (ACT == SEQ_BF16 ? 2 : 1), 4); \
     if (z.few.items && z.few.mt == 1) ATTN(page_attn_kernel, z.few, kBlock, DH, TYPE, ACT, 1);      \

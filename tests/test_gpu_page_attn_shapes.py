@@ -1,0 +1,33 @@
+"""Steps whose sequences differ in their lengths and numbers of new tokens by far, over the rules that choose kernels, blocks and
+chunks from a call's shape. Tolerances: those of test_gpu_page_attn.check."""
+import pytest
+import torch
+
+from paper_2609_29499_amd import session as S
+from tests.page_case import paged, starts
+from tests.seq_case import DTYPES, flush, randn
+from tests.test_gpu_page_attn import check
+
+pytestmark = pytest.mark.gpu
+
+
+def attended(lens, n, hq, H, dh, P, kind, act, room, max_new=None, **hints):
+    """A step against the oracle; the same bits again. room: pages of the tables behind what is needed."""
+    c, rows = paged(lens, n, H, P, dh, kind, 81, room=room, spare=0)
+    q = randn((sum(n), hq, dh), DTYPES[act], 82)
+    at = None if set(n) == {1} and max_new is None else starts(n).cuda()
+    got = S.page_attention(c, 0, q.cuda(), at, max_new=max_new, **hints)
+    again = S.page_attention(c, 0, q.cuda(), at, max_new=max_new, **hints)
+    torch.cuda.synchronize()
+    assert torch.equal(got, again)
+    check(got.double().cpu().numpy(), q.double().numpy(), rows[0], lens, n, P, act, dh ** -0.5, some=lambda m: [0, 1, 31, 32, m // 2, m - 2, m - 1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+@pytest.mark.parametrize("lens,n,hq", [([0], [64], 8), ([33, 0], [150, 64], 8), ([5, 0, 9], [513, 1, 2], 1), ([2300, 3, 90], [100, 20, 9], 8),
+                                       ([2500], [257], 2), ([100, 0, 64, 31], [70, 65, 130, 1], 8)])
+def test_many_query_rows_under_wide_tables(kind, lens, n, hq):
+    """512 query rows and more of a sequence where 2048 rows and more may be seen: whole and partial blocks, beside others that
+    fill a block, fill little of one, or are single tokens."""
+    flush(f"case wide tables {kind} {lens} {n} {hq}")
+    attended(lens, n, hq, 1, 128, 32, kind, "bf16", 70)
