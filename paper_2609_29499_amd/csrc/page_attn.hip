@@ -59,9 +59,13 @@ constexpr int kFew = 32;
 constexpr int kEight = 512, kEightRows = 2048;
 
 // Steps of 64 cache rows, in all slots, of short sequences that the wide kernel takes beside its own, in place of a second launch:
-// for float32, whose bits are the same in both kernels. (3 x 37 tokens x 24 heads behind 1001 rows: 16.5 us, 19.3 with both
-// kernels. Three single tokens behind 8191 rows, 384 steps in each of 8 slots: in BF16 beside 512 tokens 137.6 us, 131.7 with both.)
-constexpr int kAside = 2048;
+// for float32, whose bits are the same in both kernels. Both / one, 32 heads of 128 over INT8 rows: 64 tokens and 11 single ones behind
+// 1000 rows (1496 steps) 37 / 28 us, 2000 (2904) 49 / 38, 4000 (5632) 65 / 60, 8191 (11352) 99 / 105; 16 and 11 behind 1000 (1408) 34 / 26, 2000
+// (2816) 41 / 38, 4000 (5544) 51 / 58. But not where the short sequences' workgroups take a chunk from the large one's blocks or run behind them: 512
+// tokens and one behind 1000 rows 66 / 68, 2000 90 / 109, 8191 234 / 355; 1024 tokens and one behind 500 rows 82 / 69, 1000 106 / 98, 2000 151 / 172;
+// 256 tokens, whose blocks have four chunks each and lose one of them, behind 8191 rows 142 / 132. (BF16 runs both kernels, for the bits of short
+// sequences: beside 512 tokens behind 8191 rows all in the wide one took 137.6 us, both 131.7.)
+constexpr int kAside = 2048, kAsideRows = 1024;
 
 // How a kernel is launched. Sequences with least .. most query rows per cache head, in blocks of `rows` = 2^rows_log; steps of
 // `step` rows; items: chunks of all blocks, at most; cut: there may be several chunks of a block
@@ -1126,7 +1130,9 @@ Shapes shapes(const PageAttnArgs& a) {
   // One kernel for all where it is what the expected number of tokens asks for, where there is one sequence, or where the
   // others' steps take the wide kernel less time than a second launch
   const long aside = (seqs - 1) * ((most + kWideStep - 1) / kWideStep) * a.slots;
-  const bool use_wide = rows > kFew, use_few = !use_wide || aside > (a.act == SEQ_F32 ? kAside : 0);
+  const long big = (rows + 16 * 4 - 1) / (16 * 4), room = (kTarget + a.slots - 1) / a.slots, share = room / big;      // (float32's blocks and chunks)
+  const bool fits = a.max_len <= kAsideRows || share >= 3 || share * big + seqs - 1 <= room;
+  const bool use_wide = rows > kFew, use_few = !use_wide || aside > (a.act == SEQ_F32 && fits ? kAside : 0);
   constexpr int kAll = 1 << 30;
   auto fill = [&](PageShape& y, bool use, int least, int limit, int step, int mt, int block) {
     y.least = use ? least : 1;

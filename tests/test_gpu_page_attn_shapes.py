@@ -31,3 +31,12 @@ def test_many_query_rows_under_wide_tables(kind, lens, n, hq):
     fill a block, fill little of one, or are single tokens."""
     flush(f"case wide tables {kind} {lens} {n} {hq}")
     attended(lens, n, hq, 1, 128, 32, kind, "bf16", 70)
+
+
+@pytest.mark.parametrize("kind,dh", [("int8", 128), ("bf16", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("lens,n,H", [([1100, 900], [130, 1], 8), ([3000, 2000, 5], [64, 1, 1], 2), ([1500, 10], [300, 3], 16), ([100, 700], [257, 1], 12)])
+def test_float32_beside_short_sequences(kind, dh, lens, n, H):
+    """One kernel for all, or both: many query rows of one sequence, few of the others, behind short and long rows."""
+    flush(f"case float32 {kind} {dh} {lens} {n} {H}")
+    attended(lens, n, H, H, dh, 64, kind, "f32", 1, max_new=max(n), max_len=max(lens))
+    attended(lens, n, 4, 1, dh, 64, kind, "f32", 1, max_new=max(n), max_len=max(lens))
