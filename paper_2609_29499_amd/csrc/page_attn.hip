@@ -68,9 +68,9 @@ constexpr int kEight = 512, kEightRows = 2048;
 constexpr int kAside = 2048, kAsideRows = 1024;
 
 // How a kernel is launched. Sequences with least .. most query rows per cache head, in blocks of `rows` = 2^rows_log; steps of
-// `step` rows; items: chunks of all blocks, at most; cut: there may be several chunks of a block
+// `step` rows; items: chunks of all blocks, at most; cut: there may be several chunks of a block, none shorter than all steps / share
 struct PageShape {
-  int least, most, mt, rows, rows_log, step, items, cut;
+  int least, most, mt, rows, rows_log, step, items, cut, share;
   size_t ws;                           // floats of the workspace in front of its records
 };
 struct Deal {
@@ -81,7 +81,8 @@ struct Deal {
 // A lane holds four sequences. The chunk is the shortest multiple of kMinSteps that leaves at most `items` items.
 __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, int lane) {
   Deal d;
-  int steps[4], blocks[4], sum = 0, most = 0;
+  int steps[4], blocks[4], most = 0;
+  uint32_t sum = 0;                    // (of 2^13 + 256 blocks of 2^18 steps at most)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const PageSeq q = page_seq(a.start, a.N, a.c, min(4 * lane + i, a.c.batch - 1));
@@ -91,7 +92,7 @@ __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, 
     const int end = q.L < 0 ? 0 : min(q.L + d.n[i], a.c.cap);
     steps[i] = d.n[i] == 0 ? 0 : max(1, (end + y.step - 1) / y.step);
     blocks[i] = (d.n[i] * a.group + y.rows - 1) >> y.rows_log;
-    sum += steps[i] * min(blocks[i], kTarget);
+    sum += uint32_t(steps[i]) * uint32_t(min(blocks[i], kTarget));
     most = max(most, steps[i]);
   }
   d.chunk = 1 << 24;
@@ -103,10 +104,10 @@ __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, 
       for (int i = 0; i < 4; ++i) own += blocks[i] * quot_steps(steps[i] + chunk - 1, chunk, inv);
       return __builtin_amdgcn_readlane(wave_scan(own), kWave - 1);
     };
-    sum = __builtin_amdgcn_readlane(wave_scan(sum), kWave - 1);
+    sum = uint32_t(__builtin_amdgcn_readlane(wave_scan(int(sum)), kWave - 1));
     most = int(wave_max(float(most)));                 // (below 2^24)
     // in units of kMinSteps: lo may do, hi does
-    int lo = max(1, ((sum + y.items - 1) / y.items + kMinSteps - 1) / kMinSteps), hi = max(lo, (most + kMinSteps - 1) / kMinSteps);
+    int lo = max(1, int((sum + y.share - 1) / y.share + kMinSteps - 1) / kMinSteps), hi = max(lo, (most + kMinSteps - 1) / kMinSteps);
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (total(mid * kMinSteps) <= y.items) hi = mid;
@@ -1141,9 +1142,14 @@ Shapes shapes(const PageAttnArgs& a) {
     if (!use) return;
     const long blocks = std::min<long>(long(a.N) * a.group, limit == kFew ? long(seqs) * kFew : kAll) / block + seqs;    // of all sequences, at most
     const int quota = ((block == 256 ? kTarget / 2 : kTarget) + a.slots - 1) / a.slots;      // (of eight waves: half)
-    // (the join looks at every token's rows)
-    y.cut = blocks < quota && most > kMinSteps * step && long(a.N) * a.slots * a.group <= 1 << 17;
-    y.items = int(std::max<long>(blocks, y.cut ? quota : 0));
+    // Blocks enough for all workgroups are cut too where the first kernel has them: lengths differ, and one workgroup per head would walk a
+    // sequence far longer than the others by itself (131072 rows beside 63 of 1024, 32 heads: 1033 us uncut, 86 cut; three single tokens
+    // behind 65530 rows beside a prompt of 4096 tokens 705, 280). Chunks of one and a half shares of all steps and more leave sequences of
+    // like lengths whole (64 of 3072 rows 74.8 us uncut, 77.1 so, 64 of 500 18.8, 20.7: the join). The join looks at every token's rows: a bound
+    // on them, higher where the first kernel has the short sequences of a step.
+    y.cut = (blocks < quota || block <= kFew) && most > kMinSteps * step && long(a.N) * a.slots * a.group <= (limit == kFew ? 1 << 20 : 1 << 17);
+    y.share = blocks < quota ? quota : (2 * quota + 2) / 3;
+    y.items = int(y.cut ? blocks < quota ? quota : blocks + y.share : blocks);
   };
   const int mt = rows > 16 && !use_wide ? 2 : 1;       // (beside the other kernel it has single tokens, mostly)
   fill(z.few, use_few, 1, use_wide ? kFew : kAll, kStep, mt, 16 * mt);

@@ -40,3 +40,14 @@ def test_float32_beside_short_sequences(kind, dh, lens, n, H):
     flush(f"case float32 {kind} {dh} {lens} {n} {H}")
     attended(lens, n, H, H, dh, 64, kind, "f32", 1, max_new=max(n), max_len=max(lens))
     attended(lens, n, 4, 1, dh, 64, kind, "f32", 1, max_new=max(n), max_len=max(lens))
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,dh,hq,H,lens,n", [
+    ("int8", 64, 8, 8, [30000] + [100] * 63, [1] * 64), ("bf16", 128, 8, 2, [60] * 200 + [20000] + [0, 1] * 27, [1] * 255),
+    ("e4m3", 64, 4, 4, [9000] + [50] * 70, [2, 1, 3] * 23 + [1, 1]), ("int8", 128, 16, 8, [5000 - 61 * b for b in range(80)], [1] * 80),
+    ("bf16", 64, 64, 8, [0, 9000, 7000], [2500, 1, 2]), ("e4m3", 128, 16, 2, [10, 20000, 300, 40], [700, 1, 1, 1])])
+def test_one_sequence_far_longer_than_the_others(kind, dh, hq, H, lens, n, act):
+    """More blocks of query rows than there are workgroups for, and more tokens in a step than single ones: the long sequence is cut."""
+    flush(f"case long among short {kind} {dh} {hq} {H} {len(lens)} {max(lens)} {act}")
+    attended(lens, n, hq, H, dh, 64, kind, act, 0, max_new=max(n), max_len=max(lens))
