@@ -307,9 +307,9 @@ class Plan:
         B.tasp_page_bind(self.handle, cache.struct)
 
     def page_workspace(self, cache, n_tokens, max_len=None, max_new=None, stream=None):
-        """A workspace for page_forward calls of this shape."""
-        n = B.tasp_page_forward_workspace_bytes(self.handle, cache.struct, n_tokens, cache.max_seq if max_len is None else max_len,
-                                                n_tokens if max_new is None else max_new)
+        """A workspace for page_forward calls of this shape (max_new None: with start and without)."""
+        n = max(B.tasp_page_forward_workspace_bytes(self.handle, cache.struct, n_tokens, cache.max_seq if max_len is None else max_len, m)
+                for m in _expected(n_tokens, max_new))
         return _workspace(n, cache.k.device, stream)
 
     def page_forward(self, x, cache, start=None, max_len=None, max_new=None, out=None, workspace=None, stream=None):
@@ -723,10 +723,15 @@ def page_read(cache, layer, n, first=None, dtype=torch.bfloat16, out=None, strea
     return k, v
 
 
+def _expected(n_tokens, max_new):
+    """The numbers of new tokens that calls expect of a sequence where max_new is None: all of the call's, or, without start, one."""
+    return (1, n_tokens) if max_new is None else (max_new,)
+
+
 def page_attention_workspace(cache, n_q_heads, n_tokens, max_len=None, max_new=None, stream=None):
-    """A workspace for page_attention calls of this shape (any layer)."""
-    n = B.tasp_page_attention_workspace_bytes(cache.struct, n_q_heads, n_tokens, cache.max_seq if max_len is None else max_len,
-                                              n_tokens if max_new is None else max_new)
+    """A workspace for page_attention calls of this shape (any layer; max_new None: with start and without)."""
+    n = max(B.tasp_page_attention_workspace_bytes(cache.struct, n_q_heads, n_tokens, cache.max_seq if max_len is None else max_len, m)
+            for m in _expected(n_tokens, max_new))
     return _workspace(n, cache.k.device, stream)
 
 
