@@ -655,8 +655,8 @@ typedef struct {
 
 /* Write the tokens' k and v into their sequences' pages of layer `layer` (len itself stays) and rotate q: q and k are
  * turned by the tokens' positions (rope NULL: not at all), v is taken as it is. k, v: rows of n_kv_heads heads; q, q_out:
- * n_q_heads (0: no queries, both NULL), neither q_out overlapping q, k or v; all of act_type TASP_BF16 or TASP_F32 (seq
- * strides are not used). q_out of absent tokens are zeros. Arithmetic in float32, angles in float64.
+ * n_q_heads (0: no queries, both NULL); all of act_type TASP_BF16 or TASP_F32 (seq strides are not used). Rows of q_out must not
+ * overlap those of q, k or v. q_out of absent tokens are zeros. Arithmetic in float32, angles in float64.
  * Stream-ordered, asynchronous, capturable, no workspace. Errors: TASP_ERR_INVALID_ARG (NULL, types, misaligned rows),
  * TASP_ERR_SHAPE (cache fields, layer, n_tokens, head counts, rot_dim). */
 tasp_status tasp_page_append(const tasp_page_cache* cache, int32_t layer, const tasp_rope* rope,
@@ -677,9 +677,9 @@ tasp_status tasp_page_read(const tasp_page_cache* cache, int32_t layer, const in
  * tokens that see no row are zeros, and what unseen rows hold (NaN, infinities, values of any size) reaches no output (a page's scale
  * belongs to all of its rows). TASP_BF16: q exact, sums in float32, probabilities in 16 bits, or, with more than 32 query rows of a
  * sequence and cache head (batch 1: of n_tokens tokens), in 11 to 16 bits, and lost per row up to 2^-34 of the largest |v|
- * seen (8-bit pages: 2^-30 of the row's own);
- * TASP_F32: everything to 24 bits. The ends of float32 as for tasp_tree_attention. max_len, max_new: the largest length and the largest number of new tokens of a sequence
- * that are expected (max_len 0..max_pages * page_rows, max_new at least 1): they size launches and workspace; more is served too.
+ * seen (8-bit pages: 2^-30 of the row's own); TASP_F32: everything to 24 bits. The ends of float32 as for tasp_tree_attention.
+ * max_len, max_new: the largest length and the largest number of new tokens of a sequence that are expected (max_len
+ * 0..max_pages * page_rows, max_new at least 1): they size launches and workspace; more is served too.
  * workspace: device, 256-byte aligned, at least tasp_page_attention_workspace_bytes for the same cache shape, n_q_heads,
  * n_tokens, max_len and max_new; its contents need no clearing; calls that overlap need one each. Stream-ordered,
  * capturable. Errors as tasp_page_append, TASP_ERR_WORKSPACE. */
@@ -713,8 +713,8 @@ tasp_status tasp_page_forward(tasp_plan plan, const float* x, const int32_t* sta
                               const tasp_page_cache* cache, int32_t max_len, int32_t max_new,
                               float* out, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Scores of given tokens. logits (device): `rows` rows of vocab values, TASP_F32 or TASP_BF16, row_stride elements from
- * one to the next; tokens (device int32 [rows]); p = softmax(row / temperature). Per row:
+/* Scores of given tokens. logits (device): `rows` rows of vocab values, TASP_F32 or TASP_BF16, row_stride elements (vocab at
+ * least) from one to the next; tokens (device int32 [rows]); p = softmax(row / temperature). Per row:
  *   logprob (float32 [rows])   log p(token); 0 for a token outside the vocabulary (padding)
  *   entropy (float32 [rows])   of p in nats; may be NULL
  *   rank (int32 [rows])        tokens before this one in the order of logits, equal ones by id (0: the most likely); -1 for
@@ -729,7 +729,7 @@ tasp_status tasp_page_forward(tasp_plan plan, const float* x, const int32_t* sta
  * float64 behind every 512 terms of a thread.
  * workspace: device, 256-byte aligned, at least tasp_token_logprobs_workspace_bytes, needs no clearing; calls that overlap need
  * one each. Stream-ordered, capturable. Errors: TASP_ERR_INVALID_ARG (NULL, types, a temperature outside 1e-30..1e30),
- * TASP_ERR_SHAPE (rows, vocab 1..2^24, n_top, n_seqs), TASP_ERR_WORKSPACE. */
+ * TASP_ERR_SHAPE (rows, vocab 1..2^24, row_stride, n_top, n_seqs), TASP_ERR_WORKSPACE. */
 #define TASP_TOP_MAX 32
 tasp_status tasp_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes);
 tasp_status tasp_token_logprobs(const void* logits, int32_t logits_type, int64_t row_stride,

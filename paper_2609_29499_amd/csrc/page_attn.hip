@@ -20,15 +20,16 @@
 // through LDS (below).
 //
 // A workgroup takes one chunk of the cache rows of one block of query rows and cache head. Chunks have equal lengths, found
-// from the lengths on the device (no host knows them) such that there are about two workgroups per CU. A block of one
-// chunk is written at once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which
-// another launch joins in chunk order.
+// from the lengths on the device (no host knows them) such that there are about two workgroups per CU. With more blocks than that
+// the second kernel takes each whole, the first cuts those that are far longer than the others. A block of one chunk is written at
+// once; the others leave (maximum, sum, unnormalised output) per query row in the workspace, which another launch joins in chunk order.
 //
-// What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 75 us and a join of 5: 5.8 TB/s; 32 tokens over 8190
-// INT8 rows, a common prefix of 1024 read by each, 78: 5.2 TB/s); one token is latency (8.6 us and a join of 4.7 for
-// 2047 rows). The second, matrix products and the softmax's vector instructions, of which each waits for the other:
-// a prompt of 8192 tokens x 64 heads in BF16 1225 us, 898 TFLOP/s of visible pairs, 72 % of what a library product of 8192^3
-// reaches (1243); 512 tokens behind 8191 INT8 rows 108 us, 660 TFLOP/s.
+// What bounds them: the first, memory (4 tokens x 64 heads over 65,530 E4M3 rows 76 us and a join of 5: 5.8 TB/s; 32 tokens over 8190
+// INT8 rows, a common prefix of 1024 read by each, 80: 5.1 TB/s); one token is latency (8.4 us and a join of 4.3 for
+// 2047 rows). The second, matrix products and vector instructions, of which each waits for the other:
+// a prompt of 8192 tokens x 64 heads in BF16 1236 us, 890 TFLOP/s of visible pairs, 72 % of what a library product of 8192^3
+// reaches (1243): 386 M vector instructions for 68 M products, the matrix cores busy for 36 % of the cycles; 512 tokens behind 8191
+// INT8 rows 111 us, 640 TFLOP/s, 33 M for 4.4 M, busy for 26 %.
 #include <algorithm>
 #include <type_traits>
 
@@ -47,7 +48,7 @@ constexpr float kSlack = 8.0f;         // powers of two a score may pass the run
 // 8190 rows 88 / 89 / 103, 512 tokens behind 8191 rows 153 / 163 / 177: more of them leave more records to join)
 constexpr int kTarget = 512;
 // query rows of a sequence and cache head that the first kernel serves: what a wave's registers hold. (Serving all, it took 262 us for 512
-// tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 130 and 1225)
+// tokens behind 8191 rows and 3904 for a prompt of 8192 tokens x 64 heads, where the wide one takes 133 and 1236)
 constexpr int kFew = 32;
 
 // Eight waves, one workgroup per CU in place of two, may share a step in LDS: bringing it (BF16 V to FP16 above all) takes each of them
@@ -1145,7 +1146,7 @@ Shapes shapes(const PageAttnArgs& a) {
     // Blocks enough for all workgroups are cut too where the first kernel has them: lengths differ, and one workgroup per head would walk a
     // sequence far longer than the others by itself (131072 rows beside 63 of 1024, 32 heads: 1033 us uncut, 86 cut; three single tokens
     // behind 65530 rows beside a prompt of 4096 tokens 705, 280). Chunks of one and a half shares of all steps and more leave sequences of
-    // like lengths whole (64 of 3072 rows 74.8 us uncut, 77.1 so, 64 of 500 18.8, 20.7: the join). The join looks at every token's rows: a bound
+    // like lengths whole (256 of 500 rows 64.6 us uncut, 67.2 so, 64 of 500 18.8, 20.7: the join). The join looks at every token's rows: a bound
     // on them, higher where the first kernel has the short sequences of a step.
     y.cut = (blocks < quota || block <= kFew) && most > kMinSteps * step && long(a.N) * a.slots * a.group <= (limit == kFew ? 1 << 20 : 1 << 17);
     y.share = blocks < quota ? quota : (2 * quota + 2) / 3;

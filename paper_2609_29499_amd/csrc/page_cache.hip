@@ -9,8 +9,8 @@
 // that the workgroup walks.
 //
 // Bound by memory: 9750 tokens of 64 + 2 x 8 heads of 128, float32 into INT8 pages of 64, and back: 177 us, 4.5 TB/s in all (q's
-// launch 125 us at 5.1 TB/s, k and v 36, rows back 18: 160 workgroups of pages do not fill the card). A step of one token
-// each is latency (7 us).
+// launch 125 us at 5.1 TB/s, rows back 18; k and v, in 160 pages x 4 slices of heads, 36 us at 2.8 TB/s: two and a half workgroups per CU,
+// each of which waits twice per head for its largest value). A step of one token each is latency (7 us).
 #include <algorithm>
 
 #include "attn_tiles.hpp"
@@ -416,14 +416,18 @@ hipError_t launch_page_append(const PageAppendArgs& a, hipStream_t s) {
   // n tokens of a sequence touch at most n pages, and n / P + 2
   y.items = a.start ? int(std::min<long>(a.N, a.N / a.c.P + 2L * a.c.batch)) : a.c.batch;
   // two heads of k and of v per workgroup share a page's sines and cosines where that leaves enough of them (9750 tokens, pages of
-  // 64: 177.7 us in all, 180.0 with one head, 180.4 with four, 181.7 with k or v of one)
+  // 64: 177.7 us in all, 180.0 with one head, 180.4 with four, 181.7 with k or v of one; k or v of one against two heads of both, all
+  // of a call: 128 single tokens of 64 / 8 heads into INT8 14.8 / 13.6 us, 1024 tokens of 4 prompts 25.0 / 30.1, 4096 63.9 / 66.3; 32 / 8 heads into BF16
+  // pages of 16, 1024 tokens 15.1 / 15.1, 2048 20.3 / 18.6, 4096 29.1 / 24.0)
   y.per = long(y.items) * 2 * a.n_kv >= 2048 ? 4 : 1;
   y.slices = (2 * a.n_kv + y.per - 1) / y.per;
   y.tokens = a.N >= 1024 ? 4 : 1;
   y.groups = a.n_q ? (a.N + y.tokens - 1) / y.tokens : 0;
   y.rows = a.N >= 1024 ? y.tokens * a.n_q : rpp;
   y.q_slices = a.n_q ? (y.tokens * a.n_q + y.rows - 1) / y.rows : 0;
-  // Many tokens: q in a launch of its own, which has the LDS of a small page, and so more workgroups per CU
+  // Many tokens: q in a launch of its own, which has the LDS of a small page, and so more workgroups per CU (one launch / two, 64 / 8 heads of
+  // float32 into INT8 pages of 64: 512 tokens 18.3 / 22.3 us, 1000 24.5 / 23.9, 1500 31.8 / 28.5, 4096 77.5 / 64.4; 32 / 8 heads in BF16, pages of 16: 768
+  // 11.7 / 14.0, 1024 13.7 / 15.2, 2048 17.2 / 18.5, 4096 26.2 / 24.0)
   AppendShape q = y;
   const bool apart = a.N >= 1024 && y.groups > 0;
   if (apart) {

@@ -784,7 +784,7 @@ def token_logprobs_workspace(rows, vocab, n_top=0, device="cuda", stream=None):
 
 def token_logprobs(logits, tokens, n_top=0, temperature=1.0, start=None, workspace=None, stream=None):
     """Scores of tokens int32 ``[R]`` (outside the vocabulary: padding) against logits ``[R][V]`` (float32 or bfloat16, rows
-    of any stride). start int32 ``[S + 1]``: rows start[i] .. start[i + 1] - 1 are sequence i's."""
+    that do not overlap). start int32 ``[S + 1]``: rows start[i] .. start[i + 1] - 1 are sequence i's."""
     dev = _device(logits, tokens, start)
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError(f"logits must be a float32 or bfloat16 tensor [R][V] with contiguous rows, not {logits.dtype} {tuple(logits.shape)}")

@@ -50,3 +50,30 @@ def test_long_rows(V, R, top, kind):
         if a is got.logprob or a is got.rank:
             continue
         assert torch.equal(a[later], a[(torch.arange(R, device="cuda") % len(few))[later]])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [0, 3])
+def test_more_rows_than_a_grid_has(top, kind):
+    """A workgroup that takes more than one row."""
+    R, V = 140001, 40
+    flush(f"case many rows {top} {kind}")
+    x = (torch.randn((R, V), generator=gen(4)) * 2).to(DTYPES[kind]).cuda()
+    tokens = torch.randint(-1, V, (R,), generator=gen(5)).to(torch.int32).cuda()
+    start = torch.tensor([0, 65535, 65537, R], dtype=torch.int32, device="cuda")
+    got = S.token_logprobs(x, tokens, top, start=start)
+    y = x.double()
+    lps = torch.log_softmax(y, -1)
+    there, at = tokens >= 0, tokens.clamp(min=0).long()[:, None]
+    lp = torch.where(there, lps.gather(1, at)[:, 0], 0.0)
+    near = lambda a, b: bool(((a.double() - b).abs() <= math.log(2) * (E + 2.0 ** -23 * b.abs()) + 2.0 ** -24 * b.abs()).all())       # noqa: E731
+    assert near(got.logprob, lp)
+    h = -(lps.exp() * lps).sum(-1)
+    assert ((got.entropy.double() - h).abs() <= E * (1 + 2 * h) + 2.0 ** -24 * h).all()
+    yt, ids = y.gather(1, at), torch.arange(V, device="cuda")
+    assert torch.equal(got.rank.long(), torch.where(there, ((y > yt) | ((y == yt) & (ids < at))).sum(-1), -1))
+    if top:
+        best = torch.sort(y, -1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(got.top_ids.long(), best) and near(got.top_logprobs, lps.gather(1, best))
+    for i, (a, b) in enumerate(zip(start.tolist(), start.tolist()[1:])):
+        assert near(got.mean[i], lp[a:b][there[a:b]].mean())
