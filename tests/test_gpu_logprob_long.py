@@ -73,7 +73,7 @@ def test_more_rows_than_a_grid_has(top, kind):
     yt, ids = y.gather(1, at), torch.arange(V, device="cuda")
     assert torch.equal(got.rank.long(), torch.where(there, ((y > yt) | ((y == yt) & (ids < at))).sum(-1), -1))
     if top:
-        best = torch.sort(y, -1, descending=True, stable=True).indices[:, :top]
+        best = torch.sort(y, dim=-1, descending=True, stable=True).indices[:, :top]
         assert torch.equal(got.top_ids.long(), best) and near(got.top_logprobs, lps.gather(1, best))
     for i, (a, b) in enumerate(zip(start.tolist(), start.tolist()[1:])):
         assert near(got.mean[i], lp[a:b][there[a:b]].mean())
