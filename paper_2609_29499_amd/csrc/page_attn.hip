@@ -79,7 +79,7 @@ struct Deal {
   int nch[4], mine[4], before[4];      // of the lane's sequences: chunks of a block, items, items of the sequences before them
   int first[4], n[4], len[4];
 };
-// A lane holds four sequences. The chunk is the shortest multiple of kMinSteps that leaves at most `items` items.
+// A lane holds four sequences. The chunk is the shortest multiple of kMinSteps, a share of all steps at least, that leaves at most `items` items.
 __device__ __forceinline__ Deal deal(const PageAttnArgs& a, const PageShape& y, int lane) {
   Deal d;
   int steps[4], blocks[4], most = 0;
